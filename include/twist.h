@@ -420,6 +420,110 @@ int32_t twist_attn_core_fwd(const twist_attn_core_args* a /*host*/, void* stream
 int32_t twist_attn_core_bwd(const twist_attn_core_args* a /*host*/, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Positions, cache and attention of new tokens (extensions: the paper's attention has no positions of its own and its
+ * deployment mode, Sec. 4.2, is described for whole sequences).  With them an extracted subnet answers token by token:
+ * twist_subnet_attn_proj_fwd (QKV) -> twist_kv_append -> twist_attn_decode -> twist_subnet_attn_proj_fwd (O) -> FFN.
+ *
+ * twist_rope_fwd / twist_rope_bwd -- rotation of the Q and K columns of projected activations by the token's position.
+ * For pair j < rot_dims/2 of every Q and K head and a token at position t:
+ *     (x, y) <- (x cos a - y sin a,  x sin a + y cos a),   a = t * inv_freq[j]   (bwd: -a, which is the exact transpose)
+ *   TWIST_ROPE_HALF:  pair j is elements (j, j + rot_dims/2) of the head;  TWIST_ROPE_PAIRS: elements (2j, 2j + 1).
+ * Elements rot_dims .. d_head-1 of a head and the V columns are unchanged.  The angle is reduced in 64 bits, so far
+ * positions lose nothing; products are fp32, each result is rounded once.
+ *   in, out   [S][T][a' + 2 kv_max d_head], the layout of twist_attn_core_args.qkv; out may be `in` itself (then the
+ *             unchanged columns are not touched).  They must not overlap otherwise.
+ *   pos       device int32 [S][T] (>= 0) or NULL: token t of a subnet is at position t % seq_len.
+ * fwd rotates qkv between the projection and the attention core, bwd rotates the gradient d_qkv that the core's backward
+ * call wrote.  dtype TWIST_BF16 only; d_head a multiple of 8, at most 256; rot_dims even, 2 .. d_head. */
+enum { TWIST_ROPE_HALF = 0, TWIST_ROPE_PAIRS = 1 };
+typedef struct {
+  int32_t dtype, n_subnets, tokens, head_keep, kv_max, d_head;
+  int32_t rot_dims, layout, seq_len;
+  const void* in;             /* device */
+  void* out;                  /* device */
+  const double* inv_freq;     /* device fp64 [rot_dims/2] */
+  const int32_t* pos;         /* device int32 [S][T] or NULL */
+} twist_rope_args;
+
+int32_t twist_rope_fwd(const twist_rope_args* a /*host*/, void* stream);
+int32_t twist_rope_bwd(const twist_rope_args* a /*host*/, void* stream);
+
+/* The paged cache of one layer: pages of page_size tokens (a power of two, 16 .. 1024), a page [kv_max][page_size][d_head]
+ * bf16 in k_cache and in v_cache; consecutive pages are page_stride elements apart in both (page_stride >= kv_max *
+ * page_size * d_head, a multiple of 8: K and V may be interleaved in one buffer).  page_table [S][n_seqs][max_pages]:
+ * token at position t of sequence b of subnet s lives in page page_table[s][b][t / page_size], slot t % page_size.
+ * kv_len [S][n_seqs]: tokens of the sequence in the cache, the new ones of this step included.
+ *
+ * twist_kv_append -- stores K and V of new tokens, K rotated on the way, and writes the rotated Q.
+ *   qkv [S][T][a' + 2 kv_max d_head]: projected activations (unrotated) of T rows per subnet.  Which rows are which tokens:
+ *     new_begin (device int32 [S][n_seqs + 1], ascending): rows new_begin[s][b] .. new_begin[s][b+1] - 1 are the new tokens
+ *       of sequence b; rows from new_begin[s][n_seqs] on belong to none;
+ *     new_begin NULL: sequence b owns the T / n_seqs rows from b * (T / n_seqs) on (T a multiple of n_seqs), the first
+ *       new_len[s][b] of which are tokens (new_len NULL: all of them; one token per sequence is T == n_seqs).
+ *   New token i of n is at position kv_len[s][b] - n + i; its K and Q are rotated as by twist_rope_fwd (rot_dims = 0: not).
+ *   q_out: rotated Q [S][T] rows of a' elements, q_stride apart (q_stride >= a', a multiple of 8), or NULL; it may be the Q
+ *     columns of qkv itself (q_out == qkv, q_stride = a' + 2 kv_max d_head), but must not overlap it otherwise.
+ *   Rows that belong to no sequence are left as they were, in q_out and in the cache.  kv_count (device int32 [S] or NULL):
+ *   KV positions >= kv_count[s] are not stored.  Two tokens of a call must not share a slot.
+ * Index data is checked on the device: a row whose position or page lies outside the table / the pool, or whose new_begin /
+ * new_len contradict the layout, is skipped (neither q_out nor the cache is written) and TWIST_ERR_BAD_INDEX recorded.
+ * dtype TWIST_BF16 only; d_head a multiple of 8, at most 256. */
+typedef struct {
+  int32_t dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head;
+  int32_t page_size, n_pages, max_pages;
+  int32_t rot_dims, layout;
+  int64_t page_stride, q_stride;
+  const void* qkv;             /* device */
+  void* q_out;                 /* device or NULL */
+  void* k_cache;               /* device */
+  void* v_cache;               /* device */
+  const int32_t* page_table;   /* device int32 [S][n_seqs][max_pages] */
+  const int32_t* kv_len;       /* device int32 [S][n_seqs] */
+  const int32_t* new_begin;    /* device int32 [S][n_seqs + 1] or NULL */
+  const int32_t* new_len;      /* device int32 [S][n_seqs] or NULL */
+  const int32_t* kv_count;     /* device int32 [S] or NULL */
+  const double* inv_freq;      /* device fp64 [rot_dims/2]; may be NULL when rot_dims == 0 */
+} twist_kv_append_args;
+
+int32_t twist_kv_append(const twist_kv_append_args* a /*host*/, void* stream);
+
+/* twist_attn_decode -- attention of one new token per sequence over the paged cache:
+ *     out_h = sum_j softmax_j(q_h . k_j / sqrt(d_head)) v_j   over the kv_len[s][b] cached tokens (the new one included).
+ *   q    [S][n_seqs] rows of a' elements (rotated Q, as twist_kv_append writes it), q_stride apart;
+ *   out  [S][n_seqs][a'];  lse [S][head_keep][n_seqs] fp32 (log-sum-exp of the scores) or NULL.
+ *   A sequence without cached tokens gets zeros (lse -inf).
+ * Which KV position a head reads: head_idx / kv_pos / n_heads / n_kv_heads as in twist_attn_core_args.  The kept heads of a
+ * subnet are distinct, so that at most n_heads / n_kv_heads of them read one position.
+ * Long caches are split over the GPU's SMs and joined: the split follows from kv_len alone (ragged batches are balanced on
+ * the device), the order of every sum is fixed, results are deterministic.  ws: device scratch of at least
+ * twist_attn_decode_workspace_bytes(...) bytes; calls that may overlap on the GPU need scratch of their own.
+ * max_len: an upper bound of the kv_len entries that the caller knows (0: max_pages * page_size); it only chooses how the
+ * work is split, results do not depend on its being right beyond the rounding of another order of summation.
+ * Index data is checked on the device: a bad head or page entry is replaced by position 0 / page 0, a kv_len outside
+ * [0, max_pages * page_size] is clamped, heads beyond n_heads / n_kv_heads per position keep their old output, and
+ * TWIST_ERR_BAD_INDEX is recorded.
+ * dtype TWIST_BF16 only; d_head in {8, 16, 32, 64, 128}; n_subnets <= TWIST_MAX_SUBNETS, n_heads <= 1024. */
+typedef struct {
+  int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;
+  int32_t page_size, n_pages, max_pages, max_len;
+  int64_t page_stride, q_stride;
+  const void* q;               /* device */
+  const void* k_cache;         /* device */
+  const void* v_cache;         /* device */
+  const int32_t* page_table;   /* device int32 [S][n_seqs][max_pages] */
+  const int32_t* kv_len;       /* device int32 [S][n_seqs] */
+  const int32_t* head_idx;     /* device int32 [S][head_keep] or NULL (head hq reads position hq; kv_max == head_keep) */
+  const int32_t* kv_pos;       /* device int32 [S][n_kv_heads] (required with head_idx) */
+  void* out;                   /* device */
+  float* lse;                  /* device or NULL */
+  void* ws;                    /* device scratch */
+  size_t ws_bytes;
+} twist_attn_decode_args;
+
+size_t twist_attn_decode_workspace_bytes(int32_t d_head);
+int32_t twist_attn_decode(const twist_attn_decode_args* a /*host*/, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Layer normalisation of the pre-LN transformer layer (App. A, Layer Normalization: z = (x - mu) / sigma with
  * mu, sigma the mean and standard deviation of a token's d_model elements, y = gamma * z + b; Transformer
  * Layer Architecture: one normalisation before the attention block, one before the FFN block, the skip

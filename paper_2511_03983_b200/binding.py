@@ -24,6 +24,7 @@ FFN_RELU, FFN_GELU, FFN_SWIGLU = 0, 1, 2
 MODE_COVER, MODE_IID = 0, 1
 KIND_FFN, KIND_HEAD = 0, 1
 PROJ_QKV, PROJ_O = 0, 1
+ROPE_HALF, ROPE_PAIRS = 0, 1
 MAX_SEGMENTS = 8
 
 EXPORTS = [
@@ -34,6 +35,7 @@ EXPORTS = [
     "twist_hidden_mask", "twist_selftest_wait", "twist_layernorm_workspace_bytes", "twist_layernorm_fwd",
     "twist_layernorm_bwd", "twist_qkv_col_mask", "twist_apply_col_mask", "twist_plan_create", "twist_plan_destroy",
     "twist_plan_stats", "twist_workspace_bytes", "twist_aggregate_partial", "twist_aggregate_finish",
+    "twist_rope_fwd", "twist_rope_bwd", "twist_kv_append", "twist_attn_decode", "twist_attn_decode_workspace_bytes",
 ]
 
 
@@ -154,6 +156,32 @@ class LayerNormArgs(C.Structure):
                 ("v_gamma", C.c_void_p), ("m_beta", C.c_void_p), ("v_beta", C.c_void_p)]
 
 
+class RopeArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("tokens", C.c_int32), ("head_keep", C.c_int32),
+                ("kv_max", C.c_int32), ("d_head", C.c_int32), ("rot_dims", C.c_int32), ("layout", C.c_int32),
+                ("seq_len", C.c_int32), ("in_", C.c_void_p), ("out", C.c_void_p), ("inv_freq", C.c_void_p),
+                ("pos", C.c_void_p)]
+
+
+class KvAppendArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("n_seqs", C.c_int32), ("tokens", C.c_int32),
+                ("head_keep", C.c_int32), ("kv_max", C.c_int32), ("d_head", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("rot_dims", C.c_int32), ("layout", C.c_int32),
+                ("page_stride", C.c_int64), ("q_stride", C.c_int64), ("qkv", C.c_void_p), ("q_out", C.c_void_p),
+                ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("page_table", C.c_void_p), ("kv_len", C.c_void_p),
+                ("new_begin", C.c_void_p), ("new_len", C.c_void_p), ("kv_count", C.c_void_p), ("inv_freq", C.c_void_p)]
+
+
+class AttnDecodeArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("n_seqs", C.c_int32), ("head_keep", C.c_int32),
+                ("kv_max", C.c_int32), ("d_head", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("max_len", C.c_int32),
+                ("page_stride", C.c_int64), ("q_stride", C.c_int64), ("q", C.c_void_p), ("k_cache", C.c_void_p),
+                ("v_cache", C.c_void_p), ("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("head_idx", C.c_void_p),
+                ("kv_pos", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("ws", C.c_void_p),
+                ("ws_bytes", C.c_size_t)]
+
+
 _lib_handle = None
 
 
@@ -193,8 +221,11 @@ def lib() -> C.CDLL:
         h.twist_layernorm_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
         for name in ("twist_subnet_ffn_fwd", "twist_subnet_ffn_bwd", "twist_subnet_attn_proj_fwd",
                      "twist_subnet_attn_proj_bwd", "twist_attn_core_fwd", "twist_attn_core_bwd",
-                     "twist_layernorm_fwd", "twist_layernorm_bwd"):
+                     "twist_layernorm_fwd", "twist_layernorm_bwd", "twist_rope_fwd", "twist_rope_bwd", "twist_kv_append",
+                     "twist_attn_decode"):
             getattr(h, name).argtypes = [C.c_void_p, C.c_void_p]
+        h.twist_attn_decode_workspace_bytes.restype = C.c_size_t
+        h.twist_attn_decode_workspace_bytes.argtypes = [C.c_int32]
         h.twist_mse_workspace_bytes.restype = C.c_size_t
         h.twist_mse_workspace_bytes.argtypes = [C.c_int32]
         h.twist_fused_loss_workspace_bytes.restype = C.c_size_t
@@ -208,7 +239,7 @@ def lib() -> C.CDLL:
             f = getattr(h, name)
             if name not in ("twist_abi_version", "twist_strerror", "twist_last_cuda_error",
                             "twist_mse_workspace_bytes", "twist_fused_loss_workspace_bytes",
-                            "twist_layernorm_workspace_bytes"):
+                            "twist_layernorm_workspace_bytes", "twist_attn_decode_workspace_bytes"):
                 f.restype = C.c_int32
         _lib_handle = h
     return _lib_handle
@@ -396,6 +427,128 @@ def twist_attn_core_fwd(a: AttnCoreArgs):
 
 def twist_attn_core_bwd(a: AttnCoreArgs):
     _check(lib().twist_attn_core_bwd(C.byref(a), _stream()), "twist_attn_core_bwd")
+
+
+def _on_device(tensors) -> None:
+    """Every tensor of a call lies on the current device (the call runs on its current stream)."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensor on %s, current device is cuda:%d" % (t.device, dev))
+
+
+def _tensor(name: str, t: torch.Tensor, dtype: torch.dtype, numel: int) -> int:
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+        raise ValueError("%s: expected %d contiguous elements of %s, got %s of %s" % (name, numel, dtype, tuple(t.shape), t.dtype))
+    return t.data_ptr()
+
+
+def _rows(name: str, t: torch.Tensor, n_subnets: int, rows: int, width: int) -> int:
+    """Distance of the rows of a [S][rows][width] view whose rows lie evenly spaced (columns of a wider buffer)."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != n_subnets or t.shape[1] != rows or t.shape[2] != width:
+        raise ValueError("%s: expected bf16 [%d][%d][%d], got %s of %s" % (name, n_subnets, rows, width, tuple(t.shape), t.dtype))
+    s0, s1, s2 = t.stride()
+    stride = s1 if rows > 1 else (s0 if n_subnets > 1 else width)
+    if s2 != 1 or (n_subnets > 1 and s0 != rows * stride):
+        raise ValueError("%s: rows are not evenly spaced (strides %s)" % (name, (s0, s1, s2)))
+    return stride
+
+
+def _cache(k: torch.Tensor, v: torch.Tensor, kv_max: int, d_head: int):
+    """(page_size, n_pages, page_stride) of a paged cache [n_pages][kv_max][page_size][d_head]; pages may be spaced."""
+    if k.shape != v.shape or k.dim() != 4 or k.shape[1] != kv_max or k.shape[3] != d_head or \
+            k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+        raise ValueError("k_cache / v_cache: expected bf16 [pages][%d][page_size][%d], got %s and %s" % (kv_max, d_head, tuple(k.shape), tuple(v.shape)))
+    page, n = k.shape[2], k.shape[0]
+    inner = (page * d_head, d_head, 1)
+    ks, vs = k.stride(), v.stride()
+    if ks[1:] != inner or vs[1:] != inner or ks[0] != vs[0]:
+        raise ValueError("k_cache / v_cache: a page must be dense and both spaced alike (strides %s and %s)" % (ks, vs))
+    return page, n, ks[0] if n > 1 else max(ks[0], kv_max * page * d_head)
+
+
+def rope_args(dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, seq_len=0, layout=ROPE_HALF, *, in_, out,
+              inv_freq, pos=None) -> RopeArgs:
+    """Marshals twist_rope_args.  in_, out: bf16 [S][T][(head_keep + 2 kv_max) d_head] (out may be in_); inv_freq: fp64
+    [rot_dims / 2]; pos: int32 [S][T], or None for position t % seq_len."""
+    _on_device((in_, out, inv_freq, pos))
+    n = n_subnets * tokens * (head_keep + 2 * kv_max) * d_head
+    a = RopeArgs(dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, layout, seq_len,
+                 _tensor("in_", in_, torch.bfloat16, n), _tensor("out", out, torch.bfloat16, n),
+                 _tensor("inv_freq", inv_freq, torch.float64, rot_dims // 2),
+                 None if pos is None else _tensor("pos", pos, torch.int32, n_subnets * tokens))
+    a._keepalive = (in_, out, inv_freq, pos)
+    return a
+
+
+def twist_rope_fwd(a: RopeArgs):
+    _check(lib().twist_rope_fwd(C.byref(a), _stream()), "twist_rope_fwd")
+
+
+def twist_rope_bwd(a: RopeArgs):
+    _check(lib().twist_rope_bwd(C.byref(a), _stream()), "twist_rope_bwd")
+
+
+def kv_append_args(dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, rot_dims=0, layout=ROPE_HALF, *, qkv,
+                   k_cache, v_cache, page_table, kv_len, q_out=None, new_begin=None, new_len=None, kv_count=None,
+                   inv_freq=None) -> KvAppendArgs:
+    """Marshals twist_kv_append_args.  qkv: bf16 [S][T][(head_keep + 2 kv_max) d_head]; k_cache, v_cache: bf16
+    [n_pages][kv_max][page_size][d_head], pages evenly spaced (one buffer may hold both); page_table: int32
+    [S][n_seqs][max_pages]; kv_len: int32 [S][n_seqs], the new tokens included; q_out: bf16 [S][T][head_keep d_head], rows
+    evenly spaced (qkv[..., :head_keep * d_head] rotates Q in place)."""
+    _on_device((qkv, q_out, k_cache, v_cache, page_table, kv_len, new_begin, new_len, kv_count, inv_freq))
+    page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head)
+    seqs = n_subnets * n_seqs
+    max_pages = page_table.shape[-1]
+    opt = lambda name, t, dt, n: None if t is None else _tensor(name, t, dt, n)
+    q_stride = 0 if q_out is None else _rows("q_out", q_out, n_subnets, tokens, head_keep * d_head)
+    a = KvAppendArgs(dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, page, n_pages, max_pages, rot_dims, layout,
+                     stride, q_stride,
+                     _tensor("qkv", qkv, torch.bfloat16, n_subnets * tokens * (head_keep + 2 * kv_max) * d_head),
+                     None if q_out is None else q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                     _tensor("page_table", page_table, torch.int32, seqs * max_pages),
+                     _tensor("kv_len", kv_len, torch.int32, seqs),
+                     opt("new_begin", new_begin, torch.int32, n_subnets * (n_seqs + 1)),
+                     opt("new_len", new_len, torch.int32, seqs), opt("kv_count", kv_count, torch.int32, n_subnets),
+                     opt("inv_freq", inv_freq, torch.float64, rot_dims // 2))
+    a._keepalive = (qkv, q_out, k_cache, v_cache, page_table, kv_len, new_begin, new_len, kv_count, inv_freq)
+    return a
+
+
+def twist_kv_append(a: KvAppendArgs):
+    _check(lib().twist_kv_append(C.byref(a), _stream()), "twist_kv_append")
+
+
+def attn_decode_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads=0, n_kv_heads=0, max_len=0, *, q, k_cache,
+                     v_cache, page_table, kv_len, out, ws, head_idx=None, kv_pos=None, lse=None) -> AttnDecodeArgs:
+    """Marshals twist_attn_decode_args.  q: bf16 [S][n_seqs][head_keep d_head], rows evenly spaced; the cache as in
+    kv_append_args; head_idx int32 [S][head_keep] and kv_pos int32 [S][n_kv_heads] for grouped-query sharing; out bf16
+    [S][n_seqs][head_keep d_head]; lse fp32 [S][head_keep][n_seqs]; ws: scratch of at least
+    twist_attn_decode_workspace_bytes(d_head) bytes."""
+    _on_device((q, k_cache, v_cache, page_table, kv_len, out, ws, head_idx, kv_pos, lse))
+    page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head)
+    seqs = n_subnets * n_seqs
+    max_pages = page_table.shape[-1]
+    opt = lambda name, t, dt, n: None if t is None else _tensor(name, t, dt, n)
+    a = AttnDecodeArgs(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages,
+                       max_len, stride, _rows("q", q, n_subnets, n_seqs, head_keep * d_head), q.data_ptr(),
+                       k_cache.data_ptr(), v_cache.data_ptr(),
+                       _tensor("page_table", page_table, torch.int32, seqs * max_pages),
+                       _tensor("kv_len", kv_len, torch.int32, seqs),
+                       opt("head_idx", head_idx, torch.int32, n_subnets * head_keep),
+                       opt("kv_pos", kv_pos, torch.int32, n_subnets * n_kv_heads),
+                       _tensor("out", out, torch.bfloat16, seqs * head_keep * d_head),
+                       opt("lse", lse, torch.float32, seqs * head_keep), ws.data_ptr(), _ws_bytes(ws))
+    a._keepalive = (q, k_cache, v_cache, page_table, kv_len, out, ws, head_idx, kv_pos, lse)
+    return a
+
+
+def twist_attn_decode_workspace_bytes(d_head: int) -> int:
+    return lib().twist_attn_decode_workspace_bytes(d_head)
+
+
+def twist_attn_decode(a: AttnDecodeArgs):
+    _check(lib().twist_attn_decode(C.byref(a), _stream()), "twist_attn_decode")
 
 
 def layernorm_args(dtype, n_subnets, tokens, d_model, eps, lr=0.0, opt: Optional[Optimizer] = None, **t) -> LayerNormArgs:
