@@ -18,10 +18,12 @@
 // vote per tile instead of a reduction).  The probabilities enter the second product as the sum of two bf16 numbers
 // (value and remainder: 16 bits), so that rounding them costs nothing against the one rounding of the result.
 //
-// Splitting.  The work of a call is a line of tiles: sequence after sequence, KV position after KV position.  CTA c of G
-// takes the c-th G-th of the line, whatever the lengths are: a ragged batch is balanced on the device.  A CTA writes the
-// items it has whole; of an item that a CTA boundary cuts, every CTA writes its unnormalised part (fp32 sums, maximum,
-// sum) to the workspace, and a second small launch joins the parts in the order of the CTAs.
+// Splitting.  The work of a call is a line of tiles: sequence after sequence, KV position after KV position.  Warp w of G
+// takes the w-th G-th of the line, whatever the lengths are: a ragged batch is balanced on the device, and a warp's loads
+// run on across the borders of items (an item: the tiles of one KV position of one sequence).  A warp writes the items it
+// has whole; of an item that a border between warps cuts, every warp writes its unnormalised part (fp32 sums, maximum,
+// sum) to the workspace, and a second small launch joins the parts in the order of the warps.  Calls so small that
+// latency is all they cost run one CTA per item instead, whose warps join in shared memory (one launch).
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -32,6 +34,8 @@ constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kCols = 8;                   // heads per pass over the keys (columns of the MMA tile)
 constexpr int kMaxCtasPerSm = 4;
+constexpr int kMinTiles = 2;               // tiles that make a warp worth its set-up
+constexpr int kJoinThreads = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.0f;             // log2 headroom of the lazily moved reference maximum
@@ -46,14 +50,18 @@ struct DecParams {
   const int32_t* kv_pos;
   __nv_bfloat16* out;
   float* lse;
-  float* part;                // [2 G][kCols][D + 2]: sums, maximum (log2), sum of probabilities
-  int4* desc;                 // [G] the item that starts in CTA c and ends behind it: (sequence, KV position, row tile, parts)
+  float* part;                // [2 G][kCols][D + 4]: see kPartRow
+  int4* desc;                 // [items or warps] a cut item: (sequence, heads, further parts, warp that has its beginning)
   long long page_stride, q_stride;
   int S, n_seqs, heads, kv_max, per_group, n_kv_heads, row_tiles;
+  int by_item;                // desc has an entry for every item (few items), else one for every warp
   int page_shift, n_pages, max_pages;
   float scale_log2;
   int* status;
 };
+
+// Row of a part: d sums, then maximum (log2), sum of probabilities, head, padding.
+__host__ __device__ constexpr int kPartRow(int d) { return d + 4; }
 
 __device__ inline void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -72,6 +80,9 @@ __device__ inline float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// Weight of a part with maximum x (log2) and sum l against the maximum m of all parts.  A part without a reference maximum
+// has no finite score: it counts for nothing, unless its sum is NaN.
+__device__ inline float part_weight(float x, float l, float m) { return x == -INFINITY ? (l == 0.f ? 0.f : 1.f) : ex2(x - m); }
 __device__ inline uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&t);
@@ -111,58 +122,54 @@ struct Tile {
   uint32_t v[Sh::SUB][4][Sh::VCH][Sh::VW];
 };
 
-// A page of the sequence; a bad entry is replaced by page 0 and reported.
-__device__ inline long long page_of(const DecParams& p, const int32_t* table, int key) {
-  int id = table[key >> p.page_shift];
+// Page ids of coming tiles, fetched ahead, one 16-key step per lane, so that no key waits for its page entry: lane l gets
+// the page of step l % SUB of the tile `tile0 + (l / SUB) * stride` of a sequence with the given last key (-1: no keys).
+// Keys behind the end are replaced by the last one.  A bad entry is replaced by page 0 and reported.
+template <int D>
+__device__ inline int fetch_pages(const DecParams& p, long long seq, int last_key, int tile0, int stride, int lane) {
+  constexpr int SUB = Shape<D>::SUB;
+  if (last_key < 0) return 0;
+  const long long key = min((long long)last_key, ((long long)tile0 + (long long)(lane / SUB) * stride) * Shape<D>::TILE + 16 * (lane % SUB));
+  int id = p.table[seq * p.max_pages + (key >> p.page_shift)];
   if ((unsigned)id >= (unsigned)p.n_pages) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); id = 0; }
-  return id * p.page_stride;
+  return id;
 }
 
-// Keys behind the end are read as zeros: whatever lies in the unused part of a page must not reach the products.
+// The tile that begins at key0, number n of its window of fetched page ids.  Rows behind the sequence's end are replaced by
+// its last row: whatever lies in the unused part of a page must not reach the products, and the scores of such rows
+// are masked anyway.
 template <int D>
-__device__ inline void load_k(Tile<D>& x, const DecParams& p, const int32_t* table, int key0, int len, long long pos_off, int g, int t) {
+__device__ inline void load_k(Tile<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long pos_off, int g, int t) {
   using Sh = Shape<D>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
-    const int kb = key0 + 16 * s;
-    const __nv_bfloat16* base = kb < len ? p.k + page_of(p, table, kb) + pos_off : p.k;
+    const int kb = min(key0 + 16 * s, last_key & ~15), id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + s);
+    const __nv_bfloat16* base = p.k + id * p.page_stride + pos_off + (kb & ((1 << p.page_shift) - 1)) * D + t * 2 * Sh::KW;
+    const int most = last_key - kb;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int key = kb + g + 8 * r;
-      const __nv_bfloat16* row = base + (long long)(key & ((1 << p.page_shift) - 1)) * D + t * 2 * Sh::KW;
+      const __nv_bfloat16* row = base + min(g + 8 * r, most) * D;
 #pragma unroll
-      for (int c = 0; c < Sh::KCH; ++c) {
-        if (key < len) {
-          load_words<Sh::KW>(x.k[s][r][c], row + c * 8 * Sh::KW);
-        } else {
-#pragma unroll
-          for (int w = 0; w < Sh::KW; ++w) x.k[s][r][c][w] = 0;
-        }
-      }
+      for (int c = 0; c < Sh::KCH; ++c) load_words<Sh::KW>(x.k[s][r][c], row + c * 8 * Sh::KW);
     }
   }
 }
 
 template <int D>
-__device__ inline void load_v(Tile<D>& x, const DecParams& p, const int32_t* table, int key0, int len, long long pos_off, int g, int t) {
+__device__ inline void load_v(Tile<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long pos_off, int g, int t) {
   using Sh = Shape<D>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
-    const int kb = key0 + 16 * s;
-    const __nv_bfloat16* base = kb < len ? p.v + page_of(p, table, kb) + pos_off : p.v;
+    const int kb = min(key0 + 16 * s, last_key & ~15), id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + s);
+    const __nv_bfloat16* base = p.v + id * p.page_stride + pos_off + (kb & ((1 << p.page_shift) - 1)) * D;
+    const int most = last_key - kb;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int key = kb + 2 * t + (r & 1) + 8 * (r >> 1);
-      const __nv_bfloat16* row = base + (long long)(key & ((1 << p.page_shift) - 1)) * D;
+      const __nv_bfloat16* row = base + min(2 * t + (r & 1) + 8 * (r >> 1), most) * D;
 #pragma unroll
       for (int c = 0; c < Sh::VCH; ++c) {
-        if (key < len) {
-          if constexpr (D == 8) x.v[s][r][c][0] = *reinterpret_cast<const unsigned short*>(row + g);
-          else load_words<Sh::VW>(x.v[s][r][c], row + c * 64 + g * 2 * Sh::VW);
-        } else {
-#pragma unroll
-          for (int w = 0; w < Sh::VW; ++w) x.v[s][r][c][w] = 0;
-        }
+        if constexpr (D == 8) x.v[s][r][c][0] = *reinterpret_cast<const unsigned short*>(row + g);
+        else load_words<Sh::VW>(x.v[s][r][c], row + c * 64 + g * 2 * Sh::VW);
       }
     }
   }
@@ -208,101 +215,124 @@ __device__ inline void find_heads(const DecParams& p, int s, int pos, int rt, in
   __syncwarp();
 }
 
-// All tiles t0 + warp, t0 + warp + kDecWarps, ... < t1 of one item.
 template <int D>
-__device__ inline void run_tiles(State<D>& st, const DecParams& p, const int32_t* table, int len, long long pos_off,
-                                 const uint32_t (&q)[Shape<D>::KCH][Shape<D>::KW], int t0, int t1, int warp, int lane) {
-  using Sh = Shape<D>;
-  const int g = lane >> 2, t = lane & 3;
+__device__ inline void reset(State<D>& st) {
 #pragma unroll
-  for (int i = 0; i < Sh::MT; ++i)
+  for (int i = 0; i < Shape<D>::MT; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) st.o[i][e] = 0.f;
   st.m0 = st.m1 = -INFINITY;
   st.l0 = st.l1 = 0.f;
-  int tile = t0 + warp;
-  if (tile >= t1) return;
-  Tile<D> x;
-  load_k<D>(x, p, table, tile * Sh::TILE, len, pos_off, g, t);
-  load_v<D>(x, p, table, tile * Sh::TILE, len, pos_off, g, t);
-  for (; tile < t1; tile += kDecWarps) {
-    const int key0 = tile * Sh::TILE;
-    const bool more = tile + kDecWarps < t1;
-    float sc[Sh::SUB][4];
+}
+
+// Queries of the warp's columns in the order the K loads have (column g of this thread: head hq, -1: none).
+template <int D>
+__device__ inline void load_q(uint32_t (&q)[Shape<D>::KCH][Shape<D>::KW], const DecParams& p, long long seq, int hq, int t) {
+  using Sh = Shape<D>;
+  const __nv_bfloat16* row = p.q + seq * p.q_stride + (long long)(hq < 0 ? 0 : hq) * D + t * 2 * Sh::KW;
 #pragma unroll
-    for (int s = 0; s < Sh::SUB; ++s) {
+  for (int c = 0; c < Sh::KCH; ++c) {
+    load_words<Sh::KW>(q[c], row + c * 8 * Sh::KW);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sc[s][e] = 0.f;
-#pragma unroll
-      for (int c = 0; c < Sh::KCH; ++c) {
-        if constexpr (Sh::KW == 4) {
-#pragma unroll
-          for (int h = 0; h < 4; h += 2)
-            mma16816(sc[s], x.k[s][0][c][h], x.k[s][1][c][h], x.k[s][0][c][h + 1], x.k[s][1][c][h + 1], q[c][h], q[c][h + 1]);
-        } else if constexpr (Sh::KW == 2) {
-          mma16816(sc[s], x.k[s][0][c][0], x.k[s][1][c][0], x.k[s][0][c][1], x.k[s][1][c][1], q[c][0], q[c][1]);
-        } else {
-          mma16816(sc[s], x.k[s][0][c][0], x.k[s][1][c][0], 0u, 0u, q[c][0], 0u);
-        }
-      }
-    }
-    if (more) load_k<D>(x, p, table, key0 + kDecWarps * Sh::TILE, len, pos_off, g, t);
-    // scores in log2 units; keys behind the end count for nothing
-    float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-    for (int s = 0; s < Sh::SUB; ++s) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool live = key0 + 16 * s + g + 8 * (e >> 1) < len;
-        sc[s][e] = live ? sc[s][e] * p.scale_log2 : -INFINITY;
-      }
-      mx0 = fmaxf(mx0, fmaxf(sc[s][0], sc[s][2]));
-      mx1 = fmaxf(mx1, fmaxf(sc[s][1], sc[s][3]));
-    }
-    if (__any_sync(0xffffffffu, mx0 > st.m0 + kSlack || mx1 > st.m1 + kSlack)) {
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) {
-        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
-        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
-      }
-      const float n0 = fmaxf(st.m0, mx0), n1 = fmaxf(st.m1, mx1);
-      const float f0 = st.m0 == -INFINITY ? 0.f : ex2(st.m0 - n0), f1 = st.m1 == -INFINITY ? 0.f : ex2(st.m1 - n1);
-      st.m0 = n0; st.m1 = n1;
-      st.l0 *= f0; st.l1 *= f1;
-#pragma unroll
-      for (int i = 0; i < Sh::MT; ++i) { st.o[i][0] *= f0; st.o[i][1] *= f1; st.o[i][2] *= f0; st.o[i][3] *= f1; }
-    }
-    const float r0 = st.m0 == -INFINITY ? 0.f : st.m0, r1 = st.m1 == -INFINITY ? 0.f : st.m1;
-#pragma unroll
-    for (int s = 0; s < Sh::SUB; ++s) {
-      float pr[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) pr[e] = ex2(sc[s][e] - ((e & 1) ? r1 : r0));
-      st.l0 += pr[0] + pr[2];
-      st.l1 += pr[1] + pr[3];
-      const uint32_t h0 = pack_bf16(pr[0], pr[1]), h1 = pack_bf16(pr[2], pr[3]);
-      const uint32_t e0 = pack_bf16(pr[0] - lo_f(h0), pr[1] - hi_f(h0)), e1 = pack_bf16(pr[2] - lo_f(h1), pr[3] - hi_f(h1));
-      const uint32_t b0 = transpose8x8(h0), b1 = transpose8x8(h1), c0 = transpose8x8(e0), c1 = transpose8x8(e1);
-#pragma unroll
-      for (int i = 0; i < Sh::MT; ++i) {
-        uint32_t a[4];                             // (rows g, g + 8) x (keys 2t, 2t+1 | 2t+8, 2t+9): element 2i and 2i + 1
-        if constexpr (D == 8) {
-          a[0] = x.v[s][0][0][0] | (x.v[s][1][0][0] << 16);
-          a[2] = x.v[s][2][0][0] | (x.v[s][3][0][0] << 16);
-          a[1] = a[3] = 0;
-        } else {
-          const int c = i / Sh::VW, w = i % Sh::VW;
-          a[0] = __byte_perm(x.v[s][0][c][w], x.v[s][1][c][w], 0x5410);
-          a[1] = __byte_perm(x.v[s][0][c][w], x.v[s][1][c][w], 0x7632);
-          a[2] = __byte_perm(x.v[s][2][c][w], x.v[s][3][c][w], 0x5410);
-          a[3] = __byte_perm(x.v[s][2][c][w], x.v[s][3][c][w], 0x7632);
-        }
-        mma16816(st.o[i], a[0], a[1], a[2], a[3], b0, b1);
-        mma16816(st.o[i], a[0], a[1], a[2], a[3], c0, c1);
-      }
-    }
-    if (more) load_v<D>(x, p, table, key0 + kDecWarps * Sh::TILE, len, pos_off, g, t);
+    for (int w = 0; w < Sh::KW; ++w) q[c][w] = hq < 0 ? 0u : q[c][w];
   }
+}
+
+// Raw scores q . k of a tile: thread (g, t) has keys g, g + 8 of each 16 and heads 2t, 2t + 1.
+template <int D>
+__device__ inline void tile_scores(float (&sc)[Shape<D>::SUB][4], const Tile<D>& x, const uint32_t (&q)[Shape<D>::KCH][Shape<D>::KW]) {
+  using Sh = Shape<D>;
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sc[s][e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < Sh::KCH; ++c) {
+      if constexpr (Sh::KW == 4) {
+#pragma unroll
+        for (int h = 0; h < 4; h += 2)
+          mma16816(sc[s], x.k[s][0][c][h], x.k[s][1][c][h], x.k[s][0][c][h + 1], x.k[s][1][c][h + 1], q[c][h], q[c][h + 1]);
+      } else if constexpr (Sh::KW == 2) {
+        mma16816(sc[s], x.k[s][0][c][0], x.k[s][1][c][0], x.k[s][0][c][1], x.k[s][1][c][1], q[c][0], q[c][1]);
+      } else {
+        mma16816(sc[s], x.k[s][0][c][0], x.k[s][1][c][0], 0u, 0u, q[c][0], 0u);
+      }
+    }
+  }
+}
+
+// Softmax step and O^T += V^T P^T of the tile that begins at key0 of `len` keys.
+template <int D>
+__device__ inline void tile_values(State<D>& st, float (&sc)[Shape<D>::SUB][4], const Tile<D>& x, float scale_log2, int key0, int len, int g) {
+  using Sh = Shape<D>;
+  if (key0 + Sh::TILE > len) {                     // keys behind the end count for nothing
+#pragma unroll
+    for (int s = 0; s < Sh::SUB; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (key0 + 16 * s + g + 8 * (e >> 1) >= len) sc[s][e] = -INFINITY;
+  }
+  float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s) {
+    mx0 = fmaxf(mx0, fmaxf(sc[s][0], sc[s][2]));
+    mx1 = fmaxf(mx1, fmaxf(sc[s][1], sc[s][3]));
+  }
+  if (__any_sync(0xffffffffu, (mx0 - st.m0) * scale_log2 > kSlack || (mx1 - st.m1) * scale_log2 > kSlack)) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
+      mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
+    }
+    const float n0 = fmaxf(st.m0, mx0), n1 = fmaxf(st.m1, mx1);
+    const float f0 = st.m0 == -INFINITY ? 0.f : ex2((st.m0 - n0) * scale_log2);
+    const float f1 = st.m1 == -INFINITY ? 0.f : ex2((st.m1 - n1) * scale_log2);
+    st.m0 = n0; st.m1 = n1;
+    st.l0 *= f0; st.l1 *= f1;
+#pragma unroll
+    for (int i = 0; i < Sh::MT; ++i) { st.o[i][0] *= f0; st.o[i][1] *= f1; st.o[i][2] *= f0; st.o[i][3] *= f1; }
+  }
+  const float r0 = st.m0 == -INFINITY ? 0.f : st.m0 * scale_log2, r1 = st.m1 == -INFINITY ? 0.f : st.m1 * scale_log2;
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s) {
+    float pr[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) pr[e] = ex2(fmaf(sc[s][e], scale_log2, (e & 1) ? -r1 : -r0));
+    st.l0 += pr[0] + pr[2];
+    st.l1 += pr[1] + pr[3];
+    const uint32_t h0 = pack_bf16(pr[0], pr[1]), h1 = pack_bf16(pr[2], pr[3]);
+    const uint32_t e0 = pack_bf16(pr[0] - lo_f(h0), pr[1] - hi_f(h0)), e1 = pack_bf16(pr[2] - lo_f(h1), pr[3] - hi_f(h1));
+    const uint32_t b0 = transpose8x8(h0), b1 = transpose8x8(h1), c0 = transpose8x8(e0), c1 = transpose8x8(e1);
+#pragma unroll
+    for (int i = 0; i < Sh::MT; ++i) {
+      uint32_t a[4];                               // (rows g, g + 8) x (keys 2t, 2t+1 | 2t+8, 2t+9): element 2i and 2i + 1
+      if constexpr (D == 8) {
+        a[0] = x.v[s][0][0][0] | (x.v[s][1][0][0] << 16);
+        a[2] = x.v[s][2][0][0] | (x.v[s][3][0][0] << 16);
+        a[1] = a[3] = 0;
+      } else {
+        const int c = i / Sh::VW, w = i % Sh::VW;
+        a[0] = __byte_perm(x.v[s][0][c][w], x.v[s][1][c][w], 0x5410);
+        a[1] = __byte_perm(x.v[s][0][c][w], x.v[s][1][c][w], 0x7632);
+        a[2] = __byte_perm(x.v[s][2][c][w], x.v[s][3][c][w], 0x5410);
+        a[3] = __byte_perm(x.v[s][2][c][w], x.v[s][3][c][w], 0x7632);
+      }
+      mma16816(st.o[i], a[0], a[1], a[2], a[3], b0, b1);
+      mma16816(st.o[i], a[0], a[1], a[2], a[3], c0, c1);
+    }
+  }
+}
+
+// The sums of the eight thread rows; maxima in log2 units from here on.
+template <int D>
+__device__ inline void finish(State<D>& st, float scale_log2) {
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) {
+    st.l0 += __shfl_xor_sync(0xffffffffu, st.l0, o);
+    st.l1 += __shfl_xor_sync(0xffffffffu, st.l1, o);
+  }
+  st.m0 *= scale_log2;
+  st.m1 *= scale_log2;
 }
 
 // Element of the head that accumulator row (i, half) of thread g holds (half: rows g / g + 8 of the MMA tile).
@@ -321,36 +351,95 @@ __device__ inline int clamped_len(const DecParams& p, long long seq) {
   return n;
 }
 
-// One segment (tiles t0 .. t1 of the item (seq, pos, row tile)); `slot` >= 0: a part, written to the workspace.
+__device__ inline long long lse_at(const DecParams& p, long long seq, int head) {
+  const long long s = seq / p.n_seqs;
+  return (s * p.heads + head) * p.n_seqs + (seq - s * p.n_seqs);
+}
+
+// A warp's result for one of the thread's two heads (col 0, 1): the finished row, or a part.
 template <int D>
-__device__ inline void run_segment(const DecParams& p, float* sm, int (*cols)[kCols], long long seq, int pos, int rt, int len,
-                                   int t0, int t1, int slot) {
+__device__ inline void store_head(const DecParams& p, const State<D>& st, int col, long long seq, int head, int g, int len) {
   using Sh = Shape<D>;
+  const float l = col ? st.l1 : st.l0, m = col ? st.m1 : st.m0, inv = len == 0 ? 0.f : 1.f / l;
+  __nv_bfloat16* out = p.out + (seq * p.heads + head) * D;
+  if constexpr (D == 8) {
+    out[g] = __float2bfloat16(st.o[0][col] * inv);
+  } else {
+#pragma unroll
+    for (int c = 0; c < Sh::VCH; ++c) {
+      uint32_t w[Sh::VW];
+#pragma unroll
+      for (int j = 0; j < Sh::VW; ++j) w[j] = pack_bf16(st.o[c * Sh::VW + j][col] * inv, st.o[c * Sh::VW + j][2 + col] * inv);
+      __nv_bfloat16* dst = out + c * 64 + g * 2 * Sh::VW;
+      if constexpr (Sh::VW == 4) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+      else if constexpr (Sh::VW == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<uint32_t*>(dst) = w[0];
+    }
+  }
+  if (g == 0 && p.lse) p.lse[lse_at(p, seq, head)] = len == 0 ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+template <int D>
+__device__ inline void store_part(float* row, const State<D>& st, int col, int head, int g) {
+  using Sh = Shape<D>;
+  if constexpr (D == 8) {
+    row[g] = st.o[0][col];
+  } else {
+#pragma unroll
+    for (int c = 0; c < Sh::VCH; ++c)
+#pragma unroll
+      for (int j = 0; j < Sh::VW; ++j)
+        *reinterpret_cast<float2*>(row + c * 64 + g * 2 * Sh::VW + 2 * j) =
+            make_float2(st.o[c * Sh::VW + j][col], st.o[c * Sh::VW + j][2 + col]);
+  }
+  if (g == 0)
+    *reinterpret_cast<float4*>(row + D) = make_float4(col ? st.m1 : st.m0, col ? st.l1 : st.l0, __int_as_float(head), 0.f);
+}
+
+// Whole items, one CTA per (sequence, KV position, row tile): the warps take every fourth tile and join in shared memory.
+template <int D>
+__global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecParams p) {
+  using Sh = Shape<D>;
+  __shared__ float sm[kDecWarps * kCols * (D + 2)];
+  __shared__ int cols[kDecWarps][kCols];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int s = (int)(seq / p.n_seqs);
+  const int items = p.kv_max * p.row_tiles;
+  const long long seq = blockIdx.x / items;
+  const int rest = (int)(blockIdx.x - seq * items), pos = rest / p.row_tiles, rt = rest % p.row_tiles;
+  const int len = clamped_len(p, seq), tiles = (len + Sh::TILE - 1) / Sh::TILE;
   const long long pos_off = ((long long)pos << p.page_shift) * D;
-  const int32_t* table = p.table + seq * p.max_pages;
-  find_heads(p, s, pos, rt, lane, cols[warp]);
-  if (cols[warp][0] < 0) return;                    // no head reads this position: nothing to do (the same in every warp)
+  constexpr int AHEAD = 32 / Sh::SUB;
   State<D> st;
+  reset<D>(st);
+  Tile<D> x;
+  int key0 = warp * Sh::TILE, ids = 0;
+  if (warp < tiles) {
+    ids = fetch_pages<D>(p, seq, len - 1, warp, kDecWarps, lane);
+    load_k<D>(x, p, ids, 0, key0, len - 1, pos_off, g, t);
+    load_v<D>(x, p, ids, 0, key0, len - 1, pos_off, g, t);
+  }
+  // which heads, and their queries, while the first keys are on their way
+  find_heads(p, (int)(seq / p.n_seqs), pos, rt, lane, cols[warp]);
+  if (cols[warp][0] < 0) return;                   // no head reads this position (the same in every warp)
   uint32_t q[Sh::KCH][Sh::KW];
-  const int hq = cols[warp][g];
-  const __nv_bfloat16* qrow = p.q + seq * p.q_stride + (long long)(hq < 0 ? 0 : hq) * D + t * 2 * Sh::KW;
-#pragma unroll
-  for (int c = 0; c < Sh::KCH; ++c) {
-    if (hq >= 0) load_words<Sh::KW>(q[c], qrow + c * 8 * Sh::KW);
-    else
-#pragma unroll
-      for (int w = 0; w < Sh::KW; ++w) q[c][w] = 0;
+  load_q<D>(q, p, seq, cols[warp][g], t);
+  for (int tile = warp, n = 0; tile < tiles; tile += kDecWarps, key0 += kDecWarps * Sh::TILE) {
+    const bool more = tile + kDecWarps < tiles;
+    const int next0 = key0 + kDecWarps * Sh::TILE;
+    float sc[Sh::SUB][4];
+    tile_scores<D>(sc, x, q);
+    if (more) {
+      if (++n == AHEAD) {
+        ids = fetch_pages<D>(p, seq, len - 1, tile + kDecWarps, kDecWarps, lane);
+        n = 0;
+      }
+      load_k<D>(x, p, ids, n, next0, len - 1, pos_off, g, t);
+    }
+    tile_values<D>(st, sc, x, p.scale_log2, key0, len, g);
+    if (more) load_v<D>(x, p, ids, n, next0, len - 1, pos_off, g, t);
   }
-  run_tiles<D>(st, p, table, len, pos_off, q, t0, t1, warp, lane);
-  // the warps' states side by side in shared memory: [warp][head][D + 2]
-#pragma unroll
-  for (int o = 4; o < 32; o <<= 1) {
-    st.l0 += __shfl_xor_sync(0xffffffffu, st.l0, o);
-    st.l1 += __shfl_xor_sync(0xffffffffu, st.l1, o);
-  }
-  float* mine = sm + warp * kCols * (D + 2);
+  finish<D>(st, p.scale_log2);
+  float* mine = sm + warp * kCols * (D + 2);       // [head][D + 2]
 #pragma unroll
   for (int i = 0; i < Sh::MT; ++i)
 #pragma unroll
@@ -375,49 +464,56 @@ __device__ inline void run_segment(const DecParams& p, float* sm, int (*cols)[kC
     float acc = 0.f, l = 0.f;
 #pragma unroll
     for (int w = 0; w < kDecWarps; ++w) {
-      const float* x = sm + (w * kCols + h) * (D + 2);
-      const float f = x[D] == -INFINITY ? (x[D + 1] == 0.f ? 0.f : 1.f) : ex2(x[D] - m);
-      acc += f * x[d];
-      l += f * x[D + 1];
+      const float* y = sm + (w * kCols + h) * (D + 2);
+      const float f = part_weight(y[D], y[D + 1], m);
+      acc += f * y[d];
+      l += f * y[D + 1];
     }
-    if (slot >= 0) {
-      float* dst = p.part + ((long long)slot * kCols + h) * (D + 2);
-      dst[d] = acc;
-      if (d == 0) { dst[D] = m; dst[D + 1] = l; }
-    } else {
-      p.out[(seq * p.heads + head) * D + d] = __float2bfloat16(len == 0 ? 0.f : acc / l);
-      if (d == 0 && p.lse)
-        p.lse[((long long)s * p.heads + head) * p.n_seqs + seq % p.n_seqs] = len == 0 ? -INFINITY : (m + log2f(l)) * kLn2;
-    }
+    p.out[(seq * p.heads + head) * D + d] = __float2bfloat16(len == 0 ? 0.f : acc / l);
+    if (d == 0 && p.lse) p.lse[lse_at(p, seq, head)] = len == 0 ? -INFINITY : (m + log2f(l)) * kLn2;
   }
-  __syncthreads();
 }
 
-// Whole items only: one CTA per (sequence, KV position, row tile).
-template <int D>
-__global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecParams p) {
-  __shared__ float sm[kDecWarps * kCols * (D + 2)];
-  __shared__ int cols[kDecWarps][kCols];
-  const int items = p.kv_max * p.row_tiles;
-  const long long seq = blockIdx.x / items;
-  const int rest = (int)(blockIdx.x - seq * items);
-  const int len = clamped_len(p, seq);
-  run_segment<D>(p, sm, cols, seq, rest / p.row_tiles, rest % p.row_tiles, len, 0, (len + Shape<D>::TILE - 1) / Shape<D>::TILE, -1);
-}
-
-// The line of tiles.  Units of sequence i: held(s) * row_tiles * max(1, tiles of its keys).
+// The line of tiles.  Units of a sequence: held * row_tiles items of max(1, tiles of its keys) units each.
 template <int D>
 __device__ inline int tiles_of(int len) { return max(1, (len + Shape<D>::TILE - 1) / Shape<D>::TILE); }
 
+// a / b for the sizes at hand (a 64-bit division costs ten times a 32-bit one).
+__device__ inline long long divide(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// The line cut into G pieces whose sizes differ by at most one: piece w begins at w * small + min(w, extra).
+struct Cut {
+  long long small, extra;
+  __device__ long long begin(long long w) const { return w * small + min(w, extra); }
+  __device__ long long piece_of(long long u) const {
+    const long long big = extra * (small + 1);
+    return u < big ? divide(u, small + 1) : extra + divide(u - big, small);
+  }
+};
+
+// Where a warp stands in the line: an item and the range of its tiles that is the warp's.
+struct Segment {
+  long long seq;
+  int s, len, item, items, nt;        // subnet; keys; item of the sequence's `items`; tiles of an item
+  int t0, t1;
+};
+
+constexpr int kLenCache = 1024;       // sequences whose lengths a CTA keeps in shared memory
+
 template <int D>
-__global__ void __launch_bounds__(kDecThreads) decode_split_kernel(const DecParams p) {
-  __shared__ float sm[kDecWarps * kCols * (D + 2)];
+__global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecParams p) {
+  using Sh = Shape<D>;
   __shared__ int cols[kDecWarps][kCols];
   __shared__ int held[TWIST_MAX_SUBNETS];
+  __shared__ int lens[kLenCache];
   __shared__ long long warp_sum[kDecWarps];
-  __shared__ long long start_base;
-  __shared__ long long start_seq;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ long long start_base[kDecWarps];
+  __shared__ int start_seq[kDecWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int N = p.S * p.n_seqs, per = (N + kDecThreads - 1) / kDecThreads;
+  for (int i = threadIdx.x; i < min(N, kLenCache); i += kDecThreads) lens[i] = clamped_len(p, i);
   // KV positions of each subnet that some head reads: 1 + the largest entry of kv_pos
   for (int s = warp; s < p.S; s += kDecWarps) {
     int top = 0;
@@ -430,10 +526,10 @@ __global__ void __launch_bounds__(kDecThreads) decode_split_kernel(const DecPara
     if (lane == 0) held[s] = top + 1;
   }
   __syncthreads();
-  const int N = p.S * p.n_seqs, per = (N + kDecThreads - 1) / kDecThreads;
+  auto len_of = [&](int i) { return i < kLenCache ? lens[i] : clamped_len(p, i); };
   const int first = min(N, (int)threadIdx.x * per), last = min(N, first + per);
   long long mine = 0;
-  for (int i = first; i < last; ++i) mine += (long long)held[i / p.n_seqs] * p.row_tiles * tiles_of<D>(clamped_len(p, i));
+  for (int i = first; i < last; ++i) mine += (long long)held[i / p.n_seqs] * p.row_tiles * tiles_of<D>(len_of(i));
   long long incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -448,104 +544,217 @@ __global__ void __launch_bounds__(kDecThreads) decode_split_kernel(const DecPara
     if (w < warp) before += warp_sum[w];
     total += warp_sum[w];
   }
-  // as many CTAs as get a tile for each of their warps
-  const long long G = min((long long)gridDim.x, (total + kDecWarps - 1) / kDecWarps);
-  const int c = blockIdx.x;
-  if (threadIdx.x == 0) p.desc[c] = make_int4(0, 0, 0, 0);
-  if (c >= G) return;
-  const long long u0 = total * c / G, u1 = total * (c + 1) / G;
-  if (u0 >= before && u0 < before + mine) {
-    long long base = before;
-    int i = first;
-    for (;; ++i) {
-      const long long n = (long long)held[i / p.n_seqs] * p.row_tiles * tiles_of<D>(clamped_len(p, i));
-      if (u0 < base + n) break;
-      base += n;
-    }
-    start_seq = i;
-    start_base = base;
-  }
-  __syncthreads();
-  long long seq = start_seq, base = start_base, u = u0;
-  while (u < u1) {
-    const int len = clamped_len(p, seq), nt = tiles_of<D>(len);
-    const int s = (int)(seq / p.n_seqs);
-    const long long units = (long long)held[s] * p.row_tiles * nt;
-    while (u < u1 && u < base + units) {
-      const int item = (int)((u - base) / nt);
-      const long long item0 = base + (long long)item * nt;
-      const int t0 = (int)(u - item0), t1 = (int)min((long long)nt, u1 - item0);
-      int slot = -1;
-      if (t0 > 0) slot = 2 * c;
-      else if (t1 < nt) {
-        slot = 2 * c + 1;
-        // the CTA that holds the item's last tile: the largest e with total * e / G <= that tile
-        const long long end = item0 + nt - 1;
-        long long e = end * G / total;
-        while (total * (e + 1) / G <= end) ++e;
-        while (total * e / G > end) --e;
-        if (threadIdx.x == 0) p.desc[c] = make_int4((int)seq, item / p.row_tiles, item % p.row_tiles, (int)(e - c));
+  const int workers = gridDim.x * kDecWarps;
+  const long long G = min((long long)workers, max(1ll, total / kMinTiles));
+  const Cut cut{divide(total, G), total - divide(total, G) * G};
+  // the warps of this CTA whose first tile lies in this thread's sequences
+  for (int w = 0; w < kDecWarps; ++w) {
+    const long long c = (long long)blockIdx.x * kDecWarps + w;
+    if (c >= G) break;
+    const long long u = cut.begin(c);
+    if (u >= before && u < before + mine) {
+      long long base = before;
+      int i = first;
+      for (;; ++i) {
+        const long long n = (long long)held[i / p.n_seqs] * p.row_tiles * tiles_of<D>(len_of(i));
+        if (u < base + n) break;
+        base += n;
       }
-      run_segment<D>(p, sm, cols, seq, item / p.row_tiles, item % p.row_tiles, len, t0, t1, slot);
-      u = item0 + t1;
+      start_seq[w] = i;
+      start_base[w] = base;
     }
-    base += units;
-    ++seq;
   }
-}
-
-// Joins the parts of one cut item: CTA c's own (the item's beginning, slot 2c + 1) and slots 2(c+1), 2(c+2), ...
-template <int D>
-__global__ void __launch_bounds__(kDecThreads) decode_join_kernel(const DecParams p) {
-  __shared__ int cols[kCols];
-  griddep_wait();
-  const int c = blockIdx.x;
-  const int4 item = p.desc[c];
-  if (item.w <= 0) return;
-  const long long seq = item.x;
-  const int s = (int)(seq / p.n_seqs);
-  if (threadIdx.x < 32) find_heads(p, s, item.y, item.z, threadIdx.x, cols);
   __syncthreads();
-  for (int k = threadIdx.x; k < kCols * D; k += kDecThreads) {
-    const int h = k / D, d = k % D, head = cols[h];
-    if (head < 0) continue;
-    float m = -INFINITY;
-    for (int e = 0; e <= item.w; ++e)
-      m = fmaxf(m, p.part[((long long)(e ? 2 * (c + e) : 2 * c + 1) * kCols + h) * (D + 2) + D]);
-    float acc = 0.f, l = 0.f;
-    for (int e = 0; e <= item.w; ++e) {
-      const float* x = p.part + ((long long)(e ? 2 * (c + e) : 2 * c + 1) * kCols + h) * (D + 2);
-      const float f = x[D] == -INFINITY ? (x[D + 1] == 0.f ? 0.f : 1.f) : ex2(x[D] - m);
-      acc += f * x[d];
-      l += f * x[D + 1];
+  griddep_launch_dependents();
+  const int c = blockIdx.x * kDecWarps + warp;
+  if (!p.by_item && lane == 0) p.desc[c] = make_int4(0, 0, 0, 0);
+  if (c >= G) return;
+  long long left = cut.begin(c + 1) - cut.begin(c);
+  Segment now;
+  now.seq = start_seq[warp];
+  now.s = (int)now.seq / p.n_seqs;
+  now.len = len_of((int)now.seq);
+  now.nt = tiles_of<D>(now.len);
+  now.items = held[now.s] * p.row_tiles;
+  {
+    const long long at = cut.begin(c) - start_base[warp];
+    now.item = (int)divide(at, now.nt);
+    now.t0 = (int)(at - (long long)now.item * now.nt);
+  }
+  now.t1 = (int)min((long long)now.nt, now.t0 + left);
+  long long done = cut.begin(c);                    // the line's unit at the segment's beginning
+
+  constexpr int AHEAD = 32 / Sh::SUB;
+  Tile<D> x;
+  int ids = fetch_pages<D>(p, now.seq, now.len - 1, now.t0, 1, lane);
+  int next_ids = fetch_pages<D>(p, now.seq, now.len - 1, now.t0 + AHEAD, 1, lane);
+  int n = 0;                                        // number of the loaded tile in its window of page ids
+  if (now.len > 0) {
+    const long long off = ((long long)(now.item / p.row_tiles) << p.page_shift) * D;
+    load_k<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, off, g, t);
+    load_v<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, off, g, t);
+  }
+  for (;;) {
+    // the segment behind this one, and its first pages
+    left -= now.t1 - now.t0;
+    Segment next = now;
+    if (left > 0) {
+      next.t0 = 0;
+      if (++next.item == next.items) {
+        next.item = 0;
+        ++next.seq;
+        next.s = (int)next.seq / p.n_seqs;
+        next.len = len_of((int)next.seq);
+        next.nt = tiles_of<D>(next.len);
+        next.items = held[next.s] * p.row_tiles;
+      }
+      next.t1 = (int)min((long long)next.nt, left);
     }
-    p.out[(seq * p.heads + head) * D + d] = __float2bfloat16(acc / l);
-    if (d == 0 && p.lse) p.lse[((long long)s * p.heads + head) * p.n_seqs + seq % p.n_seqs] = (m + log2f(l)) * kLn2;
+    const int head_ids = left > 0 ? fetch_pages<D>(p, next.seq, next.len - 1, 0, 1, lane) : 0;
+    const int pos = now.item / p.row_tiles;
+    const long long off = ((long long)pos << p.page_shift) * D, next_off = ((long long)(next.item / p.row_tiles) << p.page_shift) * D;
+    find_heads(p, now.s, pos, now.item - pos * p.row_tiles, lane, cols[warp]);
+    const int hq = cols[warp][g];
+    uint32_t q[Sh::KCH][Sh::KW];
+    load_q<D>(q, p, now.seq, hq, t);
+    State<D> st;
+    reset<D>(st);
+    for (int tile = now.t0; tile < now.t1; ++tile) {
+      float sc[Sh::SUB][4];
+      tile_scores<D>(sc, x, q);
+      // the tile to load: the item's next one or the next item's first
+      const bool inside = tile + 1 < now.t1;
+      const int key0 = inside ? (tile + 1) * Sh::TILE : 0, last_key = inside ? now.len - 1 : next.len - 1;
+      const long long o = inside ? off : next_off;
+      const bool load = (inside || left > 0) && last_key >= 0;
+      if (inside) {
+        if (++n == AHEAD) {
+          ids = next_ids;
+          next_ids = fetch_pages<D>(p, now.seq, now.len - 1, tile + 1 + AHEAD, 1, lane);
+          n = 0;
+        }
+      } else {
+        ids = head_ids;
+        next_ids = left > 0 ? fetch_pages<D>(p, next.seq, next.len - 1, AHEAD, 1, lane) : 0;
+        n = 0;
+      }
+      if (load) load_k<D>(x, p, ids, n, key0, last_key, o, g, t);
+      if (now.len > 0) tile_values<D>(st, sc, x, p.scale_log2, tile * Sh::TILE, now.len, g);
+      if (load) load_v<D>(x, p, ids, n, key0, last_key, o, g, t);
+    }
+    finish<D>(st, p.scale_log2);
+    const bool whole = now.t0 == 0 && now.t1 == now.nt;
+    const int h0 = __shfl_sync(0xffffffffu, hq, 8 * t), h1 = __shfl_sync(0xffffffffu, hq, 8 * t + 4);
+    if (whole) {
+      if (h0 >= 0) store_head<D>(p, st, 0, now.seq, h0, g, now.len);
+      if (h1 >= 0) store_head<D>(p, st, 1, now.seq, h1, g, now.len);
+    } else {
+      float* part = p.part + (2ll * c + (now.t0 == 0)) * kCols * kPartRow(D);
+      if (h0 >= 0) store_part<D>(part + 2 * t * kPartRow(D), st, 0, h0, g);
+      if (h1 >= 0) store_part<D>(part + (2 * t + 1) * kPartRow(D), st, 1, h1, g);
+    }
+    if (now.t0 == 0 && lane == 0 && (p.by_item || !whole)) {
+      int heads = 0;
+      while (heads < kCols && cols[warp][heads] >= 0) ++heads;
+      const int parts = whole ? 0 : (int)(cut.piece_of(done + now.nt - 1) - c);        // further parts of the item
+      const long long all = (long long)p.kv_max * p.row_tiles;
+      int4* desc = p.desc + (p.by_item ? now.seq * all + now.item : c);
+      *desc = make_int4((int)now.seq, heads, parts, c);
+      if (p.by_item && now.item + 1 == now.items)                                       // positions that no head reads
+        for (long long k = 1; now.item + k < all; ++k) desc[k] = make_int4(0, 0, 0, 0);
+    }
+    if (left <= 0) break;
+    done += now.t1 - now.t0;
+    now = next;
   }
 }
 
-size_t desc_bytes() { return ((size_t)sm_count() * kMaxCtasPerSm * sizeof(int4) + 255) / 256 * 256; }
+// Joins the parts of one cut item: its beginning is slot 2c + 1 (c: the warp that has it), the others are 2(c+1), 2(c+2), ...
+// The threads of a CTA share the elements of its heads; where those are few, also the parts.
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecParams p) {
+  __shared__ float top[kCols], inv[kCols], sums[kJoinThreads];
+  griddep_wait();
+  const int4 item = p.desc[blockIdx.x];
+  const int heads = item.y, parts = item.z + 1, c = item.w;
+  if (heads <= 0 || parts <= 1) return;
+  const long long seq = item.x;
+  const int lane = threadIdx.x & 31;
+  auto row = [&](int e, int h) { return p.part + ((long long)(e ? 2 * (c + e) : 2 * c + 1) * kCols + h) * kPartRow(D); };
+  for (int h = threadIdx.x >> 5; h < heads; h += kJoinThreads / 32) {
+    float m = -INFINITY, l = 0.f;
+    for (int e = lane; e < parts; e += 32) m = fmaxf(m, row(e, h)[D]);
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int e = lane; e < parts; e += 32) {
+      const float2 y = *reinterpret_cast<const float2*>(row(e, h) + D);
+      l += part_weight(y.x, y.y, m) * y.y;
+    }
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (lane == 0) {
+      top[h] = m;
+      inv[h] = 1.f / l;
+      if (p.lse) p.lse[lse_at(p, seq, __float_as_int(row(0, h)[D + 2]))] = (m + log2f(l)) * kLn2;
+    }
+  }
+  __syncthreads();
+  const int elems = heads * D, groups = max(1, kJoinThreads / elems);                  // groups of threads that share the parts
+  for (int k0 = 0; k0 < elems; k0 += kJoinThreads) {
+    const int k = k0 + threadIdx.x % (elems < kJoinThreads ? elems : kJoinThreads), grp = elems < kJoinThreads ? threadIdx.x / elems : 0;
+    float acc = 0.f;
+    if (k < elems && grp < groups) {
+      const int h = k / D, d = k % D;
+      const float m = top[h];
+#pragma unroll 8
+      for (int e = grp; e < parts; e += groups) {
+        const float* y = row(e, h);
+        const float2 ml = *reinterpret_cast<const float2*>(y + D);
+        acc += part_weight(ml.x, ml.y, m) * y[d];
+      }
+    }
+    sums[threadIdx.x] = acc;
+    __syncthreads();
+    if (k < elems && grp == 0) {
+      const int h = k / D, d = k % D;
+      for (int e = 1; e < groups; ++e) acc += sums[threadIdx.x + e * elems];
+      p.out[(seq * p.heads + __float_as_int(row(0, h)[D + 2])) * D + d] = __float2bfloat16(acc * inv[h]);
+    }
+    __syncthreads();
+  }
+}
+
+size_t max_warps() { return (size_t)sm_count() * kMaxCtasPerSm * kDecWarps; }
+size_t desc_bytes() { return (max_warps() * sizeof(int4) + 255) / 256 * 256; }
 
 template <int D>
 int run(DecParams& p, long long max_len, cudaStream_t st) {
+  static int resident[64] = {0};
+  const int slot = device_slot();
+  if (resident[slot] == 0) {
+    int n = 0;
+    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_split_kernel<D>, kDecThreads, 0));
+    resident[slot] = n < 1 ? 1 : (n > kMaxCtasPerSm ? kMaxCtasPerSm : n);
+  }
+  const long long grid = (long long)sm_count() * resident[slot];
   const long long items = (long long)p.S * p.n_seqs * p.kv_max * p.row_tiles;
-  if (max_len <= 512 && items <= 0x7fffffffll) {
+  if (max_len <= 512 && items <= 2 * grid) {
     decode_whole_kernel<D><<<(unsigned)items, kDecThreads, 0, st>>>(p);
     TWIST_LAUNCH_CHECK();
     return TWIST_OK;
   }
-  static int ctas[64] = {0};
-  const int slot = device_slot();
-  if (ctas[slot] == 0) {
-    int n = 0;
-    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_split_kernel<D>, kDecThreads, 0));
-    ctas[slot] = n < 1 ? 1 : (n > kMaxCtasPerSm ? kMaxCtasPerSm : n);
-  }
-  const unsigned grid = (unsigned)(sm_count() * ctas[slot]);
-  decode_split_kernel<D><<<grid, kDecThreads, 0, st>>>(p);
+  p.by_item = items <= grid * kDecWarps;
+  decode_split_kernel<D><<<(unsigned)grid, kDecThreads, 0, st>>>(p);
   TWIST_LAUNCH_CHECK();
-  decode_join_kernel<D><<<grid, kDecThreads, 0, st>>>(p);
-  TWIST_LAUNCH_CHECK();
+  // programmatic stream serialisation: the join's CTAs are in place when the last part is written
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.by_item ? items : grid * kDecWarps));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  TWIST_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<D>, (const DecParams)p));
   return TWIST_OK;
 }
 
@@ -556,7 +765,7 @@ using namespace twist;
 
 extern "C" size_t twist_attn_decode_workspace_bytes(int32_t d_head) {
   if (d_head <= 0 || d_head > 128) return 0;
-  return desc_bytes() + (size_t)sm_count() * kMaxCtasPerSm * 2 * kCols * ((size_t)d_head + 2) * sizeof(float);
+  return desc_bytes() + max_warps() * 2 * kCols * kPartRow(d_head) * sizeof(float);
 }
 
 extern "C" int32_t twist_attn_decode(const twist_attn_decode_args* a, void* stream) {
