@@ -34,7 +34,8 @@ constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kCols = 8;                   // heads per pass over the keys (columns of the MMA tile)
 constexpr int kMaxCtasPerSm = 4;
-constexpr int kMinTiles = 2;               // tiles that make a warp worth its set-up
+constexpr int kItemCost = 1;               // what changing to the next item costs a warp, in tiles
+constexpr int kMinCost = 2;                // least work of a warp, in tiles
 constexpr int kJoinThreads = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.69314718055994531f;
@@ -225,17 +226,32 @@ __device__ inline void reset(State<D>& st) {
   st.l0 = st.l1 = 0.f;
 }
 
-// Queries of the warp's columns in the order the K loads have (column g of this thread: head hq, -1: none).
+// Queries of the warp's columns in the order the K loads have (column g of this thread: head hq, -1: none), copied to
+// shared memory ahead of their use: every thread copies and later reads its own words.
 template <int D>
-__device__ inline void load_q(uint32_t (&q)[Shape<D>::KCH][Shape<D>::KW], const DecParams& p, long long seq, int hq, int t) {
+struct QueryBuf {
+  uint32_t w[Shape<D>::KCH][32][Shape<D>::KW];
+};
+
+template <int D>
+__device__ inline void prefetch_q(QueryBuf<D>& buf, const DecParams& p, long long seq, int hq, int lane) {
   using Sh = Shape<D>;
-  const __nv_bfloat16* row = p.q + seq * p.q_stride + (long long)(hq < 0 ? 0 : hq) * D + t * 2 * Sh::KW;
+  const __nv_bfloat16* row = p.q + seq * p.q_stride + (long long)(hq < 0 ? 0 : hq) * D + (lane & 3) * 2 * Sh::KW;
 #pragma unroll
-  for (int c = 0; c < Sh::KCH; ++c) {
-    load_words<Sh::KW>(q[c], row + c * 8 * Sh::KW);
+  for (int c = 0; c < Sh::KCH; ++c)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(smem_u32(buf.w[c][lane])), "l"(row + c * 8 * Sh::KW),
+                 "n"(4 * Sh::KW), "r"(hq < 0 ? 0 : 4 * Sh::KW) : "memory");
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
+template <int D>
+__device__ inline void take_q(uint32_t (&q)[Shape<D>::KCH][Shape<D>::KW], const QueryBuf<D>& buf, int lane) {
+  using Sh = Shape<D>;
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
-    for (int w = 0; w < Sh::KW; ++w) q[c][w] = hq < 0 ? 0u : q[c][w];
-  }
+  for (int c = 0; c < Sh::KCH; ++c)
+#pragma unroll
+    for (int w = 0; w < Sh::KW; ++w) q[c][w] = buf.w[c][lane][w];
 }
 
 // Raw scores q . k of a tile: thread (g, t) has keys g, g + 8 of each 16 and heads 2t, 2t + 1.
@@ -402,6 +418,7 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
   using Sh = Shape<D>;
   __shared__ float sm[kDecWarps * kCols * (D + 2)];
   __shared__ int cols[kDecWarps][kCols];
+  __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int items = p.kv_max * p.row_tiles;
   const long long seq = blockIdx.x / items;
@@ -422,7 +439,8 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
   find_heads(p, (int)(seq / p.n_seqs), pos, rt, lane, cols[warp]);
   if (cols[warp][0] < 0) return;                   // no head reads this position (the same in every warp)
   uint32_t q[Sh::KCH][Sh::KW];
-  load_q<D>(q, p, seq, cols[warp][g], t);
+  prefetch_q<D>(qbuf[warp], p, seq, cols[warp][g], lane);
+  take_q<D>(q, qbuf[warp], lane);
   for (int tile = warp, n = 0; tile < tiles; tile += kDecWarps, key0 += kDecWarps * Sh::TILE) {
     const bool more = tile + kDecWarps < tiles;
     const int next0 = key0 + kDecWarps * Sh::TILE;
@@ -474,7 +492,8 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
   }
 }
 
-// The line of tiles.  Units of a sequence: held * row_tiles items of max(1, tiles of its keys) units each.
+// The line of work.  A sequence is held * row_tiles items; an item counts kItemCost units for itself (the warp that has its
+// first tile pays them) and one for each of its max(1, tiles of its keys) tiles.
 template <int D>
 __device__ inline int tiles_of(int len) { return max(1, (len + Shape<D>::TILE - 1) / Shape<D>::TILE); }
 
@@ -505,7 +524,8 @@ constexpr int kLenCache = 1024;       // sequences whose lengths a CTA keeps in 
 template <int D>
 __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecParams p) {
   using Sh = Shape<D>;
-  __shared__ int cols[kDecWarps][kCols];
+  __shared__ int cols[kDecWarps][2][kCols];
+  __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps][2];
   __shared__ int held[TWIST_MAX_SUBNETS];
   __shared__ int lens[kLenCache];
   __shared__ long long warp_sum[kDecWarps];
@@ -529,7 +549,7 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   auto len_of = [&](int i) { return i < kLenCache ? lens[i] : clamped_len(p, i); };
   const int first = min(N, (int)threadIdx.x * per), last = min(N, first + per);
   long long mine = 0;
-  for (int i = first; i < last; ++i) mine += (long long)held[i / p.n_seqs] * p.row_tiles * tiles_of<D>(len_of(i));
+  for (int i = first; i < last; ++i) mine += (long long)held[i / p.n_seqs] * p.row_tiles * (kItemCost + tiles_of<D>(len_of(i)));
   long long incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -545,7 +565,7 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
     total += warp_sum[w];
   }
   const int workers = gridDim.x * kDecWarps;
-  const long long G = min((long long)workers, max(1ll, total / kMinTiles));
+  const long long G = min((long long)workers, max(1ll, total / kMinCost));
   const Cut cut{divide(total, G), total - divide(total, G) * G};
   // the warps of this CTA whose first tile lies in this thread's sequences
   for (int w = 0; w < kDecWarps; ++w) {
@@ -556,7 +576,7 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       long long base = before;
       int i = first;
       for (;; ++i) {
-        const long long n = (long long)held[i / p.n_seqs] * p.row_tiles * tiles_of<D>(len_of(i));
+        const long long n = (long long)held[i / p.n_seqs] * p.row_tiles * (kItemCost + tiles_of<D>(len_of(i)));
         if (u < base + n) break;
         base += n;
       }
@@ -569,7 +589,8 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   const int c = blockIdx.x * kDecWarps + warp;
   if (!p.by_item && lane == 0) p.desc[c] = make_int4(0, 0, 0, 0);
   if (c >= G) return;
-  long long left = cut.begin(c + 1) - cut.begin(c);
+  long long left = cut.begin(c + 1) - cut.begin(c);       // units of the warp behind the current segment
+  long long item0;                                          // the line's unit at the current item's beginning
   Segment now;
   now.seq = start_seq[warp];
   now.s = (int)now.seq / p.n_seqs;
@@ -578,27 +599,37 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   now.items = held[now.s] * p.row_tiles;
   {
     const long long at = cut.begin(c) - start_base[warp];
-    now.item = (int)divide(at, now.nt);
-    now.t0 = (int)(at - (long long)now.item * now.nt);
+    now.item = (int)divide(at, now.nt + kItemCost);
+    const long long x0 = at - (long long)now.item * (now.nt + kItemCost), x1 = min((long long)now.nt + kItemCost, x0 + left);
+    item0 = cut.begin(c) - x0;
+    now.t0 = (int)max(0ll, x0 - kItemCost);
+    now.t1 = (int)max(0ll, x1 - kItemCost);
+    left -= x1 - x0;
   }
-  now.t1 = (int)min((long long)now.nt, now.t0 + left);
-  long long done = cut.begin(c);                    // the line's unit at the segment's beginning
+  if (now.t1 <= now.t0) return;                             // the item's own cost is all there is: the next warp has its tiles
 
   constexpr int AHEAD = 32 / Sh::SUB;
   Tile<D> x;
   int ids = fetch_pages<D>(p, now.seq, now.len - 1, now.t0, 1, lane);
   int next_ids = fetch_pages<D>(p, now.seq, now.len - 1, now.t0 + AHEAD, 1, lane);
   int n = 0;                                        // number of the loaded tile in its window of page ids
+  int pos = now.item / p.row_tiles, buf = 0;
+  find_heads(p, now.s, pos, now.item - pos * p.row_tiles, lane, cols[warp][0]);
+  prefetch_q<D>(qbuf[warp][0], p, now.seq, cols[warp][0][g], lane);
   if (now.len > 0) {
-    const long long off = ((long long)(now.item / p.row_tiles) << p.page_shift) * D;
+    const long long off = ((long long)pos << p.page_shift) * D;
     load_k<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, off, g, t);
     load_v<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, off, g, t);
   }
   for (;;) {
-    // the segment behind this one, and its first pages
-    left -= now.t1 - now.t0;
+    uint32_t q[Sh::KCH][Sh::KW];
+    take_q<D>(q, qbuf[warp][buf], lane);
+    const int hq = cols[warp][buf][g];
+    // the segment behind this one: its first pages, its heads and their queries on their way before they are needed
+    const bool more = left > kItemCost;
     Segment next = now;
-    if (left > 0) {
+    int next_pos = pos, head_ids = 0;
+    if (more) {
       next.t0 = 0;
       if (++next.item == next.items) {
         next.item = 0;
@@ -608,15 +639,13 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
         next.nt = tiles_of<D>(next.len);
         next.items = held[next.s] * p.row_tiles;
       }
-      next.t1 = (int)min((long long)next.nt, left);
+      next.t1 = (int)min((long long)next.nt, left - kItemCost);
+      next_pos = next.item / p.row_tiles;
+      head_ids = fetch_pages<D>(p, next.seq, next.len - 1, 0, 1, lane);
+      find_heads(p, next.s, next_pos, next.item - next_pos * p.row_tiles, lane, cols[warp][buf ^ 1]);
+      prefetch_q<D>(qbuf[warp][buf ^ 1], p, next.seq, cols[warp][buf ^ 1][g], lane);
     }
-    const int head_ids = left > 0 ? fetch_pages<D>(p, next.seq, next.len - 1, 0, 1, lane) : 0;
-    const int pos = now.item / p.row_tiles;
-    const long long off = ((long long)pos << p.page_shift) * D, next_off = ((long long)(next.item / p.row_tiles) << p.page_shift) * D;
-    find_heads(p, now.s, pos, now.item - pos * p.row_tiles, lane, cols[warp]);
-    const int hq = cols[warp][g];
-    uint32_t q[Sh::KCH][Sh::KW];
-    load_q<D>(q, p, now.seq, hq, t);
+    const long long off = ((long long)pos << p.page_shift) * D, next_off = ((long long)next_pos << p.page_shift) * D;
     State<D> st;
     reset<D>(st);
     for (int tile = now.t0; tile < now.t1; ++tile) {
@@ -626,7 +655,7 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       const bool inside = tile + 1 < now.t1;
       const int key0 = inside ? (tile + 1) * Sh::TILE : 0, last_key = inside ? now.len - 1 : next.len - 1;
       const long long o = inside ? off : next_off;
-      const bool load = (inside || left > 0) && last_key >= 0;
+      const bool load = (inside || more) && last_key >= 0;
       if (inside) {
         if (++n == AHEAD) {
           ids = next_ids;
@@ -635,7 +664,7 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
         }
       } else {
         ids = head_ids;
-        next_ids = left > 0 ? fetch_pages<D>(p, next.seq, next.len - 1, AHEAD, 1, lane) : 0;
+        next_ids = more ? fetch_pages<D>(p, next.seq, next.len - 1, AHEAD, 1, lane) : 0;
         n = 0;
       }
       if (load) load_k<D>(x, p, ids, n, key0, last_key, o, g, t);
@@ -653,73 +682,88 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       if (h0 >= 0) store_part<D>(part + 2 * t * kPartRow(D), st, 0, h0, g);
       if (h1 >= 0) store_part<D>(part + (2 * t + 1) * kPartRow(D), st, 1, h1, g);
     }
-    if (now.t0 == 0 && lane == 0 && (p.by_item || !whole)) {
-      int heads = 0;
-      while (heads < kCols && cols[warp][heads] >= 0) ++heads;
-      const int parts = whole ? 0 : (int)(cut.piece_of(done + now.nt - 1) - c);        // further parts of the item
-      const long long all = (long long)p.kv_max * p.row_tiles;
-      int4* desc = p.desc + (p.by_item ? now.seq * all + now.item : c);
-      *desc = make_int4((int)now.seq, heads, parts, c);
-      if (p.by_item && now.item + 1 == now.items)                                       // positions that no head reads
-        for (long long k = 1; now.item + k < all; ++k) desc[k] = make_int4(0, 0, 0, 0);
+    if (now.t0 == 0 && (p.by_item || !whole)) {
+      const int heads = __popc(__ballot_sync(0xffffffffu, hq >= 0 && t == 0));
+      if (lane == 0) {
+        const int parts = whole ? 0 : (int)(cut.piece_of(item0 + kItemCost + now.nt - 1) - c);    // further parts of the item
+        const long long all = (long long)p.kv_max * p.row_tiles;
+        int4* desc = p.desc + (p.by_item ? now.seq * all + now.item : c);
+        *desc = make_int4((int)now.seq, heads, parts, c);
+        if (p.by_item && now.item + 1 == now.items)                                               // positions that no head reads
+          for (long long k = 1; now.item + k < all; ++k) desc[k] = make_int4(0, 0, 0, 0);
+      }
     }
-    if (left <= 0) break;
-    done += now.t1 - now.t0;
+    if (!more) break;
+    item0 += now.nt + kItemCost;
+    left -= next.t1 + kItemCost;
     now = next;
+    pos = next_pos;
+    buf ^= 1;
   }
 }
 
 // Joins the parts of one cut item: its beginning is slot 2c + 1 (c: the warp that has it), the others are 2(c+1), 2(c+2), ...
-// The threads of a CTA share the elements of its heads; where those are few, also the parts.
+// A CTA takes kJoinThreads / groups elements of the item's heads; `groups` warps share the parts of each, every one
+// merging its own in order, eight at a time; the groups are merged in order through shared memory.
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecParams p) {
-  __shared__ float top[kCols], inv[kCols], sums[kJoinThreads];
+__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecParams p, int groups) {
+  __shared__ float3 sums[kJoinThreads];             // (maximum, sum, element)
   griddep_wait();
   const int4 item = p.desc[blockIdx.x];
   const int heads = item.y, parts = item.z + 1, c = item.w;
-  if (heads <= 0 || parts <= 1) return;
-  const long long seq = item.x;
-  const int lane = threadIdx.x & 31;
-  auto row = [&](int e, int h) { return p.part + ((long long)(e ? 2 * (c + e) : 2 * c + 1) * kCols + h) * kPartRow(D); };
-  for (int h = threadIdx.x >> 5; h < heads; h += kJoinThreads / 32) {
-    float m = -INFINITY, l = 0.f;
-    for (int e = lane; e < parts; e += 32) m = fmaxf(m, row(e, h)[D]);
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    for (int e = lane; e < parts; e += 32) {
-      const float2 y = *reinterpret_cast<const float2*>(row(e, h) + D);
-      l += part_weight(y.x, y.y, m) * y.y;
-    }
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (lane == 0) {
-      top[h] = m;
-      inv[h] = 1.f / l;
-      if (p.lse) p.lse[lse_at(p, seq, __float_as_int(row(0, h)[D + 2]))] = (m + log2f(l)) * kLn2;
-    }
-  }
-  __syncthreads();
-  const int elems = heads * D, groups = max(1, kJoinThreads / elems);                  // groups of threads that share the parts
-  for (int k0 = 0; k0 < elems; k0 += kJoinThreads) {
-    const int k = k0 + threadIdx.x % (elems < kJoinThreads ? elems : kJoinThreads), grp = elems < kJoinThreads ? threadIdx.x / elems : 0;
-    float acc = 0.f;
-    if (k < elems && grp < groups) {
-      const int h = k / D, d = k % D;
-      const float m = top[h];
-#pragma unroll 8
-      for (int e = grp; e < parts; e += groups) {
-        const float* y = row(e, h);
-        const float2 ml = *reinterpret_cast<const float2*>(y + D);
-        acc += part_weight(ml.x, ml.y, m) * y[d];
+  const int elems = kJoinThreads / groups, k = blockIdx.y * elems + threadIdx.x % elems, grp = threadIdx.x / elems;
+  if (parts <= 1 || (int)(blockIdx.y * elems) >= heads * D) return;
+  const int h = k / D, d = k % D;
+  float m = -INFINITY, l = 0.f, acc = 0.f;
+  if (k < heads * D) {
+    for (int e0 = grp; e0 < parts; e0 += 8 * groups) {
+      float2 ml[8];
+      float y[8];
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int e = e0 + j * groups;
+        ml[j] = make_float2(-INFINITY, 0.f);
+        y[j] = 0.f;
+        if (e < parts) {
+          const float* row = p.part + ((long long)(e ? 2 * (c + e) : 2 * c + 1) * kCols + h) * kPartRow(D);
+          ml[j] = *reinterpret_cast<const float2*>(row + D);
+          y[j] = row[d];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
+      const float f = part_weight(m, l, top);
+      acc *= f;
+      l *= f;
+      m = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float w = part_weight(ml[j].x, ml[j].y, top);
+        acc += w * y[j];
+        l += w * ml[j].y;
       }
     }
-    sums[threadIdx.x] = acc;
-    __syncthreads();
-    if (k < elems && grp == 0) {
-      const int h = k / D, d = k % D;
-      for (int e = 1; e < groups; ++e) acc += sums[threadIdx.x + e * elems];
-      p.out[(seq * p.heads + __float_as_int(row(0, h)[D + 2])) * D + d] = __float2bfloat16(acc * inv[h]);
-    }
-    __syncthreads();
   }
+  if (groups > 1) {
+    sums[threadIdx.x] = make_float3(m, l, acc);
+    __syncthreads();
+    if (grp > 0) return;
+    for (int e = 1; e < groups; ++e) m = fmaxf(m, sums[threadIdx.x + e * elems].x);
+    const float f = part_weight(sums[threadIdx.x].x, l, m);
+    l *= f;
+    acc *= f;
+    for (int e = 1; e < groups; ++e) {
+      const float3 y = sums[threadIdx.x + e * elems];
+      const float w = part_weight(y.x, y.y, m);
+      l += w * y.y;
+      acc += w * y.z;
+    }
+  }
+  if (k >= heads * D) return;
+  const int head = __float_as_int(p.part[((2ll * c + 1) * kCols + h) * kPartRow(D) + D + 2]);
+  p.out[((long long)item.x * p.heads + head) * D + d] = __float2bfloat16(acc / l);
+  if (d == 0 && p.lse) p.lse[lse_at(p, item.x, head)] = (m + log2f(l)) * kLn2;
 }
 
 size_t max_warps() { return (size_t)sm_count() * kMaxCtasPerSm * kDecWarps; }
@@ -746,7 +790,10 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   TWIST_LAUNCH_CHECK();
   // programmatic stream serialisation: the join's CTAs are in place when the last part is written
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.by_item ? items : grid * kDecWarps));
+  // An item of an even batch is cut into about warps / items parts: the fewer items, the more threads share the parts of one.
+  int groups = 1;
+  while (groups < kJoinThreads / 32 && 8ll * groups * items < grid * kDecWarps) groups *= 2;
+  cfg.gridDim = dim3((unsigned)(p.by_item ? items : grid * kDecWarps), (unsigned)((kCols * D * groups + kJoinThreads - 1) / kJoinThreads));
   cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr;
@@ -754,7 +801,7 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  TWIST_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<D>, (const DecParams)p));
+  TWIST_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<D>, (const DecParams)p, groups));
   return TWIST_OK;
 }
 
