@@ -502,7 +502,8 @@ int32_t twist_kv_append(const twist_kv_append_args* a /*host*/, void* stream);
  * Index data is checked on the device: a bad head or page entry is replaced by position 0 / page 0, a kv_len outside
  * [0, max_pages * page_size] is clamped, heads beyond n_heads / n_kv_heads per position keep their old output, and
  * TWIST_ERR_BAD_INDEX is recorded.
- * dtype TWIST_BF16 only; d_head in {8, 16, 32, 64, 128}; n_subnets <= TWIST_MAX_SUBNETS, n_heads <= 1024. */
+ * dtype TWIST_BF16 only; d_head in {8, 16, 32, 64, 128}; n_subnets <= TWIST_MAX_SUBNETS, n_heads <= 1024; n_subnets * n_seqs *
+ * kv_max * max_pages * page_size below 2^35 (the work is counted in 32 bits, in steps of 16 keys or more). */
 typedef struct {
   int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;
   int32_t page_size, n_pages, max_pages, max_len;

@@ -124,27 +124,37 @@ struct Tile {
 };
 
 // Page ids of coming tiles, fetched ahead, one 16-key step per lane, so that no key waits for its page entry: lane l gets
-// the page of step l % SUB of the tile `tile0 + (l / SUB) * stride` of a sequence with the given last key (-1: no keys).
-// Keys behind the end are replaced by the last one.  A bad entry is replaced by page 0 and reported.
+// the entry of step l % SUB of the tile `tile0 + (l / SUB) * stride`.  The read stays inside the sequence's row of the
+// table whatever its length is, so it need not wait for that.
 template <int D>
-__device__ inline int fetch_pages(const DecParams& p, long long seq, int last_key, int tile0, int stride, int lane) {
+__device__ inline uint32_t step_key(int tile0, int stride, int lane) {
   constexpr int SUB = Shape<D>::SUB;
-  if (last_key < 0) return 0;
-  const long long key = min((long long)last_key, ((long long)tile0 + (long long)(lane / SUB) * stride) * Shape<D>::TILE + 16 * (lane % SUB));
-  int id = p.table[seq * p.max_pages + (key >> p.page_shift)];
-  if ((unsigned)id >= (unsigned)p.n_pages) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); id = 0; }
+  return ((uint32_t)tile0 + (uint32_t)(lane / SUB) * stride) * Shape<D>::TILE + 16 * (lane % SUB);
+}
+template <int D>
+__device__ inline int fetch_pages(const DecParams& p, long long seq, int tile0, int stride, int lane) {
+  return p.table[seq * p.max_pages + min(step_key<D>(tile0, stride, lane) >> p.page_shift, (uint32_t)p.max_pages - 1)];
+}
+// Before use: an entry outside the pool is replaced by page 0, and reported if a key of the sequence needs it.
+template <int D>
+__device__ inline int check_pages(const DecParams& p, int id, int last_key, int tile0, int stride, int lane) {
+  if ((unsigned)id >= (unsigned)p.n_pages) {
+    if (last_key >= 0 && step_key<D>(tile0, stride, lane) <= (uint32_t)last_key) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+    id = 0;
+  }
   return id;
 }
 
-// The tile that begins at key0, number n of its window of fetched page ids.  Rows behind the sequence's end are replaced by
-// its last row: whatever lies in the unused part of a page must not reach the products, and the scores of such rows
-// are masked anyway.
+// The tile that begins at key0 <= last_key, number n of its window of page ids.  Rows behind the sequence's end are
+// replaced by rows before it: whatever lies in the unused part of a page must not reach the products, and the scores
+// of such rows are masked anyway.
 template <int D>
 __device__ inline void load_k(Tile<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long pos_off, int g, int t) {
   using Sh = Shape<D>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
-    const int kb = min(key0 + 16 * s, last_key & ~15), id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + s);
+    const int step = key0 + 16 * s <= last_key ? s : 0, kb = key0 + 16 * step;
+    const int id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + step);
     const __nv_bfloat16* base = p.k + id * p.page_stride + pos_off + (kb & ((1 << p.page_shift) - 1)) * D + t * 2 * Sh::KW;
     const int most = last_key - kb;
 #pragma unroll
@@ -161,7 +171,8 @@ __device__ inline void load_v(Tile<D>& x, const DecParams& p, int ids, int n, in
   using Sh = Shape<D>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
-    const int kb = min(key0 + 16 * s, last_key & ~15), id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + s);
+    const int step = key0 + 16 * s <= last_key ? s : 0, kb = key0 + 16 * step;
+    const int id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + step);
     const __nv_bfloat16* base = p.v + id * p.page_stride + pos_off + (kb & ((1 << p.page_shift) - 1)) * D;
     const int most = last_key - kb;
 #pragma unroll
@@ -183,19 +194,42 @@ struct State {
   float m0, m1, l0, l1;
 };
 
+// Where a CTA finds the index data of the heads: in shared memory where it fits, copied with the first loads of the kernel.
+struct Heads {
+  const int32_t* idx;         // [S][heads] or null
+  const int32_t* pos;         // [S][n_kv_heads]
+};
+constexpr int kHeadCache = 512, kPosCache = 256;
+
+__device__ inline void copy_words(int32_t* dst, const int32_t* src, int n) {
+  for (int i = threadIdx.x; i < n; i += kDecThreads)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst + i)), "l"(src + i) : "memory");
+}
+// Begins the copy of the rows of `subnets` subnets from subnet s0 on (complete after wait_copies and a barrier).
+__device__ inline Heads cache_heads(const DecParams& p, int32_t* idx, int32_t* pos, int s0, int subnets) {
+  Heads h{p.head_idx, p.kv_pos};
+  if (p.head_idx && subnets * p.heads <= kHeadCache && subnets * p.n_kv_heads <= kPosCache) {
+    copy_words(idx, p.head_idx + (long long)s0 * p.heads, subnets * p.heads);
+    copy_words(pos, p.kv_pos + (long long)s0 * p.n_kv_heads, subnets * p.n_kv_heads);
+    h.idx = idx - (long long)s0 * p.heads;                      // indexed by the subnet's own number
+    h.pos = pos - (long long)s0 * p.n_kv_heads;
+  }
+  return h;
+}
+__device__ inline void wait_copies() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // KV position among the subnet's kept groups that kept head hq reads, checked.
-__device__ inline int position_of(const DecParams& p, int s, int hq) {
-  if (!p.head_idx) return hq;
-  const int h = p.head_idx[(long long)s * p.heads + hq];
+__device__ inline int position_of(const DecParams& p, const Heads& hd, int s, int hq) {
+  const int h = hd.idx[(long long)s * p.heads + hq];
   int g = h < 0 ? -1 : h / p.per_group;
   if ((unsigned)g >= (unsigned)p.n_kv_heads) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); g = 0; }
-  int pos = p.kv_pos[(long long)s * p.n_kv_heads + g];
+  int pos = hd.pos[(long long)s * p.n_kv_heads + g];
   if ((unsigned)pos >= (unsigned)p.kv_max) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); pos = 0; }
   return pos;
 }
 
 // The kept heads number 8 rt .. 8 rt + 7 among those that read KV position `pos`, into cols[0..7] (-1: none).  One warp.
-__device__ inline void find_heads(const DecParams& p, int s, int pos, int rt, int lane, int* cols) {
+__device__ inline void find_heads(const DecParams& p, const Heads& hd, int s, int pos, int rt, int lane, int* cols) {
   if (!p.head_idx) {
     if (lane < kCols) cols[lane] = lane == 0 ? pos : -1;
     __syncwarp();
@@ -206,7 +240,7 @@ __device__ inline void find_heads(const DecParams& p, int s, int pos, int rt, in
   int seen = 0;
   for (int h0 = 0; h0 < p.heads; h0 += 32) {
     const int hq = h0 + lane;
-    const bool mine = hq < p.heads && position_of(p, s, hq) == pos;
+    const bool mine = hq < p.heads && position_of(p, hd, s, hq) == pos;
     const unsigned vote = __ballot_sync(0xffffffffu, mine);
     const int rank = seen + __popc(vote & ((1u << lane) - 1)) - kCols * rt;
     if (mine && rank >= 0 && rank < kCols) cols[rank] = hq;
@@ -360,9 +394,8 @@ __device__ inline int elem_of(int i, int half, int g) {
   return g * (D / 8) + e;
 }
 
-__device__ inline int clamped_len(const DecParams& p, long long seq) {
+__device__ inline int clamped_len(const DecParams& p, int n) {
   const int most = p.max_pages << p.page_shift;
-  int n = p.len[seq];
   if (n < 0 || n > most) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); n = n < 0 ? 0 : most; }
   return n;
 }
@@ -419,24 +452,30 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
   __shared__ float sm[kDecWarps * kCols * (D + 2)];
   __shared__ int cols[kDecWarps][kCols];
   __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps];
+  __shared__ int32_t head_cache[kHeadCache], pos_cache[kPosCache];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int items = p.kv_max * p.row_tiles;
   const long long seq = blockIdx.x / items;
   const int rest = (int)(blockIdx.x - seq * items), pos = rest / p.row_tiles, rt = rest % p.row_tiles;
-  const int len = clamped_len(p, seq), tiles = (len + Sh::TILE - 1) / Sh::TILE;
+  const int s = (int)(seq / p.n_seqs);
+  // one round trip: the length, the first pages, the heads
+  const Heads hd = cache_heads(p, head_cache, pos_cache, s, 1);
+  int ids = fetch_pages<D>(p, seq, warp, kDecWarps, lane);
+  const int len = clamped_len(p, p.len[seq]), tiles = (len + Sh::TILE - 1) / Sh::TILE;
+  ids = check_pages<D>(p, ids, len - 1, warp, kDecWarps, lane);
+  wait_copies();
   const long long pos_off = ((long long)pos << p.page_shift) * D;
   constexpr int AHEAD = 32 / Sh::SUB;
   State<D> st;
   reset<D>(st);
   Tile<D> x;
-  int key0 = warp * Sh::TILE, ids = 0;
+  int key0 = warp * Sh::TILE;
   if (warp < tiles) {
-    ids = fetch_pages<D>(p, seq, len - 1, warp, kDecWarps, lane);
     load_k<D>(x, p, ids, 0, key0, len - 1, pos_off, g, t);
     load_v<D>(x, p, ids, 0, key0, len - 1, pos_off, g, t);
   }
-  // which heads, and their queries, while the first keys are on their way
-  find_heads(p, (int)(seq / p.n_seqs), pos, rt, lane, cols[warp]);
+  __syncthreads();
+  find_heads(p, hd, s, pos, rt, lane, cols[warp]);
   if (cols[warp][0] < 0) return;                   // no head reads this position (the same in every warp)
   uint32_t q[Sh::KCH][Sh::KW];
   prefetch_q<D>(qbuf[warp], p, seq, cols[warp][g], lane);
@@ -448,7 +487,7 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
     tile_scores<D>(sc, x, q);
     if (more) {
       if (++n == AHEAD) {
-        ids = fetch_pages<D>(p, seq, len - 1, tile + kDecWarps, kDecWarps, lane);
+        ids = check_pages<D>(p, fetch_pages<D>(p, seq, tile + kDecWarps, kDecWarps, lane), len - 1, tile + kDecWarps, kDecWarps, lane);
         n = 0;
       }
       load_k<D>(x, p, ids, n, next0, len - 1, pos_off, g, t);
@@ -497,25 +536,19 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
 template <int D>
 __device__ inline int tiles_of(int len) { return max(1, (len + Shape<D>::TILE - 1) / Shape<D>::TILE); }
 
-// a / b for the sizes at hand (a 64-bit division costs ten times a 32-bit one).
-__device__ inline long long divide(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
 // The line cut into G pieces whose sizes differ by at most one: piece w begins at w * small + min(w, extra).
 struct Cut {
-  long long small, extra;
-  __device__ long long begin(long long w) const { return w * small + min(w, extra); }
-  __device__ long long piece_of(long long u) const {
-    const long long big = extra * (small + 1);
-    return u < big ? divide(u, small + 1) : extra + divide(u - big, small);
+  uint32_t small, extra;
+  __device__ uint32_t begin(uint32_t w) const { return w * small + min(w, extra); }
+  __device__ uint32_t piece_of(uint32_t u) const {
+    const uint32_t big = extra * (small + 1);
+    return u < big ? u / (small + 1) : extra + (u - big) / small;
   }
 };
 
 // Where a warp stands in the line: an item and the range of its tiles that is the warp's.
 struct Segment {
-  long long seq;
-  int s, len, item, items, nt;        // subnet; keys; item of the sequence's `items`; tiles of an item
+  int seq, s, len, item, items, nt;        // subnet; keys; item of the sequence's `items`; tiles of an item
   int t0, t1;
 };
 
@@ -527,95 +560,99 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   __shared__ int cols[kDecWarps][2][kCols];
   __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps][2];
   __shared__ int held[TWIST_MAX_SUBNETS];
-  __shared__ int lens[kLenCache];
-  __shared__ long long warp_sum[kDecWarps];
-  __shared__ long long start_base[kDecWarps];
-  __shared__ int start_seq[kDecWarps];
+  __shared__ int32_t lens[kLenCache], head_cache[kHeadCache], pos_cache[kPosCache];
+  __shared__ uint32_t warp_sum[kDecWarps];
+  __shared__ __align__(16) uint32_t before[kDecThreads];    // cost of the sequences before each thread's
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int N = p.S * p.n_seqs, per = (N + kDecThreads - 1) / kDecThreads;
-  for (int i = threadIdx.x; i < min(N, kLenCache); i += kDecThreads) lens[i] = clamped_len(p, i);
+  // one round trip: lengths, heads, positions
+  copy_words(lens, p.len, min(N, kLenCache));
+  const Heads hd = cache_heads(p, head_cache, pos_cache, 0, p.S);
+  wait_copies();
+  __syncthreads();
   // KV positions of each subnet that some head reads: 1 + the largest entry of kv_pos
   for (int s = warp; s < p.S; s += kDecWarps) {
     int top = 0;
     if (p.head_idx) {
-      for (int k = lane; k < p.n_kv_heads; k += 32) top = max(top, min(p.kv_pos[s * p.n_kv_heads + k], p.kv_max - 1));
-      for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      for (int k = lane; k < p.n_kv_heads; k += 32) top = max(top, min(hd.pos[s * p.n_kv_heads + k], p.kv_max - 1));
+      top = __reduce_max_sync(0xffffffffu, top);
     } else {
       top = p.kv_max - 1;
     }
     if (lane == 0) held[s] = top + 1;
   }
   __syncthreads();
-  auto len_of = [&](int i) { return i < kLenCache ? lens[i] : clamped_len(p, i); };
-  const int first = min(N, (int)threadIdx.x * per), last = min(N, first + per);
-  long long mine = 0;
-  for (int i = first; i < last; ++i) mine += (long long)held[i / p.n_seqs] * p.row_tiles * (kItemCost + tiles_of<D>(len_of(i)));
-  long long incl = mine;
+  auto len_of = [&](int i) { return clamped_len(p, i < kLenCache ? lens[i] : p.len[i]); };
+  uint32_t mine = 0;
+  {
+    int i = min(N, (int)threadIdx.x * per), s = i / p.n_seqs, b = i - s * p.n_seqs;
+    for (const int last = min(N, i + per); i < last; ++i) {
+      mine += (uint32_t)(held[s] * p.row_tiles) * (kItemCost + tiles_of<D>(len_of(i)));
+      if (++b == p.n_seqs) { b = 0; ++s; }
+    }
+  }
+  uint32_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+    const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += y;
   }
   if (lane == 31) warp_sum[warp] = incl;
   __syncthreads();
-  long long before = incl - mine, total = 0;
+  uint32_t mine_at = incl - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < kDecWarps; ++w) {
-    if (w < warp) before += warp_sum[w];
+    if (w < warp) mine_at += warp_sum[w];
     total += warp_sum[w];
   }
-  const int workers = gridDim.x * kDecWarps;
-  const long long G = min((long long)workers, max(1ll, total / kMinCost));
-  const Cut cut{divide(total, G), total - divide(total, G) * G};
-  // the warps of this CTA whose first tile lies in this thread's sequences
-  for (int w = 0; w < kDecWarps; ++w) {
-    const long long c = (long long)blockIdx.x * kDecWarps + w;
-    if (c >= G) break;
-    const long long u = cut.begin(c);
-    if (u >= before && u < before + mine) {
-      long long base = before;
-      int i = first;
-      for (;; ++i) {
-        const long long n = (long long)held[i / p.n_seqs] * p.row_tiles * (kItemCost + tiles_of<D>(len_of(i)));
-        if (u < base + n) break;
-        base += n;
-      }
-      start_seq[w] = i;
-      start_base[w] = base;
-    }
-  }
+  before[threadIdx.x] = mine_at;
+  const uint32_t G = min((uint32_t)gridDim.x * kDecWarps, max(1u, total / kMinCost));
+  const Cut cut{total / G, total % G};
   __syncthreads();
   griddep_launch_dependents();
-  const int c = blockIdx.x * kDecWarps + warp;
+  const uint32_t c = blockIdx.x * kDecWarps + warp;
   if (!p.by_item && lane == 0) p.desc[c] = make_int4(0, 0, 0, 0);
   if (c >= G) return;
-  long long left = cut.begin(c + 1) - cut.begin(c);       // units of the warp behind the current segment
-  long long item0;                                          // the line's unit at the current item's beginning
+  uint32_t left = cut.begin(c + 1) - cut.begin(c);          // units of the warp behind the current segment
+  uint32_t item0;                                            // the line's unit at the current item's beginning
   Segment now;
-  now.seq = start_seq[warp];
-  now.s = (int)now.seq / p.n_seqs;
-  now.len = len_of((int)now.seq);
-  now.nt = tiles_of<D>(now.len);
-  now.items = held[now.s] * p.row_tiles;
   {
-    const long long at = cut.begin(c) - start_base[warp];
-    now.item = (int)divide(at, now.nt + kItemCost);
-    const long long x0 = at - (long long)now.item * (now.nt + kItemCost), x1 = min((long long)now.nt + kItemCost, x0 + left);
-    item0 = cut.begin(c) - x0;
-    now.t0 = (int)max(0ll, x0 - kItemCost);
-    now.t1 = (int)max(0ll, x1 - kItemCost);
+    const uint32_t u = cut.begin(c);
+    int owner = -1;                                          // the last thread whose sequences begin at or before u
+    for (int k = 0; k < kDecThreads; k += 32) owner += __popc(__ballot_sync(0xffffffffu, before[k + lane] <= u));
+    uint32_t base = before[owner];
+    now.seq = owner * per;
+    now.s = now.seq / p.n_seqs;
+    int b = now.seq - now.s * p.n_seqs;
+    for (;;) {
+      now.len = len_of(now.seq);
+      now.nt = tiles_of<D>(now.len);
+      now.items = held[now.s] * p.row_tiles;
+      const uint32_t cost = (uint32_t)now.items * (now.nt + kItemCost);
+      if (u < base + cost) break;
+      base += cost;
+      ++now.seq;
+      if (++b == p.n_seqs) { b = 0; ++now.s; }
+    }
+    const uint32_t one = now.nt + kItemCost;
+    now.item = (u - base) / one;
+    const uint32_t x0 = u - base - now.item * one, x1 = min(one, x0 + left);
+    item0 = u - x0;
+    now.t0 = max(0, (int)x0 - kItemCost);
+    now.t1 = max(0, (int)x1 - kItemCost);
     left -= x1 - x0;
   }
   if (now.t1 <= now.t0) return;                             // the item's own cost is all there is: the next warp has its tiles
 
   constexpr int AHEAD = 32 / Sh::SUB;
   Tile<D> x;
-  int ids = fetch_pages<D>(p, now.seq, now.len - 1, now.t0, 1, lane);
-  int next_ids = fetch_pages<D>(p, now.seq, now.len - 1, now.t0 + AHEAD, 1, lane);
+  int ids = fetch_pages<D>(p, now.seq, now.t0, 1, lane);
+  int next_ids = fetch_pages<D>(p, now.seq, now.t0 + AHEAD, 1, lane);     // unchecked until it becomes `ids`
   int n = 0;                                        // number of the loaded tile in its window of page ids
   int pos = now.item / p.row_tiles, buf = 0;
-  find_heads(p, now.s, pos, now.item - pos * p.row_tiles, lane, cols[warp][0]);
+  find_heads(p, hd, now.s, pos, now.item - pos * p.row_tiles, lane, cols[warp][0]);
   prefetch_q<D>(qbuf[warp][0], p, now.seq, cols[warp][0][g], lane);
+  ids = check_pages<D>(p, ids, now.len - 1, now.t0, 1, lane);
   if (now.len > 0) {
     const long long off = ((long long)pos << p.page_shift) * D;
     load_k<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, off, g, t);
@@ -626,7 +663,7 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
     take_q<D>(q, qbuf[warp][buf], lane);
     const int hq = cols[warp][buf][g];
     // the segment behind this one: its first pages, its heads and their queries on their way before they are needed
-    const bool more = left > kItemCost;
+    const bool more = left > (uint32_t)kItemCost;
     Segment next = now;
     int next_pos = pos, head_ids = 0;
     if (more) {
@@ -634,15 +671,15 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       if (++next.item == next.items) {
         next.item = 0;
         ++next.seq;
-        next.s = (int)next.seq / p.n_seqs;
-        next.len = len_of((int)next.seq);
+        next.s = next.seq / p.n_seqs;
+        next.len = len_of(next.seq);
         next.nt = tiles_of<D>(next.len);
         next.items = held[next.s] * p.row_tiles;
       }
-      next.t1 = (int)min((long long)next.nt, left - kItemCost);
+      next.t1 = (int)min((uint32_t)next.nt, left - kItemCost);
       next_pos = next.item / p.row_tiles;
-      head_ids = fetch_pages<D>(p, next.seq, next.len - 1, 0, 1, lane);
-      find_heads(p, next.s, next_pos, next.item - next_pos * p.row_tiles, lane, cols[warp][buf ^ 1]);
+      head_ids = fetch_pages<D>(p, next.seq, 0, 1, lane);
+      find_heads(p, hd, next.s, next_pos, next.item - next_pos * p.row_tiles, lane, cols[warp][buf ^ 1]);
       prefetch_q<D>(qbuf[warp][buf ^ 1], p, next.seq, cols[warp][buf ^ 1][g], lane);
     }
     const long long off = ((long long)pos << p.page_shift) * D, next_off = ((long long)next_pos << p.page_shift) * D;
@@ -658,13 +695,13 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       const bool load = (inside || more) && last_key >= 0;
       if (inside) {
         if (++n == AHEAD) {
-          ids = next_ids;
-          next_ids = fetch_pages<D>(p, now.seq, now.len - 1, tile + 1 + AHEAD, 1, lane);
+          ids = check_pages<D>(p, next_ids, now.len - 1, tile + 1, 1, lane);
+          next_ids = fetch_pages<D>(p, now.seq, tile + 1 + AHEAD, 1, lane);
           n = 0;
         }
       } else {
-        ids = head_ids;
-        next_ids = more ? fetch_pages<D>(p, next.seq, next.len - 1, AHEAD, 1, lane) : 0;
+        ids = check_pages<D>(p, head_ids, more ? next.len - 1 : -1, 0, 1, lane);
+        next_ids = fetch_pages<D>(p, next.seq, AHEAD, 1, lane);
         n = 0;
       }
       if (load) load_k<D>(x, p, ids, n, key0, last_key, o, g, t);
@@ -687,8 +724,8 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       if (lane == 0) {
         const int parts = whole ? 0 : (int)(cut.piece_of(item0 + kItemCost + now.nt - 1) - c);    // further parts of the item
         const long long all = (long long)p.kv_max * p.row_tiles;
-        int4* desc = p.desc + (p.by_item ? now.seq * all + now.item : c);
-        *desc = make_int4((int)now.seq, heads, parts, c);
+        int4* desc = p.desc + (p.by_item ? now.seq * all + now.item : (long long)c);
+        *desc = make_int4(now.seq, heads, parts, (int)c);
         if (p.by_item && now.item + 1 == now.items)                                               // positions that no head reads
           for (long long k = 1; now.item + k < all; ++k) desc[k] = make_int4(0, 0, 0, 0);
       }
@@ -771,6 +808,12 @@ size_t desc_bytes() { return (max_warps() * sizeof(int4) + 255) / 256 * 256; }
 
 template <int D>
 int run(DecParams& p, long long max_len, cudaStream_t st) {
+  const long long items = (long long)p.S * p.n_seqs * p.kv_max * p.row_tiles;
+  // the line is counted in 32 bits
+  const long long longest = (((long long)p.max_pages << p.page_shift) + Shape<D>::TILE - 1) / Shape<D>::TILE + 1 + kItemCost;
+  if (items > 0x7fffffffll / longest) return TWIST_ERR_UNSUPPORTED;
+  p.status = device_status_ptr();
+  if (!p.status) return TWIST_ERR_CUDA;
   static int resident[64] = {0};
   const int slot = device_slot();
   if (resident[slot] == 0) {
@@ -779,7 +822,6 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
     resident[slot] = n < 1 ? 1 : (n > kMaxCtasPerSm ? kMaxCtasPerSm : n);
   }
   const long long grid = (long long)sm_count() * resident[slot];
-  const long long items = (long long)p.S * p.n_seqs * p.kv_max * p.row_tiles;
   if (max_len <= 512 && items <= 2 * grid) {
     decode_whole_kernel<D><<<(unsigned)items, kDecThreads, 0, st>>>(p);
     TWIST_LAUNCH_CHECK();
@@ -855,8 +897,6 @@ extern "C" int32_t twist_attn_decode(const twist_attn_decode_args* a, void* stre
   p.page_shift = 31 - __builtin_clz((unsigned)a->page_size);
   p.n_pages = a->n_pages; p.max_pages = a->max_pages;
   p.scale_log2 = kLog2e / sqrtf((float)dh);
-  p.status = device_status_ptr();
-  if (!p.status) return TWIST_ERR_CUDA;
   const long long table_len = (long long)a->max_pages * a->page_size;
   const long long max_len = a->max_len > 0 && a->max_len < table_len ? a->max_len : table_len;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
