@@ -740,15 +740,15 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
 }
 
 // Joins the parts of one cut item: its beginning is slot 2c + 1 (c: the warp that has it), the others are 2(c+1), 2(c+2), ...
-// A CTA takes kJoinThreads / groups elements of the item's heads; `groups` warps share the parts of each, every one
-// merging its own in order, eight at a time; the groups are merged in order through shared memory.
+// A CTA takes blockDim / groups elements of the item's heads; `groups` threads share the parts of each, every one merging
+// its own in order, eight at a time; the groups are merged in order through shared memory.
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecParams p, int groups) {
   __shared__ float3 sums[kJoinThreads];             // (maximum, sum, element)
   griddep_wait();
   const int4 item = p.desc[blockIdx.x];
   const int heads = item.y, parts = item.z + 1, c = item.w;
-  const int elems = kJoinThreads / groups, k = blockIdx.y * elems + threadIdx.x % elems, grp = threadIdx.x / elems;
+  const int elems = blockDim.x / groups, k = blockIdx.y * elems + threadIdx.x % elems, grp = threadIdx.x / elems;
   if (parts <= 1 || (int)(blockIdx.y * elems) >= heads * D) return;
   const int h = k / D, d = k % D;
   float m = -INFINITY, l = 0.f, acc = 0.f;
@@ -835,8 +835,10 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   // An item of an even batch is cut into about warps / items parts: the fewer items, the more threads share the parts of one.
   int groups = 1;
   while (groups < kJoinThreads / 32 && 8ll * groups * items < grid * kDecWarps) groups *= 2;
-  cfg.gridDim = dim3((unsigned)(p.by_item ? items : grid * kDecWarps), (unsigned)((kCols * D * groups + kJoinThreads - 1) / kJoinThreads));
-  cfg.blockDim = dim3(kJoinThreads);
+  const int elems = (kCols < p.per_group ? kCols : p.per_group) * D;                   // of the heads that share a position
+  const int block = elems * groups < 32 ? 32 : (elems * groups > kJoinThreads ? kJoinThreads : elems * groups);
+  cfg.gridDim = dim3((unsigned)(p.by_item ? items : grid * kDecWarps), (unsigned)((elems * groups + block - 1) / block));
+  cfg.blockDim = dim3(block);
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
