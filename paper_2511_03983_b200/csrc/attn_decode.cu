@@ -458,6 +458,8 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
   const long long seq = blockIdx.x / items;
   const int rest = (int)(blockIdx.x - seq * items), pos = rest / p.row_tiles, rt = rest % p.row_tiles;
   const int s = (int)(seq / p.n_seqs);
+  griddep_launch_dependents();
+  griddep_wait();
   // one round trip: the length, the first pages, the heads
   const Heads hd = cache_heads(p, head_cache, pos_cache, s, 1);
   int ids = fetch_pages<D>(p, seq, warp, kDecWarps, lane);
@@ -565,6 +567,8 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   __shared__ __align__(16) uint32_t before[kDecThreads];    // cost of the sequences before each thread's
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int N = p.S * p.n_seqs, per = (N + kDecThreads - 1) / kDecThreads;
+  griddep_launch_dependents();
+  griddep_wait();
   // one round trip: lengths, heads, positions
   copy_words(lens, p.len, min(N, kLenCache));
   const Heads hd = cache_heads(p, head_cache, pos_cache, 0, p.S);
@@ -609,7 +613,6 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   const uint32_t G = min((uint32_t)gridDim.x * kDecWarps, max(1u, total / kMinCost));
   const Cut cut{total / G, total % G};
   __syncthreads();
-  griddep_launch_dependents();
   const uint32_t c = blockIdx.x * kDecWarps + warp;
   if (!p.by_item && lane == 0) p.desc[c] = make_int4(0, 0, 0, 0);
   if (c >= G) return;
@@ -823,29 +826,18 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   }
   const long long grid = (long long)sm_count() * resident[slot];
   if (max_len <= 512 && items <= 2 * grid) {
-    decode_whole_kernel<D><<<(unsigned)items, kDecThreads, 0, st>>>(p);
-    TWIST_LAUNCH_CHECK();
+    TWIST_CUDA_TRY(launch_overlapped(decode_whole_kernel<D>, dim3((unsigned)items), dim3(kDecThreads), 0, st, p));
     return TWIST_OK;
   }
   p.by_item = items <= grid * kDecWarps;
-  decode_split_kernel<D><<<(unsigned)grid, kDecThreads, 0, st>>>(p);
-  TWIST_LAUNCH_CHECK();
-  // programmatic stream serialisation: the join's CTAs are in place when the last part is written
-  cudaLaunchConfig_t cfg = {};
+  TWIST_CUDA_TRY(launch_overlapped(decode_split_kernel<D>, dim3((unsigned)grid), dim3(kDecThreads), 0, st, p));
   // An item of an even batch is cut into about warps / items parts: the fewer items, the more threads share the parts of one.
   int groups = 1;
   while (groups < kJoinThreads / 32 && 8ll * groups * items < grid * kDecWarps) groups *= 2;
   const int elems = (kCols < p.per_group ? kCols : p.per_group) * D;                   // of the heads that share a position
   const int block = elems * groups < 32 ? 32 : (elems * groups > kJoinThreads ? kJoinThreads : elems * groups);
-  cfg.gridDim = dim3((unsigned)(p.by_item ? items : grid * kDecWarps), (unsigned)((elems * groups + block - 1) / block));
-  cfg.blockDim = dim3(block);
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  TWIST_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<D>, (const DecParams)p, groups));
+  const dim3 join_grid((unsigned)(p.by_item ? items : grid * kDecWarps), (unsigned)((elems * groups + block - 1) / block));
+  TWIST_CUDA_TRY(launch_overlapped(decode_join_kernel<D>, join_grid, dim3(block), 0, st, p, groups));
   return TWIST_OK;
 }
 

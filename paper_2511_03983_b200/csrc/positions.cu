@@ -15,6 +15,7 @@
 // layout one 16-byte chunk; where chunks would straddle the halves (rot_dims/2 or rot_dims not a multiple of 8) a unit
 // is a whole head, element by element.
 #include "common.cuh"
+#include "ptx.cuh"
 
 namespace twist {
 namespace {
@@ -128,12 +129,14 @@ __device__ inline void rotate_pairs(uint4& v, const float2* cs) {
 enum { MODE_HALF = 0, MODE_PAIRS = 1, MODE_SLOW_HALF = 2, MODE_SLOW_PAIRS = 3 };
 
 template <bool APPEND, int MODE>
-__global__ void __launch_bounds__(kPosThreads) rotate_rows_kernel(const PosParams p) {
+__global__ void __launch_bounds__(kPosThreads) rotate_rows_kernel(PosParams p) {
   extern __shared__ float2 table[];                 // [tile_rows][half]
   __shared__ RowInfo info[kMaxRows];
   const long long row0 = (long long)blockIdx.x * p.tile_rows;
   const int n_rows = (int)min((long long)p.tile_rows, p.rows - row0);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  griddep_launch_dependents();
+  griddep_wait();
   if constexpr (APPEND) {
     if (warp < n_rows) {
       const RowInfo ri = find_row(p, row0 + warp, lane);
@@ -233,13 +236,11 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
   if (tiles > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
   const size_t smem = (size_t)p.tile_rows * p.half * sizeof(float2);                    // at most 8 KB
   const unsigned grid = (unsigned)tiles;
-  switch (mode) {
-    case MODE_HALF: rotate_rows_kernel<APPEND, MODE_HALF><<<grid, kPosThreads, smem, st>>>(p); break;
-    case MODE_PAIRS: rotate_rows_kernel<APPEND, MODE_PAIRS><<<grid, kPosThreads, smem, st>>>(p); break;
-    case MODE_SLOW_HALF: rotate_rows_kernel<APPEND, MODE_SLOW_HALF><<<grid, kPosThreads, smem, st>>>(p); break;
-    default: rotate_rows_kernel<APPEND, MODE_SLOW_PAIRS><<<grid, kPosThreads, smem, st>>>(p); break;
-  }
-  TWIST_LAUNCH_CHECK();
+  void (*kernel)(PosParams) = mode == MODE_HALF ? rotate_rows_kernel<APPEND, MODE_HALF>
+                              : mode == MODE_PAIRS ? rotate_rows_kernel<APPEND, MODE_PAIRS>
+                              : mode == MODE_SLOW_HALF ? rotate_rows_kernel<APPEND, MODE_SLOW_HALF>
+                                                       : rotate_rows_kernel<APPEND, MODE_SLOW_PAIRS>;
+  TWIST_CUDA_TRY(launch_overlapped(kernel, dim3(grid), dim3(kPosThreads), smem, st, p));
   return TWIST_OK;
 }
 

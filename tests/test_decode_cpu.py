@@ -119,6 +119,8 @@ def test_layout_checks_of_the_python_side(B):
     with pytest.raises(ValueError):
         B._rows("q", qkv[..., :32].float(), 2, 5, 32)
     with pytest.raises(ValueError):
-        B._tensor("kv_len", torch.zeros(3, dtype=torch.int64), torch.int32, 3)
+        B._tensor("kv_len", torch.zeros(3, dtype=torch.int64), torch.int32, 3, -1)
     with pytest.raises(ValueError):
-        B._tensor("kv_len", torch.zeros(6, dtype=torch.int32)[::2], torch.int32, 3)
+        B._tensor("kv_len", torch.zeros(6, dtype=torch.int32)[::2], torch.int32, 3, -1)
+    with pytest.raises(ValueError):
+        B._tensor("kv_len", torch.zeros(3, dtype=torch.int32), torch.int32, 3, 0)      # not on the current device
