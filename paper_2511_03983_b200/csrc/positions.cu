@@ -10,6 +10,10 @@
 // reduced to a fraction of a turn there: at position 10^6 an fp32 product would be off by 0.06 rad.  The fraction, at
 // most half a turn, is exact to 2^-25 in fp32, and sincospif takes it from there.
 //
+// Bytes in flight and instructions.  A thread takes a unit (below) in kBatch rows at once: the index arithmetic of a unit is
+// done once for them and their loads are in flight together.  The loads do not depend on the angles, so a thread issues
+// its first ones before the CTA finds positions and angles.
+//
 // Rotation.  A thread's unit of work owns both elements of every pair it rotates, so rotating in place is safe without
 // any ordering between threads: in the HALF layout a unit is two 16-byte chunks half a rotation apart, in the PAIRS
 // layout one 16-byte chunk; where chunks would straddle the halves (rot_dims/2 or rot_dims not a multiple of 8) a unit
@@ -21,7 +25,8 @@ namespace twist {
 namespace {
 
 constexpr int kPosThreads = 256;
-constexpr int kMaxRows = 8;            // token rows of a tile
+constexpr int kMaxRows = 16;           // token rows of a tile
+constexpr int kBatch = 4;              // rows that a thread has in flight
 constexpr int kMaxHead = 256;
 constexpr double kInvTwoPi = 0.15915494309189533577;
 
@@ -30,6 +35,16 @@ __device__ inline float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF000
 __device__ inline uint32_t pack2(float lo, float hi) {
   __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&t);
+}
+
+// n / d by a multiplication where that is exact (n (d - 1) < 2^32 for every n that occurs).
+struct Divisor {
+  uint32_t d, m;
+  __device__ uint32_t divide(uint32_t n) const { return m ? __umulhi(n, m) : n / d; }
+};
+Divisor divisor(uint32_t d, uint64_t max_n) {
+  const bool exact = d > 1 && max_n * (d - 1) < (1ull << 32);
+  return {d, exact ? (uint32_t)(((1ull << 32) + d - 1) / d) : 0u};
 }
 
 struct PosParams {
@@ -42,7 +57,8 @@ struct PosParams {
   int T, seq_len, heads, kv, dh, width;
   int rot, half;                 // half = rot / 2
   int tile_rows;
-  int units_per_head, head_units, chunk_units, row_units;   // rotated heads' units, then 8-element chunks of V
+  int units_per_head, first_unit, head_units, row_units;    // a row's units: those of its heads, then 8-element chunks of V
+  Divisor by_units, by_head, by_half, by_chunks;
   float sign;
   int in_place;
   // append
@@ -59,29 +75,40 @@ struct RowInfo {
   int pos, valid, held;
 };
 
-// Append: which token of which sequence row (s, t) is, and where it goes.  One warp per row (lane-parallel count of the
-// sequences that begin at or before t).
+// Append: which token of which sequence row (s, t) is, and where it goes.  One warp per row; two round trips: the
+// sequences' first rows and lengths (every lane keeps the last sequence of its that begins at or before t), the page.
 __device__ inline RowInfo find_row(const PosParams& p, long long r, int lane) {
   RowInfo ri;
-  ri.valid = 0; ri.pos = 0; ri.cache = 0; ri.held = 0;
+  ri.valid = 0; ri.pos = 0; ri.cache = 0; ri.held = -1;
   const int s = (int)(r / p.T), t = (int)(r - (long long)s * p.T);
-  int b, i, n;
+  const int32_t* lens = p.kv_len + (long long)s * p.n_seqs;
+  const int held = p.kv_count ? p.kv_count[s] : p.kv;
+  int b, i, n, len;
   if (p.new_begin) {
     const int32_t* nb = p.new_begin + (long long)s * (p.n_seqs + 1);
-    int c = 0;                                        // sequences 1 .. n_seqs (n_seqs: the end) that begin at or before t
-    for (int k = 1 + lane; k <= p.n_seqs; k += 32) c += nb[k] <= t;
-    for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-    b = c;
-    if (b >= p.n_seqs || t < nb[0]) return ri;        // a row behind the last sequence (or before the first)
-    i = t - nb[b];
-    n = nb[b + 1] - nb[b];
-    if (i < 0 || i >= n) {                            // not ascending
+    int at = -1, begin = 0, end = 0, count = 0;
+    len = 0;
+    for (int k = lane; k < p.n_seqs; k += 32) {
+      const int x = nb[k], y = nb[k + 1], l = lens[k];
+      if (x <= t) { at = k; begin = x; end = y; len = l; ++count; }
+    }
+    b = __reduce_max_sync(0xffffffffu, at);
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (b < 0) return ri;                             // a row before the first sequence
+    begin = __shfl_sync(0xffffffffu, begin, b & 31);
+    end = __shfl_sync(0xffffffffu, end, b & 31);
+    len = __shfl_sync(0xffffffffu, len, b & 31);
+    if (count != b + 1) {                             // not ascending
       if (lane == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
       return ri;
     }
+    if (t >= end) return ri;                          // a row behind the last sequence
+    i = t - begin;
+    n = end - begin;
   } else {
     b = t / p.rows_per_seq;
     i = t - b * p.rows_per_seq;
+    len = lens[b];
     n = p.new_len ? p.new_len[(long long)s * p.n_seqs + b] : p.rows_per_seq;
     if (n < 0 || n > p.rows_per_seq) {
       if (lane == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
@@ -89,11 +116,9 @@ __device__ inline RowInfo find_row(const PosParams& p, long long r, int lane) {
     }
     if (i >= n) return ri;
   }
-  const long long seq = (long long)s * p.n_seqs + b;
-  const long long pos = (long long)p.kv_len[seq] - n + i;
-  const long long page_slot = pos >> p.page_shift;
+  const long long pos = (long long)len - n + i, page_slot = pos >> p.page_shift;
   int page = -1;
-  if (pos >= 0 && page_slot < p.max_pages) page = p.page_table[seq * p.max_pages + page_slot];
+  if (pos >= 0 && page_slot < p.max_pages) page = p.page_table[((long long)s * p.n_seqs + b) * p.max_pages + page_slot];
   if ((unsigned)page >= (unsigned)p.n_pages) {
     if (lane == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
     return ri;
@@ -101,7 +126,7 @@ __device__ inline RowInfo find_row(const PosParams& p, long long r, int lane) {
   ri.valid = 1;
   ri.pos = (int)pos;
   ri.cache = page * p.page_stride + (pos & ((1 << p.page_shift) - 1)) * p.dh;
-  ri.held = p.kv_count ? min(p.kv, p.kv_count[s]) : p.kv;
+  ri.held = max(0, min(p.kv, held));
   return ri;
 }
 
@@ -128,19 +153,14 @@ __device__ inline void rotate_pairs(uint4& v, const float2* cs) {
 
 enum { MODE_HALF = 0, MODE_PAIRS = 1, MODE_SLOW_HALF = 2, MODE_SLOW_PAIRS = 3 };
 
-template <bool APPEND, int MODE>
-__global__ void __launch_bounds__(kPosThreads) rotate_rows_kernel(PosParams p) {
-  extern __shared__ float2 table[];                 // [tile_rows][half]
-  __shared__ RowInfo info[kMaxRows];
-  const long long row0 = (long long)blockIdx.x * p.tile_rows;
-  const int n_rows = (int)min((long long)p.tile_rows, p.rows - row0);
+// Positions (and, appending, destinations) of the tile's rows, then their (cos, sin) table.
+template <bool APPEND>
+__device__ inline void fill_table(const PosParams& p, float2* table, RowInfo* info, long long row0, int n_rows) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  griddep_launch_dependents();
-  griddep_wait();
   if constexpr (APPEND) {
-    if (warp < n_rows) {
-      const RowInfo ri = find_row(p, row0 + warp, lane);
-      if (lane == 0) info[warp] = ri;
+    for (int r = warp; r < n_rows; r += kPosThreads / 32) {
+      const RowInfo ri = find_row(p, row0 + r, lane);
+      if (lane == 0) info[r] = ri;
     }
   } else if (threadIdx.x < n_rows) {
     const long long r = row0 + threadIdx.x;
@@ -148,7 +168,7 @@ __global__ void __launch_bounds__(kPosThreads) rotate_rows_kernel(PosParams p) {
   }
   __syncthreads();
   for (int k = threadIdx.x; k < n_rows * p.half; k += kPosThreads) {
-    const int r = k / p.half, j = k - r * p.half;
+    const int r = (int)p.by_half.divide(k), j = k - r * p.half;
     double turns = (double)info[r].pos * (p.inv_freq[j] * kInvTwoPi);
     turns -= rint(turns);
     float s, c;
@@ -156,64 +176,88 @@ __global__ void __launch_bounds__(kPosThreads) rotate_rows_kernel(PosParams p) {
     table[k] = make_float2(c, p.sign * s);
   }
   __syncthreads();
-  const int total = n_rows * p.row_units;
-  for (int k = threadIdx.x; k < total; k += kPosThreads) {
-    const int r = k / p.row_units;
-    int u = k - r * p.row_units;
-    if (APPEND && !info[r].valid) continue;
-    const __nv_bfloat16* src = p.in + (row0 + r) * p.width;
-    if (APPEND && !p.out) u += p.heads * p.units_per_head;        // Q is not wanted
-    const float2* cs = table + r * p.half;
-    if (u < p.head_units) {
-      const int h = u / p.units_per_head, j = u - h * p.units_per_head;
-      src += h * p.dh;
-      __nv_bfloat16* dst;
-      if constexpr (APPEND) {
-        if (h < p.heads) {
-          dst = p.out + (row0 + r) * p.q_stride + h * p.dh;
-        } else {
-          if (h - p.heads >= info[r].held) continue;
-          dst = p.k_cache + info[r].cache + (((long long)(h - p.heads) * p.dh) << p.page_shift);
+}
+
+template <bool APPEND, int MODE>
+__global__ void __launch_bounds__(kPosThreads, 4) rotate_rows_kernel(PosParams p) {
+  extern __shared__ float2 table[];                 // [tile_rows][half]
+  __shared__ RowInfo info[kMaxRows];
+  constexpr bool SLOW = MODE == MODE_SLOW_HALF || MODE == MODE_SLOW_PAIRS;
+  const long long row0 = (long long)blockIdx.x * p.tile_rows;
+  const int n_rows = (int)min((long long)p.tile_rows, p.rows - row0), n_heads = p.heads + p.kv, pair_units = p.half / 8;
+  // work item: unit k % row_units of the rows kBatch * (k / row_units) ...
+  const uint32_t items = (uint32_t)((n_rows + kBatch - 1) / kBatch) * p.row_units;
+  griddep_launch_dependents();
+  griddep_wait();
+  for (uint32_t k = threadIdx.x; k < items || k == threadIdx.x; k += kPosThreads) {
+    const int batch = (int)p.by_units.divide(k), u = (int)k - batch * p.row_units + p.first_unit;
+    const int r0 = batch * kBatch, n = k < items ? min(kBatch, n_rows - r0) : 0;
+    // unit j of head h, or chunk j of V (h = n_heads): elements at .. at + 7 of it, and those half a rotation further
+    const int h = u < p.head_units ? (int)p.by_head.divide(u) : n_heads, j = u - (u < p.head_units ? h * p.units_per_head : p.head_units);
+    const bool pair = MODE == MODE_HALF && h < n_heads && j < pair_units;
+    const int at = MODE == MODE_HALF && h < n_heads && !pair ? p.rot + 8 * (j - pair_units) : 8 * j;
+    const __nv_bfloat16* src = p.in + (row0 + r0) * p.width + h * p.dh + at;
+    uint4 lo[kBatch], hi[kBatch];
+    if (!SLOW || h == n_heads) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (i < n) {
+          lo[i] = *reinterpret_cast<const uint4*>(src + (long long)i * p.width);
+          if (pair) hi[i] = *reinterpret_cast<const uint4*>(src + (long long)i * p.width + p.half);
         }
-      } else {
-        dst = p.out + (row0 + r) * p.width + h * p.dh;
       }
-      if constexpr (MODE == MODE_HALF) {
-        const int pair_units = p.half / 8;
-        if (j < pair_units) {
-          uint4 lo = *reinterpret_cast<const uint4*>(src + 8 * j);
-          uint4 hi = *reinterpret_cast<const uint4*>(src + p.half + 8 * j);
-          rotate8(lo, hi, cs + 8 * j);
-          *reinterpret_cast<uint4*>(dst + 8 * j) = lo;
-          *reinterpret_cast<uint4*>(dst + p.half + 8 * j) = hi;
-        } else {
-          const int at = p.rot + 8 * (j - pair_units);
-          *reinterpret_cast<uint4*>(dst + at) = *reinterpret_cast<const uint4*>(src + at);
-        }
-      } else if constexpr (MODE == MODE_PAIRS) {
-        uint4 v = *reinterpret_cast<const uint4*>(src + 8 * j);
-        if (8 * j < p.rot) rotate_pairs(v, cs + 4 * j);
-        *reinterpret_cast<uint4*>(dst + 8 * j) = v;
+    }
+    if (k == threadIdx.x) fill_table<APPEND>(p, table, info, row0, n_rows);
+    // where the unit's rows go: a row's own place (q_stride / width apart) or its slot in the cache
+    __nv_bfloat16* dst;
+    int group = -1;                                 // appending: KV position of the unit, -1: Q
+    if constexpr (APPEND) {
+      if (h < p.heads) {
+        dst = p.out + (row0 + r0) * p.q_stride + h * p.dh + at;
+      } else if (h < n_heads) {
+        group = h - p.heads;
+        dst = p.k_cache + (((long long)group * p.dh) << p.page_shift) + at;
       } else {
-        for (int q = 0; q < p.half; ++q) {
-          const int ix = MODE == MODE_SLOW_HALF ? q : 2 * q, iy = MODE == MODE_SLOW_HALF ? q + p.half : 2 * q + 1;
-          const float x = __bfloat162float(src[ix]), y = __bfloat162float(src[iy]);
-          const float2 c = cs[q];
-          dst[ix] = __float2bfloat16(x * c.x - y * c.y);
-          dst[iy] = __float2bfloat16(x * c.y + y * c.x);
-        }
-        for (int e = p.rot; e < p.dh; ++e) dst[e] = src[e];
+        group = (int)p.by_chunks.divide(j);
+        dst = p.v_cache + (((long long)group * p.dh) << p.page_shift) + (8 * j - group * p.dh);
       }
     } else {
-      const int c = u - p.head_units, at = (p.heads + p.kv) * p.dh + 8 * c;        // a chunk of V
-      const uint4 v = *reinterpret_cast<const uint4*>(src + at);
+      dst = p.out + (row0 + r0) * p.width + h * p.dh + at;
+    }
+    const long long step = APPEND ? p.q_stride : p.width;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (i >= n) continue;
+      const int r = r0 + i;
+      __nv_bfloat16* to = dst + i * step;
       if constexpr (APPEND) {
-        const int g = 8 * c / p.dh, e = 8 * c - g * p.dh;
-        if (g >= info[r].held) continue;
-        *reinterpret_cast<uint4*>(p.v_cache + info[r].cache + (((long long)g * p.dh) << p.page_shift) + e) = v;
-      } else {
-        *reinterpret_cast<uint4*>(p.out + (row0 + r) * p.width + at) = v;
+        const RowInfo ri = info[r];
+        if (group >= ri.held) continue;             // not held, or a row of no sequence (held = -1)
+        if (group >= 0) to = dst + ri.cache;
+        else if (!ri.valid) continue;
       }
+      const float2* cs = table + r * p.half;
+      if constexpr (SLOW) {
+        if (h < n_heads) {
+          const __nv_bfloat16* x = p.in + (row0 + r) * p.width + h * p.dh;
+          for (int q = 0; q < p.half; ++q) {
+            const int ix = MODE == MODE_SLOW_HALF ? q : 2 * q, iy = MODE == MODE_SLOW_HALF ? q + p.half : 2 * q + 1;
+            const float a = __bfloat162float(x[ix]), b = __bfloat162float(x[iy]);
+            const float2 c = cs[q];
+            to[ix] = __float2bfloat16(a * c.x - b * c.y);
+            to[iy] = __float2bfloat16(a * c.y + b * c.x);
+          }
+          for (int e = p.rot; e < p.dh; ++e) to[e] = x[e];
+          continue;
+        }
+      }
+      if (MODE == MODE_HALF && pair) {
+        rotate8(lo[i], hi[i], cs + at);
+        *reinterpret_cast<uint4*>(to + p.half) = hi[i];
+      } else if (MODE == MODE_PAIRS && h < n_heads && at < p.rot) {
+        rotate_pairs(lo[i], cs + at / 2);
+      }
+      *reinterpret_cast<uint4*>(to) = lo[i];
     }
   }
 }
@@ -225,22 +269,24 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
   else mode = p.rot % 8 == 0 ? MODE_PAIRS : MODE_SLOW_PAIRS;
   if (p.rot == 0) mode = MODE_PAIRS;                                                    // plain 16-byte chunks
   p.units_per_head = mode == MODE_HALF ? p.half / 8 + (p.dh - p.rot) / 8 : mode == MODE_PAIRS ? p.dh / 8 : 1;
+  p.first_unit = APPEND && !p.out ? p.heads * p.units_per_head : 0;                     // Q is not wanted
   p.head_units = (p.heads + p.kv) * p.units_per_head;
-  p.chunk_units = p.kv * p.dh / 8;
-  p.row_units = p.head_units + (APPEND || !p.in_place ? p.chunk_units : 0);
-  if (APPEND && !p.out) p.row_units -= p.heads * p.units_per_head;
+  p.row_units = p.head_units - p.first_unit + (APPEND || !p.in_place ? p.kv * p.dh / 8 : 0);
   // Rows of a tile: as many as still give every SM several tiles.
-  const long long want = p.rows / ((long long)sm_count() * 8);
+  const long long want = p.rows / ((long long)sm_count() * 4);
   p.tile_rows = (int)(want < 1 ? 1 : (want > kMaxRows ? kMaxRows : want));
   const long long tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
   if (tiles > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
-  const size_t smem = (size_t)p.tile_rows * p.half * sizeof(float2);                    // at most 8 KB
-  const unsigned grid = (unsigned)tiles;
+  p.by_units = divisor((uint32_t)p.row_units, (uint64_t)((p.tile_rows + kBatch - 1) / kBatch) * p.row_units + kPosThreads);
+  p.by_head = divisor((uint32_t)p.units_per_head, (uint64_t)p.head_units);
+  p.by_half = divisor((uint32_t)(p.half > 0 ? p.half : 1), (uint64_t)p.tile_rows * p.half);
+  p.by_chunks = divisor((uint32_t)(p.dh / 8), (uint64_t)p.kv * p.dh / 8);
+  const size_t smem = (size_t)p.tile_rows * p.half * sizeof(float2);                    // at most 16 KB
   void (*kernel)(PosParams) = mode == MODE_HALF ? rotate_rows_kernel<APPEND, MODE_HALF>
                               : mode == MODE_PAIRS ? rotate_rows_kernel<APPEND, MODE_PAIRS>
                               : mode == MODE_SLOW_HALF ? rotate_rows_kernel<APPEND, MODE_SLOW_HALF>
                                                        : rotate_rows_kernel<APPEND, MODE_SLOW_PAIRS>;
-  TWIST_CUDA_TRY(launch_overlapped(kernel, dim3(grid), dim3(kPosThreads), smem, st, p));
+  TWIST_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)tiles), dim3(kPosThreads), smem, st, p));
   return TWIST_OK;
 }
 
