@@ -10,9 +10,11 @@
 // reduced to a fraction of a turn there: at position 10^6 an fp32 product would be off by 0.06 rad.  The fraction, at
 // most half a turn, is exact to 2^-25 in fp32, and sincospif takes it from there.
 //
-// Bytes in flight and instructions.  A thread takes a unit (below) in kBatch rows at once: the index arithmetic of a unit is
-// done once for them and their loads are in flight together.  The loads do not depend on the angles, so a thread issues
-// its first ones before the CTA finds positions and angles.
+// Bytes in flight and instructions.  A thread takes a unit (below) in several rows at once: the index arithmetic of a unit
+// is done once for them and their loads are in flight together.  Rotating, a thread holds 128 bytes and issues its first
+// loads before the CTA finds positions and angles, on which they do not depend.  Appending, finding a row's place costs
+// two dependent round trips, and rows of no sequence are not read: the places come first and more, lighter CTAs share an
+// SM to cover them (44 000 packed rows of 4.6 KB: 134 us loads first, 4 CTAs an SM; 116 us places first, 6 CTAs).
 //
 // Rotation.  A thread's unit of work owns both elements of every pair it rotates, so rotating in place is safe without
 // any ordering between threads: in the HALF layout a unit is two 16-byte chunks half a rotation apart, in the PAIRS
@@ -25,8 +27,7 @@ namespace twist {
 namespace {
 
 constexpr int kPosThreads = 256;
-constexpr int kMaxRows = 16;           // token rows of a tile
-constexpr int kBatch = 4;              // rows that a thread has in flight
+constexpr int kMaxRows = 8;            // token rows of a tile
 constexpr int kMaxHead = 256;
 constexpr double kInvTwoPi = 0.15915494309189533577;
 
@@ -153,6 +154,9 @@ __device__ inline void rotate_pairs(uint4& v, const float2* cs) {
 
 enum { MODE_HALF = 0, MODE_PAIRS = 1, MODE_SLOW_HALF = 2, MODE_SLOW_PAIRS = 3 };
 
+// Rows that a thread has in flight (see above).
+__host__ __device__ constexpr int batch_rows(bool append, int mode) { return (mode == MODE_PAIRS ? 8 : 4) / (append ? 2 : 1); }
+
 // Positions (and, appending, destinations) of the tile's rows, then their (cos, sin) table.
 template <bool APPEND>
 __device__ inline void fill_table(const PosParams& p, float2* table, RowInfo* info, long long row0, int n_rows) {
@@ -179,17 +183,19 @@ __device__ inline void fill_table(const PosParams& p, float2* table, RowInfo* in
 }
 
 template <bool APPEND, int MODE>
-__global__ void __launch_bounds__(kPosThreads, 4) rotate_rows_kernel(PosParams p) {
+__global__ void __launch_bounds__(kPosThreads, APPEND ? 6 : 4) rotate_rows_kernel(PosParams p) {
   extern __shared__ float2 table[];                 // [tile_rows][half]
   __shared__ RowInfo info[kMaxRows];
   constexpr bool SLOW = MODE == MODE_SLOW_HALF || MODE == MODE_SLOW_PAIRS;
+  constexpr int kBatch = batch_rows(APPEND, MODE);
   const long long row0 = (long long)blockIdx.x * p.tile_rows;
   const int n_rows = (int)min((long long)p.tile_rows, p.rows - row0), n_heads = p.heads + p.kv, pair_units = p.half / 8;
   // work item: unit k % row_units of the rows kBatch * (k / row_units) ...
   const uint32_t items = (uint32_t)((n_rows + kBatch - 1) / kBatch) * p.row_units;
   griddep_launch_dependents();
   griddep_wait();
-  for (uint32_t k = threadIdx.x; k < items || k == threadIdx.x; k += kPosThreads) {
+  if (APPEND) fill_table<APPEND>(p, table, info, row0, n_rows);
+  for (uint32_t k = threadIdx.x; k < items || (!APPEND && k == threadIdx.x); k += kPosThreads) {
     const int batch = (int)p.by_units.divide(k), u = (int)k - batch * p.row_units + p.first_unit;
     const int r0 = batch * kBatch, n = k < items ? min(kBatch, n_rows - r0) : 0;
     // unit j of head h, or chunk j of V (h = n_heads): elements at .. at + 7 of it, and those half a rotation further
@@ -201,13 +207,13 @@ __global__ void __launch_bounds__(kPosThreads, 4) rotate_rows_kernel(PosParams p
     if (!SLOW || h == n_heads) {
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        if (i < n) {
+        if (i < n && (!APPEND || info[r0 + i].valid)) {
           lo[i] = *reinterpret_cast<const uint4*>(src + (long long)i * p.width);
           if (pair) hi[i] = *reinterpret_cast<const uint4*>(src + (long long)i * p.width + p.half);
         }
       }
     }
-    if (k == threadIdx.x) fill_table<APPEND>(p, table, info, row0, n_rows);
+    if (!APPEND && k == threadIdx.x) fill_table<APPEND>(p, table, info, row0, n_rows);
     // where the unit's rows go: a row's own place (q_stride / width apart) or its slot in the cache
     __nv_bfloat16* dst;
     int group = -1;                                 // appending: KV position of the unit, -1: Q
@@ -277,7 +283,7 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
   p.tile_rows = (int)(want < 1 ? 1 : (want > kMaxRows ? kMaxRows : want));
   const long long tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
   if (tiles > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
-  p.by_units = divisor((uint32_t)p.row_units, (uint64_t)((p.tile_rows + kBatch - 1) / kBatch) * p.row_units + kPosThreads);
+  p.by_units = divisor((uint32_t)p.row_units, (uint64_t)((p.tile_rows + batch_rows(APPEND, mode) - 1) / batch_rows(APPEND, mode)) * p.row_units + kPosThreads);
   p.by_head = divisor((uint32_t)p.units_per_head, (uint64_t)p.head_units);
   p.by_half = divisor((uint32_t)(p.half > 0 ? p.half : 1), (uint64_t)p.tile_rows * p.half);
   p.by_chunks = divisor((uint32_t)(p.dh / 8), (uint64_t)p.kv * p.dh / 8);
