@@ -584,6 +584,29 @@ def attn_core_bwd(dA, QKV, n_seqs, seq_len, d_head, head_kv, kv_width, lowp):
 
 
 # ----------------------------------------------------------------------------------------
+# Rotation by position (an extension; the paper's attention has no positions of its own): pair j of
+# every Q and K head of a token at position t of its sequence is turned by the angle t * base^(-2j / dims).
+# The layout names the pairs: 0: elements (j, j + dims/2), 1: elements (2j, 2j + 1).  The backward pass
+# turns the gradient by the opposite angle (the transpose of a rotation).
+# ----------------------------------------------------------------------------------------
+
+def rope(QKV, seq_len, d_head, kv_width, base, dims, layout, lowp, sign=1.0, first=0):
+    """QKV [T, a' + 2 kvw] with its Q and K columns rotated; row t is at position first + t % seq_len."""
+    T, width = QKV.shape
+    out = np.array(QKV, dtype=np.float64)
+    pos = first + np.arange(T) % seq_len
+    for head in range((width - kv_width) // d_head):
+        for j in range(dims // 2):
+            i0, i1 = (j, j + dims // 2) if layout == 0 else (2 * j, 2 * j + 1)
+            c0, c1 = head * d_head + i0, head * d_head + i1
+            ang = sign * pos * base ** (-2.0 * j / dims)
+            x, y = QKV[:, c0].astype(np.float64), QKV[:, c1].astype(np.float64)
+            out[:, c0] = x * np.cos(ang) - y * np.sin(ang)
+            out[:, c1] = x * np.sin(ang) + y * np.cos(ang)
+    return _q(out, lowp)
+
+
+# ----------------------------------------------------------------------------------------
 # STACK composition: the chained transformer of App. A (Transformer Layer Architecture),
 # without layer normalisation, biases and embeddings (not on this path):
 #   x <- x + alpha_a * Concat(heads) C^attn ;  x <- x + alpha_f * FFN(x)   for every layer,
@@ -612,6 +635,8 @@ def stack_fwd(spec, layers, head_kv, X0, n_seqs, seq_len, lowp):
         else:
             x_a = x
         QKV = qkv_fwd(x_a, W["qkv"], lowp)
+        if getattr(spec, "rope_base", 0) > 0:
+            QKV = rope(QKV, seq_len, spec.d_head, kvw, spec.rope_base, spec.rot_dims, spec.rope_layout, lowp)
         A = attn_core_fwd(QKV, n_seqs, seq_len, spec.d_head, head_kv[l], kvw, lowp)
         x_mid = o_fwd(A, W["o"], alpha_a, lowp, residual=x)
         if "ln_f_g" in W:
@@ -646,6 +671,8 @@ def stack_bwd(spec, layers, head_kv, saved, dX, n_seqs, seq_len, lowp):
                                             spec.ffn_kind, alpha_f, lowp, residual=dx)
         dA, dWo = o_bwd(dx_mid, sv["A"], W["o"], alpha_a, lowp)
         dQKV = attn_core_bwd(dA, sv["QKV"], n_seqs, seq_len, spec.d_head, head_kv[l], sv["kvw"], lowp)
+        if getattr(spec, "rope_base", 0) > 0:
+            dQKV = rope(dQKV, seq_len, spec.d_head, sv["kvw"], spec.rope_base, spec.rot_dims, spec.rope_layout, lowp, sign=-1.0)
         if "ln_a" in sv:
             d_a, dWq = qkv_bwd(dQKV, sv["x_a"], W["qkv"], lowp)
             dx, g["ln_a_g"], g["ln_a_b"] = layer_norm_bwd(d_a, sv["ln_a"], W["ln_a_g"], lowp, residual=dx_mid)

@@ -20,7 +20,7 @@ from __future__ import annotations
 import math
 from contextlib import contextmanager
 from functools import partial
-from typing import Dict, List, Optional, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -897,6 +897,14 @@ class ShardedRoundEngine(RoundEngine):
         self.aggregate_finish(l, live, which)
 
 
+def rope_frequencies(w: Workload, device) -> Optional[torch.Tensor]:
+    """fp64 frequencies base^(-2j / dims), j < dims / 2, of a workload that rotates by position; None for one that does not."""
+    if w.rot_dims == 0:
+        return None
+    assert 0 < w.rot_dims <= w.d_head and w.rot_dims % 2 == 0
+    return torch.tensor([w.rope_base ** (-2.0 * j / w.rot_dims) for j in range(w.rot_dims // 2)], dtype=torch.float64, device=device)
+
+
 class StackEngine(RoundEngine):
     """One TwIST round in the chained (STACK) composition: every local step runs all layers,
     x <- x + alpha_a * O(core(QKV(LN_a(x)))),  x <- x + alpha_f * FFN(LN_f(x)),  with one loss on the final x
@@ -906,6 +914,8 @@ class StackEngine(RoundEngine):
     this engine is for the stack-shaped workloads whose activations fit; the streamed RoundEngine
     covers the per-block workloads.  Like RoundEngine it only allocates buffers and calls the C ABI.
     The normalised activations are not kept: the backward pass forms them again from the saved inputs.
+    With Workload.rope_base set, Q and K are rotated by position between the projection and the core (and the gradient
+    back behind it); extracted subnets then answer token by token through DecodeSession.
     """
 
     def __init__(self, w: Workload, n_seqs: int, seq_len: int, device: str = "cuda", keep_f32_full: bool = False):
@@ -939,6 +949,7 @@ class StackEngine(RoundEngine):
         self.grad = [act(d), act(d)]            # gradient w.r.t. the residual stream (ping-pong)
         self.stack_loss = torch.zeros(max(1, w.local_steps), S, dtype=torch.float32, device=dev)
         self.gqa = w.n_kv_heads != w.n_heads
+        self.inv_freq = rope_frequencies(w, dev)
         # layer normalisation (App. A): shared parameters, one copy per worker and layer, statistics per token
         self.ln = w.layer_norm
         if self.ln:
@@ -958,6 +969,14 @@ class StackEngine(RoundEngine):
         self._use(l)
         for n, t in self.slices[l].items():
             setattr(self, n, t)
+
+    def _rope(self, call, qkv):
+        """Rotates the Q and K columns of the bound geometry's projected activations in place (call: fwd or bwd)."""
+        w = self.w
+        with self._timed("rope"):
+            call(B.rope_args(w.dtype, w.n_subnets, w.tokens, self.head_keep, self.kv_max, w.d_head, w.rot_dims, self.seq_len,
+                             w.rope_layout, in_=qkv, out=qkv, inv_freq=self.inv_freq))
+        self.launches += 1
 
     def _core_args(self, l: int, **t):
         w = self.w
@@ -1019,6 +1038,8 @@ class StackEngine(RoundEngine):
             with self._timed("qkv_fwd"):
                 B.twist_subnet_attn_proj_fwd(self._proj_args(B.PROJ_QKV, w.dtype, S, T, d, self.nq, 1.0, 0.0, in_=x_a,
                                                          w=self.w_qkv, out=self.qkv_l[l]))
+            if self.inv_freq is not None:
+                self._rope(B.twist_rope_fwd, self.qkv_l[l])
             with self._timed("core_fwd"):
                 B.twist_attn_core_fwd(self._core_args(l, qkv=self.qkv_l[l], out=self.a_l[l], lse=self.lse[l]))
             with self._timed("o_fwd"):
@@ -1067,6 +1088,8 @@ class StackEngine(RoundEngine):
             with self._timed("core_bwd"):
                 B.twist_attn_core_bwd(self._core_args(l, qkv=self.qkv_l[l], out=self.a_l[l], lse=self.lse[l],
                                                       d_out=self.da, d_qkv=self.dqkv, delta=self.delta))
+            if self.inv_freq is not None:
+                self._rope(B.twist_rope_bwd, self.dqkv)
             x_a = self.x[l]
             if self.ln:
                 self._ln_fwd(l, "a", self.x[l], self.x_ln)
@@ -1126,3 +1149,137 @@ class StackEngine(RoundEngine):
             self.aggregate_layer(l)
             if self.ln:
                 self.aggregate_ln(l)
+
+
+class DecodeSession:
+    """Deployment (Sec. 4.2) token by token: the S subnets that StackEngine.extract gathered run forward on one new token
+    per sequence, reading the earlier tokens' keys and values from a paged cache instead of computing them again.
+
+    Every layer has a pool of pages [n_pages][kv_max][page_size][d_head] for K and one for V; one page table serves all
+    layers.  The host keeps the lengths and the free pages; like the engines the session only allocates buffers and calls
+    the C ABI.  prefill(k) runs the engine's own forward pass over its batch k (n_seqs sequences of seq_len tokens, the
+    first lengths[s][b] of which count) and stores their keys and values; step(x) takes the next token's input [S][n_seqs][d]
+    and returns the stack's output for it.  A session belongs to one stream; its cache is its own, the slices are the
+    engine's: extracting other subnets ends it."""
+
+    def __init__(self, eng: StackEngine, max_len: int, page_size: int = 16, n_pages: Optional[int] = None):
+        w = eng.w
+        S, n, d, bf, dev = w.n_subnets, eng.n_seqs, w.d_model, torch.bfloat16, eng.dev
+        if max_len < 1:
+            raise ValueError("max_len %d" % max_len)
+        self.eng, self.S, self.n, self.page_size = eng, S, n, page_size
+        self.max_pages = -(-max_len // page_size)
+        self.max_len = max_len
+        self.n_pages = S * n * self.max_pages if n_pages is None else n_pages
+        geo = [eng.geo[eng.kind_of(l)] for l in range(w.n_layers)]
+        pool = lambda gm: torch.zeros(self.n_pages, 2, gm.kv_max, page_size, w.d_head, dtype=bf, device=dev)
+        self.pools = [pool(gm) for gm in geo]                       # K and V of a page side by side
+        self.free = list(range(self.n_pages - 1, -1, -1))           # pages of the pool that no sequence holds
+        self.lens = [[0] * n for _ in range(S)]
+        self.pages: List[List[List[int]]] = [[[] for _ in range(n)] for _ in range(S)]
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.page_table = torch.zeros(S, n, self.max_pages, **i32)
+        self.kv_len = torch.zeros(S, n, **i32)
+        self.new_len = torch.zeros(S, n, **i32)
+        act = lambda width: torch.empty(S, n, width, dtype=bf, device=dev)
+        self.x = [act(d), act(d)]
+        self.x_mid = act(d)
+        per = lambda width: {kind: act(width(gm)) for kind, gm in eng.geo.items()}
+        self.qkv, self.a = per(lambda gm: gm.nq), per(lambda gm: gm.a_sub)
+        self.pre, self.hh = per(lambda gm: gm.gf), per(lambda gm: gm.f_sub)
+        self.ws = torch.empty(B.twist_attn_decode_workspace_bytes(w.d_head), dtype=torch.uint8, device=dev)
+        if eng.ln:
+            self.x_ln = act(d)
+            self.stat = [torch.empty(S, n, dtype=torch.float32, device=dev) for _ in range(2)]
+
+    def _extend(self, new):
+        """Room for new[s][b] more tokens: pages from the free list, lengths and page table to the device."""
+        need = 0
+        for s in range(self.S):
+            for b in range(self.n):
+                total = self.lens[s][b] + new[s][b]
+                if new[s][b] < 0 or total > self.max_len:
+                    raise ValueError("sequence (%d, %d): %d + %d tokens, max_len is %d" % (s, b, self.lens[s][b], new[s][b], self.max_len))
+                need += max(0, -(-total // self.page_size) - len(self.pages[s][b]))
+        if need > len(self.free):
+            raise RuntimeError("cache is full: %d pages needed, %d free" % (need, len(self.free)))
+        grown = False
+        for s in range(self.S):
+            for b in range(self.n):
+                self.lens[s][b] += new[s][b]
+                while len(self.pages[s][b]) * self.page_size < self.lens[s][b]:
+                    self.pages[s][b].append(self.free.pop())
+                    grown = True
+        if grown:
+            rows = [[p + [0] * (self.max_pages - len(p)) for p in row] for row in self.pages]
+            self.page_table.copy_(torch.tensor(rows, dtype=torch.int32))
+        self.kv_len.copy_(torch.tensor(self.lens, dtype=torch.int32))
+
+    def release(self, s: int, b: int):
+        """Forgets a sequence: its pages are free again, its next token is its first."""
+        self.free.extend(reversed(self.pages[s][b]))
+        self.pages[s][b], self.lens[s][b] = [], 0
+        self.kv_len.copy_(torch.tensor(self.lens, dtype=torch.int32))
+
+    def _cache(self, l: int):
+        return dict(k_cache=self.pools[l][:, 0], v_cache=self.pools[l][:, 1], page_table=self.page_table, kv_len=self.kv_len)
+
+    def prefill(self, k: int, lengths: Optional[Sequence[Sequence[int]]] = None) -> torch.Tensor:
+        """The prompts: the engine's forward pass over its batch k.  Sequences must be empty.  Returns the stack's outputs
+        [S][T][d] (rows behind a sequence's length mean nothing)."""
+        eng, w = self.eng, self.eng.w
+        lengths = [[eng.seq_len] * self.n for _ in range(self.S)] if lengths is None else [list(r) for r in lengths]
+        if any(m for row in self.lens for m in row):
+            raise ValueError("prefill of sequences that hold tokens already")
+        if len(lengths) != self.S or any(len(r) != self.n or max(r) > eng.seq_len for r in lengths):
+            raise ValueError("lengths: %d x %d values up to %d are expected" % (self.S, self.n, eng.seq_len))
+        self._extend(lengths)
+        self.new_len.copy_(torch.tensor(lengths, dtype=torch.int32))
+        eng.forward(k)
+        for l in range(w.n_layers):
+            eng._bind(l)
+            # the saved projections are rotated already
+            with eng._timed("append"):
+                B.twist_kv_append(B.kv_append_args(w.dtype, self.S, self.n, w.tokens, eng.head_keep, eng.kv_max, w.d_head,
+                                                   qkv=eng.qkv_l[l], new_len=self.new_len, kv_count=eng.kv_count[l],
+                                                   **self._cache(l)))
+            eng.launches += 1
+        return eng.x[w.n_layers]
+
+    def _ln(self, l: int, which: str, x, y):
+        w, p = self.eng.w, self.eng.ln_w[l]
+        B.twist_layernorm_fwd(B.layernorm_args(w.dtype, self.S, self.n, w.d_model, w.ln_eps, 0.0, x=x, y=y, mean=self.stat[0],
+                                               rstd=self.stat[1], gamma=p[f"ln_{which}_g"], beta=p[f"ln_{which}_b"]))
+        self.eng.launches += 1
+        return y
+
+    def step(self, x: torch.Tensor) -> torch.Tensor:
+        """The next token of every sequence, its input x [S][n_seqs][d]; returns the stack's output (valid until the next
+        step)."""
+        eng, w, S, n, d = self.eng, self.eng.w, self.S, self.n, self.eng.w.d_model
+        self._extend([[1] * n for _ in range(S)])
+        cur, nxt = self.x
+        cur.copy_(x)
+        for l in range(w.n_layers):
+            eng._bind(l)
+            kind = eng.kind_of(l)
+            qkv, a = self.qkv[kind], self.a[kind]
+            q = qkv[..., :eng.a_sub]
+            x_a = self._ln(l, "a", cur, self.x_ln) if eng.ln else cur
+            B.twist_subnet_attn_proj_fwd(eng._proj_args(B.PROJ_QKV, w.dtype, S, n, d, eng.nq, 1.0, 0.0, in_=x_a, w=eng.w_qkv, out=qkv))
+            with eng._timed("append"):
+                B.twist_kv_append(B.kv_append_args(w.dtype, S, n, n, eng.head_keep, eng.kv_max, w.d_head, w.rot_dims, w.rope_layout,
+                                                   qkv=qkv, q_out=q, inv_freq=eng.inv_freq, kv_count=eng.kv_count[l], **self._cache(l)))
+            share = dict(head_idx=eng.idx_head[l], kv_pos=eng.kv_pos[l]) if eng.gqa else {}
+            with eng._timed("decode"):
+                B.twist_attn_decode(B.attn_decode_args(w.dtype, S, n, eng.head_keep, eng.kv_max, w.d_head, w.n_heads, w.n_kv_heads,
+                                                       self.max_len, q=q, out=a, ws=self.ws, **share, **self._cache(l)))
+            B.twist_subnet_attn_proj_fwd(eng._proj_args(B.PROJ_O, w.dtype, S, n, d, eng.a_sub, eng.alpha_a, 0.0, in_=a, w=eng.w_o,
+                                                        out=self.x_mid, out_residual=cur))
+            x_f = self._ln(l, "f", self.x_mid, self.x_ln) if eng.ln else self.x_mid
+            B.twist_subnet_ffn_fwd(eng._ffn_args(w.ffn_kind, w.dtype, S, n, d, eng.f_sub, eng.alpha_f, 0.0, x=x_f, w_gu=eng.w_gu,
+                                                 w_down=eng.w_down, pre=self.pre[kind], hh=self.hh[kind], y=nxt,
+                                                 y_residual=self.x_mid))
+            eng.launches += 7
+            cur, nxt = nxt, cur
+        return cur

@@ -59,6 +59,9 @@ class Workload:
     shared_layers: Tuple[int, ...] = field(default_factory=tuple)   # layers every worker holds whole (N_sub = N_full)
     layer_norm: bool = False   # chained composition only: the two layer normalisations of the pre-LN layer
     ln_eps: float = 1e-5
+    rope_base: float = 0.0     # chained composition only: rotate Q and K by position, frequencies base^(-2j / dims); 0: off
+    rope_dims: int = 0         # rotated elements of a head (0: all of them)
+    rope_layout: int = 0       # 0: pairs (j, j + dims / 2) of a head, 1: pairs (2j, 2j + 1)
 
     @property
     def n_ffn_blocks(self) -> int:
@@ -71,6 +74,10 @@ class Workload:
     @property
     def a_sub(self) -> int:           # a' = H' * d_head
         return self.head_keep * self.d_head
+
+    @property
+    def rot_dims(self) -> int:        # elements of a head that the rotation by position turns (0: no rotation)
+        return (self.rope_dims or self.d_head) if self.rope_base > 0 else 0
 
     @property
     def nmat(self) -> int:
