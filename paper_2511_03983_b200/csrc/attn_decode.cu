@@ -22,8 +22,13 @@
 // takes the w-th G-th of the line, whatever the lengths are: a ragged batch is balanced on the device, and a warp's loads
 // run on across the borders of items (an item: the tiles of one KV position of one sequence).  A warp writes the items it
 // has whole; of an item that a border between warps cuts, every warp writes its unnormalised part (fp32 sums, maximum,
-// sum) to the workspace, and a second small launch joins the parts in the order of the warps.  Calls so small that
-// latency is all they cost run one CTA per item instead, whose warps join in shared memory (one launch).
+// sum) to the workspace, and a second small launch joins the parts in the order of the warps.
+//
+// Calls whose length and number of items leave little to balance take a shorter way instead: one cluster of 1 to 8 CTAs
+// per item, whose warps take the item's tiles in turn and join through (distributed) shared memory: one launch, no
+// workspace.
+#include <cooperative_groups.h>
+
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -37,6 +42,8 @@ constexpr int kMaxCtasPerSm = 4;
 constexpr int kItemCost = 1;               // what changing to the next item costs a warp, in tiles
 constexpr int kMinCost = 2;                // least work of a warp, in tiles
 constexpr int kJoinThreads = 512;
+// The short way, one cluster per item (see run).
+constexpr int kMaxCluster = 8, kShortTiles = 6, kShortWork = 6;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.0f;             // log2 headroom of the lazily moved reference maximum
@@ -145,46 +152,122 @@ __device__ inline int check_pages(const DecParams& p, int id, int last_key, int 
   return id;
 }
 
-// The tile that begins at key0 <= last_key, number n of its window of page ids.  Rows behind the sequence's end are
-// replaced by rows before it: whatever lies in the unused part of a page must not reach the products, and the scores
-// of such rows are masked anyway.
+// Rows behind a sequence's end must not reach the products, whatever they hold.  Two ways.  CLAMP: they are replaced by rows
+// before it, whose scores are masked.  Otherwise they are read as they are (a page has all its rows) and the values
+// cleared right before their product: fewer instructions in every tile (d = 64, 64 sequences of up to 16000 keys: 96 us
+// against 98), but up to 15 rows more are read per item (d = 128, 3808 items of 137 keys: 45.4 us against 43.8, and
+// nothing to gain there, where a tile has half the rows).  A predicate on the loads, or clearing the values before the
+// softmax, makes the compiler wait for them long before their use: 120 and 109 us in the first case.
 template <int D>
-__device__ inline void load_k(Tile<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long pos_off, int g, int t) {
+constexpr bool kClamp = D == 128;
+
+// The tile that begins at key0 <= last_key, number n of its window of page ids: `put(step, row, chunk, address)` is called
+// for every piece that this thread (g, t) holds.  Steps that lie wholly behind the end are replaced by the tile's first.
+template <int D, typename Put>
+__device__ inline void tile_k(const DecParams& p, int ids, int n, int key0, int last_key, long long at, int g, Put put) {
   using Sh = Shape<D>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
-    const int step = key0 + 16 * s <= last_key ? s : 0, kb = key0 + 16 * step;
+    const int step = key0 + 16 * s <= last_key ? s : 0, key = key0 + 16 * step;
     const int id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + step);
-    const __nv_bfloat16* base = p.k + id * p.page_stride + pos_off + (kb & ((1 << p.page_shift) - 1)) * D + t * 2 * Sh::KW;
-    const int most = last_key - kb;
+    const __nv_bfloat16* row = p.k + (id * p.page_stride + (key & ((1 << p.page_shift) - 1)) * D + at);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const __nv_bfloat16* row = base + min(g + 8 * r, most) * D;
+      const int down = kClamp<D> ? min(g + 8 * r, last_key - key) - g : 8 * r;
 #pragma unroll
-      for (int c = 0; c < Sh::KCH; ++c) load_words<Sh::KW>(x.k[s][r][c], row + c * 8 * Sh::KW);
+      for (int c = 0; c < Sh::KCH; ++c) put(s, r, c, row + down * D + c * 8 * Sh::KW);
     }
   }
 }
-
-template <int D>
-__device__ inline void load_v(Tile<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long pos_off, int g, int t) {
+template <int D, typename Put>
+__device__ inline void tile_v(const DecParams& p, int ids, int n, int key0, int last_key, long long at, int t, Put put) {
   using Sh = Shape<D>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
-    const int step = key0 + 16 * s <= last_key ? s : 0, kb = key0 + 16 * step;
+    const int step = key0 + 16 * s <= last_key ? s : 0, key = key0 + 16 * step;
     const int id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + step);
-    const __nv_bfloat16* base = p.v + id * p.page_stride + pos_off + (kb & ((1 << p.page_shift) - 1)) * D;
-    const int most = last_key - kb;
+    const __nv_bfloat16* row = p.v + (id * p.page_stride + (key & ((1 << p.page_shift) - 1)) * D + at);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const __nv_bfloat16* row = base + min(2 * t + (r & 1) + 8 * (r >> 1), most) * D;
+      const int to = (r & 1) + 8 * (r >> 1), down = kClamp<D> ? min(2 * t + to, last_key - key) - 2 * t : to;
 #pragma unroll
-      for (int c = 0; c < Sh::VCH; ++c) {
-        if constexpr (D == 8) x.v[s][r][c][0] = *reinterpret_cast<const unsigned short*>(row + g);
-        else load_words<Sh::VW>(x.v[s][r][c], row + c * 64 + g * 2 * Sh::VW);
-      }
+      for (int c = 0; c < Sh::VCH; ++c) put(s, r, c, row + down * D + c * 64);
     }
   }
+}
+// Offsets inside a page of the pieces of thread (g, t) for KV position `pos`: its first row and element.
+template <int D>
+__device__ inline long long at_k(const DecParams& p, int pos, int g, int t) {
+  return (((long long)pos << p.page_shift) + g) * D + t * 2 * Shape<D>::KW;
+}
+template <int D>
+__device__ inline long long at_v(const DecParams& p, int pos, int g, int t) {
+  return (((long long)pos << p.page_shift) + 2 * t) * D + (D == 8 ? g : g * 2 * Shape<D>::VW);
+}
+
+template <int D>
+__device__ inline void load_k(Tile<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long at, int g) {
+  auto put = [&](int s, int r, int c, const __nv_bfloat16* a) { load_words<Shape<D>::KW>(x.k[s][r][c], a); };
+  tile_k<D>(p, ids, n, key0, last_key, at, g, put);
+}
+template <int D>
+__device__ inline void load_v(Tile<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long at, int t) {
+  auto put = [&](int s, int r, int c, const __nv_bfloat16* a) {
+    if constexpr (D == 8) x.v[s][r][c][0] = *reinterpret_cast<const unsigned short*>(a);
+    else load_words<Shape<D>::VW>(x.v[s][r][c], a);
+  };
+  tile_v<D>(p, ids, n, key0, last_key, at, t, put);
+}
+
+// The same pieces through shared memory, two tiles deep, where registers do not suffice: every thread copies its own
+// pieces asynchronously to places of its own and reads them back itself, so nothing is waited for but the copies.
+template <int D>
+struct Stage {
+  using Sh = Shape<D>;
+  uint32_t k[Sh::SUB][2][Sh::KCH][32][Sh::KW];
+  uint32_t v[Sh::SUB][4][Sh::VCH][32][Sh::VW];
+};
+template <int BYTES>
+__device__ inline void copy_async(const void* smem, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem)), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(smem)), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ inline void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ inline void wait_copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int D>
+__device__ inline void stage_k(Stage<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long at, int lane) {
+  auto put = [&](int s, int r, int c, const __nv_bfloat16* a) { copy_async<4 * Shape<D>::KW>(x.k[s][r][c][lane], a); };
+  tile_k<D>(p, ids, n, key0, last_key, at, lane >> 2, put);
+}
+template <int D>
+__device__ inline void stage_v(Stage<D>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long at, int lane) {
+  auto put = [&](int s, int r, int c, const __nv_bfloat16* a) { copy_async<4 * Shape<D>::VW>(x.v[s][r][c][lane], a); };
+  tile_v<D>(p, ids, n, key0, last_key, at, lane & 3, put);
+}
+template <int D>
+__device__ inline void take_k(Tile<D>& x, const Stage<D>& y, int lane) {
+  using Sh = Shape<D>;
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s)
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < Sh::KCH; ++c)
+#pragma unroll
+        for (int w = 0; w < Sh::KW; ++w) x.k[s][r][c][w] = y.k[s][r][c][lane][w];
+}
+template <int D>
+__device__ inline void take_v(Tile<D>& x, const Stage<D>& y, int lane) {
+  using Sh = Shape<D>;
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < Sh::VCH; ++c)
+#pragma unroll
+        for (int w = 0; w < Sh::VW; ++w) x.v[s][r][c][w] = y.v[s][r][c][lane][w];
 }
 
 // Running state of a warp: up to eight heads (columns); the thread's columns are 2t and 2t + 1.
@@ -275,13 +358,11 @@ __device__ inline void prefetch_q(QueryBuf<D>& buf, const DecParams& p, long lon
   for (int c = 0; c < Sh::KCH; ++c)
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(smem_u32(buf.w[c][lane])), "l"(row + c * 8 * Sh::KW),
                  "n"(4 * Sh::KW), "r"(hq < 0 ? 0 : 4 * Sh::KW) : "memory");
-  asm volatile("cp.async.commit_group;" ::: "memory");
 }
 
 template <int D>
 __device__ inline void take_q(uint32_t (&q)[Shape<D>::KCH][Shape<D>::KW], const QueryBuf<D>& buf, int lane) {
   using Sh = Shape<D>;
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
   for (int c = 0; c < Sh::KCH; ++c)
 #pragma unroll
@@ -313,7 +394,7 @@ __device__ inline void tile_scores(float (&sc)[Shape<D>::SUB][4], const Tile<D>&
 
 // Softmax step and O^T += V^T P^T of the tile that begins at key0 of `len` keys.
 template <int D>
-__device__ inline void tile_values(State<D>& st, float (&sc)[Shape<D>::SUB][4], const Tile<D>& x, float scale_log2, int key0, int len, int g) {
+__device__ inline void tile_values(State<D>& st, float (&sc)[Shape<D>::SUB][4], Tile<D>& x, float scale_log2, int key0, int len, int g, int t) {
   using Sh = Shape<D>;
   if (key0 + Sh::TILE > len) {                     // keys behind the end count for nothing
 #pragma unroll
@@ -343,6 +424,7 @@ __device__ inline void tile_values(State<D>& st, float (&sc)[Shape<D>::SUB][4], 
     for (int i = 0; i < Sh::MT; ++i) { st.o[i][0] *= f0; st.o[i][1] *= f1; st.o[i][2] *= f0; st.o[i][3] *= f1; }
   }
   const float r0 = st.m0 == -INFINITY ? 0.f : st.m0 * scale_log2, r1 = st.m1 == -INFINITY ? 0.f : st.m1 * scale_log2;
+  uint32_t b0[Sh::SUB], b1[Sh::SUB], c0[Sh::SUB], c1[Sh::SUB];
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
     float pr[4];
@@ -352,7 +434,22 @@ __device__ inline void tile_values(State<D>& st, float (&sc)[Shape<D>::SUB][4], 
     st.l1 += pr[1] + pr[3];
     const uint32_t h0 = pack_bf16(pr[0], pr[1]), h1 = pack_bf16(pr[2], pr[3]);
     const uint32_t e0 = pack_bf16(pr[0] - lo_f(h0), pr[1] - hi_f(h0)), e1 = pack_bf16(pr[2] - lo_f(h1), pr[3] - hi_f(h1));
-    const uint32_t b0 = transpose8x8(h0), b1 = transpose8x8(h1), c0 = transpose8x8(e0), c1 = transpose8x8(e1);
+    b0[s] = transpose8x8(h0); b1[s] = transpose8x8(h1); c0[s] = transpose8x8(e0); c1[s] = transpose8x8(e1);
+  }
+  if (!kClamp<D> && key0 + Sh::TILE > len) {
+#pragma unroll
+    for (int s = 0; s < Sh::SUB; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (key0 + 16 * s + 2 * t + (r & 1) + 8 * (r >> 1) >= len) {
+#pragma unroll
+          for (int c = 0; c < Sh::VCH; ++c)
+#pragma unroll
+            for (int w = 0; w < Sh::VW; ++w) x.v[s][r][c][w] = 0;
+        }
+  }
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s) {
 #pragma unroll
     for (int i = 0; i < Sh::MT; ++i) {
       uint32_t a[4];                               // (rows g, g + 8) x (keys 2t, 2t+1 | 2t+8, 2t+9): element 2i and 2i + 1
@@ -367,8 +464,8 @@ __device__ inline void tile_values(State<D>& st, float (&sc)[Shape<D>::SUB][4], 
         a[2] = __byte_perm(x.v[s][2][c][w], x.v[s][3][c][w], 0x5410);
         a[3] = __byte_perm(x.v[s][2][c][w], x.v[s][3][c][w], 0x7632);
       }
-      mma16816(st.o[i], a[0], a[1], a[2], a[3], b0, b1);
-      mma16816(st.o[i], a[0], a[1], a[2], a[3], c0, c1);
+      mma16816(st.o[i], a[0], a[1], a[2], a[3], b0[s], b1[s]);
+      mma16816(st.o[i], a[0], a[1], a[2], a[3], c0[s], c1[s]);
     }
   }
 }
@@ -445,57 +542,63 @@ __device__ inline void store_part(float* row, const State<D>& st, int col, int h
     *reinterpret_cast<float4*>(row + D) = make_float4(col ? st.m1 : st.m0, col ? st.l1 : st.l0, __int_as_float(head), 0.f);
 }
 
-// Whole items, one CTA per (sequence, KV position, row tile): the warps take every fourth tile and join in shared memory.
+// Whole items, one cluster of CTAs per (sequence, KV position, row tile): its warps take the item's tiles in turn; the warps
+// of a CTA join in shared memory, the CTAs in the others' shared memory, every one for its share of the result.
 template <int D>
-__global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecParams p) {
+__global__ void __launch_bounds__(kDecThreads, D == 128 ? 3 : (D >= 32 ? 4 : 5)) decode_whole_kernel(const DecParams p) {
   using Sh = Shape<D>;
   __shared__ float sm[kDecWarps * kCols * (D + 2)];
+  __shared__ float joined[kCols * (D + 2)];
   __shared__ int cols[kDecWarps][kCols];
   __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps];
   __shared__ int32_t head_cache[kHeadCache], pos_cache[kPosCache];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int items = p.kv_max * p.row_tiles;
-  const long long seq = blockIdx.x / items;
-  const int rest = (int)(blockIdx.x - seq * items), pos = rest / p.row_tiles, rt = rest % p.row_tiles;
+  cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), stride = ctas * kDecWarps;
+  const int first = rank * kDecWarps + warp;       // the warp's first tile
+  const int items = p.kv_max * p.row_tiles, number = blockIdx.x / ctas;
+  const long long seq = number / items;
+  const int rest = number - (int)seq * items, pos = rest / p.row_tiles, rt = rest % p.row_tiles;
   const int s = (int)(seq / p.n_seqs);
   griddep_launch_dependents();
   griddep_wait();
   // one round trip: the length, the first pages, the heads
   const Heads hd = cache_heads(p, head_cache, pos_cache, s, 1);
-  int ids = fetch_pages<D>(p, seq, warp, kDecWarps, lane);
+  int ids = fetch_pages<D>(p, seq, first, stride, lane);
   const int len = clamped_len(p, p.len[seq]), tiles = (len + Sh::TILE - 1) / Sh::TILE;
-  ids = check_pages<D>(p, ids, len - 1, warp, kDecWarps, lane);
+  ids = check_pages<D>(p, ids, len - 1, first, stride, lane);
   wait_copies();
-  const long long pos_off = ((long long)pos << p.page_shift) * D;
+  const long long k_at = at_k<D>(p, pos, g, t), v_at = at_v<D>(p, pos, g, t);
   constexpr int AHEAD = 32 / Sh::SUB;
   State<D> st;
   reset<D>(st);
   Tile<D> x;
-  int key0 = warp * Sh::TILE;
-  if (warp < tiles) {
-    load_k<D>(x, p, ids, 0, key0, len - 1, pos_off, g, t);
-    load_v<D>(x, p, ids, 0, key0, len - 1, pos_off, g, t);
+  int key0 = first * Sh::TILE;
+  if (first < tiles) {
+    load_k<D>(x, p, ids, 0, key0, len - 1, k_at, g);
+    load_v<D>(x, p, ids, 0, key0, len - 1, v_at, t);
   }
   __syncthreads();
   find_heads(p, hd, s, pos, rt, lane, cols[warp]);
-  if (cols[warp][0] < 0) return;                   // no head reads this position (the same in every warp)
+  if (cols[warp][0] < 0) return;                   // no head reads this position (the same in the whole cluster)
   uint32_t q[Sh::KCH][Sh::KW];
   prefetch_q<D>(qbuf[warp], p, seq, cols[warp][g], lane);
+  wait_copies();
   take_q<D>(q, qbuf[warp], lane);
-  for (int tile = warp, n = 0; tile < tiles; tile += kDecWarps, key0 += kDecWarps * Sh::TILE) {
-    const bool more = tile + kDecWarps < tiles;
-    const int next0 = key0 + kDecWarps * Sh::TILE;
+  for (int tile = first, n = 0; tile < tiles; tile += stride, key0 += stride * Sh::TILE) {
+    const bool more = tile + stride < tiles;
+    const int next0 = key0 + stride * Sh::TILE;
     float sc[Sh::SUB][4];
     tile_scores<D>(sc, x, q);
     if (more) {
       if (++n == AHEAD) {
-        ids = check_pages<D>(p, fetch_pages<D>(p, seq, tile + kDecWarps, kDecWarps, lane), len - 1, tile + kDecWarps, kDecWarps, lane);
+        ids = check_pages<D>(p, fetch_pages<D>(p, seq, tile + stride, stride, lane), len - 1, tile + stride, stride, lane);
         n = 0;
       }
-      load_k<D>(x, p, ids, n, next0, len - 1, pos_off, g, t);
+      load_k<D>(x, p, ids, n, next0, len - 1, k_at, g);
     }
-    tile_values<D>(st, sc, x, p.scale_log2, key0, len, g);
-    if (more) load_v<D>(x, p, ids, n, next0, len - 1, pos_off, g, t);
+    tile_values<D>(st, sc, x, p.scale_log2, key0, len, g, t);
+    if (more) load_v<D>(x, p, ids, n, next0, len - 1, v_at, t);
   }
   finish<D>(st, p.scale_log2);
   float* mine = sm + warp * kCols * (D + 2);       // [head][D + 2]
@@ -514,23 +617,49 @@ __global__ void __launch_bounds__(kDecThreads) decode_whole_kernel(const DecPara
     mine[(2 * t + 1) * (D + 2) + D] = st.m1; mine[(2 * t + 1) * (D + 2) + D + 1] = st.l1;
   }
   __syncthreads();
-  for (int k = threadIdx.x; k < kCols * D; k += kDecThreads) {
-    const int h = k / D, d = k % D, head = cols[warp][h];
-    if (head < 0) continue;
-    float m = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kDecWarps; ++w) m = fmaxf(m, sm[(w * kCols + h) * (D + 2) + D]);
-    float acc = 0.f, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < kDecWarps; ++w) {
-      const float* y = sm + (w * kCols + h) * (D + 2);
+  // element (h, d) of the sum of `n` states, state i at at(i)
+  auto merge = [&](int n, auto at, int h, int d, float& m, float& l) {
+    m = -INFINITY;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, at(i)[h * (D + 2) + D]);
+    float acc = 0.f;
+    l = 0.f;
+    for (int i = 0; i < n; ++i) {
+      const float* y = at(i) + h * (D + 2);
       const float f = part_weight(y[D], y[D + 1], m);
       acc += f * y[d];
       l += f * y[D + 1];
     }
+    return acc;
+  };
+  auto store = [&](int h, int d, float acc, float m, float l) {
+    const int head = cols[warp][h];
     p.out[(seq * p.heads + head) * D + d] = __float2bfloat16(len == 0 ? 0.f : acc / l);
     if (d == 0 && p.lse) p.lse[lse_at(p, seq, head)] = len == 0 ? -INFINITY : (m + log2f(l)) * kLn2;
+  };
+  auto warps = [&](int i) { return sm + i * kCols * (D + 2); };
+  for (int k = threadIdx.x; k < kCols * D; k += kDecThreads) {
+    const int h = k / D, d = k % D;
+    if (cols[warp][h] < 0) continue;
+    float m, l;
+    const float acc = merge(kDecWarps, warps, h, d, m, l);
+    if (ctas == 1) {
+      store(h, d, acc, m, l);
+    } else {
+      joined[h * (D + 2) + d] = acc;
+      if (d == 0) { joined[h * (D + 2) + D] = m; joined[h * (D + 2) + D + 1] = l; }
+    }
   }
+  if (ctas == 1) return;
+  cluster.sync();
+  auto others = [&](int i) { return (const float*)cluster.map_shared_rank(joined, i); };
+  for (int k = rank * kDecThreads + threadIdx.x; k < kCols * D; k += ctas * kDecThreads) {
+    const int h = k / D, d = k % D;
+    if (cols[warp][h] < 0) continue;
+    float m, l;
+    const float acc = merge(ctas, others, h, d, m, l);
+    store(h, d, acc, m, l);
+  }
+  cluster.sync();                                  // the others may still be reading this CTA's sums
 }
 
 // The line of work.  A sequence is held * row_tiles items; an item counts kItemCost units for itself (the warp that has its
@@ -554,13 +683,20 @@ struct Segment {
   int t0, t1;
 };
 
-constexpr int kLenCache = 1024;       // sequences whose lengths a CTA keeps in shared memory
+constexpr int kLenCache = 512;        // sequences whose lengths a CTA keeps in shared memory
+
+// Tiles that go through shared memory in the split kernel.
+template <int D>
+constexpr bool kStaged = D == 16 || D == 32;
+template <int D>
+constexpr int kRingBytes = kStaged<D> ? 2 * kDecWarps * (int)sizeof(Stage<D>) : 0;
 
 template <int D>
 __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecParams p) {
   using Sh = Shape<D>;
   __shared__ int cols[kDecWarps][2][kCols];
-  __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps][2];
+  __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps];
+  extern __shared__ __align__(16) unsigned char ring[];       // [kDecWarps][2] stages
   __shared__ int held[TWIST_MAX_SUBNETS];
   __shared__ int32_t lens[kLenCache], head_cache[kHeadCache], pos_cache[kPosCache];
   __shared__ uint32_t warp_sum[kDecWarps];
@@ -648,22 +784,31 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   if (now.t1 <= now.t0) return;                             // the item's own cost is all there is: the next warp has its tiles
 
   constexpr int AHEAD = 32 / Sh::SUB;
+  constexpr bool STAGED = kStaged<D>;
+  Stage<D>* stages = reinterpret_cast<Stage<D>*>(ring) + 2 * warp;
   Tile<D> x;
   int ids = fetch_pages<D>(p, now.seq, now.t0, 1, lane);
   int next_ids = fetch_pages<D>(p, now.seq, now.t0 + AHEAD, 1, lane);     // unchecked until it becomes `ids`
   int n = 0;                                        // number of the loaded tile in its window of page ids
-  int pos = now.item / p.row_tiles, buf = 0;
+  int pos = now.item / p.row_tiles, buf = 0, stage = 0;
   find_heads(p, hd, now.s, pos, now.item - pos * p.row_tiles, lane, cols[warp][0]);
-  prefetch_q<D>(qbuf[warp][0], p, now.seq, cols[warp][0][g], lane);
+  prefetch_q<D>(qbuf[warp], p, now.seq, cols[warp][0][g], lane);
   ids = check_pages<D>(p, ids, now.len - 1, now.t0, 1, lane);
   if (now.len > 0) {
-    const long long off = ((long long)pos << p.page_shift) * D;
-    load_k<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, off, g, t);
-    load_v<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, off, g, t);
+    if constexpr (STAGED) stage_k<D>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D>(p, pos, g, t), lane);
+    else load_k<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D>(p, pos, g, t), g);
   }
+  commit_copies();                                  // the queries travel with the first keys
+  if (now.len > 0) {
+    if constexpr (STAGED) stage_v<D>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D>(p, pos, g, t), lane);
+    else load_v<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D>(p, pos, g, t), t);
+  }
+  commit_copies();
   for (;;) {
     uint32_t q[Sh::KCH][Sh::KW];
-    take_q<D>(q, qbuf[warp][buf], lane);
+    if constexpr (STAGED) wait_copies_but<1>();
+    else wait_copies();
+    take_q<D>(q, qbuf[warp], lane);
     const int hq = cols[warp][buf][g];
     // the segment behind this one: its first pages, its heads and their queries on their way before they are needed
     const bool more = left > (uint32_t)kItemCost;
@@ -683,18 +828,14 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       next_pos = next.item / p.row_tiles;
       head_ids = fetch_pages<D>(p, next.seq, 0, 1, lane);
       find_heads(p, hd, next.s, next_pos, next.item - next_pos * p.row_tiles, lane, cols[warp][buf ^ 1]);
-      prefetch_q<D>(qbuf[warp][buf ^ 1], p, next.seq, cols[warp][buf ^ 1][g], lane);
+      prefetch_q<D>(qbuf[warp], p, next.seq, cols[warp][buf ^ 1][g], lane);          // complete with the next tile's keys
     }
-    const long long off = ((long long)pos << p.page_shift) * D, next_off = ((long long)next_pos << p.page_shift) * D;
     State<D> st;
     reset<D>(st);
     for (int tile = now.t0; tile < now.t1; ++tile) {
-      float sc[Sh::SUB][4];
-      tile_scores<D>(sc, x, q);
       // the tile to load: the item's next one or the next item's first
       const bool inside = tile + 1 < now.t1;
-      const int key0 = inside ? (tile + 1) * Sh::TILE : 0, last_key = inside ? now.len - 1 : next.len - 1;
-      const long long o = inside ? off : next_off;
+      const int key0 = inside ? (tile + 1) * Sh::TILE : 0, last_key = inside ? now.len - 1 : next.len - 1, of = inside ? pos : next_pos;
       const bool load = (inside || more) && last_key >= 0;
       if (inside) {
         if (++n == AHEAD) {
@@ -707,9 +848,26 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
         next_ids = fetch_pages<D>(p, next.seq, AHEAD, 1, lane);
         n = 0;
       }
-      if (load) load_k<D>(x, p, ids, n, key0, last_key, o, g, t);
-      if (now.len > 0) tile_values<D>(st, sc, x, p.scale_log2, tile * Sh::TILE, now.len, g);
-      if (load) load_v<D>(x, p, ids, n, key0, last_key, o, g, t);
+      float sc[Sh::SUB][4];
+      if constexpr (STAGED) {
+        Stage<D>& to = stages[stage ^ 1];
+        if (load) stage_k<D>(to, p, ids, n, key0, last_key, at_k<D>(p, of, g, t), lane);
+        commit_copies();
+        if (load) stage_v<D>(to, p, ids, n, key0, last_key, at_v<D>(p, of, g, t), lane);
+        commit_copies();
+        wait_copies_but<3>();
+        take_k<D>(x, stages[stage], lane);
+        tile_scores<D>(sc, x, q);
+        wait_copies_but<2>();
+        take_v<D>(x, stages[stage], lane);
+        if (now.len > 0) tile_values<D>(st, sc, x, p.scale_log2, tile * Sh::TILE, now.len, g, t);
+        stage ^= 1;
+      } else {
+        tile_scores<D>(sc, x, q);
+        if (load) load_k<D>(x, p, ids, n, key0, last_key, at_k<D>(p, of, g, t), g);
+        if (now.len > 0) tile_values<D>(st, sc, x, p.scale_log2, tile * Sh::TILE, now.len, g, t);
+        if (load) load_v<D>(x, p, ids, n, key0, last_key, at_v<D>(p, of, g, t), t);
+      }
     }
     finish<D>(st, p.scale_log2);
     const bool whole = now.t0 == 0 && now.t1 == now.nt;
@@ -821,23 +979,32 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   const int slot = device_slot();
   if (resident[slot] == 0) {
     int n = 0;
-    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_split_kernel<D>, kDecThreads, 0));
+    TWIST_CUDA_TRY(cudaFuncSetAttribute(decode_split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<D>));
+    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_split_kernel<D>, kDecThreads, kRingBytes<D>));
     resident[slot] = n < 1 ? 1 : (n > kMaxCtasPerSm ? kMaxCtasPerSm : n);
   }
   const long long grid = (long long)sm_count() * resident[slot];
-  if (max_len <= 512 && items <= 2 * grid) {
-    TWIST_CUDA_TRY(launch_overlapped(decode_whole_kernel<D>, dim3((unsigned)items), dim3(kDecThreads), 0, st, p));
+  // One cluster per item where that needs few turns: two tiles a warp are taken by a single CTA, more by as many CTAs as
+  // leave a warp one, if all of them run at once.  Measured (D = 64, one sequence of 8 heads, 1024 keys): 5.1 us against 9.2
+  // through the line; the line is ahead from about kShortTiles tiles a warp, and where items times their length fill the
+  // GPU kShortWork times (256 ragged items of up to 2048 keys: 20.8 us against 27 to 34 with clusters).
+  const long long tiles = (max_len + Shape<D>::TILE - 1) / Shape<D>::TILE;
+  int cluster = 1;
+  if (tiles > 2 * kDecWarps)
+    while (cluster < kMaxCluster && 2 * cluster * items <= grid && tiles > kDecWarps * cluster) cluster *= 2;
+  if (items <= 2 * grid && tiles <= kShortTiles * kDecWarps * cluster && tiles * items <= kShortWork * grid * kDecWarps) {
+    TWIST_CUDA_TRY(launch_overlapped(decode_whole_kernel<D>, dim3((unsigned)(items * cluster)), dim3(kDecThreads), 0, st, cluster, p));
     return TWIST_OK;
   }
   p.by_item = items <= grid * kDecWarps;
-  TWIST_CUDA_TRY(launch_overlapped(decode_split_kernel<D>, dim3((unsigned)grid), dim3(kDecThreads), 0, st, p));
+  TWIST_CUDA_TRY(launch_overlapped(decode_split_kernel<D>, dim3((unsigned)grid), dim3(kDecThreads), kRingBytes<D>, st, 1, p));
   // An item of an even batch is cut into about warps / items parts: the fewer items, the more threads share the parts of one.
   int groups = 1;
   while (groups < kJoinThreads / 32 && 8ll * groups * items < grid * kDecWarps) groups *= 2;
   const int elems = (kCols < p.per_group ? kCols : p.per_group) * D;                   // of the heads that share a position
   const int block = elems * groups < 32 ? 32 : (elems * groups > kJoinThreads ? kJoinThreads : elems * groups);
   const dim3 join_grid((unsigned)(p.by_item ? items : grid * kDecWarps), (unsigned)((elems * groups + block - 1) / block));
-  TWIST_CUDA_TRY(launch_overlapped(decode_join_kernel<D>, join_grid, dim3(block), 0, st, p, groups));
+  TWIST_CUDA_TRY(launch_overlapped(decode_join_kernel<D>, join_grid, dim3(block), 0, st, 1, p, groups));
   return TWIST_OK;
 }
 

@@ -292,7 +292,7 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
                               : mode == MODE_PAIRS ? rotate_rows_kernel<APPEND, MODE_PAIRS>
                               : mode == MODE_SLOW_HALF ? rotate_rows_kernel<APPEND, MODE_SLOW_HALF>
                                                        : rotate_rows_kernel<APPEND, MODE_SLOW_PAIRS>;
-  TWIST_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)tiles), dim3(kPosThreads), smem, st, p));
+  TWIST_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)tiles), dim3(kPosThreads), smem, st, 1, p));
   return TWIST_OK;
 }
 
