@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -473,16 +474,30 @@ def _cache(k: torch.Tensor, v: torch.Tensor, kv_max: int, d_head: int):
     return page, n, strides[0] if n > 1 else max(strides[0], kv_max * page * d_head)
 
 
+# The argument structs of the per-token calls are packed in one go (field by field costs 1 us a call more), and their
+# tensors are checked in one expression; _tensor names the one that is wrong when it fails.
+_ROPE_PACK = struct.Struct("9i4x4Q")
+_APPEND_PACK = struct.Struct("12i2q10Q")
+_DECODE_PACK = struct.Struct("12i2q11Q")
+assert (_ROPE_PACK.size, _APPEND_PACK.size, _DECODE_PACK.size) == (C.sizeof(RopeArgs), C.sizeof(KvAppendArgs), C.sizeof(AttnDecodeArgs))
+
+
 def rope_args(dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, seq_len=0, layout=ROPE_HALF, *, in_, out,
               inv_freq, pos=None) -> RopeArgs:
     """Marshals twist_rope_args.  in_, out: bf16 [S][T][(head_keep + 2 kv_max) d_head] (out may be in_); inv_freq: fp64
     [rot_dims / 2]; pos: int32 [S][T], or None for position t % seq_len."""
     dev = torch.cuda.current_device()
-    n = n_subnets * tokens * (head_keep + 2 * kv_max) * d_head
-    a = RopeArgs(dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, layout, seq_len,
-                 _tensor("in_", in_, torch.bfloat16, n, dev), _tensor("out", out, torch.bfloat16, n, dev),
-                 _tensor("inv_freq", inv_freq, torch.float64, rot_dims // 2, dev),
-                 None if pos is None else _tensor("pos", pos, torch.int32, n_subnets * tokens, dev))
+    n, bf = n_subnets * tokens * (head_keep + 2 * kv_max) * d_head, torch.bfloat16
+    if not (in_.dtype is bf and in_.numel() == n and in_.is_contiguous() and in_.get_device() == dev
+            and out.dtype is bf and out.numel() == n and out.is_contiguous() and out.get_device() == dev
+            and inv_freq.dtype is torch.float64 and inv_freq.numel() == rot_dims // 2 and inv_freq.is_contiguous()
+            and inv_freq.get_device() == dev):
+        _tensor("in_", in_, bf, n, dev)
+        _tensor("out", out, bf, n, dev)
+        _tensor("inv_freq", inv_freq, torch.float64, rot_dims // 2, dev)
+    a = RopeArgs.from_buffer_copy(_ROPE_PACK.pack(
+        dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, layout, seq_len, in_.data_ptr(), out.data_ptr(),
+        inv_freq.data_ptr(), 0 if pos is None else _tensor("pos", pos, torch.int32, n_subnets * tokens, dev)))
     a._keepalive = (in_, out, inv_freq, pos)
     return a
 
@@ -503,21 +518,27 @@ def kv_append_args(dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, 
     [S][n_seqs][max_pages]; kv_len: int32 [S][n_seqs], the new tokens included; q_out: bf16 [S][T][head_keep d_head], rows
     evenly spaced (qkv[..., :head_keep * d_head] rotates Q in place)."""
     dev = torch.cuda.current_device()
-    i32 = torch.int32
+    i32, bf = torch.int32, torch.bfloat16
     page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head)
     if k_cache.get_device() != dev or v_cache.get_device() != dev or (q_out is not None and q_out.get_device() != dev):
         _elsewhere("k_cache / v_cache / q_out", k_cache, dev)
-    seqs = n_subnets * n_seqs
+    seqs, n = n_subnets * n_seqs, n_subnets * tokens * (head_keep + 2 * kv_max) * d_head
     max_pages = page_table.shape[-1]
-    a = KvAppendArgs(dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, page, n_pages, max_pages, rot_dims, layout,
-                     stride, 0 if q_out is None else _rows("q_out", q_out, n_subnets, tokens, head_keep * d_head),
-                     _tensor("qkv", qkv, torch.bfloat16, n_subnets * tokens * (head_keep + 2 * kv_max) * d_head, dev),
-                     None if q_out is None else q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                     _tensor("page_table", page_table, i32, seqs * max_pages, dev), _tensor("kv_len", kv_len, i32, seqs, dev),
-                     None if new_begin is None else _tensor("new_begin", new_begin, i32, n_subnets * (n_seqs + 1), dev),
-                     None if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
-                     None if kv_count is None else _tensor("kv_count", kv_count, i32, n_subnets, dev),
-                     None if inv_freq is None else _tensor("inv_freq", inv_freq, torch.float64, rot_dims // 2, dev))
+    if not (qkv.dtype is bf and qkv.numel() == n and qkv.is_contiguous() and qkv.get_device() == dev
+            and page_table.dtype is i32 and page_table.numel() == seqs * max_pages and page_table.is_contiguous()
+            and page_table.get_device() == dev
+            and kv_len.dtype is i32 and kv_len.numel() == seqs and kv_len.is_contiguous() and kv_len.get_device() == dev):
+        _tensor("qkv", qkv, bf, n, dev)
+        _tensor("page_table", page_table, i32, seqs * max_pages, dev)
+        _tensor("kv_len", kv_len, i32, seqs, dev)
+    a = KvAppendArgs.from_buffer_copy(_APPEND_PACK.pack(
+        dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, page, n_pages, max_pages, rot_dims, layout, stride,
+        0 if q_out is None else _rows("q_out", q_out, n_subnets, tokens, head_keep * d_head), qkv.data_ptr(),
+        0 if q_out is None else q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
+        0 if new_begin is None else _tensor("new_begin", new_begin, i32, n_subnets * (n_seqs + 1), dev),
+        0 if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
+        0 if kv_count is None else _tensor("kv_count", kv_count, i32, n_subnets, dev),
+        0 if inv_freq is None else _tensor("inv_freq", inv_freq, torch.float64, rot_dims // 2, dev)))
     a._keepalive = (qkv, q_out, k_cache, v_cache, page_table, kv_len, new_begin, new_len, kv_count, inv_freq)
     return a
 
@@ -533,21 +554,26 @@ def attn_decode_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_head
     [S][n_seqs][head_keep d_head]; lse fp32 [S][head_keep][n_seqs]; ws: scratch of at least
     twist_attn_decode_workspace_bytes(d_head) bytes."""
     dev = torch.cuda.current_device()
-    i32 = torch.int32
+    i32, bf = torch.int32, torch.bfloat16
     page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head)
     if k_cache.get_device() != dev or v_cache.get_device() != dev or q.get_device() != dev or ws.get_device() != dev:
         _elsewhere("k_cache / v_cache / q / ws", k_cache, dev)
     seqs, width = n_subnets * n_seqs, head_keep * d_head
     max_pages = page_table.shape[-1]
-    a = AttnDecodeArgs(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages,
-                       max_len, stride, _rows("q", q, n_subnets, n_seqs, width), q.data_ptr(),
-                       k_cache.data_ptr(), v_cache.data_ptr(), _tensor("page_table", page_table, i32, seqs * max_pages, dev),
-                       _tensor("kv_len", kv_len, i32, seqs, dev),
-                       None if head_idx is None else _tensor("head_idx", head_idx, i32, n_subnets * head_keep, dev),
-                       None if kv_pos is None else _tensor("kv_pos", kv_pos, i32, n_subnets * n_kv_heads, dev),
-                       _tensor("out", out, torch.bfloat16, seqs * width, dev),
-                       None if lse is None else _tensor("lse", lse, torch.float32, seqs * head_keep, dev),
-                       ws.data_ptr(), ws.numel() * ws.element_size())
+    if not (page_table.dtype is i32 and page_table.numel() == seqs * max_pages and page_table.is_contiguous()
+            and page_table.get_device() == dev
+            and kv_len.dtype is i32 and kv_len.numel() == seqs and kv_len.is_contiguous() and kv_len.get_device() == dev
+            and out.dtype is bf and out.numel() == seqs * width and out.is_contiguous() and out.get_device() == dev):
+        _tensor("page_table", page_table, i32, seqs * max_pages, dev)
+        _tensor("kv_len", kv_len, i32, seqs, dev)
+        _tensor("out", out, bf, seqs * width, dev)
+    a = AttnDecodeArgs.from_buffer_copy(_DECODE_PACK.pack(
+        dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, max_len, stride,
+        _rows("q", q, n_subnets, n_seqs, width), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
+        kv_len.data_ptr(), 0 if head_idx is None else _tensor("head_idx", head_idx, i32, n_subnets * head_keep, dev),
+        0 if kv_pos is None else _tensor("kv_pos", kv_pos, i32, n_subnets * n_kv_heads, dev), out.data_ptr(),
+        0 if lse is None else _tensor("lse", lse, torch.float32, seqs * head_keep, dev), ws.data_ptr(),
+        ws.numel() * ws.element_size()))
     a._keepalive = (q, k_cache, v_cache, page_table, kv_len, out, ws, head_idx, kv_pos, lse)
     return a
 
