@@ -662,8 +662,9 @@ __global__ void __launch_bounds__(kDecThreads, D == 128 ? 3 : (D >= 32 ? 4 : 5))
   cluster.sync();                                  // the others may still be reading this CTA's sums
 }
 
-// The line of work.  A sequence is held * row_tiles items; an item counts kItemCost units for itself (the warp that has its
-// first tile pays them) and one for each of its max(1, tiles of its keys) tiles.
+// The line of work.  A sequence has an item for every KV position that heads read and eight of them (a row tile); an item
+// counts kItemCost units for itself (the warp that has its first tile pays them) and one for each of its max(1, tiles of
+// its keys) tiles.
 template <int D>
 __device__ inline int tiles_of(int len) { return max(1, (len + Shape<D>::TILE - 1) / Shape<D>::TILE); }
 
@@ -679,7 +680,8 @@ struct Cut {
 
 // Where a warp stands in the line: an item and the range of its tiles that is the warp's.
 struct Segment {
-  int seq, s, len, item, items, nt;        // subnet; keys; item of the sequence's `items`; tiles of an item
+  int seq, s, len, nt;                // sequence, its subnet, its keys, tiles of an item
+  int pos, rt;                        // KV position and row tile of the item
   int t0, t1;
 };
 
@@ -691,18 +693,21 @@ constexpr bool kStaged = D == 16 || D == 32;
 template <int D>
 constexpr int kRingBytes = kStaged<D> ? 2 * kDecWarps * (int)sizeof(Stage<D>) : 0;
 
+constexpr int kCountCache = 256;      // KV positions of all subnets whose heads a CTA counts
+
 template <int D>
 __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecParams p) {
   using Sh = Shape<D>;
   __shared__ int cols[kDecWarps][2][kCols];
   __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps];
   extern __shared__ __align__(16) unsigned char ring[];       // [kDecWarps][2] stages
-  __shared__ int held[TWIST_MAX_SUBNETS];
+  __shared__ int items[TWIST_MAX_SUBNETS], counts[kCountCache];
   __shared__ int32_t lens[kLenCache], head_cache[kHeadCache], pos_cache[kPosCache];
   __shared__ uint32_t warp_sum[kDecWarps];
   __shared__ __align__(16) uint32_t before[kDecThreads];    // cost of the sequences before each thread's
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int N = p.S * p.n_seqs, per = (N + kDecThreads - 1) / kDecThreads;
+  for (int i = threadIdx.x; i < kCountCache; i += kDecThreads) counts[i] = 0;
   griddep_launch_dependents();
   griddep_wait();
   // one round trip: lengths, heads, positions
@@ -710,24 +715,42 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   const Heads hd = cache_heads(p, head_cache, pos_cache, 0, p.S);
   wait_copies();
   __syncthreads();
-  // KV positions of each subnet that some head reads: 1 + the largest entry of kv_pos
-  for (int s = warp; s < p.S; s += kDecWarps) {
-    int top = 0;
-    if (p.head_idx) {
-      for (int k = lane; k < p.n_kv_heads; k += 32) top = max(top, min(hd.pos[s * p.n_kv_heads + k], p.kv_max - 1));
-      top = __reduce_max_sync(0xffffffffu, top);
-    } else {
-      top = p.kv_max - 1;
+  // Items of each subnet.  One row tile: the positions up to the last that a group has.  More (sharing by more than eight
+  // heads): as many as the position's kept heads fill, counted, so that no keys are read for an empty row tile.
+  const bool counted = p.row_tiles > 1 && hd.idx != p.head_idx && p.S * p.kv_max <= kCountCache;
+  if (counted) {
+    for (int i = threadIdx.x; i < p.S * p.heads; i += kDecThreads) {
+      const int s = i / p.heads;
+      atomicAdd(&counts[s * p.kv_max + position_of(p, hd, s, i - s * p.heads)], 1);
     }
-    if (lane == 0) held[s] = top + 1;
+    __syncthreads();
+  }
+  auto count_tiles = [&](int s, int pos) { return min((counts[s * p.kv_max + pos] + kCols - 1) / kCols, p.row_tiles); };
+  for (int s = warp; s < p.S; s += kDecWarps) {
+    int n = 0;
+    if (counted) {
+      for (int k = lane; k < p.kv_max; k += 32) n += count_tiles(s, k);
+      n = __reduce_add_sync(0xffffffffu, n);
+    } else {
+      if (p.head_idx) {
+        for (int k = lane; k < p.n_kv_heads; k += 32) n = max(n, min(hd.pos[s * p.n_kv_heads + k], p.kv_max - 1));
+        n = __reduce_max_sync(0xffffffffu, n);
+      } else {
+        n = p.kv_max - 1;
+      }
+      n = (n + 1) * p.row_tiles;
+    }
+    if (lane == 0) items[s] = n;
   }
   __syncthreads();
+  // row tiles of a position (0: none; the position is behind the subnet's last one, or no head reads it)
+  auto row_tiles = [&](int s, int pos) { return counted ? count_tiles(s, pos) : (pos * p.row_tiles < items[s] ? p.row_tiles : 0); };
   auto len_of = [&](int i) { return clamped_len(p, i < kLenCache ? lens[i] : p.len[i]); };
   uint32_t mine = 0;
   {
     int i = min(N, (int)threadIdx.x * per), s = i / p.n_seqs, b = i - s * p.n_seqs;
     for (const int last = min(N, i + per); i < last; ++i) {
-      mine += (uint32_t)(held[s] * p.row_tiles) * (kItemCost + tiles_of<D>(len_of(i)));
+      mine += (uint32_t)items[s] * (kItemCost + tiles_of<D>(len_of(i)));
       if (++b == p.n_seqs) { b = 0; ++s; }
     }
   }
@@ -753,35 +776,44 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   if (!p.by_item && lane == 0) p.desc[c] = make_int4(0, 0, 0, 0);
   if (c >= G) return;
   uint32_t left = cut.begin(c + 1) - cut.begin(c);          // units of the warp behind the current segment
-  uint32_t item0;                                            // the line's unit at the current item's beginning
+  uint32_t item0;                                            // the line's unit at the beginning of the current item
   Segment now;
+  auto enter = [&](Segment& x, int seq, int s) {             // the first item of a sequence
+    x.seq = seq;
+    x.s = s;
+    x.len = len_of(seq);
+    x.nt = tiles_of<D>(x.len);
+  };
   {
     const uint32_t u = cut.begin(c);
     int owner = -1;                                          // the last thread whose sequences begin at or before u
     for (int k = 0; k < kDecThreads; k += 32) owner += __popc(__ballot_sync(0xffffffffu, before[k + lane] <= u));
-    uint32_t base = before[owner];
-    now.seq = owner * per;
-    now.s = now.seq / p.n_seqs;
-    int b = now.seq - now.s * p.n_seqs;
+    uint32_t base = before[owner], cost;
+    int seq = owner * per, s = seq / p.n_seqs, b = seq - s * p.n_seqs;
     for (;;) {
-      now.len = len_of(now.seq);
-      now.nt = tiles_of<D>(now.len);
-      now.items = held[now.s] * p.row_tiles;
-      const uint32_t cost = (uint32_t)now.items * (now.nt + kItemCost);
+      enter(now, seq, s);
+      cost = (uint32_t)items[s] * (now.nt + kItemCost);
       if (u < base + cost) break;
       base += cost;
-      ++now.seq;
-      if (++b == p.n_seqs) { b = 0; ++now.s; }
+      ++seq;
+      if (++b == p.n_seqs) { b = 0; ++s; }
     }
     const uint32_t one = now.nt + kItemCost;
-    now.item = (u - base) / one;
-    const uint32_t x0 = u - base - now.item * one, x1 = min(one, x0 + left);
+    int item = (int)((u - base) / one);
+    const uint32_t x0 = u - base - item * one, x1 = min(one, x0 + left);
     item0 = u - x0;
+    if (!counted) {
+      now.pos = item / p.row_tiles;
+      now.rt = item - now.pos * p.row_tiles;
+    } else {
+      for (now.pos = 0; item >= count_tiles(s, now.pos); ++now.pos) item -= count_tiles(s, now.pos);
+      now.rt = item;
+    }
     now.t0 = max(0, (int)x0 - kItemCost);
     now.t1 = max(0, (int)x1 - kItemCost);
     left -= x1 - x0;
   }
-  if (now.t1 <= now.t0) return;                             // the item's own cost is all there is: the next warp has its tiles
+  if (now.t1 <= now.t0) return;                           // the item's own cost is all there is: the next warp has its tiles
 
   constexpr int AHEAD = 32 / Sh::SUB;
   constexpr bool STAGED = kStaged<D>;
@@ -790,18 +822,18 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   int ids = fetch_pages<D>(p, now.seq, now.t0, 1, lane);
   int next_ids = fetch_pages<D>(p, now.seq, now.t0 + AHEAD, 1, lane);     // unchecked until it becomes `ids`
   int n = 0;                                        // number of the loaded tile in its window of page ids
-  int pos = now.item / p.row_tiles, buf = 0, stage = 0;
-  find_heads(p, hd, now.s, pos, now.item - pos * p.row_tiles, lane, cols[warp][0]);
+  int buf = 0, stage = 0;
+  find_heads(p, hd, now.s, now.pos, now.rt, lane, cols[warp][0]);
   prefetch_q<D>(qbuf[warp], p, now.seq, cols[warp][0][g], lane);
   ids = check_pages<D>(p, ids, now.len - 1, now.t0, 1, lane);
   if (now.len > 0) {
-    if constexpr (STAGED) stage_k<D>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D>(p, pos, g, t), lane);
-    else load_k<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D>(p, pos, g, t), g);
+    if constexpr (STAGED) stage_k<D>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D>(p, now.pos, g, t), lane);
+    else load_k<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D>(p, now.pos, g, t), g);
   }
   commit_copies();                                  // the queries travel with the first keys
   if (now.len > 0) {
-    if constexpr (STAGED) stage_v<D>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D>(p, pos, g, t), lane);
-    else load_v<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D>(p, pos, g, t), t);
+    if constexpr (STAGED) stage_v<D>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D>(p, now.pos, g, t), lane);
+    else load_v<D>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D>(p, now.pos, g, t), t);
   }
   commit_copies();
   for (;;) {
@@ -813,21 +845,21 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
     // the segment behind this one: its first pages, its heads and their queries on their way before they are needed
     const bool more = left > (uint32_t)kItemCost;
     Segment next = now;
-    int next_pos = pos, head_ids = 0;
+    int head_ids = 0;
     if (more) {
       next.t0 = 0;
-      if (++next.item == next.items) {
-        next.item = 0;
-        ++next.seq;
-        next.s = next.seq / p.n_seqs;
-        next.len = len_of(next.seq);
-        next.nt = tiles_of<D>(next.len);
-        next.items = held[next.s] * p.row_tiles;
+      if (++next.rt >= row_tiles(next.s, next.pos)) {
+        next.rt = 0;
+        do {
+          if (++next.pos == p.kv_max) {
+            next.pos = 0;
+            enter(next, next.seq + 1, (next.seq + 1) / p.n_seqs);
+          }
+        } while (row_tiles(next.s, next.pos) == 0);
       }
       next.t1 = (int)min((uint32_t)next.nt, left - kItemCost);
-      next_pos = next.item / p.row_tiles;
       head_ids = fetch_pages<D>(p, next.seq, 0, 1, lane);
-      find_heads(p, hd, next.s, next_pos, next.item - next_pos * p.row_tiles, lane, cols[warp][buf ^ 1]);
+      find_heads(p, hd, next.s, next.pos, next.rt, lane, cols[warp][buf ^ 1]);
       prefetch_q<D>(qbuf[warp], p, next.seq, cols[warp][buf ^ 1][g], lane);          // complete with the next tile's keys
     }
     State<D> st;
@@ -835,7 +867,7 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
     for (int tile = now.t0; tile < now.t1; ++tile) {
       // the tile to load: the item's next one or the next item's first
       const bool inside = tile + 1 < now.t1;
-      const int key0 = inside ? (tile + 1) * Sh::TILE : 0, last_key = inside ? now.len - 1 : next.len - 1, of = inside ? pos : next_pos;
+      const int key0 = inside ? (tile + 1) * Sh::TILE : 0, last_key = inside ? now.len - 1 : next.len - 1, of = inside ? now.pos : next.pos;
       const bool load = (inside || more) && last_key >= 0;
       if (inside) {
         if (++n == AHEAD) {
@@ -884,18 +916,20 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
       const int heads = __popc(__ballot_sync(0xffffffffu, hq >= 0 && t == 0));
       if (lane == 0) {
         const int parts = whole ? 0 : (int)(cut.piece_of(item0 + kItemCost + now.nt - 1) - c);    // further parts of the item
-        const long long all = (long long)p.kv_max * p.row_tiles;
-        int4* desc = p.desc + (p.by_item ? now.seq * all + now.item : (long long)c);
-        *desc = make_int4(now.seq, heads, parts, (int)c);
-        if (p.by_item && now.item + 1 == now.items)                                               // positions that no head reads
-          for (long long k = 1; now.item + k < all; ++k) desc[k] = make_int4(0, 0, 0, 0);
+        const int all = p.kv_max * p.row_tiles, item = now.pos * p.row_tiles + now.rt;
+        int4* desc = p.desc + (p.by_item ? (long long)now.seq * all : (long long)c);
+        desc[p.by_item ? item : 0] = make_int4(now.seq, heads, parts, (int)c);
+        if (p.by_item) {                            // the neighbours in the table that are no items
+          auto is_item = [&](int k) { return k % p.row_tiles < row_tiles(now.s, k / p.row_tiles); };
+          for (int k = item + 1; k < all && !is_item(k); ++k) desc[k] = make_int4(0, 0, 0, 0);
+          for (int k = item - 1; k >= 0 && !is_item(k); --k) desc[k] = make_int4(0, 0, 0, 0);
+        }
       }
     }
     if (!more) break;
     item0 += now.nt + kItemCost;
     left -= next.t1 + kItemCost;
     now = next;
-    pos = next_pos;
     buf ^= 1;
   }
 }

@@ -297,6 +297,8 @@ class Case:
             self.of = np.stack([[kv_pos[s][h // (nh // nkv)] for h in idx[s]] for s in range(S)])
             self.extra = dict(head_idx=torch.from_numpy(idx).cuda(), kv_pos=torch.from_numpy(kv_pos.astype(np.int32)).cuda())
         table, pool = scattered_pages(gen, lens.flatten().tolist(), page)
+        for i, m in enumerate(lens.flatten().tolist()):                  # entries that no key needs may hold anything
+            table[i, -(-m // page):] = (1 << 24) if i % 2 else -7
         self.table, self.lens = table.view(S, n, -1), lens
         both = rng_bf16(gen, pool, 2, self.kv_max, page, d)
         if fill is not None:                                             # whatever the unused slots hold must not matter
@@ -368,6 +370,16 @@ DECODE = [
     (4, [int(x) for x in np.random.default_rng(3).integers(0, 600, 4 * 60)], 6, (12, 4), 64, 16),      # a big ragged batch
     (1, [40000], 2, (4, 2), 8, 256),
     (1, [9000, 8999], 2, None, 32, 16),
+    # sharing by up to twelve heads: positions with one and with two passes over their keys, few items and many
+    (2, [900, 0, 3000, 17], 10, (48, 4), 64, 32),
+    (1, [5000], 13, (48, 4), 16, 16),
+    (1, [2600, 31], 9, (36, 3), 128, 16),
+    (4, [int(x) for x in np.random.default_rng(4).integers(0, 900, 4 * 120)], 10, (48, 4), 32, 16),
+    (8, [int(x) for x in np.random.default_rng(5).integers(0, 1500, 8 * 3)], 70, (96, 8), 16, 16),     # more heads than the kernel caches
+    (1, [int(x) for x in np.random.default_rng(6).integers(0, 40, 700)], 4, (8, 2), 64, 16),           # more sequences than it caches
+    # one cluster of CTAs per item: 2, 4 and 8 of them, lengths that leave some without keys
+    (1, [300, 5, 0], 2, None, 64, 16), (1, [1000, 40], 4, (8, 2), 64, 64), (1, [513], 1, None, 128, 16), (2, [700, 64], 3, (4, 2), 32, 32),
+    (1, [1500], 5, (24, 2), 16, 16), (1, [900], 2, None, 8, 16),
 ]
 
 
