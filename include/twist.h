@@ -490,7 +490,7 @@ int32_t twist_kv_append(const twist_kv_append_args* a /*host*/, void* stream);
 /* twist_attn_decode -- attention of one new token per sequence over the paged cache:
  *     out_h = sum_j softmax_j(q_h . k_j / sqrt(d_head)) v_j   over the kv_len[s][b] cached tokens (the new one included).
  *   q    [S][n_seqs] rows of a' elements (rotated Q, as twist_kv_append writes it), q_stride apart;
- *   out  [S][n_seqs][a'];  lse [S][head_keep][n_seqs] fp32 (log-sum-exp of the scores) or NULL.
+ *   out  [S][n_seqs][a'], not overlapping q;  lse [S][head_keep][n_seqs] fp32 (log-sum-exp of the scores) or NULL.
  *   A sequence without cached tokens gets zeros (lse -inf).
  * Which KV position a head reads: head_idx / kv_pos / n_heads / n_kv_heads as in twist_attn_core_args.  The kept heads of a
  * subnet are distinct, so that at most n_heads / n_kv_heads of them read one position.
@@ -502,8 +502,9 @@ int32_t twist_kv_append(const twist_kv_append_args* a /*host*/, void* stream);
  * Index data is checked on the device: a bad head or page entry is replaced by position 0 / page 0, a kv_len outside
  * [0, max_pages * page_size] is clamped, heads beyond n_heads / n_kv_heads per position keep their old output, and
  * TWIST_ERR_BAD_INDEX is recorded.
- * dtype TWIST_BF16 only; d_head in {8, 16, 32, 64, 128}; n_subnets <= TWIST_MAX_SUBNETS, n_heads <= 1024; n_subnets * n_seqs *
- * kv_max * max_pages * page_size below 2^35 (the work is counted in 32 bits, in steps of 16 keys or more). */
+ * dtype TWIST_BF16 only; d_head in {8, 16, 32, 64, 128}; n_subnets <= TWIST_MAX_SUBNETS, n_subnets * n_seqs <= 65535,
+ * head_keep and n_heads <= 1024; n_subnets * n_seqs * kv_max * max_pages * page_size below 2^35 (the work is counted in
+ * 32 bits, in steps of 16 keys or more). */
 typedef struct {
   int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;
   int32_t page_size, n_pages, max_pages, max_len;

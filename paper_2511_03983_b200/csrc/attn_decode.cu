@@ -98,15 +98,16 @@ __device__ inline uint32_t pack_bf16(float lo, float hi) {
 __device__ inline float lo_f(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ inline float hi_f(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 
-// `W` 32-bit words (W = 4, 2, 1) of a row that is read once.
+// `W` 32-bit words (W = 4, 2, 1) of a row that is read once.  Coherent loads: the launch before may still be writing the cache
+// when this one is placed (see launch_overlapped).
 template <int W>
 __device__ inline void load_words(uint32_t (&r)[W], const __nv_bfloat16* p) {
   if constexpr (W == 4)
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
   else if constexpr (W == 2)
-    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
   else
-    asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(r[0]) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(r[0]) : "l"(p));
 }
 
 // How a thread (g = lane / 4, t = lane % 4) holds a tile.  K: rows g and g + 8 of each 16 keys, KCH chunks of KW words
@@ -749,7 +750,9 @@ __global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecP
   uint32_t mine = 0;
   {
     int i = min(N, (int)threadIdx.x * per), s = i / p.n_seqs, b = i - s * p.n_seqs;
-    for (const int last = min(N, i + per); i < last; ++i) {
+    const int last = min(N, i + per);
+#pragma unroll 8
+    for (; i < last; ++i) {
       mine += (uint32_t)items[s] * (kItemCost + tiles_of<D>(len_of(i)));
       if (++b == p.n_seqs) { b = 0; ++s; }
     }
@@ -1061,7 +1064,7 @@ extern "C" int32_t twist_attn_decode(const twist_attn_decode_args* a, void* stre
   const int dh = a->d_head;
   if (dh != 8 && dh != 16 && dh != 32 && dh != 64 && dh != 128) return TWIST_ERR_UNSUPPORTED;
   if (a->n_subnets > TWIST_MAX_SUBNETS || a->n_heads > 1024 || a->head_keep > 1024) return TWIST_ERR_UNSUPPORTED;
-  if ((long long)a->n_subnets * a->n_seqs > (1 << 24)) return TWIST_ERR_UNSUPPORTED;
+  if ((long long)a->n_subnets * a->n_seqs > 65535) return TWIST_ERR_UNSUPPORTED;
   if (a->page_size < 16 || a->page_size > 1024 || (a->page_size & (a->page_size - 1))) return TWIST_ERR_UNSUPPORTED;
   if ((long long)a->max_pages * a->page_size > 0x7fffffffll - 1024) return TWIST_ERR_UNSUPPORTED;   // positions are 32-bit
   if (a->page_stride % 8 != 0 || a->page_stride < (long long)a->kv_max * a->page_size * dh) return TWIST_ERR_SHAPE;

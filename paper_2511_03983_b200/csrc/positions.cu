@@ -99,7 +99,7 @@ __device__ inline RowInfo find_row(const PosParams& p, long long r, int lane) {
     begin = __shfl_sync(0xffffffffu, begin, b & 31);
     end = __shfl_sync(0xffffffffu, end, b & 31);
     len = __shfl_sync(0xffffffffu, len, b & 31);
-    if (count != b + 1) {                             // not ascending
+    if (count != b + 1 || begin < 0 || end > p.T) {   // not ascending, or rows that the call does not have
       if (lane == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
       return ri;
     }

@@ -1257,6 +1257,8 @@ class DecodeSession:
         """The next token of every sequence, its input x [S][n_seqs][d]; returns the stack's output (valid until the next
         step)."""
         eng, w, S, n, d = self.eng, self.eng.w, self.S, self.n, self.eng.w.d_model
+        if tuple(x.shape) != (S, n, d):
+            raise ValueError("x: expected [%d][%d][%d], got %s" % (S, n, d, tuple(x.shape)))
         self._extend([[1] * n for _ in range(S)])
         cur, nxt = self.x
         cur.copy_(x)

@@ -85,7 +85,7 @@ def decode(B, **kw):
     (dict(q=OK_PTR + 2), "ERR_SHAPE"), (dict(out=OK_PTR + 8), "ERR_SHAPE"), (dict(ws=OK_PTR + 8), "ERR_SHAPE"),
     (dict(ws=None), "ERR_WORKSPACE"), (dict(ws_bytes=64), "ERR_WORKSPACE"),
     (dict(max_pages=1 << 27), "ERR_UNSUPPORTED"), (dict(n_heads=2048), "ERR_UNSUPPORTED"),
-    (dict(n_seqs=4096, max_pages=1 << 22), "ERR_UNSUPPORTED"),          # more work than the kernel's counters hold
+    (dict(n_seqs=32768), "ERR_UNSUPPORTED"), (dict(n_seqs=4096, max_pages=1 << 22), "ERR_UNSUPPORTED"),          # more work than the kernel's counters hold
 ])
 def test_decode_refusals(B, kw, status):
     h = B.lib()

@@ -267,6 +267,8 @@ def test_append_reports_bad_index_data_and_writes_nothing_for_it(B):
     assert torch.equal(k, want)
     # rows that contradict the layout
     for kw in (dict(new_begin=torch.tensor([[0, 2, 1, 3, 4, 5, 6]], dtype=torch.int32).cuda()),
+               dict(new_begin=torch.tensor([[0, 1, 2, 3, 4, 5, 7]], dtype=torch.int32).cuda()),         # more rows than there are
+               dict(new_begin=torch.tensor([[-1, 1, 2, 3, 4, 5, 6]], dtype=torch.int32).cuda()),
                dict(new_len=torch.tensor([[1, 1, 2, 1, 1, -1]], dtype=torch.int32).cuda())):
         lens6 = torch.ones(S, n, dtype=torch.int32).cuda()
         tab = torch.arange(6, dtype=torch.int32).view(S, n, 1).cuda()
@@ -530,7 +532,8 @@ def test_append_and_decode_in_a_captured_graph_replay_with_new_lengths(B):
     k = torch.full((S * n * pages, KV, page, d), float("nan"), dtype=BF, device="cuda")
     v = k.clone()
     lens = torch.zeros(S, n, dtype=torch.int32, device="cuda")
-    qkv = torch.zeros(S, n, (H + 2 * KV) * d, dtype=BF, device="cuda")
+    given = torch.zeros(S, n, (H + 2 * KV) * d, dtype=BF, device="cuda")
+    qkv = torch.zeros_like(given)
     out = torch.zeros(S, n, H * d, dtype=BF, device="cuda")
     lse = torch.zeros(S, H, n, device="cuda")
     ws = torch.empty(B.twist_attn_decode_workspace_bytes(d), dtype=torch.uint8, device="cuda")
@@ -539,6 +542,8 @@ def test_append_and_decode_in_a_captured_graph_replay_with_new_lengths(B):
     q = qkv[..., :H * d]
 
     def step():
+        qkv.copy_(given)                                                  # (a copy and a fill beside the kernels of the graph)
+        out.zero_()
         B.twist_kv_append(B.kv_append_args(B.BF16, S, n, n, H, KV, d, d, qkv=qkv, q_out=q, k_cache=k, v_cache=v, page_table=table,
                                            kv_len=lens, inv_freq=dinv))
         B.twist_attn_decode(B.attn_decode_args(B.BF16, S, n, H, KV, d, nh, nkv, q=q, k_cache=k, v_cache=v, page_table=table, kv_len=lens,
@@ -560,7 +565,7 @@ def test_append_and_decode_in_a_captured_graph_replay_with_new_lengths(B):
     rk, _ = rotate64(z[:, :, :, H:H + KV], np.broadcast_to(np.arange(30)[:, None, None], (30, S, n)), d, 0, inv)
     rk = torch.from_numpy(rk).to(BF).to(torch.float64).numpy()            # as the cache stores it
     for i in range(30):
-        qkv.copy_(rows[i])
+        given.copy_(rows[i])
         lens.fill_(i + 1)
         graph.replay()
         torch.cuda.synchronize()
