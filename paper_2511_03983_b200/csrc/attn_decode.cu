@@ -12,7 +12,11 @@
 // eight consecutive elements (the query is loaded in the same order), and the rows of V^T a thread owns are chosen as
 // eight consecutive elements of a cached row, paired over keys by a byte permute.  No shared memory, no barrier in the
 // loop; the next tile's loads are issued as soon as the registers of this one have been consumed, so a warp keeps about
-// a tile (8 KB) in flight all the time.  (tcgen05 would need 128 rows of queries to fill its smallest tile.)
+// a tile in flight all the time (4 KB and 16 warps an SM at d = 64, 8 KB and 12 warps at d = 128; at d = 64 two steps a
+// tile and 12 warps were 3 to 6 % slower, at d = 128 two steps and 8 warps 8 %).  Smaller heads spend more instructions
+// on a byte, and the registers of one tile do not cover the latency: there the tiles pass through shared memory, two
+// deep (d = 32: 113 -> 83 us for 463 MB; the same at d = 64 and 128 is 15 to 50 % slower, its copies of half and whole
+// rows being issued piece by piece through the same queue).  (tcgen05 would need 128 rows of queries for its smallest tile.)
 //
 // Softmax in fp32 with a running reference maximum per head that moves only when a score exceeds it by more than 2^8 (one
 // vote per tile instead of a reduction).  The probabilities enter the second product as the sum of two bf16 numbers
@@ -43,7 +47,7 @@ constexpr int kItemCost = 1;               // what changing to the next item cos
 constexpr int kMinCost = 2;                // least work of a warp, in tiles
 constexpr int kJoinThreads = 512;
 // The short way, one cluster per item (see run).
-constexpr int kMaxCluster = 8, kShortTiles = 6, kShortWork = 6;
+constexpr int kMaxCluster = 8, kShortTiles = 8, kShortWork = 8, kShortWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.0f;             // log2 headroom of the lazily moved reference maximum
@@ -120,7 +124,7 @@ struct Shape {
   static constexpr int VCH = D == 128 ? 2 : 1;
   static constexpr int VW = D >= 64 ? 4 : (D >= 16 ? D / 16 : 1);
   static constexpr int MT = D >= 16 ? D / 16 : 1;           // MMA tiles over d
-  static constexpr int SUB = D == 128 ? 1 : (D == 64 ? 2 : 4);
+  static constexpr int SUB = D >= 64 ? 1 : 4;
   static constexpr int TILE = 16 * SUB;
 };
 
@@ -697,7 +701,7 @@ constexpr int kRingBytes = kStaged<D> ? 2 * kDecWarps * (int)sizeof(Stage<D>) : 
 constexpr int kCountCache = 256;      // KV positions of all subnets whose heads a CTA counts
 
 template <int D>
-__global__ void __launch_bounds__(kDecThreads, 3) decode_split_kernel(const DecParams p) {
+__global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_kernel(const DecParams p) {
   using Sh = Shape<D>;
   __shared__ int cols[kDecWarps][2][kCols];
   __shared__ __align__(16) QueryBuf<D> qbuf[kDecWarps];
@@ -1022,14 +1026,17 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   }
   const long long grid = (long long)sm_count() * resident[slot];
   // One cluster per item where that needs few turns: two tiles a warp are taken by a single CTA, more by as many CTAs as
-  // leave a warp one, if all of them run at once.  Measured (D = 64, one sequence of 8 heads, 1024 keys): 5.1 us against 9.2
-  // through the line; the line is ahead from about kShortTiles tiles a warp, and where items times their length fill the
-  // GPU kShortWork times (256 ragged items of up to 2048 keys: 20.8 us against 27 to 34 with clusters).
+  // leave a warp one, if all of them run at once.  Measured (d = 64, one sequence of 8 heads, 1024 keys): 5.0 us against 9.2
+  // through the line; 512 items of 512 keys, all at once: 15 against 19.  The line is ahead where a warp would take more
+  // than kShortTiles tiles, where the items fill the GPU kShortWork tiles a warp deep (256 ragged items of up to 2048
+  // keys: 21 us against 27 to 34), and earlier where they do not run at once (512 items of 256 keys, d = 128: 18.2
+  // against 19.6).
   const long long tiles = (max_len + Shape<D>::TILE - 1) / Shape<D>::TILE;
   int cluster = 1;
   if (tiles > 2 * kDecWarps)
     while (cluster < kMaxCluster && 2 * cluster * items <= grid && tiles > kDecWarps * cluster) cluster *= 2;
-  if (items <= 2 * grid && tiles <= kShortTiles * kDecWarps * cluster && tiles * items <= kShortWork * grid * kDecWarps) {
+  if (items <= 2 * grid && tiles <= kShortTiles * kDecWarps * cluster &&
+      tiles * items <= (items <= grid ? kShortWork : kShortWaves) * grid * kDecWarps) {
     TWIST_CUDA_TRY(launch_overlapped(decode_whole_kernel<D>, dim3((unsigned)(items * cluster)), dim3(kDecThreads), 0, st, cluster, p));
     return TWIST_OK;
   }
