@@ -1160,9 +1160,13 @@ class DecodeSession:
     the C ABI.  prefill(k) runs the engine's own forward pass over its batch k (n_seqs sequences of seq_len tokens, the
     first lengths[s][b] of which count) and stores their keys and values; step(x) takes the next token's input [S][n_seqs][d]
     and returns the stack's output for it.  A session belongs to one stream; its cache is its own, the slices are the
-    engine's: extracting other subnets ends it."""
+    engine's: extracting other subnets ends it.
 
-    def __init__(self, eng: StackEngine, max_len: int, page_size: int = 16, n_pages: Optional[int] = None):
+    graph=True captures the layers of a step into a CUDA graph at the first step and replays it from then on (the page
+    table, the lengths and the input are data of the graph, so every step is the same graph): a step then costs the
+    device's time instead of the host's."""
+
+    def __init__(self, eng: StackEngine, max_len: int, page_size: int = 16, n_pages: Optional[int] = None, graph: bool = False):
         w = eng.w
         S, n, d, bf, dev = w.n_subnets, eng.n_seqs, w.d_model, torch.bfloat16, eng.dev
         if max_len < 1:
@@ -1188,6 +1192,7 @@ class DecodeSession:
         self.qkv, self.a = per(lambda gm: gm.nq), per(lambda gm: gm.a_sub)
         self.pre, self.hh = per(lambda gm: gm.gf), per(lambda gm: gm.f_sub)
         self.ws = torch.empty(B.twist_attn_decode_workspace_bytes(w.d_head), dtype=torch.uint8, device=dev)
+        self.use_graph, self.graph = graph, None
         if eng.ln:
             self.x_ln = act(d)
             self.stat = [torch.empty(S, n, dtype=torch.float32, device=dev) for _ in range(2)]
@@ -1256,12 +1261,32 @@ class DecodeSession:
     def step(self, x: torch.Tensor) -> torch.Tensor:
         """The next token of every sequence, its input x [S][n_seqs][d]; returns the stack's output (valid until the next
         step)."""
+        shape = (self.S, self.n, self.eng.w.d_model)
+        if tuple(x.shape) != shape:
+            raise ValueError("x: expected [%d][%d][%d], got %s" % (*shape, tuple(x.shape)))
+        self._extend([[1] * self.n for _ in range(self.S)])
+        self.x[0].copy_(x)
+        if not self.use_graph:
+            return self._layers()
+        if self.graph is None:
+            # the first step runs outside the capture: kernels are loaded, tensor maps encoded; capturing runs nothing
+            y = self._layers()
+            graph = torch.cuda.CUDAGraph()
+            timing, self.eng.timing = self.eng.timing, False
+            try:
+                with torch.cuda.graph(graph):
+                    self._layers()
+            finally:
+                self.eng.timing = timing
+            self.graph = graph
+            return y
+        self.graph.replay()
+        return self.x[self.eng.w.n_layers % 2]
+
+    def _layers(self) -> torch.Tensor:
+        """All layers on self.x[0]; layer l's output goes to the other of the two buffers."""
         eng, w, S, n, d = self.eng, self.eng.w, self.S, self.n, self.eng.w.d_model
-        if tuple(x.shape) != (S, n, d):
-            raise ValueError("x: expected [%d][%d][%d], got %s" % (S, n, d, tuple(x.shape)))
-        self._extend([[1] * n for _ in range(S)])
         cur, nxt = self.x
-        cur.copy_(x)
         for l in range(w.n_layers):
             eng._bind(l)
             kind = eng.kind_of(l)

@@ -128,3 +128,29 @@ def test_extracted_subnets_answer_token_by_token(B, cfg, dims, n_seqs, extra, pa
     want, _ = o.stack_fwd(w, [{m: np.asarray(v, dtype=np.float64) for m, v in o.gather_layer(w, full[l], bps[l], 0).items()} for l in range(w.n_layers)],
                           [o.head_kv_positions(bps[l], w, 0) for l in range(w.n_layers)], tok[0, 0, :1].astype(np.float64), 1, 1, True)
     assert rel_fro(y[0, 0], want[0]) < 2e-2
+
+
+@pytest.mark.parametrize("layers,ln", [(2, False), (3, True)])
+def test_a_session_as_a_replayed_graph_gives_the_same_bits(B, layers, ln):
+    """The layers of a step captured once: the steps give what the steps without a graph give, also after a sequence was
+    released and started again."""
+    from paper_2511_03983_b200.engine import DecodeSession, StackEngine
+    w = replace(I.scaled_twin(I.PRESETS[3], d_model=256, d_ff=688, d_head=64, tokens=42, n_layers=layers, local_steps=1), rope_base=10000.0,
+                layer_norm=ln)
+    eng = StackEngine(w, 2, 21)
+    fill_model(eng, w)
+    eng.X.append(dev(np.stack([I.normal(7, s, (42, w.d_model), 1.0, I.DTYPE_BF16) for s in range(w.n_subnets)])))
+    eng.extract(0)
+    tok = dev(I.normal(78, 0, (20, w.n_subnets, 2, w.d_model), 1.0, I.DTYPE_BF16))
+    outs = []
+    for graph in (False, True):
+        ses = DecodeSession(eng, max_len=48, graph=graph)
+        ses.prefill(0, [[21, 3]] * w.n_subnets)
+        got = [ses.step(tok[i]).clone() for i in range(12)]
+        ses.release(1, 0)
+        got += [ses.step(tok[i]).clone() for i in range(12, 20)]
+        outs.append(got)
+        torch.cuda.synchronize()
+        assert B.twist_device_status() == 0
+    for i, (x, y) in enumerate(zip(*outs)):
+        assert torch.equal(x, y), i
