@@ -262,15 +262,23 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
-# The raw handle of the current stream: torch.cuda.current_stream() builds a Stream object first (3.2 us against 0.4 us
+# The raw handle of the current stream: torch.cuda.current_stream() builds a Stream object first (3.2 us against 0.2 us
 # a call, a third of the host time of a small launch).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream() -> int:
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_device())
+
+
+def _device() -> int:
+    """Number of the current device."""
+    if _raw_device is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_device()
+    return _raw_device()
 
 
 def twist_abi_version() -> int:
@@ -486,7 +494,7 @@ def rope_args(dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, seq
               inv_freq, pos=None) -> RopeArgs:
     """Marshals twist_rope_args.  in_, out: bf16 [S][T][(head_keep + 2 kv_max) d_head] (out may be in_); inv_freq: fp64
     [rot_dims / 2]; pos: int32 [S][T], or None for position t % seq_len."""
-    dev = torch.cuda.current_device()
+    dev = _device()
     n, bf = n_subnets * tokens * (head_keep + 2 * kv_max) * d_head, torch.bfloat16
     if not (in_.dtype is bf and in_.numel() == n and in_.is_contiguous() and in_.get_device() == dev
             and out.dtype is bf and out.numel() == n and out.is_contiguous() and out.get_device() == dev
@@ -517,7 +525,7 @@ def kv_append_args(dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, 
     [n_pages][kv_max][page_size][d_head], pages evenly spaced (one buffer may hold both); page_table: int32
     [S][n_seqs][max_pages]; kv_len: int32 [S][n_seqs], the new tokens included; q_out: bf16 [S][T][head_keep d_head], rows
     evenly spaced (qkv[..., :head_keep * d_head] rotates Q in place)."""
-    dev = torch.cuda.current_device()
+    dev = _device()
     i32, bf = torch.int32, torch.bfloat16
     page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head)
     if k_cache.get_device() != dev or v_cache.get_device() != dev or (q_out is not None and q_out.get_device() != dev):
@@ -553,7 +561,7 @@ def attn_decode_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_head
     kv_append_args; head_idx int32 [S][head_keep] and kv_pos int32 [S][n_kv_heads] for grouped-query sharing; out bf16
     [S][n_seqs][head_keep d_head]; lse fp32 [S][head_keep][n_seqs]; ws: scratch of at least
     twist_attn_decode_workspace_bytes(d_head) bytes."""
-    dev = torch.cuda.current_device()
+    dev = _device()
     i32, bf = torch.int32, torch.bfloat16
     page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head)
     if k_cache.get_device() != dev or v_cache.get_device() != dev or q.get_device() != dev or ws.get_device() != dev:
@@ -563,16 +571,25 @@ def attn_decode_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_head
     if not (page_table.dtype is i32 and page_table.numel() == seqs * max_pages and page_table.is_contiguous()
             and page_table.get_device() == dev
             and kv_len.dtype is i32 and kv_len.numel() == seqs and kv_len.is_contiguous() and kv_len.get_device() == dev
-            and out.dtype is bf and out.numel() == seqs * width and out.is_contiguous() and out.get_device() == dev):
+            and out.dtype is bf and out.numel() == seqs * width and out.is_contiguous() and out.get_device() == dev
+            and (lse is None or (lse.dtype is torch.float32 and lse.numel() == seqs * head_keep and lse.is_contiguous()
+                                 and lse.get_device() == dev))
+            and (head_idx is None or (head_idx.dtype is i32 and head_idx.numel() == n_subnets * head_keep
+                                      and head_idx.is_contiguous() and head_idx.get_device() == dev))
+            and (kv_pos is None or (kv_pos.dtype is i32 and kv_pos.numel() == n_subnets * n_kv_heads
+                                    and kv_pos.is_contiguous() and kv_pos.get_device() == dev))):
         _tensor("page_table", page_table, i32, seqs * max_pages, dev)
         _tensor("kv_len", kv_len, i32, seqs, dev)
         _tensor("out", out, bf, seqs * width, dev)
+        for name, t, dtype_, n in (("lse", lse, torch.float32, seqs * head_keep), ("head_idx", head_idx, i32, n_subnets * head_keep),
+                                   ("kv_pos", kv_pos, i32, n_subnets * n_kv_heads)):
+            if t is not None:
+                _tensor(name, t, dtype_, n, dev)
     a = AttnDecodeArgs.from_buffer_copy(_DECODE_PACK.pack(
         dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, max_len, stride,
         _rows("q", q, n_subnets, n_seqs, width), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
-        kv_len.data_ptr(), 0 if head_idx is None else _tensor("head_idx", head_idx, i32, n_subnets * head_keep, dev),
-        0 if kv_pos is None else _tensor("kv_pos", kv_pos, i32, n_subnets * n_kv_heads, dev), out.data_ptr(),
-        0 if lse is None else _tensor("lse", lse, torch.float32, seqs * head_keep, dev), ws.data_ptr(),
+        kv_len.data_ptr(), 0 if head_idx is None else head_idx.data_ptr(), 0 if kv_pos is None else kv_pos.data_ptr(),
+        out.data_ptr(), 0 if lse is None else lse.data_ptr(), ws.data_ptr(),
         ws.numel() * ws.element_size()))
     a._keepalive = (q, k_cache, v_cache, page_table, kv_len, out, ws, head_idx, kv_pos, lse)
     return a

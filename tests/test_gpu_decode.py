@@ -606,3 +606,32 @@ def test_calls_on_two_streams_at_once(B):
     torch.cuda.synchronize()
     for c, (out, lse) in zip(cases, want):
         assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+
+
+def test_tensors_that_do_not_fit_the_call_are_refused(B):
+    c = Case(B, 1, [40, 9], 4, (8, 2), 32, 16)
+    for kw in (dict(kv_len=c.dlens.long()), dict(kv_len=c.dlens[:, :1].contiguous()), dict(page_table=c.dtable.cpu()),
+               dict(lse=c.lse.double()), dict(lse=c.lse[:, :3].contiguous()), dict(head_idx=c.extra["head_idx"].long()),
+               dict(kv_pos=c.extra["kv_pos"][:, :1].contiguous()), dict(out=c.out.float()), dict(q=c.dq.cpu()), dict(ws=c.ws.cpu()),
+               dict(k_cache=c.k[:, :1]), dict(v_cache=c.v.float()), dict(q=c.dq[..., ::2])):
+        with pytest.raises(ValueError):
+            c.args(B, **kw)
+    with pytest.raises(B.TwistError):
+        B.twist_attn_decode(c.args(B, ws=c.ws[:64]))
+    x = torch.zeros(1, 4, 96, dtype=BF, device="cuda")
+    inv = torch.ones(16, dtype=torch.float64, device="cuda")
+    good = dict(in_=x, out=x, inv_freq=inv)
+    B.twist_rope_fwd(B.rope_args(B.BF16, 1, 4, 1, 1, 32, 32, 4, **good))
+    for kw in (dict(in_=x.float()), dict(out=x[:, :2]), dict(inv_freq=inv.float()), dict(inv_freq=inv[:8]), dict(in_=x.cpu()),
+               dict(pos=torch.zeros(1, 4, device="cuda"))):
+        with pytest.raises(ValueError):
+            B.rope_args(B.BF16, 1, 4, 1, 1, 32, 32, 4, **dict(good, **kw))
+    k = torch.zeros(2, 1, 16, 32, dtype=BF, device="cuda")
+    good = dict(qkv=x, k_cache=k, v_cache=k.clone(), page_table=torch.zeros(1, 4, 1, dtype=torch.int32, device="cuda"),
+                kv_len=torch.ones(1, 4, dtype=torch.int32, device="cuda"), inv_freq=inv)
+    B.kv_append_args(B.BF16, 1, 4, 4, 1, 1, 32, 32, **good)
+    for kw in (dict(qkv=x[..., :64]), dict(q_out=x[..., :33]), dict(new_len=torch.ones(1, 3, dtype=torch.int32, device="cuda")),
+               dict(new_begin=torch.ones(1, 4, dtype=torch.int32, device="cuda")), dict(kv_count=torch.ones(2, dtype=torch.int32, device="cuda")),
+               dict(kv_len=good["kv_len"].cpu())):
+        with pytest.raises(ValueError):
+            B.kv_append_args(B.BF16, 1, 4, 4, 1, 1, 32, 32, **dict(good, **kw))
