@@ -14,12 +14,14 @@
 // is done once for them and their loads are in flight together.  Rotating, a thread holds 128 bytes and issues its first
 // loads before the CTA finds positions and angles, on which they do not depend.  Appending, finding a row's place costs
 // two dependent round trips, and rows of no sequence are not read: the places come first and more, lighter CTAs share an
-// SM to cover them (44 000 packed rows of 4.6 KB: 134 us loads first, 4 CTAs an SM; 116 us places first, 6 CTAs).
+// SM to cover them (44 000 packed rows of 4.6 KB: 134 us loads first, 4 CTAs an SM; 116 us places first, 6 CTAs; 5 CTAs
+// and fewer spilled registers: 122).
 //
 // Rotation.  A thread's unit of work owns both elements of every pair it rotates, so rotating in place is safe without
-// any ordering between threads: in the HALF layout a unit is two 16-byte chunks half a rotation apart, in the PAIRS
-// layout one 16-byte chunk; where chunks would straddle the halves (rot_dims/2 or rot_dims not a multiple of 8) a unit
-// is a whole head, element by element.
+// any ordering between threads: a unit is two 16-byte chunks half a rotation apart in the HALF layout, one chunk in the
+// PAIRS layout and in what is not rotated (appending, two neighbours where they come in twos: 116 -> 113 us in the case
+// above; rotating, twice the rows in flight are worth more: 190 us against 194); where chunks would straddle the halves
+// (rot_dims/2 or rot_dims not a multiple of 8) a unit is a whole head, element by element.
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -58,7 +60,8 @@ struct PosParams {
   int T, seq_len, heads, kv, dh, width;
   int rot, half;                 // half = rot / 2
   int tile_rows;
-  int units_per_head, first_unit, head_units, row_units;    // a row's units: those of its heads, then 8-element chunks of V
+  int units_per_head, first_unit, head_units, row_units;    // a row's units: those of its heads, then those of V
+  int wide;                      // appending: units that are not half a rotation apart are two neighbouring chunks, not one
   Divisor by_units, by_head, by_half, by_chunks;
   float sign;
   int in_place;
@@ -155,7 +158,7 @@ __device__ inline void rotate_pairs(uint4& v, const float2* cs) {
 enum { MODE_HALF = 0, MODE_PAIRS = 1, MODE_SLOW_HALF = 2, MODE_SLOW_PAIRS = 3 };
 
 // Rows that a thread has in flight (see above).
-__host__ __device__ constexpr int batch_rows(bool append, int mode) { return (mode == MODE_PAIRS ? 8 : 4) / (append ? 2 : 1); }
+__host__ __device__ constexpr int batch_rows(bool append, int mode) { return append ? 2 : (mode == MODE_PAIRS ? 8 : 4); }
 
 // Positions (and, appending, destinations) of the tile's rows, then their (cos, sin) table.
 template <bool APPEND>
@@ -198,10 +201,11 @@ __global__ void __launch_bounds__(kPosThreads, APPEND ? 6 : 4) rotate_rows_kerne
   for (uint32_t k = threadIdx.x; k < items || (!APPEND && k == threadIdx.x); k += kPosThreads) {
     const int batch = (int)p.by_units.divide(k), u = (int)k - batch * p.row_units + p.first_unit;
     const int r0 = batch * kBatch, n = k < items ? min(kBatch, n_rows - r0) : 0;
-    // unit j of head h, or chunk j of V (h = n_heads): elements at .. at + 7 of it, and those half a rotation further
+    // unit j of head h, or of V (h = n_heads): elements at .. at + 7 of it, and (two) those `hop` further
     const int h = u < p.head_units ? (int)p.by_head.divide(u) : n_heads, j = u - (u < p.head_units ? h * p.units_per_head : p.head_units);
-    const bool pair = MODE == MODE_HALF && h < n_heads && j < pair_units;
-    const int at = MODE == MODE_HALF && h < n_heads && !pair ? p.rot + 8 * (j - pair_units) : 8 * j;
+    const bool pair = MODE == MODE_HALF && h < n_heads && j < pair_units, two = pair || (APPEND && p.wide);
+    const int hop = pair ? p.half : 8, step = APPEND && p.wide ? 16 : 8;
+    const int at = pair ? 8 * j : (MODE == MODE_HALF && h < n_heads ? p.rot + step * (j - pair_units) : step * j);
     const __nv_bfloat16* src = p.in + (row0 + r0) * p.width + h * p.dh + at;
     uint4 lo[kBatch], hi[kBatch];
     if (!SLOW || h == n_heads) {
@@ -209,7 +213,7 @@ __global__ void __launch_bounds__(kPosThreads, APPEND ? 6 : 4) rotate_rows_kerne
       for (int i = 0; i < kBatch; ++i) {
         if (i < n && (!APPEND || info[r0 + i].valid)) {
           lo[i] = *reinterpret_cast<const uint4*>(src + (long long)i * p.width);
-          if (pair) hi[i] = *reinterpret_cast<const uint4*>(src + (long long)i * p.width + p.half);
+          if (two) hi[i] = *reinterpret_cast<const uint4*>(src + (long long)i * p.width + hop);
         }
       }
     }
@@ -225,17 +229,17 @@ __global__ void __launch_bounds__(kPosThreads, APPEND ? 6 : 4) rotate_rows_kerne
         dst = p.k_cache + (((long long)group * p.dh) << p.page_shift) + at;
       } else {
         group = (int)p.by_chunks.divide(j);
-        dst = p.v_cache + (((long long)group * p.dh) << p.page_shift) + (8 * j - group * p.dh);
+        dst = p.v_cache + (((long long)group * p.dh) << p.page_shift) + (at - group * p.dh);
       }
     } else {
       dst = p.out + (row0 + r0) * p.width + h * p.dh + at;
     }
-    const long long step = APPEND ? p.q_stride : p.width;
+    const long long down = APPEND ? p.q_stride : p.width;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (i >= n) continue;
       const int r = r0 + i;
-      __nv_bfloat16* to = dst + i * step;
+      __nv_bfloat16* to = dst + i * down;
       if constexpr (APPEND) {
         const RowInfo ri = info[r];
         if (group >= ri.held) continue;             // not held, or a row of no sequence (held = -1)
@@ -259,11 +263,12 @@ __global__ void __launch_bounds__(kPosThreads, APPEND ? 6 : 4) rotate_rows_kerne
       }
       if (MODE == MODE_HALF && pair) {
         rotate8(lo[i], hi[i], cs + at);
-        *reinterpret_cast<uint4*>(to + p.half) = hi[i];
       } else if (MODE == MODE_PAIRS && h < n_heads && at < p.rot) {
         rotate_pairs(lo[i], cs + at / 2);
+        if (two) rotate_pairs(hi[i], cs + at / 2 + 4);
       }
       *reinterpret_cast<uint4*>(to) = lo[i];
+      if (two) *reinterpret_cast<uint4*>(to + hop) = hi[i];
     }
   }
 }
@@ -274,10 +279,12 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
   if (layout == TWIST_ROPE_HALF) mode = p.half % 8 == 0 ? MODE_HALF : MODE_SLOW_HALF;
   else mode = p.rot % 8 == 0 ? MODE_PAIRS : MODE_SLOW_PAIRS;
   if (p.rot == 0) mode = MODE_PAIRS;                                                    // plain 16-byte chunks
-  p.units_per_head = mode == MODE_HALF ? p.half / 8 + (p.dh - p.rot) / 8 : mode == MODE_PAIRS ? p.dh / 8 : 1;
+  p.wide = APPEND && p.dh % 16 == 0 && (mode == MODE_HALF ? (p.dh - p.rot) % 16 == 0 : mode == MODE_PAIRS ? p.rot % 16 == 0 : true);
+  const int step = p.wide ? 16 : 8;
+  p.units_per_head = mode == MODE_HALF ? p.half / 8 + (p.dh - p.rot) / step : mode == MODE_PAIRS ? p.dh / step : 1;
   p.first_unit = APPEND && !p.out ? p.heads * p.units_per_head : 0;                     // Q is not wanted
   p.head_units = (p.heads + p.kv) * p.units_per_head;
-  p.row_units = p.head_units - p.first_unit + (APPEND || !p.in_place ? p.kv * p.dh / 8 : 0);
+  p.row_units = p.head_units - p.first_unit + (APPEND || !p.in_place ? p.kv * p.dh / step : 0);
   // Rows of a tile: as many as still give every SM several tiles.
   const long long want = p.rows / ((long long)sm_count() * 4);
   p.tile_rows = (int)(want < 1 ? 1 : (want > kMaxRows ? kMaxRows : want));
@@ -286,7 +293,7 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
   p.by_units = divisor((uint32_t)p.row_units, (uint64_t)((p.tile_rows + batch_rows(APPEND, mode) - 1) / batch_rows(APPEND, mode)) * p.row_units + kPosThreads);
   p.by_head = divisor((uint32_t)p.units_per_head, (uint64_t)p.head_units);
   p.by_half = divisor((uint32_t)(p.half > 0 ? p.half : 1), (uint64_t)p.tile_rows * p.half);
-  p.by_chunks = divisor((uint32_t)(p.dh / 8), (uint64_t)p.kv * p.dh / 8);
+  p.by_chunks = divisor((uint32_t)(p.dh / step), (uint64_t)p.kv * p.dh / step);
   const size_t smem = (size_t)p.tile_rows * p.half * sizeof(float2);                    // at most 16 KB
   void (*kernel)(PosParams) = mode == MODE_HALF ? rotate_rows_kernel<APPEND, MODE_HALF>
                               : mode == MODE_PAIRS ? rotate_rows_kernel<APPEND, MODE_PAIRS>
