@@ -317,6 +317,8 @@ __device__ inline int position_of(const DecParams& p, const Heads& hd, int s, in
 }
 
 // The kept heads number 8 rt .. 8 rt + 7 among those that read KV position `pos`, into cols[0..7] (-1: none).  One warp.
+// A position takes as many heads as a group has (what the join is launched for): more, by a list that repeats heads or
+// sends two groups to one position, are reported and left out.
 __device__ inline void find_heads(const DecParams& p, const Heads& hd, int s, int pos, int rt, int lane, int* cols) {
   if (!p.head_idx) {
     if (lane < kCols) cols[lane] = lane == 0 ? pos : -1;
@@ -330,11 +332,11 @@ __device__ inline void find_heads(const DecParams& p, const Heads& hd, int s, in
     const int hq = h0 + lane;
     const bool mine = hq < p.heads && position_of(p, hd, s, hq) == pos;
     const unsigned vote = __ballot_sync(0xffffffffu, mine);
-    const int rank = seen + __popc(vote & ((1u << lane) - 1)) - kCols * rt;
-    if (mine && rank >= 0 && rank < kCols) cols[rank] = hq;
+    const int number = seen + __popc(vote & ((1u << lane) - 1)), rank = number - kCols * rt;
+    if (mine && number < p.per_group && rank >= 0 && rank < kCols) cols[rank] = hq;
     seen += __popc(vote);
   }
-  if (lane == 0 && rt == 0 && seen > kCols * p.row_tiles) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+  if (lane == 0 && rt == 0 && seen > p.per_group) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
   __syncwarp();
 }
 
