@@ -1159,8 +1159,8 @@ class DecodeSession:
     layers.  The host keeps the lengths and the free pages; like the engines the session only allocates buffers and calls
     the C ABI.  prefill(k) runs the engine's own forward pass over its batch k (n_seqs sequences of seq_len tokens, the
     first lengths[s][b] of which count) and stores their keys and values; step(x) takes the next token's input [S][n_seqs][d]
-    and returns the stack's output for it.  A session belongs to one stream; its cache is its own, the slices are the
-    engine's: extracting other subnets ends it.
+    and returns the stack's output for it.  A call that raises counts for nothing: lengths and pages are as before it.  A session
+    belongs to one stream; its cache is its own, the slices are the engine's: extracting other subnets ends it.
 
     graph=True captures the layers of a step into a CUDA graph at the first step and replays it from then on (the page
     table, the lengths and the input are data of the graph, so every step is the same graph): a step then costs the
@@ -1220,6 +1220,22 @@ class DecodeSession:
             self.page_table.copy_(torch.tensor(rows, dtype=torch.int32))
         self.kv_len.copy_(torch.tensor(self.lens, dtype=torch.int32))
 
+    @contextmanager
+    def _growing(self, new):
+        """_extend for a call that uses the room: if it raises, lengths and pages go back to what they were."""
+        lens, held = [list(r) for r in self.lens], [[len(p) for p in r] for r in self.pages]
+        try:
+            self._extend(new)
+            yield
+        except BaseException:
+            self.lens = lens
+            for s in reversed(range(self.S)):                       # in the reverse order: the free list as it was
+                for b in reversed(range(self.n)):
+                    while len(self.pages[s][b]) > held[s][b]:
+                        self.free.append(self.pages[s][b].pop())
+            self.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+            raise
+
     def release(self, s: int, b: int):
         """Forgets a sequence: its pages are free again, its next token is its first."""
         self.free.extend(reversed(self.pages[s][b]))
@@ -1238,17 +1254,17 @@ class DecodeSession:
             raise ValueError("prefill of sequences that hold tokens already")
         if len(lengths) != self.S or any(len(r) != self.n or max(r) > eng.seq_len for r in lengths):
             raise ValueError("lengths: %d x %d values up to %d are expected" % (self.S, self.n, eng.seq_len))
-        self._extend(lengths)
-        self.new_len.copy_(torch.tensor(lengths, dtype=torch.int32))
-        eng.forward(k)
-        for l in range(w.n_layers):
-            eng._bind(l)
-            # the saved projections are rotated already
-            with eng._timed("append"):
-                B.twist_kv_append(B.kv_append_args(w.dtype, self.S, self.n, w.tokens, eng.head_keep, eng.kv_max, w.d_head,
-                                                   qkv=eng.qkv_l[l], new_len=self.new_len, kv_count=eng.kv_count[l],
-                                                   **self._cache(l)))
-            eng.launches += 1
+        with self._growing(lengths):
+            self.new_len.copy_(torch.tensor(lengths, dtype=torch.int32))
+            eng.forward(k)
+            for l in range(w.n_layers):
+                eng._bind(l)
+                # the saved projections are rotated already
+                with eng._timed("append"):
+                    B.twist_kv_append(B.kv_append_args(w.dtype, self.S, self.n, w.tokens, eng.head_keep, eng.kv_max, w.d_head,
+                                                       qkv=eng.qkv_l[l], new_len=self.new_len, kv_count=eng.kv_count[l],
+                                                       **self._cache(l)))
+                eng.launches += 1
         return eng.x[w.n_layers]
 
     def _ln(self, l: int, which: str, x, y):
@@ -1264,24 +1280,24 @@ class DecodeSession:
         shape = (self.S, self.n, self.eng.w.d_model)
         if tuple(x.shape) != shape:
             raise ValueError("x: expected [%d][%d][%d], got %s" % (*shape, tuple(x.shape)))
-        self._extend([[1] * self.n for _ in range(self.S)])
-        self.x[0].copy_(x)
-        if not self.use_graph:
-            return self._layers()
-        if self.graph is None:
-            # the first step runs outside the capture: kernels are loaded, tensor maps encoded; capturing runs nothing
-            y = self._layers()
-            graph = torch.cuda.CUDAGraph()
-            timing, self.eng.timing = self.eng.timing, False
-            try:
-                with torch.cuda.graph(graph):
-                    self._layers()
-            finally:
-                self.eng.timing = timing
-            self.graph = graph
-            return y
-        self.graph.replay()
-        return self.x[self.eng.w.n_layers % 2]
+        with self._growing([[1] * self.n for _ in range(self.S)]):
+            self.x[0].copy_(x)
+            if not self.use_graph:
+                return self._layers()
+            if self.graph is None:
+                # the first step runs outside the capture: kernels are loaded, tensor maps encoded; capturing runs nothing
+                y = self._layers()
+                graph = torch.cuda.CUDAGraph()
+                timing, self.eng.timing = self.eng.timing, False
+                try:
+                    with torch.cuda.graph(graph):
+                        self._layers()
+                finally:
+                    self.eng.timing = timing
+                self.graph = graph
+                return y
+            self.graph.replay()
+            return self.x[self.eng.w.n_layers % 2]
 
     def _layers(self) -> torch.Tensor:
         """All layers on self.x[0]; layer l's output goes to the other of the two buffers."""
