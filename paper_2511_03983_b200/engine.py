@@ -1025,10 +1025,15 @@ class StackEngine(RoundEngine):
         self.launches += 1
 
     # ------------------------------------------------------------------ the chained local step
-    def forward(self, k: int):
+    def forward(self, k: int, padding: Optional[torch.Tensor] = None):
+        """All layers on batch k.  padding (bool [S][T][1]): rows of the batch that are no tokens.  They go in as zeros: the
+        attention core multiplies the values of later rows by probabilities of zero, which does not remove a NaN or an
+        infinity."""
         w = self.w
         S, T, d = w.n_subnets, w.tokens, w.d_model
         self.x[0].copy_(self.X[k])
+        if padding is not None:
+            self.x[0].masked_fill_(padding, 0.0)
         for l in range(w.n_layers):
             self._bind(l)
             x_a = self.x[l]
@@ -1247,7 +1252,7 @@ class DecodeSession:
 
     def prefill(self, k: int, lengths: Optional[Sequence[Sequence[int]]] = None) -> torch.Tensor:
         """The prompts: the engine's forward pass over its batch k.  Sequences must be empty.  Returns the stack's outputs
-        [S][T][d] (rows behind a sequence's length mean nothing)."""
+        [S][T][d].  Rows behind a sequence's length may hold anything, and mean nothing in the result."""
         eng, w = self.eng, self.eng.w
         lengths = [[eng.seq_len] * self.n for _ in range(self.S)] if lengths is None else [list(r) for r in lengths]
         if any(m for row in self.lens for m in row):
@@ -1256,7 +1261,11 @@ class DecodeSession:
             raise ValueError("lengths: %d x %d values up to %d are expected" % (self.S, self.n, eng.seq_len))
         with self._growing(lengths):
             self.new_len.copy_(torch.tensor(lengths, dtype=torch.int32))
-            eng.forward(k)
+            padding = None
+            if any(m < eng.seq_len for r in lengths for m in r):
+                row = torch.arange(eng.seq_len, dtype=torch.int32, device=self.new_len.device)
+                padding = (row >= self.new_len.unsqueeze(-1)).view(self.S, self.n * eng.seq_len, 1)
+            eng.forward(k, padding)
             for l in range(w.n_layers):
                 eng._bind(l)
                 # the saved projections are rotated already
