@@ -490,7 +490,7 @@ int32_t twist_kv_append(const twist_kv_append_args* a /*host*/, void* stream);
 /* twist_attn_decode -- attention of one new token per sequence over the paged cache:
  *     out_h = sum_j softmax_j(q_h . k_j / sqrt(d_head)) v_j   over the kv_len[s][b] cached tokens (the new one included).
  *   q    [S][n_seqs] rows of a' elements (rotated Q, as twist_kv_append writes it), q_stride apart;
- *   out  [S][n_seqs][a'], not overlapping q;  lse [S][head_keep][n_seqs] fp32 (log-sum-exp of the scores) or NULL.
+ *   out  [S][n_seqs][a'], not over q (refused; beside or between its rows is fine);  lse [S][head_keep][n_seqs] fp32 (log-sum-exp of the scores) or NULL.
  *   A sequence without cached tokens gets zeros (lse -inf).
  * Which KV position a head reads: head_idx / kv_pos / n_heads / n_kv_heads as in twist_attn_core_args.  The kept heads of a
  * subnet are distinct, so that at most n_heads / n_kv_heads of them read one position.

@@ -1007,6 +1007,14 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecPara
   if (d == 0 && p.lse) p.lse[lse_at(p, item.x, head)] = (m + log2f(l)) * kLn2;
 }
 
+// Whether the output, dense, lies over one of the rows of queries (which CTAs still read when others write).
+bool over_queries(const DecParams& p, int d) {
+  const long long rows = (long long)p.S * p.n_seqs, width = 2ll * p.heads * d, stride = 2 * p.q_stride;
+  const long long at = (long long)(reinterpret_cast<uintptr_t>(p.out) - reinterpret_cast<uintptr_t>(p.q));     // from the first query
+  const long long row = at < width ? 0 : (at - width) / stride + 1;                                            // the first that ends behind it
+  return row < rows && row * stride < at + rows * width;
+}
+
 size_t max_warps() { return (size_t)sm_count() * kMaxCtasPerSm * kDecWarps; }
 size_t desc_bytes() { return (max_warps() * sizeof(int4) + 255) / 256 * 256; }
 
@@ -1016,6 +1024,7 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   // the line is counted in 32 bits
   const long long longest = (((long long)p.max_pages << p.page_shift) + Shape<D>::TILE - 1) / Shape<D>::TILE + 1 + kItemCost;
   if (items > 0x7fffffffll / longest) return TWIST_ERR_UNSUPPORTED;
+  if (over_queries(p, D)) return TWIST_ERR_SHAPE;
   p.status = device_status_ptr();
   if (!p.status) return TWIST_ERR_CUDA;
   static int resident[64] = {0};

@@ -90,3 +90,31 @@ def test_heads_beyond_a_group_are_reported_and_left_on_both_ways(B, group, H, he
     out = out.view(1, 3, H, d)
     assert torch.equal(out[:, :, :fit], want.view(1, 3, fit, d)) and torch.equal(lse[:, :fit], want_lse)
     assert bool((out[:, :, fit:] == 9.0).all()) and bool((lse[:, fit:] == 9.0).all())
+
+
+@pytest.mark.parametrize("bound", [SHORT, LINE])
+@pytest.mark.parametrize("q_stride,shift", [
+    (4 * 64, -6 * 256), (4 * 64, 6 * 256),           # right before the queries, right behind them
+    (12 * 256, 256), (12 * 256, 4 * 12 * 256 + 6 * 256 - 8),     # between two rows of queries that lie far apart
+    (12 * 256, 5 * 12 * 256 + 256),                  # right behind the last row
+])
+def test_an_output_beside_the_queries_is_taken(B, q_stride, shift, bound):
+    """Queries and output in one buffer: only an output over the queries is refused (there, nothing is written)."""
+    c = Case(B, 2, [40, 0, 700, 9, 33, 1], 4, (8, 2), 64, 16)
+    want, want_lse, _ = call(B, c, bound)
+    room = 6 * 256
+    buf = torch.full((2 * room + 6 * q_stride,), 5.0, dtype=BF, device="cuda")
+    q = torch.as_strided(buf, (2, 3, 256), (3 * q_stride, q_stride, 1), room)
+    q.copy_(c.dq)
+    before = buf.clone()
+    out = buf[room + shift:room + shift + 6 * 256].view(2, 3, 256)
+    _, lse, _ = call(B, c, bound, q=q, out=out)
+    assert B.twist_device_status() == 0
+    assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(q, c.dq)
+    out.copy_(before[room + shift:room + shift + 6 * 256].view(2, 3, 256))
+    assert torch.equal(buf, before)
+    for over in (0, 8, -8):
+        with pytest.raises(B.TwistError):
+            call(B, c, bound, q=q, out=buf[room + over:room + over + 6 * 256].view(2, 3, 256))
+    torch.cuda.synchronize()
+    assert torch.equal(buf, before)
