@@ -1027,10 +1027,12 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   if (over_queries(p, D)) return TWIST_ERR_SHAPE;
   p.status = device_status_ptr();
   if (!p.status) return TWIST_ERR_CUDA;
-  static int resident[64] = {0};
+  static int resident[64] = {0}, join_resident[64];
   const int slot = device_slot();
   if (resident[slot] == 0) {
     int n = 0;
+    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_join_kernel<D>, kJoinThreads, 0));
+    join_resident[slot] = n < 1 ? 1 : n;
     TWIST_CUDA_TRY(cudaFuncSetAttribute(decode_split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<D>));
     TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_split_kernel<D>, kDecThreads, kRingBytes<D>));
     resident[slot] = n < 1 ? 1 : (n > kMaxCtasPerSm ? kMaxCtasPerSm : n);
@@ -1053,11 +1055,15 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   }
   p.by_item = items <= grid * kDecWarps;
   TWIST_CUDA_TRY(launch_overlapped(decode_split_kernel<D>, dim3((unsigned)grid), dim3(kDecThreads), kRingBytes<D>, st, 1, p));
-  // An item of an even batch is cut into about warps / items parts: the fewer items, the more threads share the parts of one
-  // (from 16 parts a thread on; from 8 on, a join of 256 items no longer fits the GPU at once: 21.0 us against 20.0).
-  int groups = 1;
-  while (groups < kJoinThreads / 32 && 16ll * groups * items < grid * kDecWarps) groups *= 2;
+  // An item of an even batch is cut into about warps / items parts: the fewer items, the more threads share the parts of
+  // one, down to eight parts each, as long as all threads of the join run at once.  The whole call, with twice the threads
+  // against without: where they fit, four heads on a position, 16 items, d = 16 and 32: 15.9 and 16.5 us against 17.5; one
+  // head a position, 64 to 256 items, d = 64: 49.0 against 49.6.  Where they do not (262144 for 151552), eight heads on a
+  // position, d = 64, 32 to 256 items: 22.3 to 22.9 against 21.4 to 22.1; four subnets, 256 ragged items: 20.9 against 19.9.
   const int elems = (kCols < p.per_group ? kCols : p.per_group) * D;                   // of the heads that share a position
+  const long long at_once = (long long)sm_count() * join_resident[slot] * kJoinThreads;
+  int groups = 1;
+  while (groups < kJoinThreads / 32 && 8ll * groups * items < grid * kDecWarps && 2ll * groups * items * elems <= at_once) groups *= 2;
   const int block = elems * groups < 32 ? 32 : (elems * groups > kJoinThreads ? kJoinThreads : elems * groups);
   const dim3 join_grid((unsigned)(p.by_item ? items : grid * kDecWarps), (unsigned)((elems * groups + block - 1) / block));
   TWIST_CUDA_TRY(launch_overlapped(decode_join_kernel<D>, join_grid, dim3(block), 0, st, 1, p, groups));
