@@ -490,21 +490,29 @@ int32_t twist_kv_append(const twist_kv_append_args* a /*host*/, void* stream);
 /* twist_attn_decode -- attention of one new token per sequence over the paged cache:
  *     out_h = sum_j softmax_j(q_h . k_j / sqrt(d_head)) v_j   over the kv_len[s][b] cached tokens (the new one included).
  *   q    [S][n_seqs] rows of a' elements (rotated Q, as twist_kv_append writes it), q_stride apart;
- *   out  [S][n_seqs][a'], not over q (refused; beside or between its rows is fine);  lse [S][head_keep][n_seqs] fp32 (log-sum-exp of the scores) or NULL.
+ *   out  [S][n_seqs][a'], not over q (refused; beside or between its rows is fine);  lse [S][head_keep][n_seqs] fp32
+ *   (log-sum-exp of the scores) or NULL.
  *   A sequence without cached tokens gets zeros (lse -inf).
  * Which KV position a head reads: head_idx / kv_pos / n_heads / n_kv_heads as in twist_attn_core_args.  The kept heads of a
  * subnet are distinct, so that at most n_heads / n_kv_heads of them read one position.
- * Long caches are split over the GPU's SMs and joined: the split follows from kv_len alone (ragged batches are balanced on
- * the device), the order of every sum is fixed, results are deterministic.  ws: device scratch of at least
- * twist_attn_decode_workspace_bytes(...) bytes; calls that may overlap on the GPU need scratch of their own.
+ * Long caches are split over the GPU's SMs and joined (ragged batches are balanced on the device).  Which way the work goes
+ * follows from the shapes and the bound on the lengths (max_len, or the table's room without one), where it is cut from
+ * kv_len: for the same lengths, bound, table width, heads and GPU the order of every sum is the same, and so are the bits.
+ * ws: device scratch of at least twist_attn_decode_workspace_bytes(...) bytes; calls that may overlap on the GPU need
+ * scratch of their own.
  * max_len: an upper bound of the kv_len entries that the caller knows (0: max_pages * page_size); it only chooses how the
- * work is split, results do not depend on its being right beyond the rounding of another order of summation.
+ * work is split, results do not depend on its being right beyond the rounding of another order of summation.  A bound far
+ * above the lengths can send short sequences the long way.
+ * Probabilities enter the product with V as the sum of two bf16 terms (16 bits), sums are fp32 and divided at the end: values
+ * of V up to 2^88 cannot overflow them; an infinity in V makes its element of the heads that read it infinite or NaN, a NaN
+ * makes it NaN, and neither touches another element.
  * Index data is checked on the device: a bad head or page entry is replaced by position 0 / page 0, a kv_len outside
  * [0, max_pages * page_size] is clamped, heads beyond n_heads / n_kv_heads per position keep their old output, and
  * TWIST_ERR_BAD_INDEX is recorded.
  * dtype TWIST_BF16 only; d_head in {8, 16, 32, 64, 128}; n_subnets <= TWIST_MAX_SUBNETS, n_subnets * n_seqs <= 65535,
- * head_keep and n_heads <= 1024; n_subnets * n_seqs * kv_max * max_pages * page_size below 2^35 (the work is counted in
- * 32 bits, in steps of 16 keys or more). */
+ * head_keep and n_heads <= 1024.  The work is counted in 32 bits: n_subnets * n_seqs * kv_max * r * (t + 2) < 2^31, r =
+ * ceil(n_heads / n_kv_heads / 8) (1 without sharing), t = ceil(max_pages * page_size / keys of a tile), 16 keys from
+ * d_head 64 on, else 64. */
 typedef struct {
   int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;
   int32_t page_size, n_pages, max_pages, max_len;

@@ -16,7 +16,9 @@
 // tile and 12 warps were 3 to 6 % slower, at d = 128 two steps and 8 warps 8 %).  Smaller heads spend more instructions
 // on a byte, and the registers of one tile do not cover the latency: there the tiles pass through shared memory, two
 // deep (d = 32: 113 -> 83 us for 463 MB; the same at d = 64 and 128 is 15 to 50 % slower, its copies of half and whole
-// rows being issued piece by piece through the same queue).  (tcgen05 would need 128 rows of queries for its smallest tile.)
+// rows being issued piece by piece through the same queue; bulk copies of whole rows have not been tried).  (tcgen05 takes
+// its operands from shared and tensor memory, where the keys and the probabilities would have to be laid out for it first;
+// with 1 to 12 operations a byte the products are far from bounding this kernel.)
 //
 // Softmax in fp32 with a running reference maximum per head that moves only when a score exceeds it by more than 2^8 (one
 // vote per tile instead of a reduction).  The probabilities enter the second product as the sum of two bf16 numbers
@@ -159,10 +161,13 @@ __device__ inline int check_pages(const DecParams& p, int id, int last_key, int 
 
 // Rows behind a sequence's end must not reach the products, whatever they hold.  Two ways.  CLAMP: they are replaced by rows
 // before it, whose scores are masked.  Otherwise they are read as they are (a page has all its rows) and the values
-// cleared right before their product: fewer instructions in every tile (d = 64, 64 sequences of up to 16000 keys: 96 us
-// against 98), but up to 15 rows more are read per item (d = 128, 3808 items of 137 keys: 45.4 us against 43.8, and
-// nothing to gain there, where a tile has half the rows).  A predicate on the loads, or clearing the values before the
-// softmax, makes the compiler wait for them long before their use: 120 and 109 us in the first case.
+// cleared right before their product: fewer instructions in every tile, but up to 15 rows more are read per item.
+// Measured, cleared against clamped, 64 sequences of up to 16000 keys, 32 heads on 4: d = 8 51.9 us against 60.5, d = 16 33.9
+// against 35.1, d = 32 54.2 against 54.6, d = 64 91.8 against 92.5 (short items are the other way round there: 15232 of 274
+// keys, 181 against 177); d = 128, where a tile has half the rows a thread, 952 ragged sequences of up to 274 keys on 4
+// positions: 54.2 against 52.1, eight subnets of long sequences 351.8 against 350.9.  Neither a predicate on the loads nor
+// clearing the values before the softmax is an alternative: the compiler then waits for them long before their use (a fifth
+// more time with tiles of 32 keys).
 template <int D>
 constexpr bool kClamp = D == 128;
 

@@ -294,7 +294,7 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
   p.by_head = divisor((uint32_t)p.units_per_head, (uint64_t)p.head_units);
   p.by_half = divisor((uint32_t)(p.half > 0 ? p.half : 1), (uint64_t)p.tile_rows * p.half);
   p.by_chunks = divisor((uint32_t)(p.dh / step), (uint64_t)p.kv * p.dh / step);
-  const size_t smem = (size_t)p.tile_rows * p.half * sizeof(float2);                    // at most 16 KB
+  const size_t smem = (size_t)p.tile_rows * p.half * sizeof(float2);                    // at most 8 KB
   void (*kernel)(PosParams) = mode == MODE_HALF ? rotate_rows_kernel<APPEND, MODE_HALF>
                               : mode == MODE_PAIRS ? rotate_rows_kernel<APPEND, MODE_PAIRS>
                               : mode == MODE_SLOW_HALF ? rotate_rows_kernel<APPEND, MODE_SLOW_HALF>
