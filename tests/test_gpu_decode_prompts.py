@@ -1,4 +1,4 @@
-"""Padded prompts of a decoding session: what the rows behind a sequence's length hold must not reach its tokens."""
+"""Decoding sessions: what the padding rows of a prompt, and the pages of sequences that ended, hold must not reach other tokens."""
 from dataclasses import replace
 
 import numpy as np
@@ -52,3 +52,41 @@ def test_rows_behind_a_prompt_may_hold_anything(B, d_head, ln, fill):
     for i, (want, got) in enumerate(zip(*outs)):
         assert bool(torch.isfinite(want).all())
         assert torch.equal(want, got), i
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_pages_that_change_hands_on_a_side_stream(B, graph):
+    """Sequences that end and start again in a pool with few spare pages, on a stream of the caller: every output has the bits
+    that a fresh session gives for the same tokens alone."""
+    from paper_2511_03983_b200.engine import DecodeSession, StackEngine
+    n, most, steps = 3, 40, 70
+    w = replace(I.scaled_twin(I.PRESETS[3], d_model=256, d_ff=688, d_head=64, tokens=n * 8, n_layers=2, local_steps=1), rope_base=10000.0)
+    S = w.n_subnets
+    eng = StackEngine(w, n, 8)
+    fill_model(eng, w)
+    eng.extract(0)
+    gen = torch.Generator().manual_seed(5)
+    new = dev(I.normal(79, 0, (steps, S, n, w.d_model), 1.0, I.DTYPE_BF16))
+    ends = torch.randint(1, most, (steps, S, n), generator=gen)          # a sequence that is this long ends before the step
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    runs, got, started = {}, [], [[0] * n for _ in range(S)]
+    with torch.cuda.stream(side):
+        ses = DecodeSession(eng, max_len=most, n_pages=S * n * 3 - 2, graph=graph)
+        for i in range(steps):
+            for s in range(S):
+                for b in range(n):
+                    if ses.lens[s][b] >= int(ends[i, s, b]) or ses.lens[s][b] == 32:
+                        ses.release(s, b)
+                        started[s][b] = i
+                    runs[(i, s, b)] = started[s][b]
+            got.append(ses.step(new[i]).clone())
+    side.synchronize()
+    assert B.twist_device_status() == 0
+    assert len({v for v in runs.values()}) > 20                          # many sequences began in pages that others had held
+    for s, b, last in ((0, 0, steps - 1), (1, 2, 50), (S - 1, 1, 33), (2, 0, 12)):
+        first = runs[(last, s, b)]
+        fresh = DecodeSession(eng, max_len=most)
+        for i in range(first, last + 1):
+            y = fresh.step(new[i])
+            assert torch.equal(y[s, b], got[i][s, b]), (s, b, i)
