@@ -534,6 +534,171 @@ size_t twist_attn_decode_workspace_bytes(int32_t d_head);
 int32_t twist_attn_decode(const twist_attn_decode_args* a /*host*/, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * A smaller cache (extensions): held in 8 bits, and with the tokens that nothing looks at taken out.
+ *
+ * The 8-bit cache: K and V are e4m3 numbers (bytes; pages as above, page_stride in elements, a multiple of 16), and 16 tokens of
+ * a KV position -- slots 16 i .. 16 i + 15, a block -- share one scale for K and one for V: scales [n_pages][kv_max][page_size / 16]
+ * [2] fp32, (K, V) side by side, dense.  A cached value is number * scale.
+ *
+ * twist_kv_append_q8 -- twist_kv_append into such a cache.  The scale of a block is the smallest power of two 2^e, -110 <= e <=
+ * 119, whose 448-fold is not below the largest finite magnitude of the block's new tokens; if the block holds tokens before the
+ * new ones, it is not below the scale that they have either, and where it grows they are rounded again (a power of two only
+ * costs bits of numbers that become subnormal: a token keeps four significant bits down to 2^-6 of the scale).  K is rotated in fp32
+ * and rounded once.  Infinities and NaN are stored as NaN.
+ *   seen (device int32 [S][n_seqs] or NULL): tokens of the sequence so far, the new ones included, where evictions have made
+ *   the cache shorter than the sequence: new token i of n goes to slot kv_len[s][b] - n + i and is rotated by position
+ *   seen[s][b] - n + i.  NULL: slots are positions.
+ * Everything else is as in twist_kv_append.  Index data is checked on the device, by blocks: tokens of a sequence with seen <
+ * kv_len, fewer cached tokens than new ones, or more of either than the table has slots are skipped, as are tokens whose page lies
+ * outside the pool; TWIST_ERR_BAD_INDEX is recorded.
+ * dtype (of qkv and q_out) TWIST_BF16 only; d_head in {16, 32, 64, 128}. */
+typedef struct {
+  int32_t dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head;
+  int32_t page_size, n_pages, max_pages;
+  int32_t rot_dims, layout;
+  int64_t page_stride, q_stride;
+  const void* qkv;             /* device */
+  void* q_out;                 /* device or NULL */
+  void* k_cache;               /* device, e4m3 */
+  void* v_cache;               /* device, e4m3 */
+  float* scales;               /* device fp32 [n_pages][kv_max][page_size/16][2] */
+  const int32_t* page_table;   /* device int32 [S][n_seqs][max_pages] */
+  const int32_t* kv_len;       /* device int32 [S][n_seqs] */
+  const int32_t* seen;         /* device int32 [S][n_seqs] or NULL */
+  const int32_t* new_begin;    /* device int32 [S][n_seqs + 1] or NULL */
+  const int32_t* new_len;      /* device int32 [S][n_seqs] or NULL */
+  const int32_t* kv_count;     /* device int32 [S] or NULL */
+  const double* inv_freq;      /* device fp64 [rot_dims/2]; may be NULL when rot_dims == 0 */
+} twist_kv_append_q8_args;
+
+int32_t twist_kv_append_q8(const twist_kv_append_q8_args* a /*host*/, void* stream);
+
+/* twist_attn_decode_q8 -- twist_attn_decode over the 8-bit cache.  Scales may be any positive finite numbers.  Queries enter the
+ * product as fp16 brought near 2^15 by a power of two (no bits of an element are lost within 2^29 of its head's largest),
+ * probabilities as fp16 (11 bits), cached values exactly; sums are fp32 and divided at the end.  NaN in V makes its element of
+ * the heads that read it NaN and touches no other.  The workspace is that of twist_attn_decode.
+ * d_head in {16, 32, 64, 128}; the work is counted in tiles of 32 keys from d_head 64 on, else 64. */
+typedef struct {
+  int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;
+  int32_t page_size, n_pages, max_pages, max_len;
+  int64_t page_stride, q_stride;
+  const void* q;               /* device */
+  const void* k_cache;         /* device, e4m3 */
+  const void* v_cache;         /* device, e4m3 */
+  const float* scales;         /* device fp32 [n_pages][kv_max][page_size/16][2] */
+  const int32_t* page_table;   /* device int32 [S][n_seqs][max_pages] */
+  const int32_t* kv_len;       /* device int32 [S][n_seqs] */
+  const int32_t* head_idx;     /* device int32 [S][head_keep] or NULL */
+  const int32_t* kv_pos;       /* device int32 [S][n_kv_heads] (required with head_idx) */
+  void* out;                   /* device */
+  float* lse;                  /* device or NULL */
+  void* ws;                    /* device scratch */
+  size_t ws_bytes;
+} twist_attn_decode_q8_args;
+
+int32_t twist_attn_decode_q8(const twist_attn_decode_q8_args* a /*host*/, void* stream);
+
+/* The attention weight that a cached token has gathered, weights [n_pages][kv_max][page_size] fp32, and its position in the
+ * sequence, slot_pos [n_pages][kv_max][page_size] int32: for each KV position on its own, in the places of the token's K and V.
+ *
+ * twist_attn_weights -- adds what one step's queries gave:
+ *     weights[j] = (new token: 0, else prior[j]) + sum_h exp(q_h . k_j / sqrt(d_head) - lse_h)   over the heads that read the position,
+ *   for the kv_len[s][b] tokens of every sequence, and slot_pos = seen[s][b] - n + i for its last n, the new ones.
+ *   q, lse: queries and log-sum-exp of twist_attn_decode / _q8 ([S][n_seqs] rows q_stride apart; [S][head_keep][n_seqs]).
+ *   prior: like weights; may be `weights` itself, or NULL (zeros); must not overlap it otherwise.
+ *   new_len (device int32 [S][n_seqs] or NULL: 1 each): the last tokens of a sequence that have no prior weight yet.
+ *   seen (device int32 [S][n_seqs] or NULL: kv_len).  slot_pos may be NULL.
+ *   cache TWIST_CACHE_BF16 (scales NULL) or TWIST_CACHE_E4M3.  Only K is read.  Positions that no head reads, and slots from kv_len
+ *   on, are left as they were.
+ * Index data is checked on the device as by twist_attn_decode; a new_len outside [0, kv_len] is clamped and reported.  fp32
+ * sums in a fixed order.  dtype TWIST_BF16; d_head in {8, 16, 32, 64, 128}, for e4m3 from 16 on; limits as twist_attn_decode. */
+enum { TWIST_CACHE_BF16 = 0, TWIST_CACHE_E4M3 = 1 };
+typedef struct {
+  int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;
+  int32_t page_size, n_pages, max_pages, max_len, cache, reserved;
+  int64_t page_stride, q_stride;
+  const void* q;               /* device */
+  const float* lse;            /* device fp32 [S][head_keep][n_seqs] */
+  const void* k_cache;         /* device */
+  const float* scales;         /* device or NULL */
+  const int32_t* page_table;   /* device int32 [S][n_seqs][max_pages] */
+  const int32_t* kv_len;       /* device int32 [S][n_seqs] */
+  const int32_t* new_len;      /* device int32 [S][n_seqs] or NULL */
+  const int32_t* seen;         /* device int32 [S][n_seqs] or NULL */
+  const int32_t* head_idx;     /* device int32 [S][head_keep] or NULL */
+  const int32_t* kv_pos;       /* device int32 [S][n_kv_heads] (required with head_idx) */
+  const float* prior;          /* device or NULL */
+  float* weights;              /* device */
+  int32_t* slot_pos;           /* device or NULL */
+} twist_attn_weights_args;
+
+int32_t twist_attn_weights(const twist_attn_weights_args* a /*host*/, void* stream);
+
+/* twist_attn_core_weights -- the same for prompts: what the queries of every sequence gave each of its tokens under the causal mask,
+ *     weights[j] = sum_h sum_i exp(q_hi . k_j / sqrt(d_head) - lse_hi),   i >= j, i >= len - last_queries,
+ *   written (not added) for the first len = new_len[s][b] tokens (NULL: seq_len) of the n_seqs sequences of seq_len rows, token j
+ *   in slot j of the sequence's pages; slot_pos[j] = j (may be NULL).  last_queries 0: all queries.
+ *   qkv, lse, head_idx, kv_pos as in twist_attn_core_args (qkv rotated, lse from twist_attn_core_fwd).  Rows behind len may hold anything.
+ * Index data is checked on the device: a bad head entry is replaced by position 0, a len outside [0, seq_len] is clamped, tokens
+ * whose page lies outside the table or the pool are skipped, and TWIST_ERR_BAD_INDEX recorded.  fp32 sums in a fixed order.
+ * dtype TWIST_BF16; d_head in {8, 16, 32, 64, 128}. */
+typedef struct {
+  int32_t dtype, n_subnets, n_seqs, seq_len, head_keep, kv_max, d_head, n_heads, n_kv_heads;
+  int32_t page_size, n_pages, max_pages, last_queries, reserved;
+  const void* qkv;             /* device */
+  const float* lse;            /* device fp32 [S][head_keep][n_seqs * seq_len] */
+  const int32_t* page_table;   /* device int32 [S][n_seqs][max_pages] */
+  const int32_t* new_len;      /* device int32 [S][n_seqs] or NULL */
+  const int32_t* head_idx;     /* device int32 [S][head_keep] or NULL */
+  const int32_t* kv_pos;       /* device int32 [S][n_kv_heads] (required with head_idx) */
+  float* weights;              /* device fp32 [n_pages][kv_max][page_size] */
+  int32_t* slot_pos;           /* device int32 [n_pages][kv_max][page_size] or NULL */
+  twist_plan* plan;            /* optional: tensor maps come from this plan's cache */
+} twist_attn_core_weights_args;
+
+int32_t twist_attn_core_weights(const twist_attn_core_weights_args* a /*host*/, void* stream);
+
+/* twist_kv_evict -- shortens every sequence to its keep[s][b] best tokens, for each KV position on its own, in place.
+ *   The tokens of a position rank: first those with slot_pos >= seen[s][b] - min(recent, keep[s][b]) (equals among each other), then the
+ *   others by weight, heaviest first (NaN last); equals by slot, lowest first.  The first keep[s][b] stay.  Those of them in slots
+ *   from keep on move into the slots below keep that became free, both taken in ascending order; the other slots below keep are not
+ *   touched (attention does not depend on the order of keys).  A sequence with kv_len <= keep is left as it is.  The call does not
+ *   change kv_len: the caller's next calls pass min(kv_len, keep).
+ *   weights, slot_pos: in; weights_out, slot_pos_out: the same two for the slots below min(kv_len, keep) afterwards; they may be
+ *   the inputs themselves (then only the moved tokens' are written) and must not overlap them otherwise.
+ *   cache TWIST_CACHE_E4M3: a block that takes tokens in gets the smallest scale (see twist_kv_append_q8) that its rows before kv_len
+ *   need, and they are rounded to it; other blocks are not touched.  scales NULL for TWIST_CACHE_BF16.
+ *   seen (device int32 [S][n_seqs] or NULL: kv_len).  kv_count (device int32 [S] or NULL): positions >= kv_count[s] are left alone.
+ *   max_len: upper bound of the kv_len entries (0: max_pages * page_size).
+ *   ws: device scratch of at least twist_kv_evict_workspace_bytes(S, n_seqs, kv_max, max_len) bytes (max_len as the call will use it);
+ *   calls that may overlap on the GPU need scratch of their own.
+ * Index data is checked on the device: kv_len and keep outside [0, max_len] are clamped, a KV position of a sequence that has a
+ * page outside the pool is left as it is, and TWIST_ERR_BAD_INDEX is recorded.  Deterministic.
+ * dtype TWIST_BF16; d_head a multiple of 8 (e4m3: 16), at most 256; n_subnets * n_seqs * kv_max <= 2^20, max_len <= 2^26. */
+typedef struct {
+  int32_t dtype, n_subnets, n_seqs, kv_max, d_head, page_size, n_pages, max_pages;
+  int32_t max_len, recent, cache, reserved;
+  int64_t page_stride;
+  void* k_cache;               /* device */
+  void* v_cache;               /* device */
+  float* scales;               /* device or NULL */
+  const int32_t* page_table;   /* device int32 [S][n_seqs][max_pages] */
+  const int32_t* kv_len;       /* device int32 [S][n_seqs] */
+  const int32_t* keep;         /* device int32 [S][n_seqs] */
+  const int32_t* seen;         /* device int32 [S][n_seqs] or NULL */
+  const int32_t* kv_count;     /* device int32 [S] or NULL */
+  const float* weights;        /* device fp32 [n_pages][kv_max][page_size] */
+  const int32_t* slot_pos;     /* device int32 [n_pages][kv_max][page_size] */
+  float* weights_out;          /* device */
+  int32_t* slot_pos_out;       /* device */
+  void* ws;                    /* device scratch */
+  size_t ws_bytes;
+} twist_kv_evict_args;
+
+size_t twist_kv_evict_workspace_bytes(int32_t n_subnets, int32_t n_seqs, int32_t kv_max, int64_t max_len);
+int32_t twist_kv_evict(const twist_kv_evict_args* a /*host*/, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Layer normalisation of the pre-LN transformer layer (App. A, Layer Normalization: z = (x - mu) / sigma with
  * mu, sigma the mean and standard deviation of a token's d_model elements, y = gamma * z + b; Transformer
  * Layer Architecture: one normalisation before the attention block, one before the FFN block, the skip

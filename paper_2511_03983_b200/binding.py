@@ -26,6 +26,7 @@ MODE_COVER, MODE_IID = 0, 1
 KIND_FFN, KIND_HEAD = 0, 1
 PROJ_QKV, PROJ_O = 0, 1
 ROPE_HALF, ROPE_PAIRS = 0, 1
+CACHE_BF16, CACHE_E4M3 = 0, 1
 MAX_SEGMENTS = 8
 
 EXPORTS = [
@@ -37,6 +38,8 @@ EXPORTS = [
     "twist_layernorm_bwd", "twist_qkv_col_mask", "twist_apply_col_mask", "twist_plan_create", "twist_plan_destroy",
     "twist_plan_stats", "twist_workspace_bytes", "twist_aggregate_partial", "twist_aggregate_finish",
     "twist_rope_fwd", "twist_rope_bwd", "twist_kv_append", "twist_attn_decode", "twist_attn_decode_workspace_bytes",
+    "twist_kv_append_q8", "twist_attn_decode_q8", "twist_attn_weights", "twist_attn_core_weights", "twist_kv_evict",
+    "twist_kv_evict_workspace_bytes",
 ]
 
 
@@ -183,6 +186,56 @@ class AttnDecodeArgs(C.Structure):
                 ("ws_bytes", C.c_size_t)]
 
 
+class KvAppendQ8Args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("n_seqs", C.c_int32), ("tokens", C.c_int32),
+                ("head_keep", C.c_int32), ("kv_max", C.c_int32), ("d_head", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("rot_dims", C.c_int32), ("layout", C.c_int32),
+                ("page_stride", C.c_int64), ("q_stride", C.c_int64), ("qkv", C.c_void_p), ("q_out", C.c_void_p),
+                ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("scales", C.c_void_p), ("page_table", C.c_void_p),
+                ("kv_len", C.c_void_p), ("seen", C.c_void_p), ("new_begin", C.c_void_p), ("new_len", C.c_void_p),
+                ("kv_count", C.c_void_p), ("inv_freq", C.c_void_p)]
+
+
+class AttnDecodeQ8Args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("n_seqs", C.c_int32), ("head_keep", C.c_int32),
+                ("kv_max", C.c_int32), ("d_head", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("max_len", C.c_int32),
+                ("page_stride", C.c_int64), ("q_stride", C.c_int64), ("q", C.c_void_p), ("k_cache", C.c_void_p),
+                ("v_cache", C.c_void_p), ("scales", C.c_void_p), ("page_table", C.c_void_p), ("kv_len", C.c_void_p),
+                ("head_idx", C.c_void_p), ("kv_pos", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p),
+                ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class AttnWeightsArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("n_seqs", C.c_int32), ("head_keep", C.c_int32),
+                ("kv_max", C.c_int32), ("d_head", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("max_len", C.c_int32),
+                ("cache", C.c_int32), ("reserved", C.c_int32), ("page_stride", C.c_int64), ("q_stride", C.c_int64),
+                ("q", C.c_void_p), ("lse", C.c_void_p), ("k_cache", C.c_void_p), ("scales", C.c_void_p),
+                ("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("new_len", C.c_void_p), ("seen", C.c_void_p),
+                ("head_idx", C.c_void_p), ("kv_pos", C.c_void_p), ("prior", C.c_void_p), ("weights", C.c_void_p),
+                ("slot_pos", C.c_void_p)]
+
+
+class AttnCoreWeightsArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("n_seqs", C.c_int32), ("seq_len", C.c_int32),
+                ("head_keep", C.c_int32), ("kv_max", C.c_int32), ("d_head", C.c_int32), ("n_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("last_queries", C.c_int32), ("reserved", C.c_int32), ("qkv", C.c_void_p), ("lse", C.c_void_p),
+                ("page_table", C.c_void_p), ("new_len", C.c_void_p), ("head_idx", C.c_void_p), ("kv_pos", C.c_void_p),
+                ("weights", C.c_void_p), ("slot_pos", C.c_void_p), ("plan", C.c_void_p)]
+
+
+class KvEvictArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_subnets", C.c_int32), ("n_seqs", C.c_int32), ("kv_max", C.c_int32),
+                ("d_head", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("max_len", C.c_int32), ("recent", C.c_int32), ("cache", C.c_int32), ("reserved", C.c_int32),
+                ("page_stride", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("scales", C.c_void_p),
+                ("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("keep", C.c_void_p), ("seen", C.c_void_p),
+                ("kv_count", C.c_void_p), ("weights", C.c_void_p), ("slot_pos", C.c_void_p), ("weights_out", C.c_void_p),
+                ("slot_pos_out", C.c_void_p), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
 _lib_handle = None
 
 
@@ -223,10 +276,13 @@ def lib() -> C.CDLL:
         for name in ("twist_subnet_ffn_fwd", "twist_subnet_ffn_bwd", "twist_subnet_attn_proj_fwd",
                      "twist_subnet_attn_proj_bwd", "twist_attn_core_fwd", "twist_attn_core_bwd",
                      "twist_layernorm_fwd", "twist_layernorm_bwd", "twist_rope_fwd", "twist_rope_bwd", "twist_kv_append",
-                     "twist_attn_decode"):
+                     "twist_attn_decode", "twist_kv_append_q8", "twist_attn_decode_q8", "twist_attn_weights",
+                     "twist_attn_core_weights", "twist_kv_evict"):
             getattr(h, name).argtypes = [C.c_void_p, C.c_void_p]
         h.twist_attn_decode_workspace_bytes.restype = C.c_size_t
         h.twist_attn_decode_workspace_bytes.argtypes = [C.c_int32]
+        h.twist_kv_evict_workspace_bytes.restype = C.c_size_t
+        h.twist_kv_evict_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int64]
         h.twist_mse_workspace_bytes.restype = C.c_size_t
         h.twist_mse_workspace_bytes.argtypes = [C.c_int32]
         h.twist_fused_loss_workspace_bytes.restype = C.c_size_t
@@ -240,7 +296,8 @@ def lib() -> C.CDLL:
             f = getattr(h, name)
             if name not in ("twist_abi_version", "twist_strerror", "twist_last_cuda_error",
                             "twist_mse_workspace_bytes", "twist_fused_loss_workspace_bytes",
-                            "twist_layernorm_workspace_bytes", "twist_attn_decode_workspace_bytes"):
+                            "twist_layernorm_workspace_bytes", "twist_attn_decode_workspace_bytes",
+                            "twist_kv_evict_workspace_bytes"):
                 f.restype = C.c_int32
         _lib_handle = h
     return _lib_handle
@@ -469,12 +526,12 @@ def _rows(name: str, t: torch.Tensor, n_subnets: int, rows: int, width: int) -> 
     return stride
 
 
-def _cache(k: torch.Tensor, v: torch.Tensor, kv_max: int, d_head: int):
+def _cache(k: torch.Tensor, v: torch.Tensor, kv_max: int, d_head: int, dtype: torch.dtype = torch.bfloat16):
     """(page_size, n_pages, page_stride) of a paged cache [n_pages][kv_max][page_size][d_head]; pages may be spaced."""
     shape = k.shape
-    if shape != v.shape or len(shape) != 4 or shape[1] != kv_max or shape[3] != d_head or \
-            k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
-        raise ValueError("k_cache / v_cache: expected bf16 [pages][%d][page_size][%d], got %s and %s" % (kv_max, d_head, tuple(shape), tuple(v.shape)))
+    if shape != v.shape or len(shape) != 4 or shape[1] != kv_max or shape[3] != d_head or k.dtype is not dtype or v.dtype is not dtype:
+        raise ValueError("k_cache / v_cache: expected %s [pages][%d][page_size][%d], got %s and %s of %s and %s" % (
+            dtype, kv_max, d_head, tuple(shape), tuple(v.shape), k.dtype, v.dtype))
     n, _, page, _ = shape
     strides = k.stride()
     if strides != v.stride() or strides[1:] != (page * d_head, d_head, 1):
@@ -482,12 +539,30 @@ def _cache(k: torch.Tensor, v: torch.Tensor, kv_max: int, d_head: int):
     return page, n, strides[0] if n > 1 else max(strides[0], kv_max * page * d_head)
 
 
+def _scales(scales: torch.Tensor, n_pages: int, kv_max: int, page: int, dev: int) -> int:
+    """Address of the scales of an 8-bit cache, fp32 [n_pages][kv_max][page_size / 16][2] (K, V)."""
+    return _tensor("scales", scales, torch.float32, n_pages * kv_max * (page // 16) * 2, dev)
+
+
+def _cache_kind(k: torch.Tensor, scales: Optional[torch.Tensor]) -> int:
+    """CACHE_BF16 or CACHE_E4M3, by the cache's type; an 8-bit cache has scales, a bf16 cache none."""
+    kind = CACHE_E4M3 if k.dtype is torch.float8_e4m3fn else CACHE_BF16
+    if (kind == CACHE_E4M3) != (scales is not None):
+        raise ValueError("scales: an e4m3 cache has them, a bf16 cache has none (cache of %s)" % k.dtype)
+    return kind
+
+
 # The argument structs of the per-token calls are packed in one go (field by field costs 1 us a call more), and their
 # tensors are checked in one expression; _tensor names the one that is wrong when it fails.
 _ROPE_PACK = struct.Struct("9i4x4Q")
 _APPEND_PACK = struct.Struct("12i2q10Q")
 _DECODE_PACK = struct.Struct("12i2q11Q")
+_Q8_PACK = struct.Struct("12i2q12Q")
+_WEIGHTS_PACK = struct.Struct("14i2q13Q")
+_EVICT_PACK = struct.Struct("12iq14Q")
 assert (_ROPE_PACK.size, _APPEND_PACK.size, _DECODE_PACK.size) == (C.sizeof(RopeArgs), C.sizeof(KvAppendArgs), C.sizeof(AttnDecodeArgs))
+assert (_Q8_PACK.size, _Q8_PACK.size, _WEIGHTS_PACK.size, _EVICT_PACK.size) == (
+    C.sizeof(KvAppendQ8Args), C.sizeof(AttnDecodeQ8Args), C.sizeof(AttnWeightsArgs), C.sizeof(KvEvictArgs))
 
 
 def rope_args(dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, seq_len=0, layout=ROPE_HALF, *, in_, out,
@@ -601,6 +676,174 @@ def twist_attn_decode_workspace_bytes(d_head: int) -> int:
 
 def twist_attn_decode(a: AttnDecodeArgs):
     _check(lib().twist_attn_decode(C.byref(a), _stream()), "twist_attn_decode")
+
+
+def kv_append_q8_args(dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, rot_dims=0, layout=ROPE_HALF, *, qkv,
+                      k_cache, v_cache, scales, page_table, kv_len, seen=None, q_out=None, new_begin=None, new_len=None,
+                      kv_count=None, inv_freq=None) -> KvAppendQ8Args:
+    """Marshals twist_kv_append_q8_args.  As kv_append_args, but k_cache, v_cache: torch.float8_e4m3fn, scales: fp32
+    [n_pages][kv_max][page_size / 16][2]; seen: int32 [S][n_seqs], tokens of the sequence so far (None: kv_len)."""
+    dev = _device()
+    i32, bf = torch.int32, torch.bfloat16
+    page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head, torch.float8_e4m3fn)
+    if k_cache.get_device() != dev or v_cache.get_device() != dev or (q_out is not None and q_out.get_device() != dev):
+        _elsewhere("k_cache / v_cache / q_out", k_cache, dev)
+    seqs, n = n_subnets * n_seqs, n_subnets * tokens * (head_keep + 2 * kv_max) * d_head
+    max_pages = page_table.shape[-1]
+    if not (qkv.dtype is bf and qkv.numel() == n and qkv.is_contiguous() and qkv.get_device() == dev
+            and page_table.dtype is i32 and page_table.numel() == seqs * max_pages and page_table.is_contiguous()
+            and page_table.get_device() == dev
+            and kv_len.dtype is i32 and kv_len.numel() == seqs and kv_len.is_contiguous() and kv_len.get_device() == dev):
+        _tensor("qkv", qkv, bf, n, dev)
+        _tensor("page_table", page_table, i32, seqs * max_pages, dev)
+        _tensor("kv_len", kv_len, i32, seqs, dev)
+    a = KvAppendQ8Args.from_buffer_copy(_Q8_PACK.pack(
+        dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, page, n_pages, max_pages, rot_dims, layout, stride,
+        0 if q_out is None else _rows("q_out", q_out, n_subnets, tokens, head_keep * d_head), qkv.data_ptr(),
+        0 if q_out is None else q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _scales(scales, n_pages, kv_max, page, dev),
+        page_table.data_ptr(), kv_len.data_ptr(), 0 if seen is None else _tensor("seen", seen, i32, seqs, dev),
+        0 if new_begin is None else _tensor("new_begin", new_begin, i32, n_subnets * (n_seqs + 1), dev),
+        0 if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
+        0 if kv_count is None else _tensor("kv_count", kv_count, i32, n_subnets, dev),
+        0 if inv_freq is None else _tensor("inv_freq", inv_freq, torch.float64, rot_dims // 2, dev)))
+    a._keepalive = (qkv, q_out, k_cache, v_cache, scales, page_table, kv_len, seen, new_begin, new_len, kv_count, inv_freq)
+    return a
+
+
+def twist_kv_append_q8(a: KvAppendQ8Args):
+    _check(lib().twist_kv_append_q8(C.byref(a), _stream()), "twist_kv_append_q8")
+
+
+def _shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev):
+    """Addresses of the two index arrays of grouped-query sharing (0 without)."""
+    return (0 if head_idx is None else _tensor("head_idx", head_idx, torch.int32, n_subnets * head_keep, dev),
+            0 if kv_pos is None else _tensor("kv_pos", kv_pos, torch.int32, n_subnets * n_kv_heads, dev))
+
+
+def attn_decode_q8_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads=0, n_kv_heads=0, max_len=0, *, q, k_cache,
+                        v_cache, scales, page_table, kv_len, out, ws, head_idx=None, kv_pos=None, lse=None) -> AttnDecodeQ8Args:
+    """Marshals twist_attn_decode_q8_args.  As attn_decode_args, but k_cache, v_cache: torch.float8_e4m3fn, scales: fp32
+    [n_pages][kv_max][page_size / 16][2]."""
+    dev = _device()
+    i32, bf = torch.int32, torch.bfloat16
+    page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head, torch.float8_e4m3fn)
+    if k_cache.get_device() != dev or v_cache.get_device() != dev or q.get_device() != dev or ws.get_device() != dev:
+        _elsewhere("k_cache / v_cache / q / ws", k_cache, dev)
+    seqs, width = n_subnets * n_seqs, head_keep * d_head
+    max_pages = page_table.shape[-1]
+    if not (page_table.dtype is i32 and page_table.numel() == seqs * max_pages and page_table.is_contiguous()
+            and page_table.get_device() == dev
+            and kv_len.dtype is i32 and kv_len.numel() == seqs and kv_len.is_contiguous() and kv_len.get_device() == dev
+            and out.dtype is bf and out.numel() == seqs * width and out.is_contiguous() and out.get_device() == dev):
+        _tensor("page_table", page_table, i32, seqs * max_pages, dev)
+        _tensor("kv_len", kv_len, i32, seqs, dev)
+        _tensor("out", out, bf, seqs * width, dev)
+    a = AttnDecodeQ8Args.from_buffer_copy(_Q8_PACK.pack(
+        dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, max_len, stride,
+        _rows("q", q, n_subnets, n_seqs, width), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+        _scales(scales, n_pages, kv_max, page, dev), page_table.data_ptr(), kv_len.data_ptr(),
+        *_shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev), out.data_ptr(),
+        0 if lse is None else _tensor("lse", lse, torch.float32, seqs * head_keep, dev), ws.data_ptr(),
+        ws.numel() * ws.element_size()))
+    a._keepalive = (q, k_cache, v_cache, scales, page_table, kv_len, out, ws, head_idx, kv_pos, lse)
+    return a
+
+
+def twist_attn_decode_q8(a: AttnDecodeQ8Args):
+    _check(lib().twist_attn_decode_q8(C.byref(a), _stream()), "twist_attn_decode_q8")
+
+
+def attn_weights_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads=0, n_kv_heads=0, max_len=0, *, q, lse, k_cache,
+                      page_table, kv_len, weights, scales=None, prior=None, slot_pos=None, new_len=None, seen=None, head_idx=None,
+                      kv_pos=None) -> AttnWeightsArgs:
+    """Marshals twist_attn_weights_args.  q, lse, k_cache, page_table, kv_len, head_idx, kv_pos as given to the decode call
+    (k_cache bf16, or float8_e4m3fn with its scales); prior, weights: fp32 [n_pages][kv_max][page_size] (prior may be
+    weights, None: zeros); slot_pos: int32, the same shape; new_len, seen: int32 [S][n_seqs] (None: 1 each, kv_len)."""
+    dev = _device()
+    i32, f32 = torch.int32, torch.float32
+    kind = _cache_kind(k_cache, scales)
+    page, n_pages, stride = _cache(k_cache, k_cache, kv_max, d_head, k_cache.dtype if kind == CACHE_E4M3 else torch.bfloat16)
+    if k_cache.get_device() != dev or q.get_device() != dev:
+        _elsewhere("k_cache / q", k_cache, dev)
+    seqs, max_pages, slots = n_subnets * n_seqs, page_table.shape[-1], n_pages * kv_max * page
+    a = AttnWeightsArgs.from_buffer_copy(_WEIGHTS_PACK.pack(
+        dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, max_len, kind, 0, stride,
+        _rows("q", q, n_subnets, n_seqs, head_keep * d_head), q.data_ptr(), _tensor("lse", lse, f32, seqs * head_keep, dev),
+        k_cache.data_ptr(), 0 if scales is None else _scales(scales, n_pages, kv_max, page, dev),
+        _tensor("page_table", page_table, i32, seqs * max_pages, dev), _tensor("kv_len", kv_len, i32, seqs, dev),
+        0 if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
+        0 if seen is None else _tensor("seen", seen, i32, seqs, dev),
+        *_shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev),
+        0 if prior is None else _tensor("prior", prior, f32, slots, dev), _tensor("weights", weights, f32, slots, dev),
+        0 if slot_pos is None else _tensor("slot_pos", slot_pos, i32, slots, dev)))
+    a._keepalive = (q, lse, k_cache, scales, page_table, kv_len, new_len, seen, head_idx, kv_pos, prior, weights, slot_pos)
+    return a
+
+
+def twist_attn_weights(a: AttnWeightsArgs):
+    _check(lib().twist_attn_weights(C.byref(a), _stream()), "twist_attn_weights")
+
+
+def attn_core_weights_args(dtype, n_subnets, n_seqs, seq_len, head_keep, kv_max, d_head, n_heads=0, n_kv_heads=0, last_queries=0, *,
+                           qkv, lse, page_table, weights, slot_pos=None, new_len=None, head_idx=None, kv_pos=None,
+                           plan: Optional["Plan"] = None) -> AttnCoreWeightsArgs:
+    """Marshals twist_attn_core_weights_args.  qkv, lse, head_idx, kv_pos as given to the attention core; weights fp32 and
+    slot_pos int32 [n_pages][kv_max][page_size]; page_table: int32 [S][n_seqs][max_pages]; new_len: int32 [S][n_seqs]."""
+    dev = _device()
+    i32, f32 = torch.int32, torch.float32
+    if weights.dim() != 3 or weights.shape[1] != kv_max:
+        raise ValueError("weights: expected fp32 [pages][%d][page_size], got %s" % (kv_max, tuple(weights.shape)))
+    n_pages, _, page = weights.shape
+    seqs, max_pages, tokens = n_subnets * n_seqs, page_table.shape[-1], n_subnets * n_seqs * seq_len
+    a = AttnCoreWeightsArgs(
+        dtype, n_subnets, n_seqs, seq_len, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, last_queries, 0,
+        _tensor("qkv", qkv, torch.bfloat16, tokens * (head_keep + 2 * kv_max) * d_head, dev),
+        _tensor("lse", lse, f32, tokens * head_keep, dev), _tensor("page_table", page_table, i32, seqs * max_pages, dev),
+        None if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
+        *(x or None for x in _shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev)),
+        _tensor("weights", weights, f32, n_pages * kv_max * page, dev),
+        None if slot_pos is None else _tensor("slot_pos", slot_pos, i32, n_pages * kv_max * page, dev), _plan_ptr(plan))
+    a._keepalive = (qkv, lse, page_table, new_len, head_idx, kv_pos, weights, slot_pos, plan)
+    return a
+
+
+def twist_attn_core_weights(a: AttnCoreWeightsArgs):
+    _check(lib().twist_attn_core_weights(C.byref(a), _stream()), "twist_attn_core_weights")
+
+
+def kv_evict_args(dtype, n_subnets, n_seqs, kv_max, d_head, recent, max_len=0, *, k_cache, v_cache, page_table, kv_len, keep, weights,
+                  slot_pos, ws, scales=None, seen=None, kv_count=None, weights_out=None, slot_pos_out=None) -> KvEvictArgs:
+    """Marshals twist_kv_evict_args.  k_cache, v_cache: bf16, or float8_e4m3fn with their scales; kv_len, keep, seen: int32
+    [S][n_seqs]; weights fp32 and slot_pos int32 [n_pages][kv_max][page_size], written in place or to weights_out,
+    slot_pos_out; ws: scratch of at least twist_kv_evict_workspace_bytes(S, n_seqs, kv_max, max_len) bytes (max_len 0: the
+    table's room)."""
+    dev = _device()
+    i32, f32 = torch.int32, torch.float32
+    kind = _cache_kind(k_cache, scales)
+    page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head, torch.float8_e4m3fn if kind == CACHE_E4M3 else torch.bfloat16)
+    if k_cache.get_device() != dev or v_cache.get_device() != dev or ws.get_device() != dev:
+        _elsewhere("k_cache / v_cache / ws", k_cache, dev)
+    seqs, max_pages, slots = n_subnets * n_seqs, page_table.shape[-1], n_pages * kv_max * page
+    weights_out = weights if weights_out is None else weights_out
+    slot_pos_out = slot_pos if slot_pos_out is None else slot_pos_out
+    a = KvEvictArgs.from_buffer_copy(_EVICT_PACK.pack(
+        dtype, n_subnets, n_seqs, kv_max, d_head, page, n_pages, max_pages, max_len, recent, kind, 0, stride, k_cache.data_ptr(),
+        v_cache.data_ptr(), 0 if scales is None else _scales(scales, n_pages, kv_max, page, dev),
+        _tensor("page_table", page_table, i32, seqs * max_pages, dev), _tensor("kv_len", kv_len, i32, seqs, dev),
+        _tensor("keep", keep, i32, seqs, dev), 0 if seen is None else _tensor("seen", seen, i32, seqs, dev),
+        0 if kv_count is None else _tensor("kv_count", kv_count, i32, n_subnets, dev), _tensor("weights", weights, f32, slots, dev),
+        _tensor("slot_pos", slot_pos, i32, slots, dev), _tensor("weights_out", weights_out, f32, slots, dev),
+        _tensor("slot_pos_out", slot_pos_out, i32, slots, dev), ws.data_ptr(), ws.numel() * ws.element_size()))
+    a._keepalive = (k_cache, v_cache, scales, page_table, kv_len, keep, seen, kv_count, weights, slot_pos, weights_out, slot_pos_out, ws)
+    return a
+
+
+def twist_kv_evict_workspace_bytes(n_subnets: int, n_seqs: int, kv_max: int, max_len: int) -> int:
+    return lib().twist_kv_evict_workspace_bytes(n_subnets, n_seqs, kv_max, max_len)
+
+
+def twist_kv_evict(a: KvEvictArgs):
+    _check(lib().twist_kv_evict(C.byref(a), _stream()), "twist_kv_evict")
 
 
 def layernorm_args(dtype, n_subnets, tokens, d_model, eps, lr=0.0, opt: Optional[Optimizer] = None, **t) -> LayerNormArgs:

@@ -1,0 +1,461 @@
+// The attention weight that cached keys gather, summed over the queries that look at them:
+//     twist_attn_weights:       w_j = prior_j + sum_h exp(q_h . k_j / sqrt(d) - lse_h)          one new token per sequence, paged cache
+//     twist_attn_core_weights:  w_j = sum_h sum_{i >= j} exp(q_hi . k_j / sqrt(d) - lse_hi)     prompts, projected activations
+// The log-sum-exp is known, so every key is on its own: no running maximum, nothing to join, one writer per result.
+//
+// One new token.  K is read once (two bytes or one per element) against 2 operations per head and element: bound by HBM.
+// The warp's tiles and the scores are those of the decode kernel (decode_tiles.cuh: up to eight heads per pass over the keys);
+// a warp takes a run of tiles of one KV position of one sequence, and the runs of all items are dealt to the warps of the
+// GPU in turn, the first run of every item before any second one.
+#include "decode_tiles.cuh"
+
+namespace twist {
+namespace {
+
+struct WeightParams {
+  DecParams d;                 // q, k, scales, table, len, heads; out and the workspace are not used
+  const float* lse;            // [S][heads][n_seqs]
+  const int32_t* new_len;
+  const int32_t* seen;
+  const float* prior;
+  float* weights;
+  int32_t* slot_pos;
+  int run_tiles, runs;         // tiles of a run; runs of the longest sequence that can be
+  float scale;                 // 1 / sqrt(d)
+};
+
+constexpr int kLenCache = 512;
+
+// exp(score * scale - lse).  The difference is formed before it is multiplied: it is small where the weight is not.
+__device__ inline float weight_of(float score, float scale, float lse) { return ex2(fmaf(score, scale, -lse) * kLog2e); }
+
+template <int D, int B>
+__global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightParams w) {
+  using Sh = Shape<D, B>;
+  const DecParams& p = w.d;
+  __shared__ int cols[kDecWarps][kCols];
+  __shared__ __align__(16) QueryBuf<D, B> qbuf[kDecWarps];
+  __shared__ int32_t lens[kLenCache], head_cache[kHeadCache], pos_cache[kPosCache];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int N = p.S * p.n_seqs;
+  griddep_launch_dependents();
+  griddep_wait();
+  copy_words(lens, p.len, min(N, kLenCache));
+  const Heads hd = cache_heads(p, head_cache, pos_cache, 0, p.S);
+  wait_copies();
+  __syncthreads();
+  const uint32_t items = (uint32_t)N * p.kv_max, total = items * (uint32_t)w.runs;
+  for (uint32_t u = blockIdx.x * kDecWarps + warp; u < total; u += gridDim.x * kDecWarps) {
+    const uint32_t run = u / items, item = u - run * items;
+    const int seq = (int)(item / p.kv_max), pos = (int)(item - (uint32_t)seq * p.kv_max), s = seq / p.n_seqs;
+    const int len = clamped_len(p, seq < kLenCache ? lens[seq] : p.len[seq]);
+    const int tile0 = (int)run * w.run_tiles, tiles = min((len + Sh::TILE - 1) / Sh::TILE, tile0 + w.run_tiles);
+    if (tile0 >= tiles) continue;
+    int fresh = w.new_len ? w.new_len[seq] : min(1, len);
+    if (fresh < 0 || fresh > len) {
+      if (lane == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+      fresh = max(0, min(fresh, len));
+    }
+    const int first_new = len - fresh, ahead = (w.seen ? w.seen[seq] : len) - len;
+    for (int rt = 0; rt < p.row_tiles; ++rt) {
+      __syncwarp();                                  // the heads and queries of the pass before have been read
+      find_heads(p, hd, s, pos, rt, lane, cols[warp]);
+      if (cols[warp][0] < 0) break;
+      prefetch_q<D, B>(qbuf[warp], p, seq, cols[warp][g], lane);
+      const int h0 = cols[warp][2 * t], h1 = cols[warp][2 * t + 1];
+      const float l0 = h0 >= 0 ? w.lse[((long long)s * p.heads + h0) * p.n_seqs + (seq - s * p.n_seqs)] : INFINITY;
+      const float l1 = h1 >= 0 ? w.lse[((long long)s * p.heads + h1) * p.n_seqs + (seq - s * p.n_seqs)] : INFINITY;
+      Tile<D, B> x;
+      constexpr int AHEAD = 32 / Sh::SUB;
+      int ids = check_pages<D, B>(p, fetch_pages<D, B>(p, seq, tile0, 1, lane), len - 1, tile0, 1, lane), n = 0;
+      load_k<D, B>(x, p, ids, 0, tile0 * Sh::TILE, len - 1, pos, lane);
+      wait_copies();
+      Query<D, B> q;
+      take_q<D, B>(q, qbuf[warp], lane);
+      for (int tile = tile0; tile < tiles; ++tile) {
+        const int key0 = tile * Sh::TILE;
+        // where the sums of the tile go: lane (g, t) stores key g (t = 0) or g + 8 (t = 1) of every step
+        long long at[Sh::SUB];
+        float old[Sh::SUB];
+#pragma unroll
+        for (int st = 0; st < Sh::SUB; ++st) {
+          const int key = key0 + 16 * st + g + 8 * t, id = __shfl_sync(0xffffffffu, ids, n * Sh::SUB + st);
+          at[st] = ((((long long)id * p.kv_max + pos) << p.page_shift) + (key & ((1 << p.page_shift) - 1)));
+          const float* from = rt ? w.weights : w.prior;
+          old[st] = t < 2 && key < (rt ? len : first_new) && from ? from[at[st]] : 0.f;
+        }
+        float sc[Sh::SUB][4];
+        tile_scores<D, B>(sc, x, q);
+        if (tile + 1 < tiles) {
+          if (++n == AHEAD) {
+            ids = check_pages<D, B>(p, fetch_pages<D, B>(p, seq, tile + 1, 1, lane), len - 1, tile + 1, 1, lane);
+            n = 0;
+          }
+          load_k<D, B>(x, p, ids, n, key0 + Sh::TILE, len - 1, pos, lane);
+        }
+#pragma unroll
+        for (int st = 0; st < Sh::SUB; ++st) {
+          float a = weight_of(sc[st][0], w.scale, l0) + weight_of(sc[st][1], w.scale, l1);
+          float b = weight_of(sc[st][2], w.scale, l0) + weight_of(sc[st][3], w.scale, l1);
+#pragma unroll
+          for (int o = 1; o < 4; o <<= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
+          }
+          const int key = key0 + 16 * st + g + 8 * t;
+          if (t < 2 && key < len) {
+            w.weights[at[st]] = old[st] + (t ? b : a);
+            if (rt == 0 && w.slot_pos && key >= first_new) w.slot_pos[at[st]] = key + ahead;
+          }
+        }
+      }
+    }
+  }
+}
+
+template <int D, int B>
+int run_weights(WeightParams& w, long long max_len, cudaStream_t st) {
+  DecParams& p = w.d;
+  const long long items = (long long)p.S * p.n_seqs * p.kv_max;
+  const long long longest = (((long long)p.max_pages << p.page_shift) + Shape<D, B>::TILE - 1) / Shape<D, B>::TILE + 2;
+  if (items * p.row_tiles > 0x7fffffffll / longest) return TWIST_ERR_UNSUPPORTED;
+  p.status = device_status_ptr();
+  if (!p.status) return TWIST_ERR_CUDA;
+  static int resident[64] = {0};
+  const int slot = device_slot();
+  if (resident[slot] == 0) {
+    int n = 0;
+    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, weights_kernel<D, B>, kDecThreads, 0));
+    resident[slot] = n < 1 ? 1 : n;
+  }
+  const long long warps = (long long)sm_count() * resident[slot] * kDecWarps;
+  // Runs short enough that every warp has several, long enough to pay for finding the heads and their queries.
+  const long long tiles = (max_len + Shape<D, B>::TILE - 1) / Shape<D, B>::TILE;
+  long long run_tiles = tiles * items / (6 * warps);
+  w.run_tiles = (int)(run_tiles < 1 ? 1 : (run_tiles > 16 ? 16 : run_tiles));
+  // every slot that the table has is in a run: the bound only chooses how long they are
+  const long long all = (((long long)p.max_pages << p.page_shift) + Shape<D, B>::TILE - 1) / Shape<D, B>::TILE;
+  w.runs = (int)((all + w.run_tiles - 1) / w.run_tiles);
+  const long long need = (items * ((tiles + w.run_tiles - 1) / w.run_tiles) + kDecWarps - 1) / kDecWarps, most = warps / kDecWarps;
+  TWIST_CUDA_TRY(launch_overlapped(weights_kernel<D, B>, dim3((unsigned)(need < most ? need : most)), dim3(kDecThreads), 0, st, 1, w));
+  return TWIST_OK;
+}
+
+// ------------------------------------------------------------------------------------------------ prompts
+
+constexpr int kCoreWarps = 4, kCoreThreads = 32 * kCoreWarps, kQueryTile = 64;
+
+struct CoreParams {
+  const __nv_bfloat16* qkv;    // [S][T][nq]
+  const float* lse;            // [S][heads][T]
+  const int32_t *table, *new_len, *head_idx, *kv_pos;
+  float* weights;
+  int32_t* slot_pos;
+  int S, n_seqs, seq_len, heads, kv_max, per_group, n_kv_heads, nq, T, last;
+  int page_shift, n_pages, max_pages;
+  float scale;
+  int* status;
+};
+
+constexpr int kMaxHeads = 1024;
+
+// The kept heads that read KV position `pos`, in ascending order, into list; returns their number.  One warp; bad entries
+// are replaced by position 0 and reported.
+__device__ inline int heads_of(const CoreParams& p, int s, int pos, int lane, short* list) {
+  if (!p.head_idx) {
+    if (lane == 0) list[0] = (short)pos;
+    return 1;
+  }
+  int seen = 0;
+  for (int h0 = 0; h0 < p.heads; h0 += 32) {
+    const int hq = h0 + lane;
+    bool mine = false;
+    if (hq < p.heads) {
+      const int h = p.head_idx[(long long)s * p.heads + hq];
+      int g = h < 0 ? -1 : h / p.per_group;
+      if ((unsigned)g >= (unsigned)p.n_kv_heads) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); g = 0; }
+      int at = p.kv_pos[(long long)s * p.n_kv_heads + g];
+      if ((unsigned)at >= (unsigned)p.kv_max) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); at = 0; }
+      mine = at == pos;
+    }
+    const unsigned vote = __ballot_sync(0xffffffffu, mine);
+    if (mine) list[seen + __popc(vote & ((1u << lane) - 1))] = (short)hq;
+    seen += __popc(vote);
+  }
+  return seen;
+}
+
+// Tokens of sequence (s, b), checked.
+__device__ inline int prompt_len(const CoreParams& p, long long seq) {
+  int n = p.new_len ? p.new_len[seq] : p.seq_len;
+  if (n < 0 || n > p.seq_len) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); n = n < 0 ? 0 : p.seq_len; }
+  return n;
+}
+
+// Token j's sum into its page.
+__device__ inline void store_weight(const CoreParams& p, long long seq, int pos, int j, float sum) {
+  const int page = j >> p.page_shift, id = page < p.max_pages ? p.table[seq * p.max_pages + page] : -1;
+  if ((unsigned)id >= (unsigned)p.n_pages) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); return; }
+  const long long at = (((long long)id * p.kv_max + pos) << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+  p.weights[at] = sum;
+  if (p.slot_pos) p.slot_pos[at] = j;
+}
+
+// A CTA holds a tile of keys of one KV position in registers (a warp 16 * SUB * KT of them) and walks over the queries that may
+// look at them, head after head, tiles of kQueryTile through shared memory.  The sums stay in the registers of the threads
+// that own the scores and are joined over the four threads of a row at the end.
+template <int D>
+__global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CoreParams p) {
+  using Sh = Shape<D, 2>;
+  constexpr int KT = D >= 64 ? 2 : 1, WARP_KEYS = Sh::TILE * KT, KEYS = WARP_KEYS * kCoreWarps, STRIDE = D + 8;
+  __shared__ __align__(16) __nv_bfloat16 qs[kQueryTile * STRIDE];
+  __shared__ float ls[kQueryTile];
+  __shared__ short list[kMaxHeads];
+  __shared__ int n_list;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  // the tiles with the most queries first
+  const unsigned items = (unsigned)p.S * p.n_seqs * p.kv_max, item = blockIdx.x % items;
+  const int key0 = (int)(blockIdx.x / items) * KEYS, pos = (int)(item % p.kv_max);
+  const long long seq = item / p.kv_max;
+  const int s = (int)(seq / p.n_seqs), b = (int)(seq - (long long)s * p.n_seqs);
+  griddep_launch_dependents();
+  griddep_wait();
+  const int len = prompt_len(p, seq);
+  if (key0 >= len) return;
+  if (warp == 0) {
+    const int n = heads_of(p, s, pos, lane, list);
+    if (lane == 0) n_list = n;
+  }
+  const __nv_bfloat16* rows = p.qkv + ((long long)s * p.T + (long long)b * p.seq_len) * p.nq;
+  const int mine = key0 + warp * WARP_KEYS;
+  Tile<D, 2> x[KT];
+#pragma unroll
+  for (int k = 0; k < KT; ++k)
+#pragma unroll
+    for (int st = 0; st < Sh::SUB; ++st)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int key = mine + k * Sh::TILE + 16 * st + g + 8 * r;
+#pragma unroll
+        for (int c = 0; c < Sh::KCH; ++c) {
+          if (key < len) {
+            load_words<Sh::KW>(x[k].k[st][r][c], rows + (long long)key * p.nq + (p.heads + pos) * D + c * 8 * Sh::KW + t * 2 * Sh::KW);
+          } else {
+#pragma unroll
+            for (int w = 0; w < Sh::KW; ++w) x[k].k[st][r][c][w] = 0;
+          }
+        }
+      }
+  float sum[KT][Sh::SUB][2];
+#pragma unroll
+  for (int k = 0; k < KT; ++k)
+#pragma unroll
+    for (int st = 0; st < Sh::SUB; ++st) sum[k][st][0] = sum[k][st][1] = 0.f;
+  __syncthreads();
+  const int first = max(key0, p.last ? len - p.last : 0);          // the first query that counts
+  for (int i = 0; i < n_list; ++i) {
+    const int h = list[i];
+    for (int q0 = first / kQueryTile * kQueryTile; q0 < len; q0 += kQueryTile) {
+      __syncthreads();
+      for (int k = threadIdx.x; k < kQueryTile * D / 8; k += kCoreThreads) {
+        const int r = k / (D / 8), c = k % (D / 8);
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (q0 + r < len) v = *reinterpret_cast<const uint4*>(rows + (long long)(q0 + r) * p.nq + h * D + 8 * c);
+        *reinterpret_cast<uint4*>(qs + r * STRIDE + 8 * c) = v;
+      }
+      if (threadIdx.x < kQueryTile) {
+        const int q = q0 + threadIdx.x;
+        // a query that does not count gives nothing
+        ls[threadIdx.x] = q >= first && q < len ? p.lse[((long long)s * p.heads + h) * p.T + (long long)b * p.seq_len + q] : INFINITY;
+      }
+      __syncthreads();
+      const bool diagonal = q0 < key0 + KEYS;
+#pragma unroll 2
+      for (int n = 0; n < kQueryTile; n += 8) {
+        Query<D, 2> q;
+        const __nv_bfloat16* row = qs + (n + g) * STRIDE + t * 2 * Sh::KW;
+#pragma unroll
+        for (int c = 0; c < Sh::KCH; ++c) {
+          if constexpr (Sh::KW == 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(row + c * 8 * Sh::KW);
+            q.w[c][0] = v.x; q.w[c][1] = v.y; q.w[c][2] = v.z; q.w[c][3] = v.w;
+          } else {
+#pragma unroll
+            for (int w = 0; w < Sh::KW; ++w) q.w[c][w] = *reinterpret_cast<const uint32_t*>(row + 2 * w);
+          }
+        }
+        const float l0 = ls[n + 2 * t], l1 = ls[n + 2 * t + 1];
+        const int i0 = q0 + n + 2 * t;
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          float sc[Sh::SUB][4];
+          tile_scores<D, 2>(sc, x[k], q);
+#pragma unroll
+          for (int st = 0; st < Sh::SUB; ++st) {
+            const int key = mine + k * Sh::TILE + 16 * st + g;
+            float e0 = weight_of(sc[st][0], p.scale, l0), e1 = weight_of(sc[st][1], p.scale, l1);
+            float e2 = weight_of(sc[st][2], p.scale, l0), e3 = weight_of(sc[st][3], p.scale, l1);
+            if (diagonal) {
+              e0 = i0 >= key ? e0 : 0.f;
+              e1 = i0 + 1 >= key ? e1 : 0.f;
+              e2 = i0 >= key + 8 ? e2 : 0.f;
+              e3 = i0 + 1 >= key + 8 ? e3 : 0.f;
+            }
+            sum[k][st][0] += e0 + e1;
+            sum[k][st][1] += e2 + e3;
+          }
+        }
+      }
+    }
+  }
+  if (n_list == 0) return;                                         // no head reads this position
+#pragma unroll
+  for (int k = 0; k < KT; ++k)
+#pragma unroll
+    for (int st = 0; st < Sh::SUB; ++st) {
+      float a = sum[k][st][0], c = sum[k][st][1];
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        c += __shfl_xor_sync(0xffffffffu, c, o);
+      }
+      const int key = mine + k * Sh::TILE + 16 * st + g + 8 * t;
+      if (t < 2 && key < len) store_weight(p, seq, pos, key, t ? c : a);
+    }
+}
+
+template <int D>
+int run_core(CoreParams& p, cudaStream_t st) {
+  constexpr int KEYS = Shape<D, 2>::TILE * (D >= 64 ? 2 : 1) * kCoreWarps;
+  const long long grid = (long long)p.S * p.n_seqs * p.kv_max * ((p.seq_len + KEYS - 1) / KEYS);
+  if (grid > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
+  TWIST_CUDA_TRY(launch_overlapped(core_weights_kernel<D>, dim3((unsigned)grid), dim3(kCoreThreads), 0, st, 1, p));
+  return TWIST_OK;
+}
+
+bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+
+}  // namespace
+}  // namespace twist
+
+using namespace twist;
+
+extern "C" int32_t twist_attn_weights(const twist_attn_weights_args* a, void* stream) {
+  if (!a) return TWIST_ERR_NULL;
+  if (a->dtype != TWIST_BF16) return TWIST_ERR_UNSUPPORTED;
+  if (a->cache != TWIST_CACHE_BF16 && a->cache != TWIST_CACHE_E4M3) return TWIST_ERR_SHAPE;
+  const bool q8 = a->cache == TWIST_CACHE_E4M3;
+  if (a->n_subnets <= 0 || a->n_seqs <= 0 || a->head_keep <= 0 || a->kv_max <= 0 || a->d_head <= 0 || a->n_pages <= 0 ||
+      a->max_pages <= 0 || a->page_size <= 0 || a->max_len < 0)
+    return TWIST_ERR_SHAPE;
+  const int dh = a->d_head;
+  if ((dh != 8 || q8) && dh != 16 && dh != 32 && dh != 64 && dh != 128) return TWIST_ERR_UNSUPPORTED;
+  if (a->n_subnets > TWIST_MAX_SUBNETS || a->n_heads > kMaxHeads || a->head_keep > kMaxHeads) return TWIST_ERR_UNSUPPORTED;
+  if ((long long)a->n_subnets * a->n_seqs > 65535) return TWIST_ERR_UNSUPPORTED;
+  if (a->page_size < 16 || a->page_size > 1024 || (a->page_size & (a->page_size - 1))) return TWIST_ERR_UNSUPPORTED;
+  if ((long long)a->max_pages * a->page_size > 0x7fffffffll - 1024) return TWIST_ERR_UNSUPPORTED;   // positions are 32-bit
+  if (a->page_stride % (q8 ? 16 : 8) != 0 || a->page_stride < (long long)a->kv_max * a->page_size * dh) return TWIST_ERR_SHAPE;
+  if (a->q_stride % 8 != 0 || a->q_stride < (long long)a->head_keep * dh) return TWIST_ERR_SHAPE;
+  if (a->head_idx) {
+    if (!a->kv_pos || a->n_heads <= 0 || a->n_kv_heads <= 0 || a->n_heads % a->n_kv_heads != 0) return TWIST_ERR_SHAPE;
+  } else if (a->kv_max != a->head_keep) {
+    return TWIST_ERR_SHAPE;
+  }
+  if (q8 != (a->scales != nullptr)) return TWIST_ERR_SHAPE;
+  if (!a->q || !a->lse || !a->k_cache || !a->page_table || !a->kv_len || !a->weights) return TWIST_ERR_NULL;
+  if (!aligned16(a->q) || !aligned16(a->lse) || !aligned16(a->k_cache) || !aligned16(a->scales) || !aligned16(a->prior) || !aligned16(a->weights) ||
+      !aligned16(a->slot_pos))
+    return TWIST_ERR_SHAPE;
+  const long long bytes = (long long)a->n_pages * a->kv_max * a->page_size * 4;
+  if ((a->prior && a->prior != a->weights && overlap(a->prior, bytes, a->weights, bytes)) ||
+      (a->slot_pos && (overlap(a->slot_pos, bytes, a->weights, bytes) || (a->prior && overlap(a->slot_pos, bytes, a->prior, bytes)))))
+    return TWIST_ERR_SHAPE;
+  WeightParams w;
+  memset(&w, 0, sizeof(w));
+  DecParams& p = w.d;
+  p.q = static_cast<const __nv_bfloat16*>(a->q);
+  p.k = a->k_cache;
+  p.scales = reinterpret_cast<const float2*>(a->scales);
+  p.table = a->page_table; p.len = a->kv_len; p.head_idx = a->head_idx; p.kv_pos = a->kv_pos;
+  p.page_stride = a->page_stride; p.q_stride = a->q_stride;
+  p.S = a->n_subnets; p.n_seqs = a->n_seqs; p.heads = a->head_keep; p.kv_max = a->kv_max;
+  p.per_group = a->head_idx ? a->n_heads / a->n_kv_heads : 1;
+  p.n_kv_heads = a->head_idx ? a->n_kv_heads : a->kv_max;
+  p.row_tiles = (p.per_group + kCols - 1) / kCols;
+  p.page_shift = 31 - __builtin_clz((unsigned)a->page_size);
+  p.n_pages = a->n_pages; p.max_pages = a->max_pages;
+  w.lse = a->lse; w.new_len = a->new_len; w.seen = a->seen;
+  w.prior = a->prior; w.weights = a->weights; w.slot_pos = a->slot_pos;
+  w.scale = 1.0f / sqrtf((float)dh);
+  const long long table_len = (long long)a->max_pages * a->page_size;
+  const long long max_len = a->max_len > 0 && a->max_len < table_len ? a->max_len : table_len;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (q8) {
+    switch (dh) {
+      case 16: return run_weights<16, 1>(w, max_len, st);
+      case 32: return run_weights<32, 1>(w, max_len, st);
+      case 64: return run_weights<64, 1>(w, max_len, st);
+      default: return run_weights<128, 1>(w, max_len, st);
+    }
+  }
+  switch (dh) {
+    case 8: return run_weights<8, 2>(w, max_len, st);
+    case 16: return run_weights<16, 2>(w, max_len, st);
+    case 32: return run_weights<32, 2>(w, max_len, st);
+    case 64: return run_weights<64, 2>(w, max_len, st);
+    default: return run_weights<128, 2>(w, max_len, st);
+  }
+}
+
+extern "C" int32_t twist_attn_core_weights(const twist_attn_core_weights_args* a, void* stream) {
+  if (!a) return TWIST_ERR_NULL;
+  if (a->dtype != TWIST_BF16) return TWIST_ERR_UNSUPPORTED;
+  if (a->n_subnets <= 0 || a->n_seqs <= 0 || a->seq_len <= 0 || a->head_keep <= 0 || a->kv_max <= 0 || a->d_head <= 0 || a->n_pages <= 0 ||
+      a->max_pages <= 0 || a->page_size <= 0 || a->last_queries < 0)
+    return TWIST_ERR_SHAPE;
+  const int dh = a->d_head;
+  if (dh != 8 && dh != 16 && dh != 32 && dh != 64 && dh != 128) return TWIST_ERR_UNSUPPORTED;
+  if (a->n_subnets > TWIST_MAX_SUBNETS || a->head_keep > kMaxHeads || a->n_heads > kMaxHeads) return TWIST_ERR_UNSUPPORTED;
+  if (a->page_size < 16 || a->page_size > 1024 || (a->page_size & (a->page_size - 1))) return TWIST_ERR_UNSUPPORTED;
+  if ((long long)a->max_pages * a->page_size > 0x7fffffffll - 1024 || a->seq_len > 0x7fffffff - 1024) return TWIST_ERR_UNSUPPORTED;
+  if ((long long)a->n_seqs * a->seq_len > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
+  if (((long long)a->head_keep + 2ll * a->kv_max) * dh > (1 << 24)) return TWIST_ERR_UNSUPPORTED;
+  if ((long long)a->n_subnets * a->n_seqs * a->kv_max > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
+  if (a->head_idx) {
+    if (!a->kv_pos || a->n_heads <= 0 || a->n_kv_heads <= 0 || a->n_heads % a->n_kv_heads != 0) return TWIST_ERR_SHAPE;
+  } else if (a->kv_max != a->head_keep) {
+    return TWIST_ERR_SHAPE;
+  }
+  if (!a->qkv || !a->lse || !a->page_table || !a->weights) return TWIST_ERR_NULL;
+  if (!aligned16(a->qkv) || !aligned16(a->lse) || !aligned16(a->weights) || !aligned16(a->slot_pos)) return TWIST_ERR_SHAPE;
+  const long long bytes = (long long)a->n_pages * a->kv_max * a->page_size * 4;
+  if (a->slot_pos && overlap(a->slot_pos, bytes, a->weights, bytes)) return TWIST_ERR_SHAPE;
+  CoreParams p;
+  memset(&p, 0, sizeof(p));
+  p.qkv = static_cast<const __nv_bfloat16*>(a->qkv);
+  p.lse = a->lse;
+  p.table = a->page_table; p.new_len = a->new_len; p.head_idx = a->head_idx; p.kv_pos = a->kv_pos;
+  p.weights = a->weights; p.slot_pos = a->slot_pos;
+  p.S = a->n_subnets; p.n_seqs = a->n_seqs; p.seq_len = a->seq_len; p.heads = a->head_keep; p.kv_max = a->kv_max;
+  p.per_group = a->head_idx ? a->n_heads / a->n_kv_heads : 1;
+  p.n_kv_heads = a->head_idx ? a->n_kv_heads : a->kv_max;
+  p.nq = (a->head_keep + 2 * a->kv_max) * dh;
+  p.T = a->n_seqs * a->seq_len;
+  p.last = a->last_queries;
+  p.page_shift = 31 - __builtin_clz((unsigned)a->page_size);
+  p.n_pages = a->n_pages; p.max_pages = a->max_pages;
+  p.scale = 1.0f / sqrtf((float)dh);
+  p.status = device_status_ptr();
+  if (!p.status) return TWIST_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  switch (dh) {
+    case 8: return run_core<8>(p, st);
+    case 16: return run_core<16>(p, st);
+    case 32: return run_core<32>(p, st);
+    case 64: return run_core<64>(p, st);
+    default: return run_core<128>(p, st);
+  }
+}

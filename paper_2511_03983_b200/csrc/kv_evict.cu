@@ -1,0 +1,461 @@
+// twist_kv_evict: every KV position of every sequence keeps its `keep` best tokens, by the attention weight that they have gathered.
+//
+// In place, and with few moves: attention does not depend on the order of the keys, so the tokens that stay below slot
+// `keep` are not touched, and those that stay above it fill the slots below that became free (the i-th of one the i-th of
+// the other).  Sources (from keep on) and destinations (below) do not meet, so all moves run at once; a full compaction
+// would move half of the cache to drop one token.  Bytes: a weight and a position of every slot, and the rows that move.
+//
+// One cluster of 1 to 8 CTAs per (sequence, KV position); its warps take contiguous runs of slots.
+//  1. A 32-bit key for each slot that orders as the tokens rank (protected tokens highest), kept in shared memory where it fits.
+//  2. The keep-th largest key by radix selection, 11 + 11 + 10 bits: histograms in shared memory, added over the cluster.
+//  3. Equal keys are admitted in the order of slots: a running count over the runs.  Then every warp knows who stays:
+//     bits to the workspace, with the number of free slots before each 32 and the list of the tokens that move.
+//  4. A warp takes 16 destination slots at a time (a block of the 8-bit cache, whose rows share a scale).  The block that
+//     `keep` cuts holds sources too; an 8-bit cache rescales it last, when they have been read.
+#include <cooperative_groups.h>
+
+#include "e4m3.cuh"
+#include "ptx.cuh"
+
+namespace twist {
+namespace {
+
+constexpr int kEvThreads = 512, kEvWarps = kEvThreads / 32;
+constexpr int kBins = 2048;
+constexpr int kKeyCache = 24576;          // keys that a CTA keeps in shared memory
+constexpr int kMaxEvictCluster = 8, kSlotsPerCta = 1024;
+
+struct EvictParams {
+  uint8_t* k;                  // pages page_bytes apart
+  uint8_t* v;
+  float* scales;               // [n_pages][kv][page / 16][2]
+  const int32_t *table, *len, *keep, *seen, *kv_count;
+  const float* weights;
+  const int32_t* slot_pos;
+  float* weights_out;
+  int32_t* slot_pos_out;
+  int32_t* ws;
+  long long page_bytes, ws_item;
+  int n_seqs, kv, row_bytes, page_shift, n_pages, max_pages, max_len, recent, key_cache;
+  int* status;
+};
+
+// Ranks of the workspace of an item: stay bits and free slots before, one of each for 32 slots, then the list of movers.
+__host__ __device__ constexpr long long groups_of(long long max_len) { return (max_len + 31) / 32; }
+__host__ __device__ constexpr long long item_words(long long max_len) { return (2 * groups_of(max_len) + max_len / 2 + 1 + 3) / 4 * 4; }
+
+__device__ inline uint32_t rank_key(float w, bool guarded) {
+  if (guarded) return 0xffffffffu;
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.0f);                    // -0 counts as 0
+  return min(u & 0x80000000u ? ~u : u | 0x80000000u, 0xfffffffeu);
+}
+
+// The item's slots: page and offset of slot i.
+struct Slots {
+  const int32_t* table;        // of the sequence
+  long long base;              // kv position
+  int kv, page_shift, n_pages;
+  __device__ int page(int i) const { return table[i >> page_shift]; }
+  __device__ int offset(int i) const { return i & ((1 << page_shift) - 1); }
+  __device__ long long at(int i) const { return (((long long)page(i) * kv + base) << page_shift) + offset(i); }
+};
+
+__device__ inline uint8_t* row_of(const EvictParams& p, const Slots& sl, uint8_t* cache, int slot) {
+  return cache + sl.page(slot) * p.page_bytes + ((sl.base << p.page_shift) + sl.offset(slot)) * p.row_bytes;
+}
+__device__ inline float* scale_at(const EvictParams& p, const Slots& sl, int slot, int which) {
+  return p.scales + 2 * ((((long long)sl.page(slot) * p.kv + sl.base) << (p.page_shift - 4)) + (sl.offset(slot) >> 4)) + which;
+}
+
+// Sources of the 16 slots from slot0 on, one per lane (of the first 16): itself, a mover, or -1 for a slot behind `end`.
+__device__ inline int source_of(const int32_t* bits, const int32_t* before, const int32_t* movers, int slot0, int keep, int end, int lane) {
+  const int slot = slot0 + (lane & 15), grp = slot >> 5, bit = slot & 31;
+  if (slot >= end) return -1;
+  if (slot >= keep) return slot;
+  const uint32_t stay = (uint32_t)bits[grp];
+  if (stay >> bit & 1) return slot;
+  const uint32_t live = (2u << min(31, keep - 1 - 32 * grp)) - 1;      // slots of the 32 that are below keep
+  return movers[before[grp] + __popc(~stay & live & ((1u << bit) - 1))];
+}
+
+// Rows of a bf16 cache: the moved ones, 16 bytes a lane.
+__device__ inline void move_rows(const EvictParams& p, const Slots& sl, int slot0, int from, unsigned moved, int lane) {
+  const int chunks = p.row_bytes / 16, n = __popc(moved) * 2 * chunks;
+  for (int k0 = 0; k0 < n; k0 += 4 * 32) {
+    uint4 x[4];
+    uint8_t* to[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = k0 + 32 * j + lane, which = k / chunks, c = k - which * chunks;
+      const int i = k < n ? (int)__fns(moved, 0, (which >> 1) + 1) : 0;
+      const int src = __shfl_sync(0xffffffffu, from, i & 15);
+      to[j] = nullptr;
+      if (k < n) {
+        uint8_t* cache = which & 1 ? p.v : p.k;
+        x[j] = *reinterpret_cast<const uint4*>(row_of(p, sl, cache, src) + 16 * c);
+        to[j] = row_of(p, sl, cache, slot0 + i) + 16 * c;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (to[j]) *reinterpret_cast<uint4*>(to[j]) = x[j];
+  }
+}
+
+// A block of an 8-bit cache that takes tokens in: all its rows coded anew with the scale that they need.
+template <int D>
+__device__ inline void move_block(const EvictParams& p, const Slots& sl, int slot0, int from, int lane) {
+  constexpr int CH = D / 16, N = D >= 32 ? D / 32 : 1;               // pieces of 16 numbers of a row, of a lane
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    uint8_t* cache = which ? p.v : p.k;
+    uint4 x[N];
+    float scale[N], top = 0.f;
+    int src[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int k = 32 * j + lane, r = k / CH, c = k % CH;
+      src[j] = __shfl_sync(0xffffffffu, from, r & 15);
+      if (r >= 16) src[j] = -1;
+      if (src[j] >= 0) {
+        x[j] = *reinterpret_cast<const uint4*>(row_of(p, sl, cache, src[j]) + 16 * c);
+        scale[j] = *scale_at(p, sl, src[j], which);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (src[j] < 0) continue;
+      const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+      float m = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a[4];
+        widen4(a, w[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(a[e]));           // a NaN counts for nothing
+      }
+      top = fmaxf(top, m * scale[j]);
+    }
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+    const float now = scale_for(top), inv = inverse_scale(now);
+    __syncwarp();                                                      // everything has been read
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int k = 32 * j + lane, r = k / CH, c = k % CH;
+      if (src[j] < 0 || (src[j] == slot0 + r && scale[j] == now)) continue;
+      const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+      const float f = scale[j] * inv;
+      uint32_t y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a[4];
+        widen4(a, w[i]);
+        y[i] = narrow4(a[0] * f, a[1] * f, a[2] * f, a[3] * f);
+      }
+      *reinterpret_cast<uint4*>(row_of(p, sl, cache, slot0 + r) + 16 * c) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    if (lane == 0) *scale_at(p, sl, slot0, which) = now;
+  }
+}
+
+// D: elements of a row of an 8-bit cache; 0: a bf16 cache.
+template <int D>
+__global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) {
+  extern __shared__ uint32_t keys[];
+  __shared__ uint32_t hist[kBins];
+  __shared__ int warp_sum[kEvWarps], counts[2][kEvWarps];
+  __shared__ int guarded, bad, found_bin, found_above;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const long long item = blockIdx.x / ctas;
+  const long long seq = item / p.kv;
+  const int pos = (int)(item - seq * p.kv), s = (int)(seq / p.n_seqs);
+  auto sync = [&] {
+    if (ctas == 1) __syncthreads();
+    else cluster.sync();
+  };
+  griddep_launch_dependents();
+  griddep_wait();
+  if (p.kv_count && pos >= p.kv_count[s]) return;
+  int len = p.len[seq], keep = p.keep[seq];
+  const int seen = p.seen ? p.seen[seq] : len;
+  if (len < 0 || len > p.max_len || keep < 0 || keep > p.max_len) {
+    if (threadIdx.x == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+    len = max(0, min(len, p.max_len));
+    keep = max(0, min(keep, p.max_len));
+  }
+  const Slots sl{p.table + seq * p.max_pages, pos, p.kv, p.page_shift, p.n_pages};
+  const bool in_place = p.weights == p.weights_out;
+  if (len <= keep) {                                                   // all stay
+    if (in_place) return;
+    for (int i = rank * kEvThreads + threadIdx.x; i < len; i += ctas * kEvThreads) {
+      if ((unsigned)sl.page(i) >= (unsigned)p.n_pages) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); continue; }
+      p.weights_out[sl.at(i)] = p.weights[sl.at(i)];
+      p.slot_pos_out[sl.at(i)] = p.slot_pos[sl.at(i)];
+    }
+    return;
+  }
+  if (keep == 0) return;
+  const long long guard = (long long)seen - min(p.recent, keep);
+  // the warp's run of slots
+  const int warps = ctas * kEvWarps, me = rank * kEvWarps + warp;
+  const int run = ((len + warps - 1) / warps + 31) / 32 * 32;
+  const int lo = (int)min((long long)len, (long long)me * run), hi = min(len, lo + run);
+  const int key0 = warp * run;                                         // of the run in shared memory
+  auto compute_key = [&](int i) {
+    const long long at = sl.at(i);
+    return rank_key(p.weights[at], p.slot_pos[at] >= guard);
+  };
+  auto key_at = [&](int i) { return key0 + (i - lo) < p.key_cache ? keys[key0 + (i - lo)] : compute_key(i); };
+
+  // 1. keys
+  if (threadIdx.x == 0) { guarded = 0; bad = 0; }
+  for (int b = threadIdx.x; b < kBins; b += kEvThreads) hist[b] = 0;
+  __syncthreads();
+  {
+    int mine = 0;
+    bool wrong = false;
+    for (int i = lo + lane; i < hi; i += 32) {
+      if ((unsigned)sl.page(i) >= (unsigned)p.n_pages) { wrong = true; continue; }
+      const uint32_t key = compute_key(i);
+      if (key0 + (i - lo) < p.key_cache) keys[key0 + (i - lo)] = key;
+      if (key == 0xffffffffu) ++mine;
+      else atomicAdd(&hist[key >> 21], 1u);
+    }
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (lane == 0 && mine) atomicAdd(&guarded, mine);
+    if (wrong) bad = 1;
+  }
+  sync();
+  int total_guarded = 0, any_bad = 0;
+  for (int c = 0; c < ctas; ++c) {
+    total_guarded += *cluster.map_shared_rank(&guarded, c);
+    any_bad |= *cluster.map_shared_rank(&bad, c);
+  }
+  // 2. the threshold: keys above it stay, and `quota` of those equal to it
+  uint32_t threshold = 0xffffffffu;
+  int quota = keep;
+  if (total_guarded < keep && !any_bad) {
+    int need = keep - total_guarded;
+    uint32_t prefix = 0;
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : kBins;
+      if (pass > 0) {
+        const int above = pass == 1 ? 21 : 10;
+        for (int i = lo + lane; i < hi; i += 32) {
+          const uint32_t key = key_at(i);
+          if (key != 0xffffffffu && key >> above == prefix >> above) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
+        }
+        sync();
+      }
+      // bins from the top: thread t has four of them
+      constexpr int PER = kBins / kEvThreads;
+      uint32_t h[PER], sum = 0;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const int b = bins - 1 - (int)(threadIdx.x * PER + j);
+        h[j] = 0;
+        if (b >= 0)
+          for (int c = 0; c < ctas; ++c) h[j] += cluster.map_shared_rank(hist, c)[b];
+        sum += h[j];
+      }
+      uint32_t upto = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      if (lane == 31) warp_sum[warp] = (int)upto;
+      sync();                                                          // the histograms have been read, too
+      uint32_t above = upto - sum;
+      for (int w = 0; w < warp; ++w) above += (uint32_t)warp_sum[w];
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        if (above < (uint32_t)need && (uint32_t)need <= above + h[j]) {
+          found_bin = bins - 1 - (int)(threadIdx.x * PER + j);
+          found_above = (int)above;
+        }
+        above += h[j];
+      }
+      for (int b = threadIdx.x; b < kBins; b += kEvThreads) hist[b] = 0;
+      __syncthreads();
+      prefix |= (uint32_t)found_bin << shift;
+      need -= found_above;
+    }
+    threshold = prefix;
+    quota = need;
+  } else {
+    sync();                                                            // the counters have been read
+  }
+  if (any_bad) {
+    if (threadIdx.x == 0 && rank == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+    return;
+  }
+  // numbers of the runs before this warp's
+  auto before_me = [&](const int* of) {
+    int n = 0;
+    for (int w = lane; w < me; w += 32) n += cluster.map_shared_rank(of, w / kEvWarps)[w % kEvWarps];
+    return __reduce_add_sync(0xffffffffu, n);
+  };
+  // 3. equal keys in the order of slots
+  {
+    int n = 0;
+    for (int i = lo + lane; i < hi; i += 32) n += key_at(i) == threshold;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) counts[0][warp] = n;
+  }
+  sync();
+  int equal = before_me(counts[0]);
+  int32_t* bits = p.ws + item * p.ws_item;
+  int32_t* before = bits + groups_of(p.max_len);
+  int32_t* movers = before + groups_of(p.max_len);
+  int free_n = 0, move_n = 0;
+  for (int g0 = lo; g0 < hi; g0 += 32) {
+    const int i = g0 + lane;
+    const uint32_t key = i < hi ? key_at(i) : 0u;
+    const unsigned same = __ballot_sync(0xffffffffu, i < hi && key == threshold);
+    const bool stays = i < hi && (key > threshold || (key == threshold && equal + __popc(same & ((1u << lane) - 1)) < quota));
+    const unsigned stay = __ballot_sync(0xffffffffu, stays);
+    equal += __popc(same);
+    free_n += __popc(__ballot_sync(0xffffffffu, i < keep && !stays));
+    move_n += __popc(__ballot_sync(0xffffffffu, i >= keep && stays));
+    if (lane == 0) bits[g0 >> 5] = (int32_t)stay;
+  }
+  if (lane == 0) counts[1][warp] = free_n;
+  sync();                                                              // everybody has read counts[0]
+  if (lane == 0) counts[0][warp] = move_n;
+  int free_at = before_me(counts[1]);
+  sync();
+  int move_at = before_me(counts[0]);
+  for (int g0 = lo; g0 < hi; g0 += 32) {
+    const int i = g0 + lane;
+    const uint32_t stay = (uint32_t)bits[g0 >> 5];                     // the warp's own words
+    const bool moves = i >= keep && i < hi && (stay >> lane & 1);
+    const unsigned all = __ballot_sync(0xffffffffu, moves);
+    if (moves) movers[move_at + __popc(all & ((1u << lane) - 1))] = i;
+    move_at += __popc(all);
+    if (lane == 0) before[g0 >> 5] = free_at;
+    free_at += __popc(__ballot_sync(0xffffffffu, i < keep && !(stay >> lane & 1)));
+  }
+  sync();
+  // 4. the moves
+  const bool q8 = D > 0;
+  const int cut = q8 && (keep & 15) ? keep >> 4 : -1;                  // the block that keep cuts
+  auto fill = [&](int block) {
+    const int slot0 = block << 4, end = q8 ? min(len, slot0 + 16) : min(keep, slot0 + 16);
+    const int from = source_of(bits, before, movers, slot0, keep, end, lane), slot = slot0 + (lane & 15);
+    const unsigned moved = __ballot_sync(0xffffffffu, lane < 16 && from >= 0 && from != slot);
+    if (lane < 16 && from >= 0 && slot < keep && (from != slot || !in_place)) {
+      const long long to = sl.at(slot), at = sl.at(from);
+      const float w = p.weights[at];
+      const int32_t x = p.slot_pos[at];
+      p.weights_out[to] = w;
+      p.slot_pos_out[to] = x;
+    }
+    if (!moved) return;
+    if constexpr (D > 0) move_block<D>(p, sl, slot0, from, lane);
+    else move_rows(p, sl, slot0, from, moved, lane);
+  };
+  const int blocks = (keep + 15) >> 4;
+  for (int b = me; b < blocks; b += warps)
+    if (b != cut) fill(b);
+  if (cut >= 0) {
+    sync();
+    if (me == 0) fill(cut);
+  }
+}
+
+template <int D>
+int run_evict(EvictParams& p, long long items, cudaStream_t st) {
+  const int sms = sm_count();
+  // CTAs of an item: as many as still have kSlotsPerCta slots each and run at once.
+  int ctas = 1;
+  while (ctas < kMaxEvictCluster && p.max_len > ctas * kSlotsPerCta && items * ctas * 2 <= 2ll * sms) ctas *= 2;
+  const long long run = ((p.max_len + (long long)ctas * kEvWarps - 1) / ((long long)ctas * kEvWarps) + 31) / 32 * 32;
+  p.key_cache = (int)(run * kEvWarps < kKeyCache ? run * kEvWarps : kKeyCache);
+  static bool ready[64] = {false};
+  const int slot = device_slot();
+  if (!ready[slot]) {
+    TWIST_CUDA_TRY(cudaFuncSetAttribute(evict_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeyCache * 4));
+    ready[slot] = true;
+  }
+  TWIST_CUDA_TRY(launch_overlapped(evict_kernel<D>, dim3((unsigned)(items * ctas)), dim3(kEvThreads), (size_t)p.key_cache * 4, st, ctas, p));
+  return TWIST_OK;
+}
+
+bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+
+constexpr long long kMaxItems = 1 << 20, kMaxSlots = 1 << 26;
+
+}  // namespace
+}  // namespace twist
+
+using namespace twist;
+
+extern "C" size_t twist_kv_evict_workspace_bytes(int32_t n_subnets, int32_t n_seqs, int32_t kv_max, int64_t max_len) {
+  if (n_subnets <= 0 || n_seqs <= 0 || kv_max <= 0 || max_len <= 0 || max_len > kMaxSlots) return 0;
+  if ((long long)n_subnets * n_seqs > kMaxItems || (long long)n_subnets * n_seqs * kv_max > kMaxItems) return 0;
+  return (size_t)n_subnets * n_seqs * kv_max * item_words(max_len) * 4;
+}
+
+extern "C" int32_t twist_kv_evict(const twist_kv_evict_args* a, void* stream) {
+  if (!a) return TWIST_ERR_NULL;
+  if (a->dtype != TWIST_BF16) return TWIST_ERR_UNSUPPORTED;
+  if (a->cache != TWIST_CACHE_BF16 && a->cache != TWIST_CACHE_E4M3) return TWIST_ERR_SHAPE;
+  const bool q8 = a->cache == TWIST_CACHE_E4M3;
+  if (a->n_subnets <= 0 || a->n_seqs <= 0 || a->kv_max <= 0 || a->d_head <= 0 || a->n_pages <= 0 || a->max_pages <= 0 || a->page_size <= 0 ||
+      a->max_len < 0 || a->recent < 0)
+    return TWIST_ERR_SHAPE;
+  const int dh = a->d_head;
+  if (q8 ? dh != 16 && dh != 32 && dh != 64 && dh != 128 : dh % 8 != 0 || dh > 256) return TWIST_ERR_UNSUPPORTED;
+  if (a->page_size < 16 || a->page_size > 1024 || (a->page_size & (a->page_size - 1))) return TWIST_ERR_UNSUPPORTED;
+  const long long table_len = (long long)a->max_pages * a->page_size;
+  const long long max_len = a->max_len > 0 && a->max_len < table_len ? a->max_len : table_len;
+  if (max_len > kMaxSlots || (long long)a->n_subnets * a->n_seqs > kMaxItems || (long long)a->n_subnets * a->n_seqs * a->kv_max > kMaxItems)
+    return TWIST_ERR_UNSUPPORTED;
+  if (a->page_stride % (q8 ? 16 : 8) != 0 || a->page_stride < (long long)a->kv_max * a->page_size * dh) return TWIST_ERR_SHAPE;
+  if (q8 != (a->scales != nullptr)) return TWIST_ERR_SHAPE;
+  if (!a->k_cache || !a->v_cache || !a->page_table || !a->kv_len || !a->keep || !a->weights || !a->slot_pos || !a->weights_out || !a->slot_pos_out)
+    return TWIST_ERR_NULL;
+  if (!aligned16(a->k_cache) || !aligned16(a->v_cache) || !aligned16(a->scales) || !aligned16(a->weights) || !aligned16(a->slot_pos) ||
+      !aligned16(a->weights_out) || !aligned16(a->slot_pos_out) || !aligned16(a->ws))
+    return TWIST_ERR_SHAPE;
+  const long long bytes = (long long)a->n_pages * a->kv_max * a->page_size * 4;
+  const bool in_place = a->weights == a->weights_out;
+  if (in_place != (a->slot_pos == a->slot_pos_out)) return TWIST_ERR_SHAPE;
+  if (overlap(a->weights, bytes, a->slot_pos, bytes) || overlap(a->weights_out, bytes, a->slot_pos_out, bytes) ||
+      (!in_place && (overlap(a->weights, bytes, a->weights_out, bytes) || overlap(a->weights, bytes, a->slot_pos_out, bytes) ||
+                     overlap(a->slot_pos, bytes, a->weights_out, bytes) || overlap(a->slot_pos, bytes, a->slot_pos_out, bytes))))
+    return TWIST_ERR_SHAPE;
+  if (!a->ws || a->ws_bytes < twist_kv_evict_workspace_bytes(a->n_subnets, a->n_seqs, a->kv_max, max_len)) return TWIST_ERR_WORKSPACE;
+  EvictParams p;
+  memset(&p, 0, sizeof(p));
+  p.k = static_cast<uint8_t*>(a->k_cache);
+  p.v = static_cast<uint8_t*>(a->v_cache);
+  p.scales = a->scales;
+  p.table = a->page_table; p.len = a->kv_len; p.keep = a->keep; p.seen = a->seen; p.kv_count = a->kv_count;
+  p.weights = a->weights; p.slot_pos = a->slot_pos; p.weights_out = a->weights_out; p.slot_pos_out = a->slot_pos_out;
+  p.ws = static_cast<int32_t*>(a->ws);
+  p.row_bytes = dh * (q8 ? 1 : 2);
+  p.page_bytes = a->page_stride * (q8 ? 1 : 2);
+  p.ws_item = item_words(max_len);
+  p.n_seqs = a->n_seqs; p.kv = a->kv_max;
+  p.page_shift = 31 - __builtin_clz((unsigned)a->page_size);
+  p.n_pages = a->n_pages; p.max_pages = a->max_pages; p.max_len = (int)max_len; p.recent = a->recent;
+  p.status = device_status_ptr();
+  if (!p.status) return TWIST_ERR_CUDA;
+  const long long items = (long long)a->n_subnets * a->n_seqs * a->kv_max;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!q8) return run_evict<0>(p, items, st);
+  switch (dh) {
+    case 16: return run_evict<16>(p, items, st);
+    case 32: return run_evict<32>(p, items, st);
+    case 64: return run_evict<64>(p, items, st);
+    default: return run_evict<128>(p, items, st);
+  }
+}

@@ -1,0 +1,409 @@
+// twist_kv_append_q8: new K and V rows into a paged cache of 8-bit numbers, K rotated by position on the way, and the
+// rotated Q.
+//
+// A block is 16 slots of a KV position; its numbers are e4m3, value = number * scale with a power-of-two scale:
+//     scale = max(scale of the tokens it holds already, smallest 2^e with max |x| <= 448 * 2^e over the new ones).
+// The scale is known only when the whole block has been seen, and a block that holds tokens may have to be rounded again,
+// so a block's new tokens belong to one warp: it rotates 16 rows of a head in registers (fp32), finds the largest
+// magnitude with one shuffle reduction, and writes each number once.  The work is moving bytes (2 read and 1 written
+// per element of K and V, 2 and 2 for Q): HBM-bound for prompts, latency-bound for the rows of a decoding step.
+//
+// A CTA takes the new tokens of one block of one sequence, all heads: the tokens are neighbouring rows at neighbouring
+// positions, so the index data of a CTA is found once, and one table of (cos, sin) serves its heads (angles as in
+// positions.cu: reduced in 64 bits).  A warp takes a head at a time.  Both elements of a pair are read by the lanes
+// that own either of them (the second read hits L1), so that a lane's work is the same in all layouts; rotating in
+// place is safe because a head's rows are read by one warp before it writes any of them.
+#include "common.cuh"
+#include "e4m3.cuh"
+#include "ptx.cuh"
+
+namespace twist {
+namespace {
+
+constexpr int kAppThreads = 256, kAppWarps = kAppThreads / 32;
+constexpr double kInvTwoPi = 0.15915494309189533577;
+
+struct AppendParams {
+  const __nv_bfloat16* in;       // [S * T][width]
+  __nv_bfloat16* q_out;          // rows q_stride apart, or null
+  uint8_t* k_cache;
+  uint8_t* v_cache;
+  float* scales;                 // [n_pages][kv][page / 16][2]
+  const double* inv_freq;
+  const int32_t *page_table, *kv_len, *seen, *new_begin, *new_len, *kv_count;
+  long long q_stride, page_stride;
+  int T, heads, kv, width, rot, half;
+  int n_seqs, rows_per_seq, per_seq, per_subnet;      // CTAs of a sequence (padded rows) / of a subnet
+  int page_shift, n_pages, max_pages;
+  int* status;
+};
+
+// What a CTA appends: `count` rows from row `row` of [S * T] on to the slots first .. of the block that begins at slot in_page of
+// the page; the first is at position `pos` of its sequence.  held: KV positions to write.
+struct Run {
+  long long row, page;
+  int count, first, in_page, pos, held;
+};
+
+__device__ inline void report(const AppendParams& p, bool mine) {
+  if (mine) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+}
+
+// Blocks that the n new tokens at the end of `len` slots span; 0 if the sequence's numbers contradict each other.
+__device__ inline int blocks_of(const AppendParams& p, int n, int len, int seen, bool& bad) {
+  bad = n > 0 && (len < n || (long long)len > ((long long)p.max_pages << p.page_shift) || seen < len);
+  return n <= 0 || bad ? 0 : (((len - n) & 15) + n + 15) >> 4;
+}
+
+// One warp.  count == 0: nothing to do.
+__device__ inline Run find_run(const AppendParams& p, int lane) {
+  Run r;
+  r.count = 0;
+  const int s = blockIdx.x / p.per_subnet;
+  int j = blockIdx.x - s * p.per_subnet, b, n, len, seen, begin;
+  const int32_t* lens = p.kv_len + (long long)s * p.n_seqs;
+  const int32_t* seens = p.seen ? p.seen + (long long)s * p.n_seqs : lens;
+  const int held = p.kv_count ? p.kv_count[s] : p.kv;
+  if (p.new_begin) {
+    // the sequence in whose blocks number j falls: lanes take sequences, a running sum over them
+    const int32_t* nb = p.new_begin + (long long)s * (p.n_seqs + 1);
+    int before = 0;
+    bool found = false, broken = false;
+    b = n = len = seen = begin = 0;
+    for (int k0 = 0; k0 < p.n_seqs; k0 += 32) {
+      const int k = k0 + lane;
+      int x = 0, y = 0, l = 0, sn = 0, blocks = 0;
+      if (k < p.n_seqs) {
+        x = nb[k]; y = nb[k + 1]; l = lens[k]; sn = seens[k];
+        if (x < 0 || y < x || y > p.T) {
+          broken = true;
+        } else {
+          bool bad;
+          blocks = blocks_of(p, y - x, l, sn, bad);
+          report(p, bad);
+        }
+      }
+      int upto = blocks;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const int from = before + upto - blocks;
+      const unsigned hit = __ballot_sync(0xffffffffu, j >= from && j < from + blocks);
+      if (hit && !found) {
+        const int at = __ffs(hit) - 1;
+        found = true;
+        b = k0 + at;
+        begin = __shfl_sync(0xffffffffu, x, at);
+        n = __shfl_sync(0xffffffffu, y, at) - begin;
+        len = __shfl_sync(0xffffffffu, l, at);
+        seen = __shfl_sync(0xffffffffu, sn, at);
+        j -= __shfl_sync(0xffffffffu, from, at);
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (__any_sync(0xffffffffu, broken)) {            // not ascending, or rows that the call does not have
+      report(p, lane == 0);
+      return r;
+    }
+    if (!found) return r;
+  } else {
+    b = j / p.per_seq;
+    j -= b * p.per_seq;
+    begin = b * p.rows_per_seq;
+    n = p.new_len ? p.new_len[(long long)s * p.n_seqs + b] : p.rows_per_seq;
+    len = lens[b];
+    seen = seens[b];
+    bool bad = n < 0 || n > p.rows_per_seq, bad2 = false;
+    if (!bad && j >= blocks_of(p, n, len, seen, bad2)) {
+      report(p, bad2 && lane == 0);
+      return r;
+    }
+    if (bad) {
+      report(p, lane == 0);
+      return r;
+    }
+  }
+  const int slot0 = len - n, block0 = ((slot0 >> 4) + j) << 4;
+  const int page = p.page_table[((long long)s * p.n_seqs + b) * p.max_pages + (block0 >> p.page_shift)];
+  if ((unsigned)page >= (unsigned)p.n_pages) {
+    report(p, lane == 0);
+    return r;
+  }
+  r.first = max(slot0 - block0, 0);
+  const int i = max(block0 - slot0, 0);               // the first token's number among the new ones
+  r.count = min(16 - r.first, n - i);
+  r.row = (long long)s * p.T + begin + i;
+  r.pos = seen - n + i;
+  r.held = max(0, min(p.kv, held));
+  r.page = page;
+  r.in_page = block0 & ((1 << p.page_shift) - 1);
+  return r;
+}
+
+__device__ inline float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ inline float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+__device__ inline void spread(float (&x)[8], const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = bf_lo(w[i]); x[2 * i + 1] = bf_hi(w[i]); }
+}
+
+enum { MODE_HALF = 0, MODE_PAIRS = 1, MODE_SLOW_HALF = 2, MODE_SLOW_PAIRS = 3 };
+
+// 16 rows of a head: lane's item i is the eight elements from 8 * c on of row r, c = (32 i + lane) % (D / 8).
+template <int D>
+struct Rows {
+  static constexpr int CHUNKS = D / 8, ITEMS = D / 16;
+  float x[ITEMS][8];
+};
+
+template <int D, int MODE>
+__device__ inline void load_rows(Rows<D>& y, const AppendParams& p, const __nv_bfloat16* src, const float2* table, int count, bool turn, int lane) {
+  using R = Rows<D>;
+  constexpr bool SLOW = MODE == MODE_SLOW_HALF || MODE == MODE_SLOW_PAIRS;
+  uint4 own[R::ITEMS], other[R::ITEMS];
+#pragma unroll
+  for (int i = 0; i < R::ITEMS; ++i) {
+    const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+    if (r < count) {
+      own[i] = *reinterpret_cast<const uint4*>(src + (long long)r * p.width + 8 * c);
+      if (MODE == MODE_HALF && turn && 8 * c < p.rot)
+        other[i] = *reinterpret_cast<const uint4*>(src + (long long)r * p.width + (8 * c < p.half ? 8 * c + p.half : 8 * c - p.half));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R::ITEMS; ++i) {
+    const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+    float (&x)[8] = y.x[i];
+    if (r >= count) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      continue;
+    }
+    spread(x, own[i]);
+    if (!turn || 8 * c >= p.rot) continue;
+    const float2* cs = table + r * p.half;
+    if constexpr (MODE == MODE_HALF) {
+      float z[8];
+      spread(z, other[i]);
+      const bool low = 8 * c < p.half;
+      const float2* at = cs + (low ? 8 * c : 8 * c - p.half);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = low ? x[e] * at[e].x - z[e] * at[e].y : z[e] * at[e].y + x[e] * at[e].x;
+    } else if constexpr (MODE == MODE_PAIRS) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float2 a = cs[4 * c + e / 2];
+        const float u = x[e], v = x[e + 1];
+        x[e] = u * a.x - v * a.y;
+        x[e + 1] = u * a.y + v * a.x;
+      }
+    } else if constexpr (SLOW) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int el = 8 * c + e;
+        if (el < p.rot) {
+          const bool low = MODE == MODE_SLOW_HALF ? el < p.half : el % 2 == 0;
+          const int pair = MODE == MODE_SLOW_HALF ? (low ? el : el - p.half) : el / 2;
+          const int mate = MODE == MODE_SLOW_HALF ? (low ? el + p.half : el - p.half) : el ^ 1;
+          const float z = __bfloat162float(src[(long long)r * p.width + mate]);
+          const float2 a = cs[pair];
+          x[e] = low ? x[e] * a.x - z * a.y : z * a.y + x[e] * a.x;
+        }
+      }
+    }
+  }
+  __syncwarp();                                       // the rows have been read: now they may be written
+}
+
+// The rows as numbers of a block: `cache` is the block's first row, `scale` its scale.
+template <int D>
+__device__ inline void store_block(const Rows<D>& y, uint8_t* cache, float* scale, const Run& run, int lane) {
+  using R = Rows<D>;
+  const float old = run.first > 0 ? *scale : 0.f;
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < R::ITEMS; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float a = fabsf(y.x[i][e]);
+      top = fmaxf(top, a < INFINITY ? a : 0.f);
+    }
+  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+  const float now = fmaxf(scale_for(top), old);       // a NaN for an old scale counts for nothing
+  const float inv = inverse_scale(now);
+  if (run.first > 0 && now != old) {                  // the tokens that the block holds, rounded to the new scale
+    const float f = old * inv;
+    for (int k = lane; k < run.first * D / 8; k += 32) {
+      uint2* at = reinterpret_cast<uint2*>(cache) + k;
+      const uint2 v = *at;
+      uint32_t w[2] = {v.x, v.y};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float a[4];
+        widen4(a, w[i]);
+        w[i] = narrow4(a[0] * f, a[1] * f, a[2] * f, a[3] * f);
+      }
+      *at = make_uint2(w[0], w[1]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R::ITEMS; ++i) {
+    const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+    const float (&x)[8] = y.x[i];
+    if (r < run.count)
+      *reinterpret_cast<uint2*>(cache + (run.first + r) * D + 8 * c) =
+          make_uint2(narrow4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), narrow4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+  }
+  if (lane == 0) *scale = now;
+}
+
+template <int D, int MODE>
+__global__ void __launch_bounds__(kAppThreads, D == 128 ? 2 : 3) append_q8_kernel(const AppendParams p) {
+  using R = Rows<D>;
+  __shared__ Run shared;
+  extern __shared__ float2 table[];                   // [16][half]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  griddep_launch_dependents();
+  griddep_wait();
+  if (warp == 0) {
+    const Run r = find_run(p, lane);
+    if (lane == 0) shared = r;
+  }
+  __syncthreads();
+  const Run run = shared;
+  if (run.count == 0) return;
+  for (int k = threadIdx.x; k < run.count * p.half; k += kAppThreads) {
+    const int r = k / p.half, j = k - r * p.half;
+    double turns = (double)(run.pos + r) * (p.inv_freq[j] * kInvTwoPi);
+    turns -= rint(turns);
+    float s, c;
+    sincospif(2.0f * (float)turns, &s, &c);
+    table[k] = make_float2(c, s);
+  }
+  __syncthreads();
+  const __nv_bfloat16* rows = p.in + run.row * p.width;
+  // heads in the order K, V, Q
+  for (int u = warp; u < 2 * p.kv + (p.q_out ? p.heads : 0); u += kAppWarps) {
+    Rows<D> y;
+    if (u < 2 * p.kv) {
+      const bool is_k = u < p.kv;
+      const int group = is_k ? u : u - p.kv;
+      if (group >= run.held) continue;
+      load_rows<D, MODE>(y, p, rows + (p.heads + u) * D, table, run.count, is_k, lane);
+      store_block<D>(y, (is_k ? p.k_cache : p.v_cache) + run.page * p.page_stride + (((long long)group << p.page_shift) + run.in_page) * D,
+                     p.scales + 2 * (((run.page * p.kv + group) << (p.page_shift - 4)) + (run.in_page >> 4)) + !is_k, run, lane);
+    } else {
+      const int h = u - 2 * p.kv;
+      load_rows<D, MODE>(y, p, rows + h * D, table, run.count, true, lane);
+      __nv_bfloat16* out = p.q_out + run.row * p.q_stride + h * D;
+#pragma unroll
+      for (int i = 0; i < R::ITEMS; ++i) {
+        const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+        const float (&x)[8] = y.x[i];
+        if (r < run.count) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+            w[e] = *reinterpret_cast<const uint32_t*>(&t);
+          }
+          *reinterpret_cast<uint4*>(out + r * p.q_stride + 8 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+  }
+}
+
+bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+
+template <int D>
+int launch(const AppendParams& p, int S, int layout, cudaStream_t st) {
+  int mode;
+  if (layout == TWIST_ROPE_HALF) mode = p.half % 8 == 0 ? MODE_HALF : MODE_SLOW_HALF;
+  else mode = p.rot % 8 == 0 ? MODE_PAIRS : MODE_SLOW_PAIRS;
+  if (p.rot == 0) mode = MODE_PAIRS;
+  const long long grid = (long long)S * p.per_subnet;
+  if (grid > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
+  void (*kernel)(AppendParams) = mode == MODE_HALF ? append_q8_kernel<D, MODE_HALF>
+                                 : mode == MODE_PAIRS ? append_q8_kernel<D, MODE_PAIRS>
+                                 : mode == MODE_SLOW_HALF ? append_q8_kernel<D, MODE_SLOW_HALF>
+                                                          : append_q8_kernel<D, MODE_SLOW_PAIRS>;
+  TWIST_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)grid), dim3(kAppThreads), 16 * p.half * sizeof(float2), st, 1, p));
+  return TWIST_OK;
+}
+
+}  // namespace
+}  // namespace twist
+
+using namespace twist;
+
+extern "C" int32_t twist_kv_append_q8(const twist_kv_append_q8_args* a, void* stream) {
+  if (!a) return TWIST_ERR_NULL;
+  if (a->dtype != TWIST_BF16) return TWIST_ERR_UNSUPPORTED;
+  if (a->n_subnets <= 0 || a->n_seqs <= 0 || a->tokens <= 0 || a->head_keep <= 0 || a->kv_max <= 0 || a->d_head <= 0 || a->n_pages <= 0 ||
+      a->max_pages <= 0 || a->page_size <= 0)
+    return TWIST_ERR_SHAPE;
+  const int dh = a->d_head;
+  if (dh != 16 && dh != 32 && dh != 64 && dh != 128) return TWIST_ERR_UNSUPPORTED;
+  if (a->rot_dims < 0 || a->rot_dims > dh || a->rot_dims % 2 != 0) return TWIST_ERR_SHAPE;
+  if (a->layout != TWIST_ROPE_HALF && a->layout != TWIST_ROPE_PAIRS) return TWIST_ERR_SHAPE;
+  const long long width = ((long long)a->head_keep + 2ll * a->kv_max) * dh, a_sub = (long long)a->head_keep * dh;
+  if (width > (1 << 24)) return TWIST_ERR_UNSUPPORTED;
+  if (a->page_size < 16 || a->page_size > 1024 || (a->page_size & (a->page_size - 1))) return TWIST_ERR_UNSUPPORTED;
+  if ((long long)a->max_pages * a->page_size > 0x7fffffffll - 1024) return TWIST_ERR_UNSUPPORTED;      // positions are 32-bit
+  if (a->page_stride % 16 != 0 || a->page_stride < (long long)a->kv_max * a->page_size * dh) return TWIST_ERR_SHAPE;
+  if (!a->new_begin && a->tokens % a->n_seqs != 0) return TWIST_ERR_SHAPE;
+  if (a->new_begin && a->new_len) return TWIST_ERR_SHAPE;
+  if (a->q_out && (a->q_stride % 8 != 0 || a->q_stride < a_sub)) return TWIST_ERR_SHAPE;
+  if (!a->qkv || !a->k_cache || !a->v_cache || !a->scales || !a->page_table || !a->kv_len || (a->rot_dims > 0 && !a->inv_freq)) return TWIST_ERR_NULL;
+  if (!aligned16(a->qkv) || !aligned16(a->q_out) || !aligned16(a->k_cache) || !aligned16(a->v_cache) || !aligned16(a->scales) ||
+      (reinterpret_cast<uintptr_t>(a->inv_freq) & 7))
+    return TWIST_ERR_SHAPE;
+  AppendParams p;
+  memset(&p, 0, sizeof(p));
+  const long long rows = (long long)a->n_subnets * a->tokens;
+  if (a->q_out && !(a->q_out == a->qkv && (a->q_stride == width || rows == 1)) &&
+      overlap(a->qkv, rows * width * 2, a->q_out, ((rows - 1) * a->q_stride + a_sub) * 2))
+    return TWIST_ERR_SHAPE;
+  p.in = static_cast<const __nv_bfloat16*>(a->qkv);
+  p.q_out = static_cast<__nv_bfloat16*>(a->q_out);
+  p.k_cache = static_cast<uint8_t*>(a->k_cache);
+  p.v_cache = static_cast<uint8_t*>(a->v_cache);
+  p.scales = a->scales;
+  p.inv_freq = a->inv_freq;
+  p.page_table = a->page_table; p.kv_len = a->kv_len; p.seen = a->seen;
+  p.new_begin = a->new_begin; p.new_len = a->new_len; p.kv_count = a->kv_count;
+  p.q_stride = a->q_stride; p.page_stride = a->page_stride;
+  p.T = a->tokens; p.heads = a->head_keep; p.kv = a->kv_max; p.width = (int)width;
+  p.rot = a->rot_dims; p.half = a->rot_dims / 2;
+  p.n_seqs = a->n_seqs;
+  p.page_shift = 31 - __builtin_clz((unsigned)a->page_size);
+  p.n_pages = a->n_pages; p.max_pages = a->max_pages;
+  // Blocks that n tokens can span: (n + 14) / 16 + 1.  Packed rows: as many as all sequences together can.
+  if (a->new_begin) {
+    p.rows_per_seq = p.per_seq = 1;
+    const long long n = (long long)a->tokens / 16 + 2ll * (a->n_seqs < a->tokens ? a->n_seqs : a->tokens) + 1;
+    if (n > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
+    p.per_subnet = (int)n;
+  } else {
+    p.rows_per_seq = a->tokens / a->n_seqs;
+    p.per_seq = (p.rows_per_seq + 14) / 16 + 1;
+    if ((long long)p.per_seq * a->n_seqs > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
+    p.per_subnet = p.per_seq * a->n_seqs;
+  }
+  p.status = device_status_ptr();
+  if (!p.status) return TWIST_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  switch (dh) {
+    case 16: return launch<16>(p, a->n_subnets, a->layout, st);
+    case 32: return launch<32>(p, a->n_subnets, a->layout, st);
+    case 64: return launch<64>(p, a->n_subnets, a->layout, st);
+    default: return launch<128>(p, a->n_subnets, a->layout, st);
+  }
+}
