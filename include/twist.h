@@ -577,7 +577,8 @@ int32_t twist_kv_append_q8(const twist_kv_append_q8_args* a /*host*/, void* stre
  * product as fp16 brought near 2^15 by a power of two (no bits of an element are lost within 2^29 of its head's largest),
  * probabilities as fp16 (11 bits), cached values exactly; sums are fp32 and divided at the end.  NaN in V makes its element of
  * the heads that read it NaN and touches no other.  The workspace is that of twist_attn_decode.
- * d_head in {16, 32, 64, 128}; the work is counted in tiles of 32 keys from d_head 64 on, else 64. */
+ * d_head in {16, 32, 64, 128}; limits as twist_attn_decode, t + 4 in place of t + 2, tiles of 64 keys, of 32 at d_head 64 and of 16
+ * at 128. */
 typedef struct {
   int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;
   int32_t page_size, n_pages, max_pages, max_len;

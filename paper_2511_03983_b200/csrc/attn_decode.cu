@@ -41,7 +41,10 @@ namespace twist {
 namespace {
 
 constexpr int kMaxCtasPerSm = 4;
-constexpr int kItemCost = 1;               // what changing to the next item costs a warp, in tiles
+// What changing to the next item costs a warp, in tiles.  8 bits, 1 / 2 / 3 / 5: 952 ragged sequences of up to 274 keys on 4
+// positions of d = 128 57.3 / 50.4 / 48.5 / 48.1 us, eight subnets of long ones 194.8 / 195.8 / 187.5 / 186.9.
+template <int B>
+constexpr int kItemCost = B == 1 ? 3 : 1;
 constexpr int kMinCost = 2;                // least work of a warp, in tiles
 constexpr int kJoinThreads = 512;
 // The short way, one cluster per item (see run).
@@ -59,7 +62,7 @@ template <int D, int B>
 struct State {
   float o[Shape<D, B>::MT][4];
   float m0, m1, l0, l1;
-  float unit;                 // 8 bits: the sums o count in this (a scale of V)
+  float unit, inverse;        // 8 bits: the sums o count in this (a scale of V); its inverse
 };
 
 template <int D, int B>
@@ -71,6 +74,7 @@ __device__ inline void reset(State<D, B>& st) {
   st.m0 = st.m1 = -INFINITY;
   st.l0 = st.l1 = 0.f;
   st.unit = 0.f;
+  st.inverse = INFINITY;
 }
 
 // Values of keys behind the end of `len` keys, cleared (see kClamp).
@@ -97,25 +101,27 @@ __device__ inline void clear_behind(Tile<D, B>& x, int key0, int len, int t) {
 // 2^4 of it no bits are lost and nothing overflows (a probability is at most 2^8); a scale further off becomes the unit, and the
 // sums so far are converted to it.
 template <int D>
-__device__ inline void add_values8(State<D, 1>& st, const float (&sc)[Shape<D, 1>::SUB][4], Tile<D, 1>& x, float2 scale, float scale_log2,
+__device__ inline void add_values8(State<D, 1>& st, const float (&sc)[Shape<D, 1>::SUB][4], Tile<D, 1>& x, const Scales<D, 1>& scale, float scale_log2,
                                    float r0, float r1, int key0, int len, int t) {
   using Sh = Shape<D, 1>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
+    if (s > 0 && key0 + 16 * s >= len) break;                          // nothing has been copied
     float pr[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) pr[e] = ex2(fmaf(sc[s][e], scale_log2, (e & 1) ? -r1 : -r0));
     st.l0 += pr[0] + pr[2];
     st.l1 += pr[1] + pr[3];
-    const float unit = scale_of<D, 1>(scale, s).y;
-    float f = __fdividef(unit, st.unit);
+    const float unit = scale.of[s].y;
+    float f = unit * st.inverse;
     if (!(f <= 16.f && f >= 0.0625f)) {
-      const float down = st.unit / unit;
+      const float inverse = 1.f / unit, down = st.unit * inverse;
 #pragma unroll
       for (int i = 0; i < Sh::MT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) st.o[i][e] *= down;
       st.unit = unit;
+      st.inverse = inverse;
       f = 1.f;
     }
     const uint32_t b0 = transpose8x8(pack_f16(pr[0] * f, pr[1] * f)), b1 = transpose8x8(pack_f16(pr[2] * f, pr[3] * f));
@@ -140,7 +146,7 @@ __device__ inline void add_values8(State<D, 1>& st, const float (&sc)[Shape<D, 1
 
 // Softmax step and O^T += V^T P^T of the tile that begins at key0 of `len` keys.
 template <int D, int B>
-__device__ inline void tile_values(State<D, B>& st, float (&sc)[Shape<D, B>::SUB][4], Tile<D, B>& x, float2 scale, float scale_log2, int key0, int len, int g, int t) {
+__device__ inline void tile_values(State<D, B>& st, float (&sc)[Shape<D, B>::SUB][4], Tile<D, B>& x, const Scales<D, B>& scale, float scale_log2, int key0, int len, int g, int t) {
   using Sh = Shape<D, B>;
   if (key0 + Sh::TILE > len) {                     // keys behind the end count for nothing
 #pragma unroll
@@ -315,14 +321,15 @@ __global__ void __launch_bounds__(kDecThreads, D == 128 ? 3 : (D >= 32 ? 4 : 5))
   const int len = clamped_len(p, p.len[seq]), tiles = (len + Sh::TILE - 1) / Sh::TILE;
   ids = check_pages<D, B>(p, ids, len - 1, first, stride, lane);
   wait_copies();
+  const long long k_at = at_k<D, B>(p, pos, g, t), v_at = at_v<D, B>(p, pos, g, t);
   constexpr int AHEAD = 32 / Sh::SUB;
   State<D, B> st;
   reset<D, B>(st);
   Tile<D, B> x;
   int key0 = first * Sh::TILE;
   if (first < tiles) {
-    load_k<D, B>(x, p, ids, 0, key0, len - 1, pos, lane);
-    load_v<D, B>(x, p, ids, 0, key0, len - 1, pos, lane);
+    load_k<D, B>(x, p, ids, 0, key0, len - 1, pos, k_at, lane);
+    load_v<D, B>(x, p, ids, 0, key0, len - 1, v_at, lane);
   }
   __syncthreads();
   find_heads(p, hd, s, pos, rt, lane, cols[warp]);
@@ -335,17 +342,17 @@ __global__ void __launch_bounds__(kDecThreads, D == 128 ? 3 : (D >= 32 ? 4 : 5))
     const bool more = tile + stride < tiles;
     const int next0 = key0 + stride * Sh::TILE;
     float sc[Sh::SUB][4];
-    tile_scores<D, B>(sc, x, q);
-    const float2 scale = x.scale;                  // the next keys bring theirs
+    const Scales<D, B> scale = gather_scales(x);
+    tile_scores<D, B>(sc, x, q, scale);
     if (more) {
       if (++n == AHEAD) {
         ids = check_pages<D, B>(p, fetch_pages<D, B>(p, seq, tile + stride, stride, lane), len - 1, tile + stride, stride, lane);
         n = 0;
       }
-      load_k<D, B>(x, p, ids, n, next0, len - 1, pos, lane);
+      load_k<D, B>(x, p, ids, n, next0, len - 1, pos, k_at, lane);
     }
     tile_values<D, B>(st, sc, x, scale, p.scale_log2, key0, len, g, t);
-    if (more) load_v<D, B>(x, p, ids, n, next0, len - 1, pos, lane);
+    if (more) load_v<D, B>(x, p, ids, n, next0, len - 1, v_at, lane);
   }
   finish<D, B>(st, p.scale_log2);
   float* mine = sm + warp * kCols * (D + 2);       // [head][D + 2]
@@ -434,11 +441,67 @@ struct Segment {
 
 constexpr int kLenCache = 512;        // sequences whose lengths a CTA keeps in shared memory
 
+// An 8-bit cache's tiles in the split kernel: a ring of them per warp, filled by bulk copies (the 16 rows of a step lie next to
+// each other in their page: one copy for K, one for V).  Half the bytes for the same arithmetic: with the next tile in
+// registers, as in 16 bits, the loads in flight do not cover a tile's time (eight subnets of d = 128 246 us, 64 ragged sequences
+// with 32 heads on 4 positions of d = 64 75; through rings 205 and 60).  Three tiles of 16 keys and 12 warps an SM at d = 128
+// (two: 199 us against 195, two of 32 keys and 8 warps: 204), two of 32 keys and 16 warps at d = 64 (of 64 keys and 12 warps:
+// 63 against 58, three of 32 and 12: 63, three of 16 keys: 63 to 70).
+template <int D>
+constexpr int kRing = D == 128 ? 3 : 2;
+template <int D>
+struct Ring {
+  using Sh = Shape<D, 1>;
+  struct alignas(16) {
+    uint8_t k[Sh::TILE * D], v[Sh::TILE * D];
+  } tile[kRing<D>];
+  float2 scale[kRing<D>][Sh::SUB];
+  alignas(16) uint64_t full[kRing<D>];           // 2 SUB arrivals: of every step, its bytes to expect and its scales
+};
+
+template <int W>
+__device__ inline void take_words(uint32_t (&r)[W], const uint8_t* a) {
+  if constexpr (W == 4) {
+    const uint4 v = *reinterpret_cast<const uint4*>(a);
+    r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
+  } else if constexpr (W == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(a);
+    r[0] = v.x; r[1] = v.y;
+  } else {
+    r[0] = *reinterpret_cast<const uint32_t*>(a);
+  }
+}
+template <int D>
+__device__ inline void take_keys(Tile<D, 1>& x, const uint8_t* k, int g, int t) {
+  using Sh = Shape<D, 1>;
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s)
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < Sh::KCH; ++c) take_words<Sh::KW>(x.k[s][r][c], k + (16 * s + 8 * r + g) * D + 4 * Sh::KW * (4 * c + t));
+}
+template <int D>
+__device__ inline void take_values(Tile<D, 1>& x, const uint8_t* v, int g, int t) {
+  using Sh = Shape<D, 1>;
+#pragma unroll
+  for (int s = 0; s < Sh::SUB; ++s)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < Sh::VCH; ++c) {
+        const uint8_t* row = v + (16 * s + 2 * t + (r & 1) + 8 * (r >> 1)) * D;
+        if constexpr (Sh::HALF_V) x.v[s][r][c][0] = *reinterpret_cast<const unsigned short*>(row + 2 * g);
+        else take_words<Sh::VW>(x.v[s][r][c], row + 4 * Sh::VW * (8 * c + g));
+      }
+}
+
 // Tiles that go through shared memory in the split kernel.
 template <int D, int B>
-constexpr bool kStaged = D == 32 || (D == 16 && B == 2);
+constexpr bool kStaged = B == 2 && (D == 16 || D == 32);
+
 template <int D, int B>
-constexpr int kRingBytes = kStaged<D, B> ? 2 * kDecWarps * (int)sizeof(Stage<D, B>) : 0;
+constexpr int kRingBytes = B == 1 ? kDecWarps * (int)sizeof(Ring<D>) : (kStaged<D, B> ? 2 * kDecWarps * (int)sizeof(Stage<D, B>) : 0);
 
 constexpr int kCountCache = 256;      // KV positions of all subnets whose heads a CTA counts
 
@@ -447,14 +510,16 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
   using Sh = Shape<D, B>;
   __shared__ int cols[kDecWarps][2][kCols];
   __shared__ __align__(16) QueryBuf<D, B> qbuf[kDecWarps];
-  extern __shared__ __align__(16) unsigned char ring[];       // [kDecWarps][2] stages
+  extern __shared__ __align__(16) unsigned char ring[];       // [kDecWarps][2] stages, or [kDecWarps] rings
   __shared__ int items[TWIST_MAX_SUBNETS], counts[kCountCache];
   __shared__ int32_t lens[kLenCache], head_cache[kHeadCache], pos_cache[kPosCache];
   __shared__ uint32_t warp_sum[kDecWarps];
   __shared__ __align__(16) uint32_t before[kDecThreads];    // cost of the sequences before each thread's
+  __shared__ volatile int abort_flag;                       // a wait for a copy ran out
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int N = p.S * p.n_seqs, per = (N + kDecThreads - 1) / kDecThreads;
   for (int i = threadIdx.x; i < kCountCache; i += kDecThreads) counts[i] = 0;
+  if (B == 1 && threadIdx.x == 0) abort_flag = 0;
   griddep_launch_dependents();
   griddep_wait();
   // one round trip: lengths, heads, positions
@@ -499,7 +564,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     const int last = min(N, i + per);
 #pragma unroll 8
     for (; i < last; ++i) {
-      mine += (uint32_t)items[s] * (kItemCost + tiles_of<D, B>(len_of(i)));
+      mine += (uint32_t)items[s] * (kItemCost<B> + tiles_of<D, B>(len_of(i)));
       if (++b == p.n_seqs) { b = 0; ++s; }
     }
   }
@@ -541,13 +606,13 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     int seq = owner * per, s = seq / p.n_seqs, b = seq - s * p.n_seqs;
     for (;;) {
       enter(now, seq, s);
-      cost = (uint32_t)items[s] * (now.nt + kItemCost);
+      cost = (uint32_t)items[s] * (now.nt + kItemCost<B>);
       if (u < base + cost) break;
       base += cost;
       ++seq;
       if (++b == p.n_seqs) { b = 0; ++s; }
     }
-    const uint32_t one = now.nt + kItemCost;
+    const uint32_t one = now.nt + kItemCost<B>;
     int item = (int)((u - base) / one);
     const uint32_t x0 = u - base - item * one, x1 = min(one, x0 + left);
     item0 = u - x0;
@@ -558,14 +623,176 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
       for (now.pos = 0; item >= count_tiles(s, now.pos); ++now.pos) item -= count_tiles(s, now.pos);
       now.rt = item;
     }
-    now.t0 = max(0, (int)x0 - kItemCost);
-    now.t1 = max(0, (int)x1 - kItemCost);
+    now.t0 = max(0, (int)x0 - kItemCost<B>);
+    now.t1 = max(0, (int)x1 - kItemCost<B>);
     left -= x1 - x0;
   }
   if (now.t1 <= now.t0) return;                           // the item's own cost is all there is: the next warp has its tiles
 
   constexpr int AHEAD = 32 / Sh::SUB;
+  // the item behind another one (its t1 is the caller's)
+  auto following = [&](Segment x) {
+    x.t0 = 0;
+    if (++x.rt >= row_tiles(x.s, x.pos)) {
+      x.rt = 0;
+      do {
+        if (++x.pos == p.kv_max) {
+          x.pos = 0;
+          enter(x, x.seq + 1, (x.seq + 1) / p.n_seqs);
+        }
+      } while (row_tiles(x.s, x.pos) == 0);
+    }
+    return x;
+  };
+  // a segment's result
+  auto store = [&](const State<D, B>& st, const Segment& now, int hq) {
+    const bool whole = now.t0 == 0 && now.t1 == now.nt;
+    const int h0 = __shfl_sync(0xffffffffu, hq, 8 * t), h1 = __shfl_sync(0xffffffffu, hq, 8 * t + 4);
+    if (whole) {
+      if (h0 >= 0) store_head<D, B>(p, st, 0, now.seq, h0, g, now.len);
+      if (h1 >= 0) store_head<D, B>(p, st, 1, now.seq, h1, g, now.len);
+    } else {
+      float* part = p.part + (2ll * c + (now.t0 == 0)) * kCols * kPartRow(D);
+      if (h0 >= 0) store_part<D, B>(part + 2 * t * kPartRow(D), st, 0, h0, g);
+      if (h1 >= 0) store_part<D, B>(part + (2 * t + 1) * kPartRow(D), st, 1, h1, g);
+    }
+    if (now.t0 == 0 && (p.by_item || !whole)) {
+      const int heads = __popc(__ballot_sync(0xffffffffu, hq >= 0 && t == 0));
+      if (lane == 0) {
+        const int parts = whole ? 0 : (int)(cut.piece_of(item0 + kItemCost<B> + now.nt - 1) - c);    // further parts of the item
+        const int all = p.kv_max * p.row_tiles, item = now.pos * p.row_tiles + now.rt;
+        int4* desc = p.desc + (p.by_item ? (long long)now.seq * all : (long long)c);
+        desc[p.by_item ? item : 0] = make_int4(now.seq, heads, parts, (int)c);
+        if (p.by_item) {                            // the neighbours in the table that are no items
+          auto is_item = [&](int k) { return k % p.row_tiles < row_tiles(now.s, k / p.row_tiles); };
+          for (int k = item + 1; k < all && !is_item(k); ++k) desc[k] = make_int4(0, 0, 0, 0);
+          for (int k = item - 1; k >= 0 && !is_item(k); --k) desc[k] = make_int4(0, 0, 0, 0);
+        }
+      }
+    }
+  };
+  if constexpr (B == 1) {
+    Ring<D>& ring8 = reinterpret_cast<Ring<D>*>(ring)[warp];
+    if (lane == 0) {
+      for (int i = 0; i < kRing<D>; ++i) mbar_init(smem_u32(&ring8.full[i]), 2 * Sh::SUB);
+      fence_async_smem();
+    }
+    __syncwarp();
+    // The filling side walks the line by itself, kRing tiles ahead of the other: its segment, the one behind it, and where the
+    // lane's step of the current AHEAD tiles lies (lane l: step l % SUB of the l / SUB-th).
+    Segment at = now, behind = now;
+    uint32_t at_left = left;
+    bool at_more = false, live = false;
+    int tile = now.t0, n = 0, head_ids = 0, to = 0;
+    long long from = 0, scale_from = 0;
+    int next_ids = fetch_pages<D, B>(p, now.seq, now.t0, 1, lane);
+    auto window = [&](int ids) {                     // the page ids of the AHEAD tiles from `tile` on have come
+      ids = check_pages<D, B>(p, ids, at.len - 1, tile, 1, lane);
+      next_ids = fetch_pages<D, B>(p, at.seq, tile + AHEAD, 1, lane);
+      const int key = (int)step_key<D, B>(tile, 1, lane), in_page = key & ((1 << p.page_shift) - 1);
+      live = key < at.len;
+      from = ids * p.page_stride + (((long long)at.pos << p.page_shift) + in_page) * D;
+      scale_from = (((long long)ids * p.kv_max + at.pos) << (p.page_shift - 4)) + (in_page >> 4);
+      n = 0;
+    };
+    auto look = [&] {
+      at_more = at_left > (uint32_t)kItemCost<B>;
+      if (at_more) {
+        behind = following(at);
+        behind.t1 = (int)min((uint32_t)behind.nt, at_left - kItemCost<B>);
+        head_ids = fetch_pages<D, B>(p, behind.seq, 0, 1, lane);
+      }
+    };
+    auto fill = [&] {                                // a group of copies, empty behind the last tile
+      while (tile >= at.t1 || at.len == 0) {
+        if (!at_more) { commit_copies(); return; }
+        at_left -= behind.t1 + kItemCost<B>;
+        at = behind;
+        tile = 0;
+        window(head_ids);
+        look();
+      }
+      if (n == AHEAD) window(next_ids);
+      if (lane / Sh::SUB == n) {
+        const int step = lane % Sh::SUB;
+        const uint32_t bar = smem_u32(&ring8.full[to]);
+        if (live) {
+          mbar_expect_tx(bar, 32 * D);
+          bulk_load(smem_u32(ring8.tile[to].k + 16 * D * step), static_cast<const uint8_t*>(p.k) + from, 16 * D, bar);
+          bulk_load(smem_u32(ring8.tile[to].v + 16 * D * step), static_cast<const uint8_t*>(p.v) + from, 16 * D, bar);
+          copy_async<8>(&ring8.scale[to][step], p.scales + scale_from);
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+        } else {                                       // a step behind the end
+          mbar_arrive(bar);
+          mbar_arrive(bar);
+        }
+      }
+      commit_copies();
+      to = to + 1 == kRing<D> ? 0 : to + 1;
+      ++tile;
+      ++n;
+    };
+    find_heads(p, hd, now.s, now.pos, now.rt, lane, cols[warp][0]);
+    prefetch_q<D, B>(qbuf[warp], p, now.seq, cols[warp][0][g], lane);
+    commit_copies();
+    window(next_ids);
+    look();
+#pragma unroll 1
+    for (int i = 0; i < kRing<D>; ++i) fill();
+    int buf = 0, slot = 0, since = kRing<D>;
+    uint32_t parity = 0;
+    bool ok = true;
+    for (;;) {
+      // the queries: their group is older than those of the tiles filled since, of which the newest need not have come
+      Query<D, B> q;
+      if (since >= 2) wait_copies_but<2>();
+      else wait_copies();
+      take_q<D, B>(q, qbuf[warp], lane);
+      const int hq = cols[warp][buf][g];
+      const bool more = left > (uint32_t)kItemCost<B>;
+      Segment next = now;
+      if (more) {
+        next = following(now);
+        next.t1 = (int)min((uint32_t)next.nt, left - kItemCost<B>);
+        find_heads(p, hd, next.s, next.pos, next.rt, lane, cols[warp][buf ^ 1]);
+        prefetch_q<D, B>(qbuf[warp], p, next.seq, cols[warp][buf ^ 1][g], lane);
+      }
+      commit_copies();
+      since = now.len > 0 ? now.t1 - now.t0 : 0;
+      State<D, B> st;
+      reset<D, B>(st);
+      if (now.len > 0) {
+        for (int i = now.t0; i < now.t1; ++i) {
+          ok = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&ring8.full[slot]), parity, &abort_flag, p.status));
+          if (!ok) break;
+          Tile<D, B> x;
+          Scales<D, B> scale;
+          float sc[Sh::SUB][4];
+#pragma unroll
+          for (int s = 0; s < Sh::SUB; ++s) scale.of[s] = ring8.scale[slot][s];
+          take_keys<D>(x, ring8.tile[slot].k, g, t);
+          tile_scores<D, B>(sc, x, q, scale);
+          take_values<D>(x, ring8.tile[slot].v, g, t);
+          tile_values<D, B>(st, sc, x, scale, p.scale_log2, i * Sh::TILE, now.len, g, t);
+          __syncwarp();                                // the tile has been read
+          if (++slot == kRing<D>) { slot = 0; parity ^= 1; }
+          fill();
+        }
+      }
+      if (!ok) break;
+      finish<D, B>(st, p.scale_log2);
+      store(st, now, hq);
+      if (!more) break;
+      item0 += now.nt + kItemCost<B>;
+      left -= next.t1 + kItemCost<B>;
+      now = next;
+      buf ^= 1;
+    }
+    if (!ok) drain_after_abort(&abort_flag);
+    return;
+  } else {
   constexpr bool STAGED = kStaged<D, B>;
+  const Scales<D, B> none{};
   Stage<D, B>* stages = reinterpret_cast<Stage<D, B>*>(ring) + 2 * warp;
   Tile<D, B> x;
   int ids = fetch_pages<D, B>(p, now.seq, now.t0, 1, lane);
@@ -576,13 +803,13 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
   prefetch_q<D, B>(qbuf[warp], p, now.seq, cols[warp][0][g], lane);
   ids = check_pages<D, B>(p, ids, now.len - 1, now.t0, 1, lane);
   if (now.len > 0) {
-    if constexpr (STAGED) stage_k<D, B>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, now.pos, lane);
-    else load_k<D, B>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, now.pos, lane);
+    if constexpr (STAGED) stage_k<D, B>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D, B>(p, now.pos, g, t), lane);
+    else load_k<D, B>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, now.pos, at_k<D, B>(p, now.pos, g, t), lane);
   }
   commit_copies();                                  // the queries travel with the first keys
   if (now.len > 0) {
-    if constexpr (STAGED) stage_v<D, B>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, now.pos, lane);
-    else load_v<D, B>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, now.pos, lane);
+    if constexpr (STAGED) stage_v<D, B>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D, B>(p, now.pos, g, t), lane);
+    else load_v<D, B>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_v<D, B>(p, now.pos, g, t), lane);
   }
   commit_copies();
   for (;;) {
@@ -592,21 +819,12 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     take_q<D, B>(q, qbuf[warp], lane);
     const int hq = cols[warp][buf][g];
     // the segment behind this one: its first pages, its heads and their queries on their way before they are needed
-    const bool more = left > (uint32_t)kItemCost;
+    const bool more = left > (uint32_t)kItemCost<B>;
     Segment next = now;
     int head_ids = 0;
     if (more) {
-      next.t0 = 0;
-      if (++next.rt >= row_tiles(next.s, next.pos)) {
-        next.rt = 0;
-        do {
-          if (++next.pos == p.kv_max) {
-            next.pos = 0;
-            enter(next, next.seq + 1, (next.seq + 1) / p.n_seqs);
-          }
-        } while (row_tiles(next.s, next.pos) == 0);
-      }
-      next.t1 = (int)min((uint32_t)next.nt, left - kItemCost);
+      next = following(now);
+      next.t1 = (int)min((uint32_t)next.nt, left - kItemCost<B>);
       head_ids = fetch_pages<D, B>(p, next.seq, 0, 1, lane);
       find_heads(p, hd, next.s, next.pos, next.rt, lane, cols[warp][buf ^ 1]);
       prefetch_q<D, B>(qbuf[warp], p, next.seq, cols[warp][buf ^ 1][g], lane);          // complete with the next tile's keys
@@ -632,55 +850,32 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
       float sc[Sh::SUB][4];
       if constexpr (STAGED) {
         Stage<D, B>& to = stages[stage ^ 1];
-        if (load) stage_k<D, B>(to, p, ids, n, key0, last_key, of, lane);
+        if (load) stage_k<D, B>(to, p, ids, n, key0, last_key, at_k<D, B>(p, of, g, t), lane);
         commit_copies();
-        if (load) stage_v<D, B>(to, p, ids, n, key0, last_key, of, lane);
+        if (load) stage_v<D, B>(to, p, ids, n, key0, last_key, at_v<D, B>(p, of, g, t), lane);
         commit_copies();
         wait_copies_but<3>();
         take_k<D, B>(x, stages[stage], lane);
-        tile_scores<D, B>(sc, x, q);
+        tile_scores<D, B>(sc, x, q, none);
         wait_copies_but<2>();
         take_v<D, B>(x, stages[stage], lane);
-        if (now.len > 0) tile_values<D, B>(st, sc, x, x.scale, p.scale_log2, tile * Sh::TILE, now.len, g, t);
+        if (now.len > 0) tile_values<D, B>(st, sc, x, none, p.scale_log2, tile * Sh::TILE, now.len, g, t);
         stage ^= 1;
       } else {
-        tile_scores<D, B>(sc, x, q);
-        const float2 scale = x.scale;
-        if (load) load_k<D, B>(x, p, ids, n, key0, last_key, of, lane);
-        if (now.len > 0) tile_values<D, B>(st, sc, x, scale, p.scale_log2, tile * Sh::TILE, now.len, g, t);
-        if (load) load_v<D, B>(x, p, ids, n, key0, last_key, of, lane);
+        tile_scores<D, B>(sc, x, q, none);
+        if (load) load_k<D, B>(x, p, ids, n, key0, last_key, of, at_k<D, B>(p, of, g, t), lane);
+        if (now.len > 0) tile_values<D, B>(st, sc, x, none, p.scale_log2, tile * Sh::TILE, now.len, g, t);
+        if (load) load_v<D, B>(x, p, ids, n, key0, last_key, at_v<D, B>(p, of, g, t), lane);
       }
     }
     finish<D, B>(st, p.scale_log2);
-    const bool whole = now.t0 == 0 && now.t1 == now.nt;
-    const int h0 = __shfl_sync(0xffffffffu, hq, 8 * t), h1 = __shfl_sync(0xffffffffu, hq, 8 * t + 4);
-    if (whole) {
-      if (h0 >= 0) store_head<D, B>(p, st, 0, now.seq, h0, g, now.len);
-      if (h1 >= 0) store_head<D, B>(p, st, 1, now.seq, h1, g, now.len);
-    } else {
-      float* part = p.part + (2ll * c + (now.t0 == 0)) * kCols * kPartRow(D);
-      if (h0 >= 0) store_part<D, B>(part + 2 * t * kPartRow(D), st, 0, h0, g);
-      if (h1 >= 0) store_part<D, B>(part + (2 * t + 1) * kPartRow(D), st, 1, h1, g);
-    }
-    if (now.t0 == 0 && (p.by_item || !whole)) {
-      const int heads = __popc(__ballot_sync(0xffffffffu, hq >= 0 && t == 0));
-      if (lane == 0) {
-        const int parts = whole ? 0 : (int)(cut.piece_of(item0 + kItemCost + now.nt - 1) - c);    // further parts of the item
-        const int all = p.kv_max * p.row_tiles, item = now.pos * p.row_tiles + now.rt;
-        int4* desc = p.desc + (p.by_item ? (long long)now.seq * all : (long long)c);
-        desc[p.by_item ? item : 0] = make_int4(now.seq, heads, parts, (int)c);
-        if (p.by_item) {                            // the neighbours in the table that are no items
-          auto is_item = [&](int k) { return k % p.row_tiles < row_tiles(now.s, k / p.row_tiles); };
-          for (int k = item + 1; k < all && !is_item(k); ++k) desc[k] = make_int4(0, 0, 0, 0);
-          for (int k = item - 1; k >= 0 && !is_item(k); --k) desc[k] = make_int4(0, 0, 0, 0);
-        }
-      }
-    }
+    store(st, now, hq);
     if (!more) break;
-    item0 += now.nt + kItemCost;
-    left -= next.t1 + kItemCost;
+    item0 += now.nt + kItemCost<B>;
+    left -= next.t1 + kItemCost<B>;
     now = next;
     buf ^= 1;
+  }
   }
 }
 
@@ -763,7 +958,7 @@ template <int D, int B>
 int run(DecParams& p, long long max_len, cudaStream_t st) {
   const long long items = (long long)p.S * p.n_seqs * p.kv_max * p.row_tiles;
   // the line is counted in 32 bits
-  const long long longest = (((long long)p.max_pages << p.page_shift) + Shape<D, B>::TILE - 1) / Shape<D, B>::TILE + 1 + kItemCost;
+  const long long longest = (((long long)p.max_pages << p.page_shift) + Shape<D, B>::TILE - 1) / Shape<D, B>::TILE + 1 + kItemCost<B>;
   if (items > 0x7fffffffll / longest) return TWIST_ERR_UNSUPPORTED;
   if (over_queries(p, D)) return TWIST_ERR_SHAPE;
   p.status = device_status_ptr();
@@ -784,8 +979,10 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   // through the line; 512 items of 512 keys, all at once: 15 against 19.  The line is ahead where a warp would take more
   // than kShortTiles tiles, where the items fill the GPU kShortWork tiles a warp deep (256 ragged items of up to 2048
   // keys: 21 us against 27 to 34), and earlier where they do not run at once (512 items of 256 keys, d = 128: 18.2
-  // against 19.6).
-  const long long tiles = (max_len + Shape<D, B>::TILE - 1) / Shape<D, B>::TILE;
+  // against 19.6).  An 8-bit cache is counted in the same 16 keys from d = 64 on (256 ragged items of up to 2048 keys, d = 64:
+  // 18.4 us through the line, 22.1 the short way; 512 items of 512 keys 12.9 the short way, 16.7 through the line).
+  constexpr int UNIT = D >= 64 ? 16 : Shape<D, B>::TILE;
+  const long long tiles = (max_len + UNIT - 1) / UNIT;
   int cluster = 1;
   if (tiles > 2 * kDecWarps)
     while (cluster < kMaxCluster && 2 * cluster * items <= grid && tiles > kDecWarps * cluster) cluster *= 2;

@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
       if (lane == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
       fresh = max(0, min(fresh, len));
     }
+    const long long k_at = at_k<D, B>(p, pos, g, t);
     const int first_new = len - fresh, ahead = (w.seen ? w.seen[seq] : len) - len;
     for (int rt = 0; rt < p.row_tiles; ++rt) {
       __syncwarp();                                  // the heads and queries of the pass before have been read
@@ -68,7 +69,7 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
       Tile<D, B> x;
       constexpr int AHEAD = 32 / Sh::SUB;
       int ids = check_pages<D, B>(p, fetch_pages<D, B>(p, seq, tile0, 1, lane), len - 1, tile0, 1, lane), n = 0;
-      load_k<D, B>(x, p, ids, 0, tile0 * Sh::TILE, len - 1, pos, lane);
+      load_k<D, B>(x, p, ids, 0, tile0 * Sh::TILE, len - 1, pos, k_at, lane);
       wait_copies();
       Query<D, B> q;
       take_q<D, B>(q, qbuf[warp], lane);
@@ -85,13 +86,13 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
           old[st] = t < 2 && key < (rt ? len : first_new) && from ? from[at[st]] : 0.f;
         }
         float sc[Sh::SUB][4];
-        tile_scores<D, B>(sc, x, q);
+        tile_scores<D, B>(sc, x, q, gather_scales(x));
         if (tile + 1 < tiles) {
           if (++n == AHEAD) {
             ids = check_pages<D, B>(p, fetch_pages<D, B>(p, seq, tile + 1, 1, lane), len - 1, tile + 1, 1, lane);
             n = 0;
           }
-          load_k<D, B>(x, p, ids, n, key0 + Sh::TILE, len - 1, pos, lane);
+          load_k<D, B>(x, p, ids, n, key0 + Sh::TILE, len - 1, pos, k_at, lane);
         }
 #pragma unroll
         for (int st = 0; st < Sh::SUB; ++st) {
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CorePa
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
           float sc[Sh::SUB][4];
-          tile_scores<D, 2>(sc, x[k], q);
+          tile_scores<D, 2>(sc, x[k], q, Scales<D, 2>{});
 #pragma unroll
           for (int st = 0; st < Sh::SUB; ++st) {
             const int key = mine + k * Sh::TILE + 16 * st + g;

@@ -107,7 +107,7 @@ struct Shape {
   static constexpr int VW = ROW >= 32 ? 4 : (HALF_V ? 1 : ROW / 8);
   static constexpr int VCH = HALF_V ? 1 : ROW / (8 * VW);
   static constexpr int MT = D >= 16 ? D / 16 : 1;           // MMA tiles over d
-  static constexpr int SUB = D >= 64 ? 2 / B : 4;
+  static constexpr int SUB = D >= 64 ? (D == 64 && B == 1 ? 2 : 1) : 4;      // steps of 16 keys
   static constexpr int TILE = 16 * SUB;
   static constexpr int QW = KW * 2 / B;                     // words of a query beside KW words of a key
   static constexpr int PER = 4 / B;                         // elements of a word
@@ -214,30 +214,24 @@ __device__ inline float2 load_scale(const float2* a) {
 }
 
 template <int D, int B>
-__device__ inline void load_k(Tile<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, int pos, int lane) {
+__device__ inline void load_k(Tile<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, int pos, long long at, int lane) {
   if constexpr (B == 1) x.scale = load_scale(scale_at<D, B>(p, ids, n, key0, last_key, pos, lane));
   auto put = [&](int s, int r, int c, const Elem<B>* a) { load_words<Shape<D, B>::KW>(x.k[s][r][c], a); };
-  tile_k<D, B>(p, ids, n, key0, last_key, at_k<D, B>(p, pos, lane >> 2, lane & 3), lane >> 2, put);
+  tile_k<D, B>(p, ids, n, key0, last_key, at, lane >> 2, put);
 }
 template <int D, int B>
-__device__ inline void load_v(Tile<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, int pos, int lane) {
+__device__ inline void load_v(Tile<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long at, int lane) {
   auto put = [&](int s, int r, int c, const Elem<B>* a) {
     if constexpr (Shape<D, B>::HALF_V) x.v[s][r][c][0] = *reinterpret_cast<const unsigned short*>(a);
     else load_words<Shape<D, B>::VW>(x.v[s][r][c], a);
   };
-  tile_v<D, B>(p, ids, n, key0, last_key, at_v<D, B>(p, pos, lane >> 2, lane & 3), lane & 3, put);
+  tile_v<D, B>(p, ids, n, key0, last_key, at, lane & 3, put);
 }
 
 // The same pieces through shared memory, two tiles deep, where registers do not suffice: every thread copies its own
 // pieces asynchronously to places of its own and reads them back itself, so nothing is waited for but the copies.
-template <int B>
-struct StageScales {};
-template <>
-struct StageScales<1> {
-  float2 scale[32];
-};
 template <int D, int B>
-struct Stage : StageScales<B> {
+struct Stage {
   using Sh = Shape<D, B>;
   uint32_t k[Sh::SUB][2][Sh::KCH][32][Sh::KW];
   uint32_t v[Sh::SUB][4][Sh::VCH][32][Sh::VW];
@@ -251,20 +245,18 @@ __device__ inline void commit_copies() { asm volatile("cp.async.commit_group;" :
 template <int N>
 __device__ inline void wait_copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 template <int D, int B>
-__device__ inline void stage_k(Stage<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, int pos, int lane) {
-  if constexpr (B == 1) copy_async<8>(x.scale + lane, scale_at<D, B>(p, ids, n, key0, last_key, pos, lane));
+__device__ inline void stage_k(Stage<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long at, int lane) {
   auto put = [&](int s, int r, int c, const Elem<B>* a) { copy_async<4 * Shape<D, B>::KW>(x.k[s][r][c][lane], a); };
-  tile_k<D, B>(p, ids, n, key0, last_key, at_k<D, B>(p, pos, lane >> 2, lane & 3), lane >> 2, put);
+  tile_k<D, B>(p, ids, n, key0, last_key, at, lane >> 2, put);
 }
 template <int D, int B>
-__device__ inline void stage_v(Stage<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, int pos, int lane) {
+__device__ inline void stage_v(Stage<D, B>& x, const DecParams& p, int ids, int n, int key0, int last_key, long long at, int lane) {
   auto put = [&](int s, int r, int c, const Elem<B>* a) { copy_async<4 * Shape<D, B>::VW>(x.v[s][r][c][lane], a); };
-  tile_v<D, B>(p, ids, n, key0, last_key, at_v<D, B>(p, pos, lane >> 2, lane & 3), lane & 3, put);
+  tile_v<D, B>(p, ids, n, key0, last_key, at, lane & 3, put);
 }
 template <int D, int B>
 __device__ inline void take_k(Tile<D, B>& x, const Stage<D, B>& y, int lane) {
   using Sh = Shape<D, B>;
-  if constexpr (B == 1) x.scale = y.scale[lane];
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s)
 #pragma unroll
@@ -402,16 +394,26 @@ __device__ inline void take_q(Query<D, B>& q, const QueryBuf<D, B>& buf, int lan
   }
 }
 
-// The scale (K in x, V in y) of step s of a tile.
+// The scales (K in x, V in y) of a tile's steps (8 bits).
 template <int D, int B>
-__device__ inline float2 scale_of(const float2 mine, int s) {
-  if constexpr (Shape<D, B>::SUB == 1) return mine;
-  return make_float2(__shfl_sync(0xffffffffu, mine.x, s), __shfl_sync(0xffffffffu, mine.y, s));
+struct Scales {
+  float2 of[B == 1 ? Shape<D, B>::SUB : 1];
+};
+// From the lanes that loaded them.
+template <int D, int B>
+__device__ inline Scales<D, B> gather_scales(const Tile<D, B>& x) {
+  Scales<D, B> r{};
+  if constexpr (B == 1) {
+#pragma unroll
+    for (int s = 0; s < Shape<D, B>::SUB; ++s)
+      r.of[s] = Shape<D, B>::SUB == 1 ? x.scale : make_float2(__shfl_sync(0xffffffffu, x.scale.x, s), __shfl_sync(0xffffffffu, x.scale.y, s));
+  }
+  return r;
 }
 
 // Scores q . k of a tile: thread (g, t) has keys g, g + 8 of each 16 and heads 2t, 2t + 1.
 template <int D, int B>
-__device__ inline void tile_scores(float (&sc)[Shape<D, B>::SUB][4], const Tile<D, B>& x, const Query<D, B>& q) {
+__device__ inline void tile_scores(float (&sc)[Shape<D, B>::SUB][4], const Tile<D, B>& x, const Query<D, B>& q, const Scales<D, B>& scale) {
   using Sh = Shape<D, B>;
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
@@ -438,7 +440,7 @@ __device__ inline void tile_scores(float (&sc)[Shape<D, B>::SUB][4], const Tile<
       }
     }
     if constexpr (B == 1) {
-      const float scale = scale_of<D, B>(x.scale, s).x, f0 = scale * q.f0, f1 = scale * q.f1;
+      const float f0 = scale.of[s].x * q.f0, f1 = scale.of[s].x * q.f1;
       sc[s][0] *= f0; sc[s][1] *= f1; sc[s][2] *= f0; sc[s][3] *= f1;
     }
   }
