@@ -22,8 +22,10 @@ namespace {
 
 constexpr int kEvThreads = 512, kEvWarps = kEvThreads / 32;
 constexpr int kBins = 2048;
-constexpr int kKeyCache = 24576;          // keys that a CTA keeps in shared memory
+constexpr int kKeyCache = 20480;          // keys that a CTA keeps in shared memory
 constexpr int kMaxEvictCluster = 8, kSlotsPerCta = 1024;
+constexpr int kLocalLen = 4096;           // longest sequence whose lists a CTA keeps there
+constexpr int kTableCache = 1024;         // page ids that a CTA keeps there
 
 struct EvictParams {
   uint8_t* k;                  // pages page_bytes apart
@@ -37,12 +39,15 @@ struct EvictParams {
   int32_t* ws;
   long long page_bytes, ws_item;
   int n_seqs, kv, row_bytes, page_shift, n_pages, max_pages, max_len, recent, key_cache;
+  int local;                   // the workspace of an item fits into shared memory
   int* status;
 };
 
-// Ranks of the workspace of an item: stay bits and free slots before, one of each for 32 slots, then the list of movers.
+// The workspace of an item: stay bits and free slots before, one of each for 32 slots, the list of the tokens that move and that
+// of the slots that they move to (at most half of the slots each).
 __host__ __device__ constexpr long long groups_of(long long max_len) { return (max_len + 31) / 32; }
-__host__ __device__ constexpr long long item_words(long long max_len) { return (2 * groups_of(max_len) + max_len / 2 + 1 + 3) / 4 * 4; }
+__host__ __device__ constexpr long long list_of(long long max_len) { return max_len / 2 + 1; }
+__host__ __device__ constexpr long long item_words(long long max_len) { return (2 * groups_of(max_len) + 2 * list_of(max_len) + 3) / 4 * 4; }
 
 __device__ inline uint32_t rank_key(float w, bool guarded) {
   if (guarded) return 0xffffffffu;
@@ -53,7 +58,7 @@ __device__ inline uint32_t rank_key(float w, bool guarded) {
 
 // The item's slots: page and offset of slot i.
 struct Slots {
-  const int32_t* table;        // of the sequence
+  const int32_t* table;        // of the sequence, in shared memory where it fits
   long long base;              // kv position
   int kv, page_shift, n_pages;
   __device__ int page(int i) const { return table[i >> page_shift]; }
@@ -61,14 +66,15 @@ struct Slots {
   __device__ long long at(int i) const { return (((long long)page(i) * kv + base) << page_shift) + offset(i); }
 };
 
-__device__ inline uint8_t* row_of(const EvictParams& p, const Slots& sl, uint8_t* cache, int slot) {
-  return cache + sl.page(slot) * p.page_bytes + ((sl.base << p.page_shift) + sl.offset(slot)) * p.row_bytes;
+// Byte offset of slot's row in the caches.
+__device__ inline long long row_of(const EvictParams& p, const Slots& sl, int slot) {
+  return sl.page(slot) * p.page_bytes + ((sl.base << p.page_shift) + sl.offset(slot)) * p.row_bytes;
 }
 __device__ inline float* scale_at(const EvictParams& p, const Slots& sl, int slot, int which) {
   return p.scales + 2 * ((((long long)sl.page(slot) * p.kv + sl.base) << (p.page_shift - 4)) + (sl.offset(slot) >> 4)) + which;
 }
 
-// Sources of the 16 slots from slot0 on, one per lane (of the first 16): itself, a mover, or -1 for a slot behind `end`.
+// Sources of the 16 slots of a block, one per lane (of the first 16): itself, a token that moves, or -1 for a slot behind `end`.
 __device__ inline int source_of(const int32_t* bits, const int32_t* before, const int32_t* movers, int slot0, int keep, int end, int lane) {
   const int slot = slot0 + (lane & 15), grp = slot >> 5, bit = slot & 31;
   if (slot >= end) return -1;
@@ -79,27 +85,55 @@ __device__ inline int source_of(const int32_t* bits, const int32_t* before, cons
   return movers[before[grp] + __popc(~stay & live & ((1u << bit) - 1))];
 }
 
-// Rows of a bf16 cache: the moved ones, 16 bytes a lane.
-__device__ inline void move_rows(const EvictParams& p, const Slots& sl, int slot0, int from, unsigned moved, int lane) {
-  const int chunks = p.row_bytes / 16, n = __popc(moved) * 2 * chunks;
-  for (int k0 = 0; k0 < n; k0 += 4 * 32) {
-    uint4 x[4];
-    uint8_t* to[4];
+// Rows of a bf16 cache: the tokens movers[i] to slots[i].  A warp takes 32 at a time: a lane finds the places of one, then all
+// of them carry 16 bytes of K or V per turn, kTurns turns in flight.  CH: 16-byte pieces of a row, 1 to 16, a power of two.
+constexpr int kTurns = 4;                 // 64 items of up to 16000 tokens, d = 128: 61.6 us; eight turns (spilled) 80, two 63
+template <int CH>
+__device__ inline void carry_rows(const EvictParams& p, long long from, long long to, int n, int lane) {
+  constexpr int PER = 32 / (2 * CH);                                  // tokens of a turn
+  constexpr int TURNS = 2 * CH < kTurns ? 2 * CH : kTurns;            // in flight; 2 CH turns carry 32 tokens
+  const int mine = lane / (2 * CH), piece = lane % (2 * CH);
+  uint8_t* cache = (piece >= CH ? p.v : p.k) + 16 * (piece % CH);
+#pragma unroll 1
+  for (int k = 0; k < 32 && k < n; k += PER * TURNS) {
+    uint4 x[TURNS];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = k0 + 32 * j + lane, which = k / chunks, c = k - which * chunks;
-      const int i = k < n ? (int)__fns(moved, 0, (which >> 1) + 1) : 0;
-      const int src = __shfl_sync(0xffffffffu, from, i & 15);
-      to[j] = nullptr;
-      if (k < n) {
-        uint8_t* cache = which & 1 ? p.v : p.k;
-        x[j] = *reinterpret_cast<const uint4*>(row_of(p, sl, cache, src) + 16 * c);
-        to[j] = row_of(p, sl, cache, slot0 + i) + 16 * c;
-      }
+    for (int j = 0; j < TURNS; ++j) {
+      const int i = k + j * PER + mine;
+      const long long at = __shfl_sync(0xffffffffu, from, i);
+      if (i < n) x[j] = *reinterpret_cast<const uint4*>(cache + at);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (to[j]) *reinterpret_cast<uint4*>(to[j]) = x[j];
+    for (int j = 0; j < TURNS; ++j) {
+      const int i = k + j * PER + mine;
+      const long long at = __shfl_sync(0xffffffffu, to, i);
+      if (i < n) *reinterpret_cast<uint4*>(cache + at) = x[j];
+    }
+  }
+}
+// CH 0: rows of other sizes.
+template <int CH>
+__device__ inline void move_rows(const EvictParams& p, const Slots& sl, const int32_t* movers, const int32_t* slots, int n, int warp, int warps, int lane) {
+  for (int base = 32 * warp; base < n; base += 32 * warps) {
+    const int i = base + lane, m = min(32, n - base);
+    long long from = 0, to = 0;
+    if (i < n) {
+      const int a = movers[i], b = slots[i];
+      from = row_of(p, sl, a);
+      to = row_of(p, sl, b);
+      const float w = p.weights[sl.at(a)];
+      const int32_t x = p.slot_pos[sl.at(a)];
+      p.weights_out[sl.at(b)] = w;
+      p.slot_pos_out[sl.at(b)] = x;
+    }
+    if constexpr (CH > 0) {
+      carry_rows<CH>(p, from, to, m, lane);
+    } else {                                                           // a lane its own token
+      for (int c = 0; i < n && c < p.row_bytes; c += 16) {
+        *reinterpret_cast<uint4*>(p.k + to + c) = *reinterpret_cast<const uint4*>(p.k + from + c);
+        *reinterpret_cast<uint4*>(p.v + to + c) = *reinterpret_cast<const uint4*>(p.v + from + c);
+      }
+    }
   }
 }
 
@@ -119,7 +153,7 @@ __device__ inline void move_block(const EvictParams& p, const Slots& sl, int slo
       src[j] = __shfl_sync(0xffffffffu, from, r & 15);
       if (r >= 16) src[j] = -1;
       if (src[j] >= 0) {
-        x[j] = *reinterpret_cast<const uint4*>(row_of(p, sl, cache, src[j]) + 16 * c);
+        x[j] = *reinterpret_cast<const uint4*>(cache + row_of(p, sl, src[j]) + 16 * c);
         scale[j] = *scale_at(p, sl, src[j], which);
       }
     }
@@ -153,19 +187,32 @@ __device__ inline void move_block(const EvictParams& p, const Slots& sl, int slo
         widen4(a, w[i]);
         y[i] = narrow4(a[0] * f, a[1] * f, a[2] * f, a[3] * f);
       }
-      *reinterpret_cast<uint4*>(row_of(p, sl, cache, slot0 + r) + 16 * c) = make_uint4(y[0], y[1], y[2], y[3]);
+      *reinterpret_cast<uint4*>(cache + row_of(p, sl, slot0 + r) + 16 * c) = make_uint4(y[0], y[1], y[2], y[3]);
     }
     if (lane == 0) *scale_at(p, sl, slot0, which) = now;
   }
 }
 
-// D: elements of a row of an 8-bit cache; 0: a bf16 cache.
+__device__ inline uint32_t inclusive(uint32_t v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
+
+// D: elements of a row of an 8-bit cache; of a bf16 cache minus the 16-byte pieces of a row, 0 for sizes that move_rows has no own
+// form for.
 template <int D>
-__global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) {
+__global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams p) {
+  constexpr int WARPS = kEvWarps, THREADS = kEvThreads;
   extern __shared__ uint32_t keys[];
-  __shared__ uint32_t hist[kBins];
-  __shared__ int warp_sum[kEvWarps], counts[2][kEvWarps];
-  __shared__ int guarded, bad, found_bin, found_above;
+  __shared__ int32_t table[kTableCache];
+  __shared__ __align__(16) uint32_t hist[3][kBins];
+  __shared__ int counts[3][WARPS];
+  __shared__ uint32_t sums[WARPS];
+  __shared__ int guarded, bad;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -186,11 +233,16 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) 
     len = max(0, min(len, p.max_len));
     keep = max(0, min(keep, p.max_len));
   }
-  const Slots sl{p.table + seq * p.max_pages, pos, p.kv, p.page_shift, p.n_pages};
+  const int pages = (len + (1 << p.page_shift) - 1) >> p.page_shift;
+  if (pages <= kTableCache) {
+    for (int i = threadIdx.x; i < pages; i += THREADS) table[i] = p.table[seq * p.max_pages + i];
+    __syncthreads();
+  }
+  const Slots sl{pages <= kTableCache ? table : p.table + seq * p.max_pages, pos, p.kv, p.page_shift, p.n_pages};
   const bool in_place = p.weights == p.weights_out;
   if (len <= keep) {                                                   // all stay
     if (in_place) return;
-    for (int i = rank * kEvThreads + threadIdx.x; i < len; i += ctas * kEvThreads) {
+    for (int i = rank * THREADS + threadIdx.x; i < len; i += ctas * THREADS) {
       if ((unsigned)sl.page(i) >= (unsigned)p.n_pages) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); continue; }
       p.weights_out[sl.at(i)] = p.weights[sl.at(i)];
       p.slot_pos_out[sl.at(i)] = p.slot_pos[sl.at(i)];
@@ -200,7 +252,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) 
   if (keep == 0) return;
   const long long guard = (long long)seen - min(p.recent, keep);
   // the warp's run of slots
-  const int warps = ctas * kEvWarps, me = rank * kEvWarps + warp;
+  const int warps = ctas * WARPS, me = rank * WARPS + warp;
   const int run = ((len + warps - 1) / warps + 31) / 32 * 32;
   const int lo = (int)min((long long)len, (long long)me * run), hi = min(len, lo + run);
   const int key0 = warp * run;                                         // of the run in shared memory
@@ -210,107 +262,146 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) 
   };
   auto key_at = [&](int i) { return key0 + (i - lo) < p.key_cache ? keys[key0 + (i - lo)] : compute_key(i); };
 
+  // Weights lie close together: lanes that hit the same bin add up first (one by one in shared memory they would wait in line).
+  auto count = [&](uint32_t* bins, uint32_t bin, bool mine) {
+    const unsigned same = __match_any_sync(0xffffffffu, mine ? bin : 0xffffffffu);
+    if (mine && lane == __ffs(same) - 1) atomicAdd(&bins[bin], (uint32_t)__popc(same));
+  };
   // 1. keys
   if (threadIdx.x == 0) { guarded = 0; bad = 0; }
-  for (int b = threadIdx.x; b < kBins; b += kEvThreads) hist[b] = 0;
+  for (int b = threadIdx.x; b < 3 * kBins; b += THREADS) hist[0][b] = 0;
   __syncthreads();
   {
     int mine = 0;
     bool wrong = false;
-    for (int i = lo + lane; i < hi; i += 32) {
-      if ((unsigned)sl.page(i) >= (unsigned)p.n_pages) { wrong = true; continue; }
-      const uint32_t key = compute_key(i);
-      if (key0 + (i - lo) < p.key_cache) keys[key0 + (i - lo)] = key;
-      if (key == 0xffffffffu) ++mine;
-      else atomicAdd(&hist[key >> 21], 1u);
+    constexpr int BATCH = 4;                                           // groups whose loads are in flight
+    for (int g0 = lo; g0 < hi; g0 += 32 * BATCH) {
+      float w[BATCH];
+      int32_t x[BATCH];
+      bool fine[BATCH];
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int i = g0 + 32 * j + lane;
+        const bool there = i < hi;
+        fine[j] = there && (unsigned)sl.page(i) < (unsigned)p.n_pages;
+        wrong |= there && !fine[j];
+        if (fine[j]) {
+          const long long at = sl.at(i);
+          w[j] = p.weights[at];
+          x[j] = p.slot_pos[at];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int i = g0 + 32 * j + lane;
+        if (g0 + 32 * j >= hi) break;
+        uint32_t key = 0;
+        if (fine[j]) {
+          key = rank_key(w[j], x[j] >= guard);
+          if (key0 + (i - lo) < p.key_cache) keys[key0 + (i - lo)] = key;
+        }
+        const bool guards = fine[j] && key == 0xffffffffu;
+        mine += guards;
+        count(hist[0], key >> 21, fine[j] && !guards);
+      }
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0 && mine) atomicAdd(&guarded, mine);
     if (wrong) bad = 1;
   }
   sync();
-  int total_guarded = 0, any_bad = 0;
-  for (int c = 0; c < ctas; ++c) {
-    total_guarded += *cluster.map_shared_rank(&guarded, c);
-    any_bad |= *cluster.map_shared_rank(&bad, c);
+  int total_guarded = guarded, any_bad = bad;
+  if (ctas > 1) {
+    total_guarded = any_bad = 0;
+    for (int c = 0; c < ctas; ++c) {
+      total_guarded += *cluster.map_shared_rank(&guarded, c);
+      any_bad |= *cluster.map_shared_rank(&bad, c);
+    }
   }
-  // 2. the threshold: keys above it stay, and `quota` of those equal to it
+  if (any_bad) {
+    if (threadIdx.x == 0 && rank == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+    sync();                                                            // the others have read the counters
+    return;
+  }
+  // 2. the threshold: keys above it stay, and `quota` of the `equal` ones that are it
   uint32_t threshold = 0xffffffffu;
-  int quota = keep;
-  if (total_guarded < keep && !any_bad) {
+  int quota = keep, equals = total_guarded;
+  if (total_guarded < keep) {
     int need = keep - total_guarded;
     uint32_t prefix = 0;
+#pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : kBins;
+      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
+      constexpr int kLast = 1024;
+      const int bins = pass == 2 ? kLast : kBins;
       if (pass > 0) {
         const int above = pass == 1 ? 21 : 10;
-        for (int i = lo + lane; i < hi; i += 32) {
-          const uint32_t key = key_at(i);
-          if (key != 0xffffffffu && key >> above == prefix >> above) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
+        for (int g0 = lo; g0 < hi; g0 += 32) {
+          const int i = g0 + lane;
+          const uint32_t key = i < hi ? key_at(i) : 0xffffffffu;
+          count(hist[pass], (key >> shift) & (bins - 1), key != 0xffffffffu && key >> above == prefix >> above);
         }
         sync();
       }
-      // bins from the top: thread t has four of them
-      constexpr int PER = kBins / kEvThreads;
-      uint32_t h[PER], sum = 0;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const int b = bins - 1 - (int)(threadIdx.x * PER + j);
-        h[j] = 0;
-        if (b >= 0)
-          for (int c = 0; c < ctas; ++c) h[j] += cluster.map_shared_rank(hist, c)[b];
-        sum += h[j];
-      }
-      uint32_t upto = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
-      }
-      if (lane == 31) warp_sum[warp] = (int)upto;
-      sync();                                                          // the histograms have been read, too
-      uint32_t above = upto - sum;
-      for (int w = 0; w < warp; ++w) above += (uint32_t)warp_sum[w];
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        if (above < (uint32_t)need && (uint32_t)need <= above + h[j]) {
-          found_bin = bins - 1 - (int)(threadIdx.x * PER + j);
-          found_above = (int)above;
+      // The bin from the top in which the need-th key is: every warp adds up a 16th of the bins, then every warp finds the 16th
+      // and the bin in it.
+      auto four = [&](int b) {                                         // bins b .. b + 3 of all CTAs
+        if (ctas == 1) return *reinterpret_cast<const uint4*>(hist[pass] + b);
+        uint4 v = make_uint4(0, 0, 0, 0);
+        for (int c = 0; c < ctas; ++c) {
+          const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(hist[pass], c) + b);
+          v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
         }
-        above += h[j];
+        return v;
+      };
+      const int group = bins / WARPS;                                  // 128, or 64: half of the lanes
+      const bool reads = 4 * lane < group;
+      {
+        const uint4 v = reads ? four(warp * group + 4 * lane) : make_uint4(0, 0, 0, 0);
+        const uint32_t all = __reduce_add_sync(0xffffffffu, v.x + v.y + v.z + v.w);
+        if (lane == 0) sums[warp] = all;
       }
-      for (int b = threadIdx.x; b < kBins; b += kEvThreads) hist[b] = 0;
       __syncthreads();
+      const uint32_t part = lane < WARPS ? sums[WARPS - 1 - lane] : 0u, upto = inclusive(part, lane);
+      const int at = __ffs(__ballot_sync(0xffffffffu, upto >= (uint32_t)need)) - 1;
+      const int top = bins - at * group - 4 - 4 * lane;                // the lane's four bins of it, from the highest down
+      const uint4 v = reads ? four(top) : make_uint4(0, 0, 0, 0);
+      const uint32_t mine = v.x + v.y + v.z + v.w;
+      const uint32_t before_mine = __shfl_sync(0xffffffffu, upto - part, at) + inclusive(mine, lane) - mine;
+      const int here = __ffs(__ballot_sync(0xffffffffu, before_mine + mine >= (uint32_t)need)) - 1;
+      uint32_t over = before_mine, n_bin = v.w;
+      int bin = top + 3;
+      if (over + n_bin < (uint32_t)need) { over += n_bin; n_bin = v.z; --bin; }
+      if (over + n_bin < (uint32_t)need) { over += n_bin; n_bin = v.y; --bin; }
+      if (over + n_bin < (uint32_t)need) { over += n_bin; n_bin = v.x; --bin; }
+      const int found_bin = __shfl_sync(0xffffffffu, bin, here), found_above = (int)__shfl_sync(0xffffffffu, over, here);
+      equals = (int)__shfl_sync(0xffffffffu, n_bin, here);
       prefix |= (uint32_t)found_bin << shift;
       need -= found_above;
     }
     threshold = prefix;
     quota = need;
-  } else {
-    sync();                                                            // the counters have been read
-  }
-  if (any_bad) {
-    if (threadIdx.x == 0 && rank == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
-    return;
   }
   // numbers of the runs before this warp's
   auto before_me = [&](const int* of) {
     int n = 0;
-    for (int w = lane; w < me; w += 32) n += cluster.map_shared_rank(of, w / kEvWarps)[w % kEvWarps];
+    for (int w = lane; w < me; w += 32) n += ctas == 1 ? of[w] : cluster.map_shared_rank(of, w / WARPS)[w % WARPS];
     return __reduce_add_sync(0xffffffffu, n);
   };
-  // 3. equal keys in the order of slots
-  {
+  // 3. equal keys in the order of slots, if not all of them stay
+  int equal = 0;
+  if (equals > quota) {
     int n = 0;
     for (int i = lo + lane; i < hi; i += 32) n += key_at(i) == threshold;
     n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) counts[0][warp] = n;
+    sync();
+    equal = before_me(counts[0]);
   }
-  sync();
-  int equal = before_me(counts[0]);
-  int32_t* bits = p.ws + item * p.ws_item;
+  int32_t* bits = p.local ? reinterpret_cast<int32_t*>(keys + p.key_cache) : p.ws + item * p.ws_item;
   int32_t* before = bits + groups_of(p.max_len);
   int32_t* movers = before + groups_of(p.max_len);
+  int32_t* slots = movers + list_of(p.max_len);
   int free_n = 0, move_n = 0;
   for (int g0 = lo; g0 < hi; g0 += 32) {
     const int i = g0 + lane;
@@ -318,33 +409,51 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) 
     const unsigned same = __ballot_sync(0xffffffffu, i < hi && key == threshold);
     const bool stays = i < hi && (key > threshold || (key == threshold && equal + __popc(same & ((1u << lane) - 1)) < quota));
     const unsigned stay = __ballot_sync(0xffffffffu, stays);
+    const unsigned below = keep >= g0 + 32 ? 0xffffffffu : (keep <= g0 ? 0u : (1u << (keep - g0)) - 1);
     equal += __popc(same);
-    free_n += __popc(__ballot_sync(0xffffffffu, i < keep && !stays));
-    move_n += __popc(__ballot_sync(0xffffffffu, i >= keep && stays));
+    free_n += __popc(~stay & below);
+    move_n += __popc(stay & ~below);
     if (lane == 0) bits[g0 >> 5] = (int32_t)stay;
   }
-  if (lane == 0) counts[1][warp] = free_n;
-  sync();                                                              // everybody has read counts[0]
-  if (lane == 0) counts[0][warp] = move_n;
-  int free_at = before_me(counts[1]);
+  if (lane == 0) {
+    counts[1][warp] = free_n;
+    counts[2][warp] = move_n;
+  }
   sync();
-  int move_at = before_me(counts[0]);
+  int free_at = before_me(counts[1]), move_at = before_me(counts[2]), moves = 0;
+  if (D <= 0) {
+    for (int w = lane; w < warps; w += 32) moves += ctas == 1 ? counts[2][w] : cluster.map_shared_rank(counts[2], w / WARPS)[w % WARPS];
+    moves = __reduce_add_sync(0xffffffffu, moves);
+  }
   for (int g0 = lo; g0 < hi; g0 += 32) {
-    const int i = g0 + lane;
     const uint32_t stay = (uint32_t)bits[g0 >> 5];                     // the warp's own words
-    const bool moves = i >= keep && i < hi && (stay >> lane & 1);
-    const unsigned all = __ballot_sync(0xffffffffu, moves);
-    if (moves) movers[move_at + __popc(all & ((1u << lane) - 1))] = i;
+    const uint32_t below = keep >= g0 + 32 ? 0xffffffffu : (keep <= g0 ? 0u : (1u << (keep - g0)) - 1);
+    const uint32_t open = ~stay & below, all = stay & ~below, under = (1u << lane) - 1;
+    if (all >> lane & 1) movers[move_at + __popc(all & under)] = g0 + lane;
+    if (D > 0) {
+      if (lane == 0) before[g0 >> 5] = free_at;
+    } else if (open >> lane & 1) {
+      slots[free_at + __popc(open & under)] = g0 + lane;
+    }
     move_at += __popc(all);
-    if (lane == 0) before[g0 >> 5] = free_at;
-    free_at += __popc(__ballot_sync(0xffffffffu, i < keep && !(stay >> lane & 1)));
+    free_at += __popc(open);
   }
   sync();
   // 4. the moves
-  const bool q8 = D > 0;
-  const int cut = q8 && (keep & 15) ? keep >> 4 : -1;                  // the block that keep cuts
+  if constexpr (D <= 0) {
+    move_rows<-D>(p, sl, movers, slots, moves, me, warps, lane);
+    const int first = rank * THREADS + threadIdx.x, stride = ctas * THREADS;
+    if (!in_place)
+      for (int i = first; i < keep; i += stride)
+        if ((uint32_t)bits[i >> 5] >> (i & 31) & 1) {
+          p.weights_out[sl.at(i)] = p.weights[sl.at(i)];
+          p.slot_pos_out[sl.at(i)] = p.slot_pos[sl.at(i)];
+        }
+    return;
+  }
+  const int cut = keep & 15 ? keep >> 4 : -1;                          // the block that keep cuts
   auto fill = [&](int block) {
-    const int slot0 = block << 4, end = q8 ? min(len, slot0 + 16) : min(keep, slot0 + 16);
+    const int slot0 = block << 4, end = min(len, slot0 + 16);
     const int from = source_of(bits, before, movers, slot0, keep, end, lane), slot = slot0 + (lane & 15);
     const unsigned moved = __ballot_sync(0xffffffffu, lane < 16 && from >= 0 && from != slot);
     if (lane < 16 && from >= 0 && slot < keep && (from != slot || !in_place)) {
@@ -356,7 +465,6 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) 
     }
     if (!moved) return;
     if constexpr (D > 0) move_block<D>(p, sl, slot0, from, lane);
-    else move_rows(p, sl, slot0, from, moved, lane);
   };
   const int blocks = (keep + 15) >> 4;
   for (int b = me; b < blocks; b += warps)
@@ -369,11 +477,10 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictParams p) 
 
 template <int D>
 int run_evict(EvictParams& p, long long items, cudaStream_t st) {
-  const int sms = sm_count();
-  // CTAs of an item: as many as still have kSlotsPerCta slots each and run at once.
+  // CTAs of an item: as many as still have kSlotsPerCta slots each, two for an SM (four: 129 us against 74 in the case above).
   int ctas = 1;
-  while (ctas < kMaxEvictCluster && p.max_len > ctas * kSlotsPerCta && items * ctas * 2 <= 2ll * sms) ctas *= 2;
-  const long long run = ((p.max_len + (long long)ctas * kEvWarps - 1) / ((long long)ctas * kEvWarps) + 31) / 32 * 32;
+  while (ctas < kMaxEvictCluster && p.max_len > ctas * kSlotsPerCta && items * ctas <= sm_count()) ctas *= 2;
+  const long long warps = (long long)ctas * kEvWarps, run = ((p.max_len + warps - 1) / warps + 31) / 32 * 32;
   p.key_cache = (int)(run * kEvWarps < kKeyCache ? run * kEvWarps : kKeyCache);
   static bool ready[64] = {false};
   const int slot = device_slot();
@@ -381,7 +488,9 @@ int run_evict(EvictParams& p, long long items, cudaStream_t st) {
     TWIST_CUDA_TRY(cudaFuncSetAttribute(evict_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeyCache * 4));
     ready[slot] = true;
   }
-  TWIST_CUDA_TRY(launch_overlapped(evict_kernel<D>, dim3((unsigned)(items * ctas)), dim3(kEvThreads), (size_t)p.key_cache * 4, st, ctas, p));
+  p.local = ctas == 1 && p.max_len <= kLocalLen;
+  const size_t smem = ((size_t)p.key_cache + (p.local ? item_words(p.max_len) : 0)) * 4;
+  TWIST_CUDA_TRY(launch_overlapped(evict_kernel<D>, dim3((unsigned)(items * ctas)), dim3(kEvThreads), smem, st, ctas, p));
   return TWIST_OK;
 }
 
@@ -451,7 +560,16 @@ extern "C" int32_t twist_kv_evict(const twist_kv_evict_args* a, void* stream) {
   if (!p.status) return TWIST_ERR_CUDA;
   const long long items = (long long)a->n_subnets * a->n_seqs * a->kv_max;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (!q8) return run_evict<0>(p, items, st);
+  if (!q8) {
+    switch (dh) {
+      case 8: return run_evict<-1>(p, items, st);
+      case 16: return run_evict<-2>(p, items, st);
+      case 32: return run_evict<-4>(p, items, st);
+      case 64: return run_evict<-8>(p, items, st);
+      case 128: return run_evict<-16>(p, items, st);
+      default: return run_evict<0>(p, items, st);
+    }
+  }
   switch (dh) {
     case 16: return run_evict<16>(p, items, st);
     case 32: return run_evict<32>(p, items, st);
