@@ -317,9 +317,9 @@ __global__ void __launch_bounds__(kDecThreads, D == 128 ? 3 : (D >= 32 ? 4 : 5))
   griddep_wait();
   // one round trip: the length, the first pages, the heads
   const Heads hd = cache_heads(p, head_cache, pos_cache, s, 1);
-  int ids = fetch_pages<D, B>(p, seq, first, stride, lane);
+  int ids = fetch_pages<Sh::SUB>(p, seq, first, stride, lane);
   const int len = clamped_len(p, p.len[seq]), tiles = (len + Sh::TILE - 1) / Sh::TILE;
-  ids = check_pages<D, B>(p, ids, len - 1, first, stride, lane);
+  ids = check_pages<Sh::SUB>(p, ids, len - 1, first, stride, lane);
   wait_copies();
   const long long k_at = at_k<D, B>(p, pos, g, t), v_at = at_v<D, B>(p, pos, g, t);
   constexpr int AHEAD = 32 / Sh::SUB;
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 128 ? 3 : (D >= 32 ? 4 : 5))
     tile_scores<D, B>(sc, x, q, scale);
     if (more) {
       if (++n == AHEAD) {
-        ids = check_pages<D, B>(p, fetch_pages<D, B>(p, seq, tile + stride, stride, lane), len - 1, tile + stride, stride, lane);
+        ids = check_pages<Sh::SUB>(p, fetch_pages<Sh::SUB>(p, seq, tile + stride, stride, lane), len - 1, tile + stride, stride, lane);
         n = 0;
       }
       load_k<D, B>(x, p, ids, n, next0, len - 1, pos, k_at, lane);
@@ -459,28 +459,6 @@ struct Ring {
   alignas(16) uint64_t full[kRing<D>];           // 2 SUB arrivals: of every step, its bytes to expect and its scales
 };
 
-template <int W>
-__device__ inline void take_words(uint32_t (&r)[W], const uint8_t* a) {
-  if constexpr (W == 4) {
-    const uint4 v = *reinterpret_cast<const uint4*>(a);
-    r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
-  } else if constexpr (W == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(a);
-    r[0] = v.x; r[1] = v.y;
-  } else {
-    r[0] = *reinterpret_cast<const uint32_t*>(a);
-  }
-}
-template <int D>
-__device__ inline void take_keys(Tile<D, 1>& x, const uint8_t* k, int g, int t) {
-  using Sh = Shape<D, 1>;
-#pragma unroll
-  for (int s = 0; s < Sh::SUB; ++s)
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-      for (int c = 0; c < Sh::KCH; ++c) take_words<Sh::KW>(x.k[s][r][c], k + (16 * s + 8 * r + g) * D + 4 * Sh::KW * (4 * c + t));
-}
 template <int D>
 __device__ inline void take_values(Tile<D, 1>& x, const uint8_t* v, int g, int t) {
   using Sh = Shape<D, 1>;
@@ -685,11 +663,11 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     bool at_more = false, live = false;
     int tile = now.t0, n = 0, head_ids = 0, to = 0;
     long long from = 0, scale_from = 0;
-    int next_ids = fetch_pages<D, B>(p, now.seq, now.t0, 1, lane);
+    int next_ids = fetch_pages<Sh::SUB>(p, now.seq, now.t0, 1, lane);
     auto window = [&](int ids) {                     // the page ids of the AHEAD tiles from `tile` on have come
-      ids = check_pages<D, B>(p, ids, at.len - 1, tile, 1, lane);
-      next_ids = fetch_pages<D, B>(p, at.seq, tile + AHEAD, 1, lane);
-      const int key = (int)step_key<D, B>(tile, 1, lane), in_page = key & ((1 << p.page_shift) - 1);
+      ids = check_pages<Sh::SUB>(p, ids, at.len - 1, tile, 1, lane);
+      next_ids = fetch_pages<Sh::SUB>(p, at.seq, tile + AHEAD, 1, lane);
+      const int key = (int)step_key<Sh::SUB>(tile, 1, lane), in_page = key & ((1 << p.page_shift) - 1);
       live = key < at.len;
       from = ids * p.page_stride + (((long long)at.pos << p.page_shift) + in_page) * D;
       scale_from = (((long long)ids * p.kv_max + at.pos) << (p.page_shift - 4)) + (in_page >> 4);
@@ -700,7 +678,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
       if (at_more) {
         behind = following(at);
         behind.t1 = (int)min((uint32_t)behind.nt, at_left - kItemCost<B>);
-        head_ids = fetch_pages<D, B>(p, behind.seq, 0, 1, lane);
+        head_ids = fetch_pages<Sh::SUB>(p, behind.seq, 0, 1, lane);
       }
     };
     auto fill = [&] {                                // a group of copies, empty behind the last tile
@@ -770,7 +748,8 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
           float sc[Sh::SUB][4];
 #pragma unroll
           for (int s = 0; s < Sh::SUB; ++s) scale.of[s] = ring8.scale[slot][s];
-          take_keys<D>(x, ring8.tile[slot].k, g, t);
+#pragma unroll
+          for (int s = 0; s < Sh::SUB; ++s) take_keys<D, B>(x.k[s], ring8.tile[slot].k + 16 * D * s, g, t);
           tile_scores<D, B>(sc, x, q, scale);
           take_values<D>(x, ring8.tile[slot].v, g, t);
           tile_values<D, B>(st, sc, x, scale, p.scale_log2, i * Sh::TILE, now.len, g, t);
@@ -795,13 +774,13 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
   const Scales<D, B> none{};
   Stage<D, B>* stages = reinterpret_cast<Stage<D, B>*>(ring) + 2 * warp;
   Tile<D, B> x;
-  int ids = fetch_pages<D, B>(p, now.seq, now.t0, 1, lane);
-  int next_ids = fetch_pages<D, B>(p, now.seq, now.t0 + AHEAD, 1, lane);     // unchecked until it becomes `ids`
+  int ids = fetch_pages<Sh::SUB>(p, now.seq, now.t0, 1, lane);
+  int next_ids = fetch_pages<Sh::SUB>(p, now.seq, now.t0 + AHEAD, 1, lane);     // unchecked until it becomes `ids`
   int n = 0;                                        // number of the loaded tile in its window of page ids
   int buf = 0, stage = 0;
   find_heads(p, hd, now.s, now.pos, now.rt, lane, cols[warp][0]);
   prefetch_q<D, B>(qbuf[warp], p, now.seq, cols[warp][0][g], lane);
-  ids = check_pages<D, B>(p, ids, now.len - 1, now.t0, 1, lane);
+  ids = check_pages<Sh::SUB>(p, ids, now.len - 1, now.t0, 1, lane);
   if (now.len > 0) {
     if constexpr (STAGED) stage_k<D, B>(stages[0], p, ids, 0, now.t0 * Sh::TILE, now.len - 1, at_k<D, B>(p, now.pos, g, t), lane);
     else load_k<D, B>(x, p, ids, 0, now.t0 * Sh::TILE, now.len - 1, now.pos, at_k<D, B>(p, now.pos, g, t), lane);
@@ -825,7 +804,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     if (more) {
       next = following(now);
       next.t1 = (int)min((uint32_t)next.nt, left - kItemCost<B>);
-      head_ids = fetch_pages<D, B>(p, next.seq, 0, 1, lane);
+      head_ids = fetch_pages<Sh::SUB>(p, next.seq, 0, 1, lane);
       find_heads(p, hd, next.s, next.pos, next.rt, lane, cols[warp][buf ^ 1]);
       prefetch_q<D, B>(qbuf[warp], p, next.seq, cols[warp][buf ^ 1][g], lane);          // complete with the next tile's keys
     }
@@ -838,13 +817,13 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
       const bool load = (inside || more) && last_key >= 0;
       if (inside) {
         if (++n == AHEAD) {
-          ids = check_pages<D, B>(p, next_ids, now.len - 1, tile + 1, 1, lane);
-          next_ids = fetch_pages<D, B>(p, now.seq, tile + 1 + AHEAD, 1, lane);
+          ids = check_pages<Sh::SUB>(p, next_ids, now.len - 1, tile + 1, 1, lane);
+          next_ids = fetch_pages<Sh::SUB>(p, now.seq, tile + 1 + AHEAD, 1, lane);
           n = 0;
         }
       } else {
-        ids = check_pages<D, B>(p, head_ids, more ? next.len - 1 : -1, 0, 1, lane);
-        next_ids = fetch_pages<D, B>(p, next.seq, AHEAD, 1, lane);
+        ids = check_pages<Sh::SUB>(p, head_ids, more ? next.len - 1 : -1, 0, 1, lane);
+        next_ids = fetch_pages<Sh::SUB>(p, next.seq, AHEAD, 1, lane);
         n = 0;
       }
       float sc[Sh::SUB][4];

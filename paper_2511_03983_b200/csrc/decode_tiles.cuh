@@ -124,20 +124,19 @@ struct Tile {
 // Page ids of coming tiles, fetched ahead, one 16-key step per lane, so that no key waits for its page entry: lane l gets
 // the entry of step l % SUB of the tile `tile0 + (l / SUB) * stride`.  The read stays inside the sequence's row of the
 // table whatever its length is, so it need not wait for that.
-template <int D, int B>
+template <int SUB>
 __device__ inline uint32_t step_key(int tile0, int stride, int lane) {
-  constexpr int SUB = Shape<D, B>::SUB;
-  return ((uint32_t)tile0 + (uint32_t)(lane / SUB) * stride) * Shape<D, B>::TILE + 16 * (lane % SUB);
+  return ((uint32_t)tile0 + (uint32_t)(lane / SUB) * stride) * (16 * SUB) + 16 * (lane % SUB);
 }
-template <int D, int B>
+template <int SUB>
 __device__ inline int fetch_pages(const DecParams& p, long long seq, int tile0, int stride, int lane) {
-  return p.table[seq * p.max_pages + min(step_key<D, B>(tile0, stride, lane) >> p.page_shift, (uint32_t)p.max_pages - 1)];
+  return p.table[seq * p.max_pages + min(step_key<SUB>(tile0, stride, lane) >> p.page_shift, (uint32_t)p.max_pages - 1)];
 }
 // Before use: an entry outside the pool is replaced by page 0, and reported if a key of the sequence needs it.
-template <int D, int B>
+template <int SUB>
 __device__ inline int check_pages(const DecParams& p, int id, int last_key, int tile0, int stride, int lane) {
   if ((unsigned)id >= (unsigned)p.n_pages) {
-    if (last_key >= 0 && step_key<D, B>(tile0, stride, lane) <= (uint32_t)last_key) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
+    if (last_key >= 0 && step_key<SUB>(tile0, stride, lane) <= (uint32_t)last_key) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
     id = 0;
   }
   return id;
@@ -279,6 +278,28 @@ __device__ inline void take_v(Tile<D, B>& x, const Stage<D, B>& y, int lane) {
         for (int w = 0; w < Sh::VW; ++w) x.v[s][r][c][w] = y.v[s][r][c][lane][w];
 }
 
+template <int W>
+__device__ inline void take_words(uint32_t (&r)[W], const uint8_t* a) {
+  if constexpr (W == 4) {
+    const uint4 v = *reinterpret_cast<const uint4*>(a);
+    r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
+  } else if constexpr (W == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(a);
+    r[0] = v.x; r[1] = v.y;
+  } else {
+    r[0] = *reinterpret_cast<const uint32_t*>(a);
+  }
+}
+// 16 keys whose rows lie one behind another in shared memory.
+template <int D, int B>
+__device__ inline void take_keys(uint32_t (&x)[2][Shape<D, B>::KCH][Shape<D, B>::KW], const uint8_t* k, int g, int t) {
+  using Sh = Shape<D, B>;
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < Sh::KCH; ++c) take_words<Sh::KW>(x[r][c], k + (8 * r + g) * D * B + 4 * Sh::KW * (4 * c + t));
+}
+
 // Where a CTA finds the index data of the heads: in shared memory where it fits, copied with the first loads of the kernel.
 struct Heads {
   const int32_t* idx;         // [S][heads] or null
@@ -411,39 +432,40 @@ __device__ inline Scales<D, B> gather_scales(const Tile<D, B>& x) {
   return r;
 }
 
-// Scores q . k of a tile: thread (g, t) has keys g, g + 8 of each 16 and heads 2t, 2t + 1.
+// Scores q . k of 16 keys: thread (g, t) has keys g, g + 8 and heads 2t, 2t + 1.
 template <int D, int B>
-__device__ inline void tile_scores(float (&sc)[Shape<D, B>::SUB][4], const Tile<D, B>& x, const Query<D, B>& q, const Scales<D, B>& scale) {
+__device__ inline void step_scores(float (&sc)[4], const uint32_t (&k)[2][Shape<D, B>::KCH][Shape<D, B>::KW], const Query<D, B>& q, float scale) {
   using Sh = Shape<D, B>;
 #pragma unroll
-  for (int s = 0; s < Sh::SUB; ++s) {
+  for (int e = 0; e < 4; ++e) sc[e] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sc[s][e] = 0.f;
-#pragma unroll
-    for (int c = 0; c < Sh::KCH; ++c) {
-      if constexpr (B == 1) {
-#pragma unroll
-        for (int w = 0; w < Sh::KW; ++w) {
-          uint32_t a0, a1, a2, a3;
-          widen(x.k[s][0][c][w], a0, a2);
-          widen(x.k[s][1][c][w], a1, a3);
-          mma16816_f16(sc[s], a0, a1, a2, a3, q.w[c][2 * w], q.w[c][2 * w + 1]);
-        }
-      } else if constexpr (Sh::KW == 4) {
-#pragma unroll
-        for (int h = 0; h < 4; h += 2)
-          mma16816(sc[s], x.k[s][0][c][h], x.k[s][1][c][h], x.k[s][0][c][h + 1], x.k[s][1][c][h + 1], q.w[c][h], q.w[c][h + 1]);
-      } else if constexpr (Sh::KW == 2) {
-        mma16816(sc[s], x.k[s][0][c][0], x.k[s][1][c][0], x.k[s][0][c][1], x.k[s][1][c][1], q.w[c][0], q.w[c][1]);
-      } else {
-        mma16816(sc[s], x.k[s][0][c][0], x.k[s][1][c][0], 0u, 0u, q.w[c][0], 0u);
-      }
-    }
+  for (int c = 0; c < Sh::KCH; ++c) {
     if constexpr (B == 1) {
-      const float f0 = scale.of[s].x * q.f0, f1 = scale.of[s].x * q.f1;
-      sc[s][0] *= f0; sc[s][1] *= f1; sc[s][2] *= f0; sc[s][3] *= f1;
+#pragma unroll
+      for (int w = 0; w < Sh::KW; ++w) {
+        uint32_t a0, a1, a2, a3;
+        widen(k[0][c][w], a0, a2);
+        widen(k[1][c][w], a1, a3);
+        mma16816_f16(sc, a0, a1, a2, a3, q.w[c][2 * w], q.w[c][2 * w + 1]);
+      }
+    } else if constexpr (Sh::KW == 4) {
+#pragma unroll
+      for (int h = 0; h < 4; h += 2) mma16816(sc, k[0][c][h], k[1][c][h], k[0][c][h + 1], k[1][c][h + 1], q.w[c][h], q.w[c][h + 1]);
+    } else if constexpr (Sh::KW == 2) {
+      mma16816(sc, k[0][c][0], k[1][c][0], k[0][c][1], k[1][c][1], q.w[c][0], q.w[c][1]);
+    } else {
+      mma16816(sc, k[0][c][0], k[1][c][0], 0u, 0u, q.w[c][0], 0u);
     }
   }
+  if constexpr (B == 1) {
+    const float f0 = scale * q.f0, f1 = scale * q.f1;
+    sc[0] *= f0; sc[1] *= f1; sc[2] *= f0; sc[3] *= f1;
+  }
+}
+template <int D, int B>
+__device__ inline void tile_scores(float (&sc)[Shape<D, B>::SUB][4], const Tile<D, B>& x, const Query<D, B>& q, const Scales<D, B>& scale) {
+#pragma unroll
+  for (int s = 0; s < Shape<D, B>::SUB; ++s) step_scores<D, B>(sc[s], x.k[s], q, B == 1 ? scale.of[B == 1 ? s : 0].x : 1.f);
 }
 
 __device__ inline int clamped_len(const DecParams& p, int n) {
