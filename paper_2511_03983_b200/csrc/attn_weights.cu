@@ -27,14 +27,14 @@ struct WeightParams {
   float scale;                 // 1 / sqrt(d)
 };
 
-constexpr int kLenCache = 512, kCountCache = 256, kMaxRun = 64;
+constexpr int kLenCache = 512, kCountCache = 256, kMaxRun = 16;
 
 // exp(score * scale - lse).  The difference is formed before it is multiplied: it is small where the weight is not.
 __device__ inline float weight_of(float score, float scale, float lse) { return ex2(fmaf(score, scale, -lse) * kLog2e); }
 
 // A warp's ring of two tiles of SUB * 16 keys, filled by bulk copies: the 16 rows of a step lie next to each other in their page,
 // and so do their prior weights.  Tiles of up to 4 KB and 16 warps an SM.  Measured (eight subnets of 16 ragged sequences of up to
-// 8192 keys, e4m3, d = 128, 630 MB: 132 us; 64 ragged sequences of up to 16000, 32 heads on 4 positions of d = 64, 152 MB: 50):
+// 8192 keys, e4m3, d = 128, 630 MB: 132 us; 64 ragged sequences of up to 16000, 32 heads on 4 positions of d = 64, 152 MB: 53):
 // three tiles 157 and 64, d = 128 by 4 steps 155; keys straight into registers 180 and 84 to 105, 16 keys (32 at d = 64) at a
 // time through rings 181 and 75: what a tile costs beside its keys has to be spread over many of them.
 constexpr int kRing = 2;
@@ -285,8 +285,8 @@ int run_weights(WeightParams& w, long long max_len, cudaStream_t st) {
   }
   const long long warps = (long long)sm_count() * resident[slot] * kDecWarps;
   const long long tiles = (max_len + KeyRing<D, B>::TILE - 1) / KeyRing<D, B>::TILE;
-  // One run a warp, but not so long that ragged lengths leave warps idle (runs of half the length, 256 ragged items of up to 2048
-  // keys: 12.2 us against 10.7).
+  // One run a warp, but not so long that ragged lengths leave warps idle (twice as many runs, 256 ragged items of up to 2048 keys:
+  // 12.2 us against 10.7; runs of up to 64 tiles, the first of the cases above: 156).
   const long long run_tiles = (tiles * items + warps - 1) / warps;
   w.run_tiles = (int)(run_tiles < kMaxRun ? run_tiles : kMaxRun);
   // every slot that the table has is in a run: the bound only chooses how long they are

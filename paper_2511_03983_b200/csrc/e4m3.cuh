@@ -26,6 +26,13 @@ __device__ inline uint32_t narrow2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// The same for values that are finite.
+__device__ inline uint32_t narrow4_finite(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+      : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
 __device__ inline uint32_t narrow4(float a, float b, float c, float d) { return narrow2(a, b) | (narrow2(c, d) << 16); }
 
 // Four e4m3 numbers (exact).

@@ -150,93 +150,91 @@ __device__ inline void spread(float (&x)[8], const uint4& v) {
   for (int i = 0; i < 4; ++i) { x[2 * i] = bf_lo(w[i]); x[2 * i + 1] = bf_hi(w[i]); }
 }
 
+#ifndef AP64
+#define AP64 3
+#define AP128 2
+#endif
 enum { MODE_HALF = 0, MODE_PAIRS = 1, MODE_SLOW_HALF = 2, MODE_SLOW_PAIRS = 3 };
 
 // 16 rows of a head: lane's item i is the eight elements from 8 * c on of row r, c = (32 i + lane) % (D / 8).
 template <int D>
 struct Rows {
   static constexpr int CHUNKS = D / 8, ITEMS = D / 16;
-  float x[ITEMS][8];
 };
 
-template <int D, int MODE>
-__device__ inline void load_rows(Rows<D>& y, const AppendParams& p, const __nv_bfloat16* src, const float2* table, int count, bool turn, int lane) {
-  using R = Rows<D>;
-  constexpr bool SLOW = MODE == MODE_SLOW_HALF || MODE == MODE_SLOW_PAIRS;
-  uint4 own[R::ITEMS], other[R::ITEMS];
+// Eight elements of row r's head, rotated where the head is: `own` holds them.  other: the eight that they are paired with, half a
+// rotation away (MODE_HALF).
+template <int MODE>
+__device__ inline void rotate(float (&x)[8], const AppendParams& p, const uint4& own, const uint4& other, const __nv_bfloat16* row, const float2* cs, int c) {
+  spread(x, own);
+  if (8 * c >= p.rot) return;
+  if constexpr (MODE == MODE_HALF) {
+    float z[8];
+    spread(z, other);
+    const bool low = 8 * c < p.half;
+    const float4* at = reinterpret_cast<const float4*>(cs + (low ? 8 * c : 8 * c - p.half));
+    const float sign = low ? -1.f : 1.f;
 #pragma unroll
-  for (int i = 0; i < R::ITEMS; ++i) {
-    const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
-    if (r < count) {
-      own[i] = *reinterpret_cast<const uint4*>(src + (long long)r * p.width + 8 * c);
-      if (MODE == MODE_HALF && turn && 8 * c < p.rot)
-        other[i] = *reinterpret_cast<const uint4*>(src + (long long)r * p.width + (8 * c < p.half ? 8 * c + p.half : 8 * c - p.half));
+    for (int e = 0; e < 8; e += 2) {
+      const float4 a = at[e / 2];                     // (cos, sin) of two pairs
+      x[e] = fmaf(sign * z[e], a.y, x[e] * a.x);
+      x[e + 1] = fmaf(sign * z[e + 1], a.w, x[e + 1] * a.z);
     }
-  }
+  } else if constexpr (MODE == MODE_PAIRS) {
+    const float4* at = reinterpret_cast<const float4*>(cs + 4 * c);
 #pragma unroll
-  for (int i = 0; i < R::ITEMS; ++i) {
-    const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
-    float (&x)[8] = y.x[i];
-    if (r >= count) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
-      continue;
+    for (int e = 0; e < 8; e += 4) {
+      const float4 a = at[e / 4];
+      const float u = x[e], v = x[e + 1], y = x[e + 2], z = x[e + 3];
+      x[e] = u * a.x - v * a.y;
+      x[e + 1] = u * a.y + v * a.x;
+      x[e + 2] = y * a.z - z * a.w;
+      x[e + 3] = y * a.w + z * a.z;
     }
-    spread(x, own[i]);
-    if (!turn || 8 * c >= p.rot) continue;
-    const float2* cs = table + r * p.half;
-    if constexpr (MODE == MODE_HALF) {
-      float z[8];
-      spread(z, other[i]);
-      const bool low = 8 * c < p.half;
-      const float2* at = cs + (low ? 8 * c : 8 * c - p.half);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = low ? x[e] * at[e].x - z[e] * at[e].y : z[e] * at[e].y + x[e] * at[e].x;
-    } else if constexpr (MODE == MODE_PAIRS) {
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float2 a = cs[4 * c + e / 2];
-        const float u = x[e], v = x[e + 1];
-        x[e] = u * a.x - v * a.y;
-        x[e + 1] = u * a.y + v * a.x;
-      }
-    } else if constexpr (SLOW) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int el = 8 * c + e;
-        if (el < p.rot) {
-          const bool low = MODE == MODE_SLOW_HALF ? el < p.half : el % 2 == 0;
-          const int pair = MODE == MODE_SLOW_HALF ? (low ? el : el - p.half) : el / 2;
-          const int mate = MODE == MODE_SLOW_HALF ? (low ? el + p.half : el - p.half) : el ^ 1;
-          const float z = __bfloat162float(src[(long long)r * p.width + mate]);
-          const float2 a = cs[pair];
-          x[e] = low ? x[e] * a.x - z * a.y : z * a.y + x[e] * a.x;
-        }
-      }
-    }
-  }
-  __syncwarp();                                       // the rows have been read: now they may be written
-}
-
-// The rows as numbers of a block: `cache` is the block's first row, `scale` its scale.
-template <int D>
-__device__ inline void store_block(const Rows<D>& y, uint8_t* cache, float* scale, const Run& run, int lane) {
-  using R = Rows<D>;
-  const float old = run.first > 0 ? *scale : 0.f;
-  float top = 0.f;
-#pragma unroll
-  for (int i = 0; i < R::ITEMS; ++i)
+  } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float a = fabsf(y.x[i][e]);
-      top = fmaxf(top, a < INFINITY ? a : 0.f);
+      const int el = 8 * c + e;
+      if (el < p.rot) {
+        const bool low = MODE == MODE_SLOW_HALF ? el < p.half : el % 2 == 0;
+        const int pair = MODE == MODE_SLOW_HALF ? (low ? el : el - p.half) : el / 2;
+        const int mate = MODE == MODE_SLOW_HALF ? (low ? el + p.half : el - p.half) : el ^ 1;
+        const float z = __bfloat162float(row[mate]);
+        const float2 a = cs[pair];
+        x[e] = low ? x[e] * a.x - z * a.y : z * a.y + x[e] * a.x;
+      }
     }
-  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+  }
+}
+
+__device__ inline uint4 pack_bf16x8(const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+    w[e] = *reinterpret_cast<const uint32_t*>(&t);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Eight values as numbers.  FINITE: all of them are.
+template <bool FINITE>
+__device__ inline uint2 numbers(const float (&x)[8], float inv) {
+  if constexpr (FINITE) {
+    return make_uint2(narrow4_finite(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), narrow4_finite(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+  } else {
+    return make_uint2(narrow4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), narrow4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+  }
+}
+constexpr uint32_t kInfinity = 0x7f800000u;
+
+// The scale of a block from the largest magnitude of its new tokens, and the tokens that it holds rounded to it.  `lanes` lanes
+// take part, this one is number `lane` of them.
+template <int D>
+__device__ inline float rescale(uint8_t* cache, float* scale, float old, float top, int first, int lane, int lanes) {
   const float now = fmaxf(scale_for(top), old);       // a NaN for an old scale counts for nothing
-  const float inv = inverse_scale(now);
-  if (run.first > 0 && now != old) {                  // the tokens that the block holds, rounded to the new scale
-    const float f = old * inv;
-    for (int k = lane; k < run.first * D / 8; k += 32) {
+  if (first > 0 && now != old) {
+    const float f = old * inverse_scale(now);
+    for (int k = lane; k < first * D / 8; k += lanes) {
       uint2* at = reinterpret_cast<uint2*>(cache) + k;
       const uint2 v = *at;
       uint32_t w[2] = {v.x, v.y};
@@ -249,22 +247,27 @@ __device__ inline void store_block(const Rows<D>& y, uint8_t* cache, float* scal
       *at = make_uint2(w[0], w[1]);
     }
   }
-#pragma unroll
-  for (int i = 0; i < R::ITEMS; ++i) {
-    const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
-    const float (&x)[8] = y.x[i];
-    if (r < run.count)
-      *reinterpret_cast<uint2*>(cache + (run.first + r) * D + 8 * c) =
-          make_uint2(narrow4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), narrow4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
-  }
   if (lane == 0) *scale = now;
+  return now;
+}
+
+// Positions first .. of `count` rows as (cos, sin).
+__device__ inline void fill_table(const AppendParams& p, float2* table, int pos, int count) {
+  for (int k = threadIdx.x; k < count * p.half; k += blockDim.x) {
+    const int r = k / p.half, j = k - r * p.half;
+    double turns = (double)(pos + r) * (p.inv_freq[j] * kInvTwoPi);
+    turns -= rint(turns);
+    float s, c;
+    sincospif(2.0f * (float)turns, &s, &c);
+    table[k] = make_float2(c, s);
+  }
 }
 
 template <int D, int MODE>
-__global__ void __launch_bounds__(kAppThreads, D == 128 ? 2 : 3) append_q8_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kAppThreads, D == 128 ? AP128 : D == 64 ? AP64 : 3) append_q8_kernel(const AppendParams p) {
   using R = Rows<D>;
   __shared__ Run shared;
-  extern __shared__ float2 table[];                   // [16][half]
+  extern __shared__ __align__(16) float2 table[];     // [16][half]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   griddep_launch_dependents();
   griddep_wait();
@@ -275,45 +278,206 @@ __global__ void __launch_bounds__(kAppThreads, D == 128 ? 2 : 3) append_q8_kerne
   __syncthreads();
   const Run run = shared;
   if (run.count == 0) return;
-  for (int k = threadIdx.x; k < run.count * p.half; k += kAppThreads) {
-    const int r = k / p.half, j = k - r * p.half;
-    double turns = (double)(run.pos + r) * (p.inv_freq[j] * kInvTwoPi);
-    turns -= rint(turns);
-    float s, c;
-    sincospif(2.0f * (float)turns, &s, &c);
-    table[k] = make_float2(c, s);
-  }
-  __syncthreads();
   const __nv_bfloat16* rows = p.in + run.row * p.width;
-  // heads in the order K, V, Q
-  for (int u = warp; u < 2 * p.kv + (p.q_out ? p.heads : 0); u += kAppWarps) {
-    Rows<D> y;
-    if (u < 2 * p.kv) {
-      const bool is_k = u < p.kv;
-      const int group = is_k ? u : u - p.kv;
-      if (group >= run.held) continue;
-      load_rows<D, MODE>(y, p, rows + (p.heads + u) * D, table, run.count, is_k, lane);
-      store_block<D>(y, (is_k ? p.k_cache : p.v_cache) + run.page * p.page_stride + (((long long)group << p.page_shift) + run.in_page) * D,
-                     p.scales + 2 * (((run.page * p.kv + group) << (p.page_shift - 4)) + (run.in_page >> 4)) + !is_k, run, lane);
-    } else {
-      const int h = u - 2 * p.kv;
-      load_rows<D, MODE>(y, p, rows + h * D, table, run.count, true, lane);
-      __nv_bfloat16* out = p.q_out + run.row * p.q_stride + h * D;
+  const int units = 2 * p.kv + (p.q_out ? p.heads : 0);
+  // heads in the order K, V, Q; the first one's rows travel while the table is filled, the next one's while one is worked on
+  auto column = [&](int u) { return (u < 2 * p.kv ? p.heads + u : u - 2 * p.kv) * D; };
+  auto load = [&](uint4 (&own)[R::ITEMS], int u) {
+#pragma unroll
+    for (int i = 0; i < R::ITEMS; ++i) {
+      const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+      own[i] = make_uint4(0, 0, 0, 0);
+      if (r < run.count) own[i] = *reinterpret_cast<const uint4*>(rows + (r * p.width + column(u) + 8 * c));
+    }
+  };
+  uint4 own[R::ITEMS];
+  if (warp < units) load(own, warp);
+  fill_table(p, table, run.pos, run.count);
+  __syncthreads();
+#pragma unroll 1
+  for (int u = warp; u < units; u += kAppWarps) {
+    uint4 next[R::ITEMS];
+    const bool is_q = u >= 2 * p.kv, is_k = u < p.kv;
+    const int group = is_q ? -1 : (is_k ? u : u - p.kv);
+    // what the elements are paired with: the lanes that own it have just read it
+    uint4 other[MODE == MODE_HALF ? R::ITEMS : 1];
+    if (MODE == MODE_HALF && (is_q || is_k)) {
 #pragma unroll
       for (int i = 0; i < R::ITEMS; ++i) {
         const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
-        const float (&x)[8] = y.x[i];
-        if (r < run.count) {
-          uint32_t w[4];
+        if (r < run.count && 8 * c < p.rot)
+          other[i] = *reinterpret_cast<const uint4*>(rows + (r * p.width + column(u) + (8 * c < p.half ? 8 * c + p.half : 8 * c - p.half)));
+      }
+    }
+    if (u + kAppWarps < units) load(next, u + kAppWarps);
+    __syncwarp();                                     // the head's rows have been read: now they may be written
+    if (is_q) {
+      __nv_bfloat16* out = p.q_out + run.row * p.q_stride + (u - 2 * p.kv) * D;
+      if (MODE == MODE_SLOW_HALF || MODE == MODE_SLOW_PAIRS) {
+        uint4 y[R::ITEMS];                            // reads its rows once more
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
-            w[e] = *reinterpret_cast<const uint32_t*>(&t);
+        for (int i = 0; i < R::ITEMS; ++i) {
+          const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+          float x[8];
+          if (r < run.count) {
+            rotate<MODE>(x, p, own[i], own[i], rows + r * p.width + column(u), table + r * p.half, c);
+            y[i] = pack_bf16x8(x);
           }
-          *reinterpret_cast<uint4*>(out + r * p.q_stride + 8 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < R::ITEMS; ++i) {
+          const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+          if (r < run.count) *reinterpret_cast<uint4*>(out + r * p.q_stride + 8 * c) = y[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < R::ITEMS; ++i) {
+          const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+          float x[8];
+          if (r < run.count) {
+            rotate<MODE>(x, p, own[i], other[MODE == MODE_HALF ? i : 0], nullptr, table + r * p.half, c);
+            *reinterpret_cast<uint4*>(out + r * p.q_stride + 8 * c) = pack_bf16x8(x);
+          }
+        }
+      }
+    } else if (group < run.held) {
+      uint8_t* cache = (is_k ? p.k_cache : p.v_cache) + run.page * p.page_stride + (((long long)group << p.page_shift) + run.in_page) * D;
+      float* scale = p.scales + 2 * (((run.page * p.kv + group) << (p.page_shift - 4)) + (run.in_page >> 4)) + !is_k;
+      const float old = run.first > 0 ? *scale : 0.f;
+      uint8_t* to = cache + run.first * D;
+      if (is_k) {
+        float x[R::ITEMS][8];
+        uint32_t top = 0;                             // of the magnitudes' bits, which order as the magnitudes do
+#pragma unroll
+        for (int i = 0; i < R::ITEMS; ++i) {
+          const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
+          if (r < run.count) rotate<MODE>(x[i], p, own[i], other[MODE == MODE_HALF ? i : 0], rows + r * p.width + column(u), table + r * p.half, c);
+          else spread(x[i], own[i]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[i][e]) & 0x7fffffffu);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        const bool finite = top < kInfinity;
+        if (!finite) {                                // once more without what is not
+          float m = 0.f;
+#pragma unroll
+          for (int i = 0; i < R::ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[i][e]) < INFINITY ? fabsf(x[i][e]) : 0.f);
+          top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+        }
+        const float inv = inverse_scale(rescale<D>(cache, scale, old, __uint_as_float(top), run.first, lane, 32));
+#pragma unroll
+        for (int i = 0; i < R::ITEMS; ++i) {
+          const int k = 32 * i + lane, r = k / R::CHUNKS;
+          if (r < run.count) *reinterpret_cast<uint2*>(to + 8 * k) = finite ? numbers<true>(x[i], inv) : numbers<false>(x[i], inv);
+        }
+      } else {
+        uint32_t both = 0;                            // two bf16 magnitudes
+#pragma unroll
+        for (int i = 0; i < R::ITEMS; ++i) {
+          both = __vmaxu2(both, own[i].x & 0x7fff7fffu);
+          both = __vmaxu2(both, own[i].y & 0x7fff7fffu);
+          both = __vmaxu2(both, own[i].z & 0x7fff7fffu);
+          both = __vmaxu2(both, own[i].w & 0x7fff7fffu);
+        }
+        uint32_t top = __reduce_max_sync(0xffffffffu, max(both << 16, both & 0xffff0000u));
+        const bool finite = top < kInfinity;
+        if (!finite) {
+          float m = 0.f;
+#pragma unroll
+          for (int i = 0; i < R::ITEMS; ++i) {
+            float x[8];
+            spread(x, own[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.f);
+          }
+          top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+        }
+        const float inv = inverse_scale(rescale<D>(cache, scale, old, __uint_as_float(top), run.first, lane, 32));
+#pragma unroll
+        for (int i = 0; i < R::ITEMS; ++i) {
+          const int k = 32 * i + lane, r = k / R::CHUNKS;
+          float x[8];
+          spread(x, own[i]);
+          if (r < run.count) *reinterpret_cast<uint2*>(to + 8 * k) = finite ? numbers<true>(x, inv) : numbers<false>(x, inv);
         }
       }
     }
+#pragma unroll
+    for (int i = 0; i < R::ITEMS; ++i) own[i] = next[i];
+  }
+}
+
+// One token of every sequence: a CTA a token, D / 8 lanes a head, all heads at once.  Everything that does not hang on the page
+// -- the row, the frequencies, the lengths -- is read in one round trip.
+template <int D, int MODE>
+__global__ void __launch_bounds__(kAppThreads) append_one_q8_kernel(const AppendParams p) {
+  constexpr int LANES = D / 8, HEADS = 32 / LANES;    // of a head; of a warp
+  __shared__ __align__(16) float2 table[D / 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LANES;
+  const int seq = blockIdx.x, s = seq / p.n_seqs, warps = blockDim.x >> 5;
+  griddep_launch_dependents();
+  griddep_wait();
+  const __nv_bfloat16* row = p.in + (long long)seq * p.width;
+  const int units = 2 * p.kv + (p.q_out ? p.heads : 0);
+  auto column = [&](int u) { return (u < 2 * p.kv ? p.heads + u : u - 2 * p.kv) * D; };
+  int u = warp * HEADS + lane / LANES;
+  uint4 own = make_uint4(0, 0, 0, 0);
+  if (u < units) own = *reinterpret_cast<const uint4*>(row + column(u) + 8 * c);
+  const int n = p.new_len ? p.new_len[seq] : 1, len = p.kv_len[seq], seen = p.seen ? p.seen[seq] : len;
+  const int held = p.kv_count ? max(0, min(p.kv, p.kv_count[s])) : p.kv;
+  bool bad = false;
+  if (n < 0 || n > 1) bad = true;
+  else if (blocks_of(p, n, len, seen, bad) == 0 && !bad) return;     // no new token
+  if (bad) {
+    report(p, threadIdx.x == 0);
+    return;
+  }
+  const int slot = len - 1, first = slot & 15;
+  const int page = p.page_table[(long long)seq * p.max_pages + (slot >> p.page_shift)];
+  fill_table(p, table, seen - 1, 1);
+  __syncthreads();
+  if ((unsigned)page >= (unsigned)p.n_pages) {
+    report(p, threadIdx.x == 0);
+    return;
+  }
+  const int in_page = slot & ((1 << p.page_shift) - 1) & ~15;
+#pragma unroll 1
+  for (; __any_sync(0xffffffffu, u < units); u += warps * HEADS) {
+    const bool live = u < units, is_q = u >= 2 * p.kv, is_k = u < p.kv;
+    const int group = is_k ? u : u - p.kv;
+    const __nv_bfloat16* head = row + (live ? column(u) : 0);
+    uint4 other = own;
+    if (MODE == MODE_HALF && live && (is_q || is_k) && 8 * c < p.rot)
+      other = *reinterpret_cast<const uint4*>(head + (8 * c < p.half ? 8 * c + p.half : 8 * c - p.half));
+    const bool stores = live && !is_q && group < held;
+    float* scale = nullptr;
+    uint8_t* cache = nullptr;
+    float old = 0.f;
+    if (stores) {
+      cache = (is_k ? p.k_cache : p.v_cache) + page * p.page_stride + (((long long)group << p.page_shift) + in_page) * D;
+      scale = p.scales + 2 * ((((long long)page * p.kv + group) << (p.page_shift - 4)) + (in_page >> 4)) + !is_k;
+      if (first > 0) old = *scale;
+    }
+    float x[8];
+    if (live && (is_q || is_k)) rotate<MODE>(x, p, own, other, head, table, c);
+    else spread(x, own);
+    __syncwarp();                                     // the head has been read: now it may be written
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.f);
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (live && is_q) {
+      *reinterpret_cast<uint4*>(p.q_out + (long long)seq * p.q_stride + (u - 2 * p.kv) * D + 8 * c) = pack_bf16x8(x);
+    } else if (stores) {
+      const float inv = inverse_scale(rescale<D>(cache, scale, old, top, first, c, LANES));
+      *reinterpret_cast<uint2*>(cache + first * D + 8 * c) = numbers<false>(x, inv);
+    }
+    const int next = u + warps * HEADS;
+    if (next < units) own = *reinterpret_cast<const uint4*>(row + column(next) + 8 * c);
   }
 }
 
@@ -328,6 +492,16 @@ int launch(const AppendParams& p, int S, int layout, cudaStream_t st) {
   if (layout == TWIST_ROPE_HALF) mode = p.half % 8 == 0 ? MODE_HALF : MODE_SLOW_HALF;
   else mode = p.rot % 8 == 0 ? MODE_PAIRS : MODE_SLOW_PAIRS;
   if (p.rot == 0) mode = MODE_PAIRS;
+  if (!p.new_begin && p.rows_per_seq == 1) {
+    // as many warps as take all heads at once, if a CTA may have them
+    const int units = 2 * p.kv + (p.q_out ? p.heads : 0), heads = 256 / D, warps = (units + heads - 1) / heads;
+    void (*kernel)(AppendParams) = mode == MODE_HALF ? append_one_q8_kernel<D, MODE_HALF>
+                                   : mode == MODE_PAIRS ? append_one_q8_kernel<D, MODE_PAIRS>
+                                   : mode == MODE_SLOW_HALF ? append_one_q8_kernel<D, MODE_SLOW_HALF>
+                                                            : append_one_q8_kernel<D, MODE_SLOW_PAIRS>;
+    TWIST_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)(S * p.n_seqs)), dim3(32 * (warps < kAppWarps ? warps : kAppWarps)), 0, st, 1, p));
+    return TWIST_OK;
+  }
   const long long grid = (long long)S * p.per_subnet;
   if (grid > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
   void (*kernel)(AppendParams) = mode == MODE_HALF ? append_q8_kernel<D, MODE_HALF>
@@ -368,6 +542,7 @@ extern "C" int32_t twist_kv_append_q8(const twist_kv_append_q8_args* a, void* st
   AppendParams p;
   memset(&p, 0, sizeof(p));
   const long long rows = (long long)a->n_subnets * a->tokens;
+  if (rows > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
   if (a->q_out && !(a->q_out == a->qkv && (a->q_stride == width || rows == 1)) &&
       overlap(a->qkv, rows * width * 2, a->q_out, ((rows - 1) * a->q_stride + a_sub) * 2))
     return TWIST_ERR_SHAPE;
