@@ -10,9 +10,12 @@
 //
 // A CTA takes the new tokens of one block of one sequence, all heads: the tokens are neighbouring rows at neighbouring
 // positions, so the index data of a CTA is found once, and one table of (cos, sin) serves its heads (angles as in
-// positions.cu: reduced in 64 bits).  A warp takes a head at a time.  Both elements of a pair are read by the lanes
-// that own either of them (the second read hits L1), so that a lane's work is the same in all layouts; rotating in
-// place is safe because a head's rows are read by one warp before it writes any of them.
+// positions.cu: reduced in 64 bits).  A warp takes a head at a time, the rows of its next one on their way, and hands the
+// elements of a pair from lane to lane; rotating in place is safe because a head's rows are read by one warp before it writes
+// any of them.  Magnitudes are compared as integers, which finds what is not finite on the way: only then is every value looked at.
+//
+// One token of every sequence has a kernel of its own: D / 8 lanes a head, all heads at once, and one round trip for everything
+// that does not hang on the page (512 tokens of 16 + 2 * 4 heads of 64: 10.3 us by blocks, 3.6).
 #include "common.cuh"
 #include "e4m3.cuh"
 #include "ptx.cuh"
@@ -150,10 +153,6 @@ __device__ inline void spread(float (&x)[8], const uint4& v) {
   for (int i = 0; i < 4; ++i) { x[2 * i] = bf_lo(w[i]); x[2 * i + 1] = bf_hi(w[i]); }
 }
 
-#ifndef AP64
-#define AP64 3
-#define AP128 2
-#endif
 enum { MODE_HALF = 0, MODE_PAIRS = 1, MODE_SLOW_HALF = 2, MODE_SLOW_PAIRS = 3 };
 
 // 16 rows of a head: lane's item i is the eight elements from 8 * c on of row r, c = (32 i + lane) % (D / 8).
@@ -161,6 +160,17 @@ template <int D>
 struct Rows {
   static constexpr int CHUNKS = D / 8, ITEMS = D / 16;
 };
+
+// Where a row's table of (cos, sin) has pair j.  Lanes that own neighbouring chunks of a head read 16 bytes (two pairs) each at a
+// time: those lie next to each other.
+template <int MODE>
+__device__ inline int pair_at(int j, int half) {
+  if constexpr (MODE == MODE_HALF || MODE == MODE_PAIRS) {
+    constexpr int PER = MODE == MODE_HALF ? 8 : 4;    // pairs of a chunk
+    return 2 * (j % PER / 2 * (half / PER) + j / PER) + j % 2;
+  }
+  return j;
+}
 
 // Eight elements of row r's head, rotated where the head is: `own` holds them.  other: the eight that they are paired with, half a
 // rotation away (MODE_HALF).
@@ -172,19 +182,19 @@ __device__ inline void rotate(float (&x)[8], const AppendParams& p, const uint4&
     float z[8];
     spread(z, other);
     const bool low = 8 * c < p.half;
-    const float4* at = reinterpret_cast<const float4*>(cs + (low ? 8 * c : 8 * c - p.half));
+    const float4* at = reinterpret_cast<const float4*>(cs) + (low ? c : c - p.half / 8);
     const float sign = low ? -1.f : 1.f;
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-      const float4 a = at[e / 2];                     // (cos, sin) of two pairs
+      const float4 a = at[e / 2 * (p.half / 8)];      // (cos, sin) of two pairs
       x[e] = fmaf(sign * z[e], a.y, x[e] * a.x);
       x[e + 1] = fmaf(sign * z[e + 1], a.w, x[e + 1] * a.z);
     }
   } else if constexpr (MODE == MODE_PAIRS) {
-    const float4* at = reinterpret_cast<const float4*>(cs + 4 * c);
+    const float4* at = reinterpret_cast<const float4*>(cs) + c;
 #pragma unroll
     for (int e = 0; e < 8; e += 4) {
-      const float4 a = at[e / 4];
+      const float4 a = at[e / 4 * (p.half / 4)];
       const float u = x[e], v = x[e + 1], y = x[e + 2], z = x[e + 3];
       x[e] = u * a.x - v * a.y;
       x[e + 1] = u * a.y + v * a.x;
@@ -252,6 +262,7 @@ __device__ inline float rescale(uint8_t* cache, float* scale, float old, float t
 }
 
 // Positions first .. of `count` rows as (cos, sin).
+template <int MODE>
 __device__ inline void fill_table(const AppendParams& p, float2* table, int pos, int count) {
   for (int k = threadIdx.x; k < count * p.half; k += blockDim.x) {
     const int r = k / p.half, j = k - r * p.half;
@@ -259,12 +270,12 @@ __device__ inline void fill_table(const AppendParams& p, float2* table, int pos,
     turns -= rint(turns);
     float s, c;
     sincospif(2.0f * (float)turns, &s, &c);
-    table[k] = make_float2(c, s);
+    table[r * p.half + pair_at<MODE>(j, p.half)] = make_float2(c, s);
   }
 }
 
 template <int D, int MODE>
-__global__ void __launch_bounds__(kAppThreads, D == 128 ? AP128 : D == 64 ? AP64 : 3) append_q8_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kAppThreads, D == 128 ? 2 : 3) append_q8_kernel(const AppendParams p) {
   using R = Rows<D>;
   __shared__ Run shared;
   extern __shared__ __align__(16) float2 table[];     // [16][half]
@@ -292,25 +303,21 @@ __global__ void __launch_bounds__(kAppThreads, D == 128 ? AP128 : D == 64 ? AP64
   };
   uint4 own[R::ITEMS];
   if (warp < units) load(own, warp);
-  fill_table(p, table, run.pos, run.count);
+  fill_table<MODE>(p, table, run.pos, run.count);
   __syncthreads();
 #pragma unroll 1
   for (int u = warp; u < units; u += kAppWarps) {
     uint4 next[R::ITEMS];
     const bool is_q = u >= 2 * p.kv, is_k = u < p.kv;
     const int group = is_q ? -1 : (is_k ? u : u - p.kv);
-    // what the elements are paired with: the lanes that own it have just read it
-    uint4 other[MODE == MODE_HALF ? R::ITEMS : 1];
-    if (MODE == MODE_HALF && (is_q || is_k)) {
-#pragma unroll
-      for (int i = 0; i < R::ITEMS; ++i) {
-        const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
-        if (r < run.count && 8 * c < p.rot)
-          other[i] = *reinterpret_cast<const uint4*>(rows + (r * p.width + column(u) + (8 * c < p.half ? 8 * c + p.half : 8 * c - p.half)));
-      }
-    }
     if (u + kAppWarps < units) load(next, u + kAppWarps);
-    __syncwarp();                                     // the head's rows have been read: now they may be written
+    // the eight elements that an item is paired with: another lane has them
+    auto paired = [&](const uint4& v) {
+      if constexpr (MODE != MODE_HALF) return v;
+      const int c = lane % R::CHUNKS, hop = p.half / 8, from = 8 * c >= p.rot ? lane : (c < hop ? lane + hop : lane - hop);
+      return make_uint4(__shfl_sync(0xffffffffu, v.x, from), __shfl_sync(0xffffffffu, v.y, from), __shfl_sync(0xffffffffu, v.z, from),
+                        __shfl_sync(0xffffffffu, v.w, from));
+    };
     if (is_q) {
       __nv_bfloat16* out = p.q_out + run.row * p.q_stride + (u - 2 * p.kv) * D;
       if (MODE == MODE_SLOW_HALF || MODE == MODE_SLOW_PAIRS) {
@@ -335,8 +342,9 @@ __global__ void __launch_bounds__(kAppThreads, D == 128 ? AP128 : D == 64 ? AP64
         for (int i = 0; i < R::ITEMS; ++i) {
           const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
           float x[8];
+          const uint4 other = paired(own[i]);
           if (r < run.count) {
-            rotate<MODE>(x, p, own[i], other[MODE == MODE_HALF ? i : 0], nullptr, table + r * p.half, c);
+            rotate<MODE>(x, p, own[i], other, nullptr, table + r * p.half, c);
             *reinterpret_cast<uint4*>(out + r * p.q_stride + 8 * c) = pack_bf16x8(x);
           }
         }
@@ -352,7 +360,8 @@ __global__ void __launch_bounds__(kAppThreads, D == 128 ? AP128 : D == 64 ? AP64
 #pragma unroll
         for (int i = 0; i < R::ITEMS; ++i) {
           const int k = 32 * i + lane, r = k / R::CHUNKS, c = k % R::CHUNKS;
-          if (r < run.count) rotate<MODE>(x[i], p, own[i], other[MODE == MODE_HALF ? i : 0], rows + r * p.width + column(u), table + r * p.half, c);
+          const uint4 other = paired(own[i]);
+          if (r < run.count) rotate<MODE>(x[i], p, own[i], other, rows + r * p.width + column(u), table + r * p.half, c);
           else spread(x[i], own[i]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[i][e]) & 0x7fffffffu);
@@ -437,7 +446,7 @@ __global__ void __launch_bounds__(kAppThreads) append_one_q8_kernel(const Append
   }
   const int slot = len - 1, first = slot & 15;
   const int page = p.page_table[(long long)seq * p.max_pages + (slot >> p.page_shift)];
-  fill_table(p, table, seen - 1, 1);
+  fill_table<MODE>(p, table, seen - 1, 1);
   __syncthreads();
   if ((unsigned)page >= (unsigned)p.n_pages) {
     report(p, threadIdx.x == 0);
@@ -450,8 +459,11 @@ __global__ void __launch_bounds__(kAppThreads) append_one_q8_kernel(const Append
     const int group = is_k ? u : u - p.kv;
     const __nv_bfloat16* head = row + (live ? column(u) : 0);
     uint4 other = own;
-    if (MODE == MODE_HALF && live && (is_q || is_k) && 8 * c < p.rot)
-      other = *reinterpret_cast<const uint4*>(head + (8 * c < p.half ? 8 * c + p.half : 8 * c - p.half));
+    if constexpr (MODE == MODE_HALF) {
+      const int hop = p.half / 8, from = 8 * c >= p.rot ? lane : (c < hop ? lane + hop : lane - hop);
+      other = make_uint4(__shfl_sync(0xffffffffu, own.x, from), __shfl_sync(0xffffffffu, own.y, from), __shfl_sync(0xffffffffu, own.z, from),
+                         __shfl_sync(0xffffffffu, own.w, from));
+    }
     const bool stores = live && !is_q && group < held;
     float* scale = nullptr;
     uint8_t* cache = nullptr;
