@@ -43,13 +43,6 @@ constexpr int kHalf = 64;                // forward: keys per S / P half block
 constexpr int kFwdTmemCols = 256;       // S halves: columns 0..63 and 64..127, O: 128..191, P halves (bf16 pairs): 192..223, 224..255
 constexpr float kRescaleLog2 = 8.f;     // growth of a row maximum (log2 domain) tolerated before O is rescaled
 
-__device__ inline void mma1(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
 // A operand in tensor memory (lane = row of A, two 16-bit elements of the contraction per 32-bit column)
 __device__ inline void mma1_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -57,14 +50,6 @@ __device__ inline void mma1_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ inline void commit1(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// fp32 accumulate, bf16 x bf16, M x N tile, operand majors (0: K-major, 1: MN-major)
-__host__ __device__ constexpr uint32_t idesc_bf16(int a_major, int b_major, int M, int N) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_major << 15) | ((uint32_t)b_major << 16) |
-         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 __device__ inline uint32_t pack2(float lo, float hi) {
   __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);

@@ -10,7 +10,9 @@
 //
 // Prompts.  A CTA holds 128 (small heads: 256) keys and walks over the queries behind them: 2 d operations and an exponential
 // for each pair of a query and a key of each head, nothing to speak of from memory.
+#include "attn_weights.cuh"
 #include "decode_tiles.cuh"
+#include "plan.cuh"
 
 namespace twist {
 namespace {
@@ -301,62 +303,6 @@ int run_weights(WeightParams& w, long long max_len, cudaStream_t st) {
 
 constexpr int kCoreWarps = 4, kCoreThreads = 32 * kCoreWarps, kQueryTile = 64;
 
-struct CoreParams {
-  const __nv_bfloat16* qkv;    // [S][T][nq]
-  const float* lse;            // [S][heads][T]
-  const int32_t *table, *new_len, *head_idx, *kv_pos;
-  float* weights;
-  int32_t* slot_pos;
-  int S, n_seqs, seq_len, heads, kv_max, per_group, n_kv_heads, nq, T, last;
-  int page_shift, n_pages, max_pages;
-  float scale;
-  int* status;
-};
-
-constexpr int kMaxHeads = 1024;
-
-// The kept heads that read KV position `pos`, in ascending order, into list; returns their number.  One warp; bad entries
-// are replaced by position 0 and reported.
-__device__ inline int heads_of(const CoreParams& p, int s, int pos, int lane, short* list) {
-  if (!p.head_idx) {
-    if (lane == 0) list[0] = (short)pos;
-    return 1;
-  }
-  int seen = 0;
-  for (int h0 = 0; h0 < p.heads; h0 += 32) {
-    const int hq = h0 + lane;
-    bool mine = false;
-    if (hq < p.heads) {
-      const int h = p.head_idx[(long long)s * p.heads + hq];
-      int g = h < 0 ? -1 : h / p.per_group;
-      if ((unsigned)g >= (unsigned)p.n_kv_heads) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); g = 0; }
-      int at = p.kv_pos[(long long)s * p.n_kv_heads + g];
-      if ((unsigned)at >= (unsigned)p.kv_max) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); at = 0; }
-      mine = at == pos;
-    }
-    const unsigned vote = __ballot_sync(0xffffffffu, mine);
-    if (mine) list[seen + __popc(vote & ((1u << lane) - 1))] = (short)hq;
-    seen += __popc(vote);
-  }
-  return seen;
-}
-
-// Tokens of sequence (s, b), checked.
-__device__ inline int prompt_len(const CoreParams& p, long long seq) {
-  int n = p.new_len ? p.new_len[seq] : p.seq_len;
-  if (n < 0 || n > p.seq_len) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); n = n < 0 ? 0 : p.seq_len; }
-  return n;
-}
-
-// Token j's sum into its page.
-__device__ inline void store_weight(const CoreParams& p, long long seq, int pos, int j, float sum) {
-  const int page = j >> p.page_shift, id = page < p.max_pages ? p.table[seq * p.max_pages + page] : -1;
-  if ((unsigned)id >= (unsigned)p.n_pages) { atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX); return; }
-  const long long at = (((long long)id * p.kv_max + pos) << p.page_shift) + (j & ((1 << p.page_shift) - 1));
-  p.weights[at] = sum;
-  if (p.slot_pos) p.slot_pos[at] = j;
-}
-
 // A CTA holds a tile of keys of one KV position in registers (a warp 16 * SUB * KT of them) and walks over the queries that may
 // look at them, head after head, tiles of kQueryTile through shared memory.  The sums stay in the registers of the threads
 // that own the scores and are joined over the four threads of a row at the end.
@@ -611,7 +557,8 @@ extern "C" int32_t twist_attn_core_weights(const twist_attn_core_weights_args* a
     case 8: return run_core<8>(p, st);
     case 16: return run_core<16>(p, st);
     case 32: return run_core<32>(p, st);
-    case 64: return run_core<64>(p, st);
-    default: return run_core<128>(p, st);
+    default: break;
   }
+  PlanScope scope(a->plan);
+  return core_weights_tc(p, dh, st);
 }

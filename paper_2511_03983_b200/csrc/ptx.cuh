@@ -232,5 +232,21 @@ __device__ inline uint64_t smem_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_
          (1ull << 46) | (2ull << 61);
 }
 
+// MMA of one CTA, both operands in shared memory, fp32 accumulators in tensor memory, and its completion on a barrier.
+__device__ inline void mma1(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ inline void commit1(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// fp32 accumulate, bf16 x bf16, M x N tile, operand majors (0: K-major, 1: MN-major)
+__host__ __device__ constexpr uint32_t idesc_bf16(int a_major, int b_major, int M, int N) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_major << 15) | ((uint32_t)b_major << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
 
 }  // namespace twist
