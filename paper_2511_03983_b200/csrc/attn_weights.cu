@@ -303,15 +303,16 @@ int run_weights(WeightParams& w, long long max_len, cudaStream_t st) {
 
 constexpr int kCoreWarps = 4, kCoreThreads = 32 * kCoreWarps, kQueryTile = 64;
 
-// A CTA holds a tile of keys of one KV position in registers (a warp 16 * SUB * KT of them) and walks over the queries that may
-// look at them, head after head, tiles of kQueryTile through shared memory.  The sums stay in the registers of the threads
-// that own the scores and are joined over the four threads of a row at the end.
+
+// Small heads.  A CTA holds a tile of 256 keys of one KV position in registers (a warp 64 of them) and walks over the queries that
+// may look at them, head after head, tiles of kQueryTile through shared memory, the next one on its way.  The sums stay in the
+// registers of the threads that own the scores and are joined over the four threads of a row at the end.
 template <int D>
 __global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CoreParams p) {
   using Sh = Shape<D, 2>;
-  constexpr int KT = D >= 64 ? 2 : 1, WARP_KEYS = Sh::TILE * KT, KEYS = WARP_KEYS * kCoreWarps, STRIDE = D + 8;
-  __shared__ __align__(16) __nv_bfloat16 qs[kQueryTile * STRIDE];
-  __shared__ float ls[kQueryTile];
+  constexpr int SUB = Sh::SUB, WARP_KEYS = Sh::TILE, KEYS = WARP_KEYS * kCoreWarps, STRIDE = D + 8;
+  __shared__ __align__(16) __nv_bfloat16 qs[2][kQueryTile * STRIDE];
+  __shared__ float ls[2][kQueryTile];
   __shared__ short list[kMaxHeads];
   __shared__ int n_list;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -330,105 +331,95 @@ __global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CorePa
   }
   const __nv_bfloat16* rows = p.qkv + ((long long)s * p.T + (long long)b * p.seq_len) * p.nq;
   const int mine = key0 + warp * WARP_KEYS;
-  Tile<D, 2> x[KT];
+  uint32_t x[SUB][2][Sh::KCH][Sh::KW];
 #pragma unroll
-  for (int k = 0; k < KT; ++k)
+  for (int st = 0; st < SUB; ++st)
 #pragma unroll
-    for (int st = 0; st < Sh::SUB; ++st)
+    for (int r = 0; r < 2; ++r) {
+      const int key = mine + 16 * st + g + 8 * r;
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int key = mine + k * Sh::TILE + 16 * st + g + 8 * r;
+      for (int c = 0; c < Sh::KCH; ++c) {
+        if (key < len) {
+          load_words<Sh::KW>(x[st][r][c], rows + (long long)key * p.nq + (p.heads + pos) * D + c * 8 * Sh::KW + t * 2 * Sh::KW);
+        } else {
 #pragma unroll
-        for (int c = 0; c < Sh::KCH; ++c) {
-          if (key < len) {
-            load_words<Sh::KW>(x[k].k[st][r][c], rows + (long long)key * p.nq + (p.heads + pos) * D + c * 8 * Sh::KW + t * 2 * Sh::KW);
-          } else {
-#pragma unroll
-            for (int w = 0; w < Sh::KW; ++w) x[k].k[st][r][c][w] = 0;
-          }
+          for (int w = 0; w < Sh::KW; ++w) x[st][r][c][w] = 0;
         }
       }
-  float sum[KT][Sh::SUB][2];
+    }
+  float sum[SUB][2];
 #pragma unroll
-  for (int k = 0; k < KT; ++k)
-#pragma unroll
-    for (int st = 0; st < Sh::SUB; ++st) sum[k][st][0] = sum[k][st][1] = 0.f;
+  for (int st = 0; st < SUB; ++st) sum[st][0] = sum[st][1] = 0.f;
   __syncthreads();
-  const int first = max(key0, p.last ? len - p.last : 0);          // the first query that counts
-  for (int i = 0; i < n_list; ++i) {
-    const int h = list[i];
-    for (int q0 = first / kQueryTile * kQueryTile; q0 < len; q0 += kQueryTile) {
-      __syncthreads();
-      for (int k = threadIdx.x; k < kQueryTile * D / 8; k += kCoreThreads) {
-        const int r = k / (D / 8), c = k % (D / 8);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (q0 + r < len) v = *reinterpret_cast<const uint4*>(rows + (long long)(q0 + r) * p.nq + h * D + 8 * c);
-        *reinterpret_cast<uint4*>(qs + r * STRIDE + 8 * c) = v;
-      }
-      if (threadIdx.x < kQueryTile) {
-        const int q = q0 + threadIdx.x;
-        // a query that does not count gives nothing
-        ls[threadIdx.x] = q >= first && q < len ? p.lse[((long long)s * p.heads + h) * p.T + (long long)b * p.seq_len + q] : INFINITY;
-      }
-      __syncthreads();
-      const bool diagonal = q0 < key0 + KEYS;
-#pragma unroll 2
-      for (int n = 0; n < kQueryTile; n += 8) {
-        Query<D, 2> q;
-        const __nv_bfloat16* row = qs + (n + g) * STRIDE + t * 2 * Sh::KW;
-#pragma unroll
-        for (int c = 0; c < Sh::KCH; ++c) {
-          if constexpr (Sh::KW == 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(row + c * 8 * Sh::KW);
-            q.w[c][0] = v.x; q.w[c][1] = v.y; q.w[c][2] = v.z; q.w[c][3] = v.w;
-          } else {
-#pragma unroll
-            for (int w = 0; w < Sh::KW; ++w) q.w[c][w] = *reinterpret_cast<const uint32_t*>(row + 2 * w);
-          }
-        }
-        const float l0 = ls[n + 2 * t], l1 = ls[n + 2 * t + 1];
-        const int i0 = q0 + n + 2 * t;
-#pragma unroll
-        for (int k = 0; k < KT; ++k) {
-          float sc[Sh::SUB][4];
-          tile_scores<D, 2>(sc, x[k], q, Scales<D, 2>{});
-#pragma unroll
-          for (int st = 0; st < Sh::SUB; ++st) {
-            const int key = mine + k * Sh::TILE + 16 * st + g;
-            float e0 = weight_of(sc[st][0], p.scale, l0), e1 = weight_of(sc[st][1], p.scale, l1);
-            float e2 = weight_of(sc[st][2], p.scale, l0), e3 = weight_of(sc[st][3], p.scale, l1);
-            if (diagonal) {
-              e0 = i0 >= key ? e0 : 0.f;
-              e1 = i0 + 1 >= key ? e1 : 0.f;
-              e2 = i0 >= key + 8 ? e2 : 0.f;
-              e3 = i0 + 1 >= key + 8 ? e3 : 0.f;
-            }
-            sum[k][st][0] += e0 + e1;
-            sum[k][st][1] += e2 + e3;
-          }
-        }
-      }
-    }
-  }
   if (n_list == 0) return;                                         // no head reads this position
-#pragma unroll
-  for (int k = 0; k < KT; ++k)
-#pragma unroll
-    for (int st = 0; st < Sh::SUB; ++st) {
-      float a = sum[k][st][0], c = sum[k][st][1];
-#pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        a += __shfl_xor_sync(0xffffffffu, a, o);
-        c += __shfl_xor_sync(0xffffffffu, c, o);
-      }
-      const int key = mine + k * Sh::TILE + 16 * st + g + 8 * t;
-      if (t < 2 && key < len) store_weight(p, seq, pos, key, t ? c : a);
+  const int first = max(key0, p.last ? len - p.last : 0);          // the first query that counts
+  const int begin = first / kQueryTile * kQueryTile;
+  auto fetch = [&](int buf, int h, int q0) {                       // rows behind the end become zeros
+    for (int k = threadIdx.x; k < kQueryTile * D / 8; k += kCoreThreads) {
+      const int r = k / (D / 8), c = k % (D / 8), there = q0 + r < len;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(qs[buf] + r * STRIDE + 8 * c)),
+                   "l"(rows + (long long)(there ? q0 + r : 0) * p.nq + h * D + 8 * c), "r"(there ? 16 : 0) : "memory");
     }
+    if (threadIdx.x < kQueryTile) {
+      const int q = q0 + threadIdx.x, there = q < len;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(ls[buf] + threadIdx.x)),
+                   "l"(p.lse + ((long long)s * p.heads + h) * p.T + (long long)b * p.seq_len + (there ? q : 0)), "r"(there ? 4 : 0) : "memory");
+    }
+    commit_copies();
+  };
+  fetch(0, list[0], begin);
+  int head = 0, q0 = begin;
+  for (int buf = 0; head < n_list; buf ^= 1) {
+    const int at = q0;
+    if ((q0 += kQueryTile) >= len) { q0 = begin; ++head; }
+    if (head < n_list) fetch(buf ^ 1, list[head], q0);
+    else commit_copies();
+    wait_copies_but<1>();
+    __syncthreads();
+    const bool edge = at < max(first, key0 + KEYS) || at + kQueryTile > len;
+#pragma unroll 2
+    for (int n = 0; n < kQueryTile; n += 8) {
+      Query<D, 2> q;
+      const __nv_bfloat16* row = qs[buf] + (n + g) * STRIDE + t * 2 * Sh::KW;
+#pragma unroll
+      for (int c = 0; c < Sh::KCH; ++c) take_words<Sh::KW>(q.w[c], reinterpret_cast<const uint8_t*>(row + c * 8 * Sh::KW));
+      const float l0 = ls[buf][n + 2 * t], l1 = ls[buf][n + 2 * t + 1];
+      const int i0 = at + n + 2 * t;
+#pragma unroll
+      for (int st = 0; st < SUB; ++st) {
+        float sc[4];
+        step_scores<D, 2>(sc, x[st], q, 1.f);
+        float e0 = weight_of(sc[0], p.scale, l0), e1 = weight_of(sc[1], p.scale, l1);
+        float e2 = weight_of(sc[2], p.scale, l0), e3 = weight_of(sc[3], p.scale, l1);
+        if (edge) {
+          const int key = mine + 16 * st + g, a = max(key, first), c = max(key + 8, first);
+          e0 = i0 >= a && i0 < len ? e0 : 0.f;
+          e1 = i0 + 1 >= a && i0 + 1 < len ? e1 : 0.f;
+          e2 = i0 >= c && i0 < len ? e2 : 0.f;
+          e3 = i0 + 1 >= c && i0 + 1 < len ? e3 : 0.f;
+        }
+        sum[st][0] += e0 + e1;
+        sum[st][1] += e2 + e3;
+      }
+    }
+    __syncthreads();                                               // the tile has been read
+  }
+#pragma unroll
+  for (int st = 0; st < SUB; ++st) {
+    float a = sum[st][0], c = sum[st][1];
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      a += __shfl_xor_sync(0xffffffffu, a, o);
+      c += __shfl_xor_sync(0xffffffffu, c, o);
+    }
+    const int key = mine + 16 * st + g + 8 * t;
+    if (t < 2 && key < len) store_weight(p, seq, pos, key, t ? c : a);
+  }
 }
 
 template <int D>
 int run_core(CoreParams& p, cudaStream_t st) {
-  constexpr int KEYS = Shape<D, 2>::TILE * (D >= 64 ? 2 : 1) * kCoreWarps;
+  constexpr int KEYS = Shape<D, 2>::TILE * kCoreWarps;
   const long long grid = (long long)p.S * p.n_seqs * p.kv_max * ((p.seq_len + KEYS - 1) / KEYS);
   if (grid > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
   TWIST_CUDA_TRY(launch_overlapped(core_weights_kernel<D>, dim3((unsigned)grid), dim3(kCoreThreads), 0, st, 1, p));

@@ -8,8 +8,14 @@
 // exponentials are taken.  Warps 0-7: exponentials (two per lane quarter, 64 queries each); warp 8, one lane: TMA and MMA issue.
 // Two CTAs share an SM.
 //
-// Bound by the exponentials: an SM's special-function units give 16 a cycle, 1024 cycles a block, against 128 (d = 64) of MMA.
+// Bound by the exponentials: an SM's special-function units give 16 a cycle, 1024 cycles a block, against 128 (d = 64) of MMA,
+// and by the instructions beside them.  4 subnets of 4 prompts of 2048, 16 heads on 4 positions of d = 64 (130 us of special-function
+// unit): 531 us with warp-level MMA from shared memory, 192 us first on tcgen05, 172 with the log-sum-exps staged for eight blocks
+// at a time instead of for each, 160 with every fourth pair of exponentials by a polynomial (half of them: more instructions
+// than the unit has to spare).  Sixteen warps of 32 queries each: 182.
 // Every wait is bounded; on expiry the CTA records TWIST_ERR_DEVICE_TIMEOUT and leaves.
+#include <type_traits>
+
 #include "attn_weights.cuh"
 #include "ptx.cuh"
 
@@ -17,9 +23,12 @@ namespace twist {
 namespace {
 
 constexpr int kBlock = 128;
-constexpr int kThreads = 288;
+constexpr int kParts = 2, kCols = kBlock / kParts, kEw = 4 * kParts;      // warps to a lane quarter, columns of each
+constexpr int kThreads = 32 * (kEw + 1);
+constexpr int kChunk = 8;                // blocks of a head whose log-sum-exps are staged together
 constexpr int kTmemCols = 256;           // two S^T buffers of 128 columns
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPolyPairs = 1;            // of four pairs of exponentials, how many are taken without the special-function unit
 
 __device__ inline float ex2(float x) {
   float y;
@@ -35,22 +44,77 @@ struct Tc {
   static constexpr int SMEM = BLOCK * (1 + STAGES) + 1024 + 256;
 };
 
-// Sum over 32 columns of one row.  MASKED: columns lo <= c < hi count.
+// Two fp32 numbers at a time: half the issue slots.
+using f32x2 = unsigned long long;
+__device__ inline f32x2 pair(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ inline void split(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ inline f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ inline f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ inline f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^t without the special-function unit, t <= 64 or so: t = n + f with n whole and |f| <= 1/2, 2^f by the polynomial of degree 5 of
+// least relative error there (7.5e-8, by Remez exchange), n into the exponent.  What is below 2^-126 comes out as 2^-126.
+__device__ inline f32x2 exp2_poly(f32x2 t) {
+  float a, b;
+  split(t, a, b);
+  t = pair(fmaxf(a, -126.f), fmaxf(b, -126.f));
+  const f32x2 magic = pair(12582912.f, 12582912.f), z = add2(t, magic);            // 1.5 * 2^23: the sum's low bits are n
+  const f32x2 f = add2(t, mul2(add2(z, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f)));
+  f32x2 y = fma2(pair(1.32764721678e-3f, 1.32764721678e-3f), f, pair(9.67554133102e-3f, 9.67554133102e-3f));
+  y = fma2(y, f, pair(5.55071327288e-2f, 5.55071327288e-2f));
+  y = fma2(y, f, pair(2.40221197240e-1f, 2.40221197240e-1f));
+  y = fma2(y, f, pair(6.93146967065e-1f, 6.93146967065e-1f));
+  y = fma2(y, f, pair(1.00000007165f, 1.00000007165f));
+  float ya, yb, za, zb;
+  split(y, ya, yb);
+  split(z, za, zb);
+  return pair(__int_as_float(__float_as_int(ya) + (__float_as_int(za) << 23)), __int_as_float(__float_as_int(yb) + (__float_as_int(zb) << 23)));
+}
+
+// Adds 16 columns of one row to the sums; `lse` holds their log-sum-exps, negated.  MASKED: columns lo <= c < hi count.
 template <bool MASKED>
-__device__ inline float row_sum(const uint32_t (&v)[32], uint32_t lse, float scale, int lo, int hi) {
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+__device__ inline void add_row(f32x2 (&sum)[4], const uint32_t (&v)[16], const float* lse, float scale, int lo, int hi) {
+  const f32x2 scale2 = pair(scale, scale), log2e2 = pair(kLog2e, kLog2e);
 #pragma unroll
-  for (int i = 0; i < 32; i += 4) {
-    const uint4 l = lds128(lse + 4 * i);
-    const float w[4] = {__uint_as_float(l.x), __uint_as_float(l.y), __uint_as_float(l.z), __uint_as_float(l.w)};
+  for (int i = 0; i < 16; i += 4) {
+    const float4 l = *reinterpret_cast<const float4*>(lse + i);
+    const f32x2 w[2] = {pair(l.x, l.y), pair(l.z, l.w)};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float e = ex2(fmaf(__uint_as_float(v[i + j]), scale, -w[j]) * kLog2e);
-      if (MASKED) e = i + j >= lo && i + j < hi ? e : 0.f;
-      sum[j] += e;
+    for (int j = 0; j < 2; ++j) {
+      const int c = i + 2 * j;
+      const f32x2 t = mul2(fma2(pair(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, w[j]), log2e2);
+      f32x2 e;
+      if (!MASKED && c / 2 % 4 < kPolyPairs) {
+        e = exp2_poly(t);
+      } else {
+        float a, b;
+        split(t, a, b);
+        a = ex2(a);
+        b = ex2(b);
+        if (MASKED) {
+          a = c >= lo && c < hi ? a : 0.f;
+          b = c + 1 >= lo && c + 1 < hi ? b : 0.f;
+        }
+        e = pair(a, b);
+      }
+      sum[c / 2 % 4] = add2(sum[c / 2 % 4], e);
     }
   }
-  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 // qkv viewed as [S * n_seqs][seq_len][nq]: rows past the end of a sequence read as zeros.
@@ -60,8 +124,8 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
   extern __shared__ unsigned char smem_raw[];
   __shared__ short list[kMaxHeads];
   __shared__ int n_list_s;
-  __shared__ __align__(16) float lse_w[8][64];                // per warp: its 64 queries
-  __shared__ float halves[kBlock];
+  __shared__ __align__(16) float lse_s[2][kChunk * kBlock];   // negated log-sum-exps of the queries of a chunk and the next
+  __shared__ float sums[kParts][kBlock];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* gen = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t k_s = base, q_s = base + T::BLOCK, bar0 = q_s + T::STAGES * T::BLOCK;
@@ -73,9 +137,9 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned items = (unsigned)p.S * p.n_seqs * p.kv_max, item = blockIdx.x % items;
   const int kb = (int)(blockIdx.x / items), pos = (int)(item % p.kv_max), z = (int)(item / p.kv_max), s = z / p.n_seqs, b = z - s * p.n_seqs;
-  if (threadIdx.x == 256) {
+  if (threadIdx.x == 32 * kEw) {
     tma_prefetch_desc(&map);
-    for (int i = 0; i < N_BARS; ++i) mbar_init(bar(i), i >= S_FREE ? 8 : 1);
+    for (int i = 0; i < N_BARS; ++i) mbar_init(bar(i), i >= S_FREE ? kEw : 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -83,11 +147,17 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
   griddep_wait();
   const int len = prompt_len(p, z);
   if (kb * kBlock >= len) return;
+  auto load = [&](uint32_t to, uint32_t full, int col, int block) {
+    mbar_expect_tx(full, T::BLOCK);
+#pragma unroll
+    for (int j = 0; j < T::PANELS; ++j) tma_load_3d_local(to + j * T::BOX, &map, full, col + 64 * j, block * kBlock, z);
+  };
+  if (threadIdx.x == 32 * kEw) load(k_s, bar(K_FULL), (p.heads + pos) * D, kb);
   if (warp == 0) {
     const int n = heads_of(p, s, pos, lane, list);
     if (lane == 0) n_list_s = n;
   }
-  if (warp == 8) {
+  if (warp == kEw) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"((uint32_t)kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -99,20 +169,14 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
   const uint32_t tmem = *tmem_slot;
   const int first = max(kb * kBlock, p.last ? len - p.last : 0);       // the first query that counts
   const int i0 = first / kBlock, per_head = (len + kBlock - 1) / kBlock - i0, total = n_list_s * per_head;
-  if (warp == 8) {
-    if (lane == 0 && total > 0) {
-      auto load = [&](uint32_t to, uint32_t full, int col, int block) {
-        mbar_expect_tx(full, T::BLOCK);
-#pragma unroll
-        for (int j = 0; j < T::PANELS; ++j) tma_load_3d_local(to + j * T::BOX, &map, full, col + 64 * j, block * kBlock, z);
-      };
+  if (warp == kEw) {
+    if (lane == 0) {                       // also without heads: the keys are on their way
       int head = 0, block = i0, filled = 0;                            // of the next unit to load
       auto load_q = [&] {
         load(q_s + filled % T::STAGES * T::BLOCK, bar(Q_FULL + filled % T::STAGES), list[head] * D, block);
         ++filled;
         if (++block == i0 + per_head) { block = i0; ++head; }
       };
-      load(k_s, bar(K_FULL), (p.heads + pos) * D, kb);
       while (filled < T::STAGES && filled < total) load_q();
       constexpr uint32_t idesc = idesc_bf16(0, 0, kBlock, kBlock);     // S^T = K Q^T, both K-major
       bool ok = mbar_wait_cta(bar(K_FULL), 0, abort_flag, p.status);
@@ -138,51 +202,81 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
       }
     }
   } else {
-    const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane, key = kb * kBlock + r;
-    const uint32_t t_s = tmem + ((uint32_t)(quarter * 32) << 16) + 64u * half, lse_s = smem_u32(lse_w[warp]);
-    // the statistics of the warp's 64 queries, one unit ahead in registers (a lane: queries lane and lane + 32 of its half)
-    int head = 0, block = i0;
-    float l0 = INFINITY, l1 = INFINITY;
-    auto next_lse = [&] {
-      l0 = l1 = INFINITY;
-      if (head == n_list_s) return;
-      const float* lse = p.lse + ((long long)s * p.heads + list[head]) * p.T + (long long)b * p.seq_len;
-      const int q = block * kBlock + 64 * half + lane;
-      if (q < len) l0 = lse[q];
-      if (q + 32 < len) l1 = lse[q + 32];
-      if (++block == i0 + per_head) { block = i0; ++head; }
+    const int quarter = warp & 3, part = warp >> 2, r = quarter * 32 + lane, key = kb * kBlock + r;
+    const uint32_t t_s = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(kCols * part);
+    constexpr int STAGED = kChunk * kBlock / (32 * kEw);                 // of a chunk, by a thread
+    float ahead[STAGED];
+    auto fetch = [&](int head, int c0) {                                 // of the chunk that begins at block c0
+      if (head >= n_list_s) return;
+      const float* lse = p.lse + ((long long)s * p.heads + list[head]) * p.T + (long long)b * p.seq_len + c0 * kBlock;
+#pragma unroll
+      for (int j = 0; j < STAGED; ++j) {
+        const int q = 32 * kEw * j + threadIdx.x;
+        ahead[j] = c0 * kBlock + q < len ? -lse[q] : 0.f;
+      }
     };
-    next_lse();
+    auto stage = [&](int to) {
+#pragma unroll
+      for (int j = 0; j < STAGED; ++j) lse_s[to][32 * kEw * j + threadIdx.x] = ahead[j];
+    };
+    fetch(0, i0);
+    stage(0);
     float sum = 0.f;
     bool ok = true;
-    for (int n = 0, i = i0; n < total; ++n) {
-      __syncwarp();                                                    // the unit before has read the staging area
-      lse_w[warp][lane] = l0;
-      lse_w[warp][lane + 32] = l1;
-      __syncwarp();
-      next_lse();
-      const int buf = n & 1;
-      if (!__all_sync(0xffffffffu, mbar_wait_cta(bar(S_FULL + buf), n >> 1 & 1, abort_flag, p.status))) { ok = false; break; }
-      tc_fence_after();
-      uint32_t va[32], vb[32];
-      tc_ld32(t_s + 128u * buf, va);
-      tc_ld32(t_s + 128u * buf + 32, vb);
-      tc_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(S_FREE + buf));
-      const int q0 = i * kBlock + 64 * half;
-      if (i * kBlock < max(first, (kb + 1) * kBlock) || (i + 1) * kBlock > len) {
-        const int lo = max(first, key) - q0, hi = len - q0;
-        sum += row_sum<true>(va, lse_s, p.scale, lo, hi) + row_sum<true>(vb, lse_s + 128, p.scale, lo - 32, hi - 32);
-      } else {
-        sum += row_sum<false>(va, lse_s, p.scale, 0, 0) + row_sum<false>(vb, lse_s + 128, p.scale, 0, 0);
+    const int end = i0 + per_head;
+    int n = 0, chunk = 0;
+    for (int head = 0, c0 = i0; head < n_list_s; ++chunk) {           // a warp that gave up still meets the others
+      // the chunk's statistics are there, and nobody reads those of the one before
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * kEw) : "memory");
+      const int last = min(c0 + kChunk, end), next_c0 = last == end ? i0 : last, next_head = head + (last == end);
+      fetch(next_head, next_c0);
+      const float* lse = lse_s[chunk & 1] + kCols * part;
+      for (int i = c0; ok && i < last; ++i, ++n, lse += kBlock) {
+        const int buf = n & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(bar(S_FULL + buf), n >> 1 & 1, abort_flag, p.status))) { ok = false; break; }
+        tc_fence_after();
+        // 16 columns at a time, the next ones on their way out of tensor memory
+        const uint32_t from = t_s + 128u * buf;
+        f32x2 sum4[4] = {0, 0, 0, 0};
+        auto unit = [&](auto masked) {
+          constexpr bool MASKED = decltype(masked)::value;
+          const int q0 = i * kBlock + kCols * part, lo = max(first, key) - q0, hi = len - q0;
+          uint32_t va[16], vb[16];
+          tc_ld16(from, va);
+          tc_wait_ld();
+#pragma unroll
+          for (int c = 0; c < kCols; c += 32) {
+            tc_ld16(from + c + 16, vb);
+            add_row<MASKED>(sum4, va, lse + c, p.scale, lo - c, hi - c);
+            tc_wait_ld();
+            if (c + 32 < kCols) {
+              tc_ld16(from + c + 32, va);
+            } else {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(S_FREE + buf));
+            }
+            add_row<MASKED>(sum4, vb, lse + c + 16, p.scale, lo - c - 16, hi - c - 16);
+            if (c + 32 < kCols) tc_wait_ld();
+          }
+        };
+        if (i * kBlock < max(first, (kb + 1) * kBlock) || (i + 1) * kBlock > len) unit(std::true_type{});
+        else unit(std::false_type{});
+        float x, y;
+        split(add2(add2(sum4[0], sum4[1]), add2(sum4[2], sum4[3])), x, y);
+        sum += x + y;
       }
-      if (++i == i0 + per_head) i = i0;
+      stage(chunk + 1 & 1);
+      head = next_head;
+      c0 = next_c0;
     }
-    if (half == 1) halves[r] = sum;
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (half == 0 && ok && n_list_s > 0 && key < len) store_weight(p, z, pos, key, sum + halves[r]);
+    sums[part][r] = sum;
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kEw) : "memory");
+    if (part == 0 && ok && n_list_s > 0 && key < len) {
+#pragma unroll
+      for (int j = 1; j < kParts; ++j) sum += sums[j][r];
+      store_weight(p, z, pos, key, sum);
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -190,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
     drain_after_abort(abort_flag);
     __syncthreads();
   }
-  if (warp == 8) {
+  if (warp == kEw) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kTmemCols) : "memory");
   }
