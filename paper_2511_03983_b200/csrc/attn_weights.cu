@@ -8,7 +8,7 @@
 // of tiles of one KV position of one sequence, the first run of every item before any second one, and its copies run on ahead
 // from one run to the next.
 //
-// Prompts.  A CTA holds 128 (small heads: 256) keys and walks over the queries behind them: 2 d operations and an exponential
+// Prompts.  A CTA holds 128 (small heads: 64) keys and walks over the queries behind them: 2 d operations and an exponential
 // for each pair of a query and a key of each head, nothing to speak of from memory.
 #include "attn_weights.cuh"
 #include "decode_tiles.cuh"
@@ -301,18 +301,19 @@ int run_weights(WeightParams& w, long long max_len, cudaStream_t st) {
 
 // ------------------------------------------------------------------------------------------------ prompts
 
-constexpr int kCoreWarps = 4, kCoreThreads = 32 * kCoreWarps, kQueryTile = 64;
+constexpr int kCoreWarps = 4, kCoreThreads = 32 * kCoreWarps, kCoreKeys = 16 * kCoreWarps;
 
-
-// Small heads.  A CTA holds a tile of 256 keys of one KV position in registers (a warp 64 of them) and walks over the queries that
-// may look at them, head after head, tiles of kQueryTile through shared memory, the next one on its way.  The sums stay in the
-// registers of the threads that own the scores and are joined over the four threads of a row at the end.
-template <int D>
+// Small heads.  A CTA holds a tile of 64 keys of one KV position in registers (a warp 16 of them) and walks over the queries that
+// may look at them, head after head, tiles of QT through shared memory, the next one on its way.  The sums stay in the
+// registers of the threads that own the scores and are joined over the four threads of a row at the end.  Bound by the
+// chains of dependent instructions: more keys a warp mean longer ones and fewer CTAs (4 subnets of 4 prompts of 2048, 16 heads on 4
+// positions of d = 32: 16, 32 and 64 keys a warp 326, 454 and 544 us; the special-function units alone take 130).
+template <int D, int QT>
 __global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CoreParams p) {
   using Sh = Shape<D, 2>;
-  constexpr int SUB = Sh::SUB, WARP_KEYS = Sh::TILE, KEYS = WARP_KEYS * kCoreWarps, STRIDE = D + 8;
-  __shared__ __align__(16) __nv_bfloat16 qs[2][kQueryTile * STRIDE];
-  __shared__ float ls[2][kQueryTile];
+  constexpr int KEYS = kCoreKeys, STRIDE = D + 8;
+  __shared__ __align__(16) __nv_bfloat16 qs[2][QT * STRIDE];
+  __shared__ float ls[2][QT];
   __shared__ short list[kMaxHeads];
   __shared__ int n_list;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -330,37 +331,33 @@ __global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CorePa
     if (lane == 0) n_list = n;
   }
   const __nv_bfloat16* rows = p.qkv + ((long long)s * p.T + (long long)b * p.seq_len) * p.nq;
-  const int mine = key0 + warp * WARP_KEYS;
-  uint32_t x[SUB][2][Sh::KCH][Sh::KW];
+  const int mine = key0 + 16 * warp;
+  uint32_t x[2][Sh::KCH][Sh::KW];
 #pragma unroll
-  for (int st = 0; st < SUB; ++st)
+  for (int r = 0; r < 2; ++r) {
+    const int key = mine + g + 8 * r;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int key = mine + 16 * st + g + 8 * r;
+    for (int c = 0; c < Sh::KCH; ++c) {
+      if (key < len) {
+        load_words<Sh::KW>(x[r][c], rows + (long long)key * p.nq + (p.heads + pos) * D + c * 8 * Sh::KW + t * 2 * Sh::KW);
+      } else {
 #pragma unroll
-      for (int c = 0; c < Sh::KCH; ++c) {
-        if (key < len) {
-          load_words<Sh::KW>(x[st][r][c], rows + (long long)key * p.nq + (p.heads + pos) * D + c * 8 * Sh::KW + t * 2 * Sh::KW);
-        } else {
-#pragma unroll
-          for (int w = 0; w < Sh::KW; ++w) x[st][r][c][w] = 0;
-        }
+        for (int w = 0; w < Sh::KW; ++w) x[r][c][w] = 0;
       }
     }
-  float sum[SUB][2];
-#pragma unroll
-  for (int st = 0; st < SUB; ++st) sum[st][0] = sum[st][1] = 0.f;
+  }
+  float sum0 = 0.f, sum1 = 0.f;                                    // of keys g and g + 8
   __syncthreads();
   if (n_list == 0) return;                                         // no head reads this position
   const int first = max(key0, p.last ? len - p.last : 0);          // the first query that counts
-  const int begin = first / kQueryTile * kQueryTile;
+  const int begin = first / QT * QT;
   auto fetch = [&](int buf, int h, int q0) {                       // rows behind the end become zeros
-    for (int k = threadIdx.x; k < kQueryTile * D / 8; k += kCoreThreads) {
+    for (int k = threadIdx.x; k < QT * D / 8; k += kCoreThreads) {
       const int r = k / (D / 8), c = k % (D / 8), there = q0 + r < len;
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(qs[buf] + r * STRIDE + 8 * c)),
                    "l"(rows + (long long)(there ? q0 + r : 0) * p.nq + h * D + 8 * c), "r"(there ? 16 : 0) : "memory");
     }
-    if (threadIdx.x < kQueryTile) {
+    if (threadIdx.x < QT) {
       const int q = q0 + threadIdx.x, there = q < len;
       asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(ls[buf] + threadIdx.x)),
                    "l"(p.lse + ((long long)s * p.heads + h) * p.T + (long long)b * p.seq_len + (there ? q : 0)), "r"(there ? 4 : 0) : "memory");
@@ -371,58 +368,52 @@ __global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CorePa
   int head = 0, q0 = begin;
   for (int buf = 0; head < n_list; buf ^= 1) {
     const int at = q0;
-    if ((q0 += kQueryTile) >= len) { q0 = begin; ++head; }
+    if ((q0 += QT) >= len) { q0 = begin; ++head; }
     if (head < n_list) fetch(buf ^ 1, list[head], q0);
     else commit_copies();
     wait_copies_but<1>();
     __syncthreads();
-    const bool edge = at < max(first, key0 + KEYS) || at + kQueryTile > len;
+    const bool edge = at < max(first, key0 + KEYS) || at + QT > len;
 #pragma unroll 2
-    for (int n = 0; n < kQueryTile; n += 8) {
+    for (int n = 0; n < QT; n += 8) {
       Query<D, 2> q;
       const __nv_bfloat16* row = qs[buf] + (n + g) * STRIDE + t * 2 * Sh::KW;
 #pragma unroll
       for (int c = 0; c < Sh::KCH; ++c) take_words<Sh::KW>(q.w[c], reinterpret_cast<const uint8_t*>(row + c * 8 * Sh::KW));
       const float l0 = ls[buf][n + 2 * t], l1 = ls[buf][n + 2 * t + 1];
-      const int i0 = at + n + 2 * t;
-#pragma unroll
-      for (int st = 0; st < SUB; ++st) {
-        float sc[4];
-        step_scores<D, 2>(sc, x[st], q, 1.f);
-        float e0 = weight_of(sc[0], p.scale, l0), e1 = weight_of(sc[1], p.scale, l1);
-        float e2 = weight_of(sc[2], p.scale, l0), e3 = weight_of(sc[3], p.scale, l1);
-        if (edge) {
-          const int key = mine + 16 * st + g, a = max(key, first), c = max(key + 8, first);
-          e0 = i0 >= a && i0 < len ? e0 : 0.f;
-          e1 = i0 + 1 >= a && i0 + 1 < len ? e1 : 0.f;
-          e2 = i0 >= c && i0 < len ? e2 : 0.f;
-          e3 = i0 + 1 >= c && i0 + 1 < len ? e3 : 0.f;
-        }
-        sum[st][0] += e0 + e1;
-        sum[st][1] += e2 + e3;
+      float sc[4];
+      step_scores<D, 2>(sc, x, q, 1.f);
+      float e0 = weight_of(sc[0], p.scale, l0), e1 = weight_of(sc[1], p.scale, l1);
+      float e2 = weight_of(sc[2], p.scale, l0), e3 = weight_of(sc[3], p.scale, l1);
+      if (edge) {                                                  // queries a .. len - 1 (c .. for the second key) count
+        const int i0 = at + n + 2 * t, a = max(mine + g, first), c = max(mine + g + 8, first);
+        e0 = (unsigned)(i0 - a) < (unsigned)(len - a) ? e0 : 0.f;
+        e1 = (unsigned)(i0 + 1 - a) < (unsigned)(len - a) ? e1 : 0.f;
+        e2 = (unsigned)(i0 - c) < (unsigned)(len - c) ? e2 : 0.f;
+        e3 = (unsigned)(i0 + 1 - c) < (unsigned)(len - c) ? e3 : 0.f;
       }
+      sum0 += e0 + e1;
+      sum1 += e2 + e3;
     }
     __syncthreads();                                               // the tile has been read
   }
 #pragma unroll
-  for (int st = 0; st < SUB; ++st) {
-    float a = sum[st][0], c = sum[st][1];
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      a += __shfl_xor_sync(0xffffffffu, a, o);
-      c += __shfl_xor_sync(0xffffffffu, c, o);
-    }
-    const int key = mine + 16 * st + g + 8 * t;
-    if (t < 2 && key < len) store_weight(p, seq, pos, key, t ? c : a);
+  for (int o = 1; o < 4; o <<= 1) {
+    sum0 += __shfl_xor_sync(0xffffffffu, sum0, o);
+    sum1 += __shfl_xor_sync(0xffffffffu, sum1, o);
   }
+  const int key = mine + g + 8 * t;
+  if (t < 2 && key < len) store_weight(p, seq, pos, key, t ? sum1 : sum0);
 }
 
 template <int D>
 int run_core(CoreParams& p, cudaStream_t st) {
-  constexpr int KEYS = Shape<D, 2>::TILE * kCoreWarps;
-  const long long grid = (long long)p.S * p.n_seqs * p.kv_max * ((p.seq_len + KEYS - 1) / KEYS);
+  const long long grid = (long long)p.S * p.n_seqs * p.kv_max * ((p.seq_len + kCoreKeys - 1) / kCoreKeys);
   if (grid > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
-  TWIST_CUDA_TRY(launch_overlapped(core_weights_kernel<D>, dim3((unsigned)grid), dim3(kCoreThreads), 0, st, 1, p));
+  // Half as many queries a tile where a prompt has few tiles (6 prompts of 77, the last 32 queries, d = 32: 5.8 us against 8.4; the
+  // long ones above 363 against 326).
+  void (*kernel)(CoreParams) = p.seq_len <= 256 ? core_weights_kernel<D, 32> : core_weights_kernel<D, 64>;
+  TWIST_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)grid), dim3(kCoreThreads), 0, st, 1, p));
   return TWIST_OK;
 }
 
