@@ -1169,20 +1169,45 @@ class DecodeSession:
 
     graph=True captures the layers of a step into a CUDA graph at the first step and replays it from then on (the page
     table, the lengths and the input are data of the graph, so every step is the same graph): a step then costs the
-    device's time instead of the host's."""
+    device's time instead of the host's.
 
-    def __init__(self, eng: StackEngine, max_len: int, page_size: int = 16, n_pages: Optional[int] = None, graph: bool = False):
+    cache_bits=8 holds the cache in 8 bits (e4m3, a scale for each 16 tokens of a KV position): half the memory and half the
+    bytes of a step's attention.
+
+    keep=K bounds the cache: the session adds up the attention weight that every cached token gathers, from the prompt's
+    queries (its last `last_queries`, 0: all of them) and from every step's, and a sequence that has grown `slack` tokens (one
+    page unless said otherwise) beyond K is cut to its K tokens of most weight, the `recent` newest always among them, before
+    the next step.  The cut is each KV position's own.  max_len then bounds what a sequence holds, not how long it gets.  (What the
+    layers of a step that raises had added to the weights stays.)"""
+
+    # what a session without these options has
+    cache_bits, keep = 16, None
+
+    def __init__(self, eng: StackEngine, max_len: int, page_size: int = 16, n_pages: Optional[int] = None, graph: bool = False,
+                 cache_bits: int = 16, keep: Optional[int] = None, recent: int = 0, slack: Optional[int] = None,
+                 last_queries: int = 0):
         w = eng.w
         S, n, d, bf, dev = w.n_subnets, eng.n_seqs, w.d_model, torch.bfloat16, eng.dev
         if max_len < 1:
             raise ValueError("max_len %d" % max_len)
+        if cache_bits not in (8, 16) or (cache_bits == 8 and w.d_head not in (16, 32, 64, 128)):
+            raise ValueError("cache_bits %r: 16, or 8 with heads of 16, 32, 64 or 128 (d_head %d)" % (cache_bits, w.d_head))
+        slack = page_size if slack is None else slack
+        if keep is not None and (keep < 1 or slack < 1 or recent < 0 or last_queries < 0 or keep + slack > max_len):
+            raise ValueError("keep %d, slack %d, recent %d, last_queries %d: keep + slack up to max_len (%d) are expected" % (
+                keep, slack, recent, last_queries, max_len))
+        self.cache_bits, self.keep, self.recent, self.slack, self.last_queries = cache_bits, keep, recent, slack, last_queries
         self.eng, self.S, self.n, self.page_size = eng, S, n, page_size
         self.max_pages = -(-max_len // page_size)
         self.max_len = max_len
         self.n_pages = S * n * self.max_pages if n_pages is None else n_pages
         geo = [eng.geo[eng.kind_of(l)] for l in range(w.n_layers)]
-        pool = lambda gm: torch.zeros(self.n_pages, 2, gm.kv_max, page_size, w.d_head, dtype=bf, device=dev)
+        pool = lambda gm: torch.zeros(self.n_pages, 2, gm.kv_max, page_size, w.d_head, dtype=bf if cache_bits == 16 else torch.uint8,
+                                      device=dev)
         self.pools = [pool(gm) for gm in geo]                       # K and V of a page side by side
+        if cache_bits == 8:
+            self.pools = [t.view(torch.float8_e4m3fn) for t in self.pools]
+            self.scales = [torch.ones(self.n_pages, gm.kv_max, page_size // 16, 2, dtype=torch.float32, device=dev) for gm in geo]
         self.free = list(range(self.n_pages - 1, -1, -1))           # pages of the pool that no sequence holds
         self.lens = [[0] * n for _ in range(S)]
         self.pages: List[List[List[int]]] = [[[] for _ in range(n)] for _ in range(S)]
@@ -1198,6 +1223,15 @@ class DecodeSession:
         self.pre, self.hh = per(lambda gm: gm.gf), per(lambda gm: gm.f_sub)
         self.ws = torch.empty(B.twist_attn_decode_workspace_bytes(w.d_head), dtype=torch.uint8, device=dev)
         self.use_graph, self.graph = graph, None
+        if keep is not None:
+            slots = lambda gm: (self.n_pages, gm.kv_max, page_size)
+            self.weights = [torch.zeros(slots(gm), dtype=torch.float32, device=dev) for gm in geo]
+            self.slot_pos = [torch.zeros(slots(gm), **i32) for gm in geo]
+            self.lse = {kind: torch.empty(S, gm.head_keep, n, dtype=torch.float32, device=dev) for kind, gm in eng.geo.items()}
+            self.seen = [[0] * n for _ in range(S)]                 # tokens of a sequence so far, those that were cut included
+            self.seen_len, self.keep_len, self.new_pos = (torch.zeros(S, n, **i32) for _ in range(3))
+            self.evict_ws = torch.empty(B.twist_kv_evict_workspace_bytes(S, n, max(gm.kv_max for gm in geo), self.max_pages * page_size),
+                                        dtype=torch.uint8, device=dev)
         if eng.ln:
             self.x_ln = act(d)
             self.stat = [torch.empty(S, n, dtype=torch.float32, device=dev) for _ in range(2)]
@@ -1220,15 +1254,26 @@ class DecodeSession:
                 while len(self.pages[s][b]) * self.page_size < self.lens[s][b]:
                     self.pages[s][b].append(self.free.pop())
                     grown = True
+                if self.keep is not None:
+                    self.seen[s][b] += new[s][b]
         if grown:
             rows = [[p + [0] * (self.max_pages - len(p)) for p in row] for row in self.pages]
             self.page_table.copy_(torch.tensor(rows, dtype=torch.int32))
+        self._lengths()
+
+    def _lengths(self):
+        """The lengths to the device."""
         self.kv_len.copy_(torch.tensor(self.lens, dtype=torch.int32))
+        if self.keep is not None:
+            seen = torch.tensor(self.seen, dtype=torch.int32)
+            self.seen_len.copy_(seen)
+            self.new_pos.copy_(seen - 1)
 
     @contextmanager
     def _growing(self, new):
         """_extend for a call that uses the room: if it raises, lengths and pages go back to what they were."""
         lens, held = [list(r) for r in self.lens], [[len(p) for p in r] for r in self.pages]
+        seen = None if self.keep is None else [list(r) for r in self.seen]
         try:
             self._extend(new)
             yield
@@ -1238,17 +1283,53 @@ class DecodeSession:
                 for b in reversed(range(self.n)):
                     while len(self.pages[s][b]) > held[s][b]:
                         self.free.append(self.pages[s][b].pop())
-            self.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+            if seen is not None:
+                self.seen = seen
+            self._lengths()
             raise
 
     def release(self, s: int, b: int):
         """Forgets a sequence: its pages are free again, its next token is its first."""
         self.free.extend(reversed(self.pages[s][b]))
         self.pages[s][b], self.lens[s][b] = [], 0
-        self.kv_len.copy_(torch.tensor(self.lens, dtype=torch.int32))
+        if self.keep is not None:
+            self.seen[s][b] = 0
+        self._lengths()
 
     def _cache(self, l: int):
-        return dict(k_cache=self.pools[l][:, 0], v_cache=self.pools[l][:, 1], page_table=self.page_table, kv_len=self.kv_len)
+        scales = dict(scales=self.scales[l]) if self.cache_bits == 8 else {}
+        return dict(k_cache=self.pools[l][:, 0], v_cache=self.pools[l][:, 1], page_table=self.page_table, kv_len=self.kv_len, **scales)
+
+    def evict(self, beyond: int = 0):
+        """Cuts every sequence that holds at least keep + max(1, beyond) tokens to its `keep` best; their spare pages are free again.  step
+        does this by itself, with beyond = slack."""
+        if self.keep is None:
+            raise ValueError("a session without keep holds every token")
+        over = max(1, beyond)
+        lens = [[self.keep if m >= self.keep + over else m for m in row] for row in self.lens]
+        if lens == self.lens:
+            return
+        w, eng = self.eng.w, self.eng
+        self.keep_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        for l in range(w.n_layers):
+            eng._bind(l)
+            with eng._timed("evict"):
+                B.twist_kv_evict(B.kv_evict_args(w.dtype, self.S, self.n, eng.kv_max, w.d_head, self.recent, weights=self.weights[l],
+                                                 slot_pos=self.slot_pos[l], keep=self.keep_len, seen=self.seen_len,
+                                                 kv_count=eng.kv_count[l], ws=self.evict_ws, **self._cache(l)))
+            eng.launches += 1
+        self.lens = lens
+        for s in range(self.S):
+            for b in range(self.n):
+                while (len(self.pages[s][b]) - 1) * self.page_size >= max(1, lens[s][b]):
+                    self.free.append(self.pages[s][b].pop())
+        self._lengths()
+
+    def _append(self, l: int, tokens: int, **t):
+        """twist_kv_append into layer l's cache, whatever it is held in."""
+        eng, w = self.eng, self.eng.w
+        call, args = (B.twist_kv_append_q8, B.kv_append_q8_args) if self.cache_bits == 8 else (B.twist_kv_append, B.kv_append_args)
+        call(args(w.dtype, self.S, self.n, tokens, eng.head_keep, eng.kv_max, w.d_head, kv_count=eng.kv_count[l], **t, **self._cache(l)))
 
     def prefill(self, k: int, lengths: Optional[Sequence[Sequence[int]]] = None) -> torch.Tensor:
         """The prompts: the engine's forward pass over its batch k.  Sequences must be empty.  Returns the stack's outputs
@@ -1270,10 +1351,16 @@ class DecodeSession:
                 eng._bind(l)
                 # the saved projections are rotated already
                 with eng._timed("append"):
-                    B.twist_kv_append(B.kv_append_args(w.dtype, self.S, self.n, w.tokens, eng.head_keep, eng.kv_max, w.d_head,
-                                                       qkv=eng.qkv_l[l], new_len=self.new_len, kv_count=eng.kv_count[l],
-                                                       **self._cache(l)))
+                    self._append(l, w.tokens, qkv=eng.qkv_l[l], new_len=self.new_len)
                 eng.launches += 1
+                if self.keep is not None:
+                    share = dict(head_idx=eng.idx_head[l], kv_pos=eng.kv_pos[l]) if eng.gqa else {}
+                    with eng._timed("weights"):
+                        B.twist_attn_core_weights(B.attn_core_weights_args(
+                            w.dtype, self.S, self.n, eng.seq_len, eng.head_keep, eng.kv_max, w.d_head, w.n_heads, w.n_kv_heads,
+                            self.last_queries, qkv=eng.qkv_l[l], lse=eng.lse[l], page_table=self.page_table, new_len=self.new_len,
+                            weights=self.weights[l], slot_pos=self.slot_pos[l], plan=eng.plan, **share))
+                    eng.launches += 1
         return eng.x[w.n_layers]
 
     def _ln(self, l: int, which: str, x, y):
@@ -1289,6 +1376,8 @@ class DecodeSession:
         shape = (self.S, self.n, self.eng.w.d_model)
         if tuple(x.shape) != shape:
             raise ValueError("x: expected [%d][%d][%d], got %s" % (*shape, tuple(x.shape)))
+        if self.keep is not None:
+            self.evict(self.slack)
         with self._growing([[1] * self.n for _ in range(self.S)]):
             self.x[0].copy_(x)
             if not self.use_graph:
@@ -1319,13 +1408,31 @@ class DecodeSession:
             q = qkv[..., :eng.a_sub]
             x_a = self._ln(l, "a", cur, self.x_ln) if eng.ln else cur
             B.twist_subnet_attn_proj_fwd(eng._proj_args(B.PROJ_QKV, w.dtype, S, n, d, eng.nq, 1.0, 0.0, in_=x_a, w=eng.w_qkv, out=qkv))
+            rot = dict(rot_dims=w.rot_dims, layout=w.rope_layout, inv_freq=eng.inv_freq, q_out=q)
+            if self.keep is not None and self.cache_bits == 8:
+                rot["seen"] = self.seen_len
+            elif self.keep is not None and w.rot_dims:              # positions run ahead of slots: rotated before, not on the way
+                B.twist_rope_fwd(B.rope_args(w.dtype, S, n, eng.head_keep, eng.kv_max, w.d_head, w.rot_dims, layout=w.rope_layout,
+                                             in_=qkv, out=qkv, inv_freq=eng.inv_freq, pos=self.new_pos))
+                eng.launches += 1
+                rot = {}
             with eng._timed("append"):
-                B.twist_kv_append(B.kv_append_args(w.dtype, S, n, n, eng.head_keep, eng.kv_max, w.d_head, w.rot_dims, w.rope_layout,
-                                                   qkv=qkv, q_out=q, inv_freq=eng.inv_freq, kv_count=eng.kv_count[l], **self._cache(l)))
+                self._append(l, n, qkv=qkv, **rot)
             share = dict(head_idx=eng.idx_head[l], kv_pos=eng.kv_pos[l]) if eng.gqa else {}
+            decode, args = (B.twist_attn_decode_q8, B.attn_decode_q8_args) if self.cache_bits == 8 else (B.twist_attn_decode, B.attn_decode_args)
+            lse = dict(lse=self.lse[kind]) if self.keep is not None else {}
             with eng._timed("decode"):
-                B.twist_attn_decode(B.attn_decode_args(w.dtype, S, n, eng.head_keep, eng.kv_max, w.d_head, w.n_heads, w.n_kv_heads,
-                                                       self.max_len, q=q, out=a, ws=self.ws, **share, **self._cache(l)))
+                decode(args(w.dtype, S, n, eng.head_keep, eng.kv_max, w.d_head, w.n_heads, w.n_kv_heads, self.max_len, q=q, out=a,
+                            ws=self.ws, **lse, **share, **self._cache(l)))
+            if self.keep is not None:
+                cache = self._cache(l)
+                cache.pop("v_cache")
+                with eng._timed("weights"):
+                    B.twist_attn_weights(B.attn_weights_args(
+                        w.dtype, S, n, eng.head_keep, eng.kv_max, w.d_head, w.n_heads, w.n_kv_heads, self.max_len, q=q,
+                        lse=self.lse[kind], seen=self.seen_len, prior=self.weights[l], weights=self.weights[l],
+                        slot_pos=self.slot_pos[l], **share, **cache))
+                eng.launches += 1
             B.twist_subnet_attn_proj_fwd(eng._proj_args(B.PROJ_O, w.dtype, S, n, d, eng.a_sub, eng.alpha_a, 0.0, in_=a, w=eng.w_o,
                                                         out=self.x_mid, out_residual=cur))
             x_f = self._ln(l, "f", self.x_mid, self.x_ln) if eng.ln else self.x_mid
