@@ -511,6 +511,19 @@ def _tensor(name: str, t: torch.Tensor, dtype: torch.dtype, numel: int, dev: int
     return t.data_ptr()
 
 
+def _addresses(dev: int, *specs):
+    """Addresses (0 for None) of tensors given as (name, tensor, dtype, numel), all dense and on the current device."""
+    out = []
+    for name, t, dtype, numel in specs:
+        if t is None:
+            out.append(0)
+        elif t.dtype is dtype and t.numel() == numel and t.get_device() == dev and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            out.append(_tensor(name, t, dtype, numel, dev))
+    return out
+
+
 def _elsewhere(name: str, t: torch.Tensor, dev: int):
     raise ValueError("%s: tensor on %s, current device is cuda:%d" % (name, t.device, dev))
 
@@ -539,11 +552,6 @@ def _cache(k: torch.Tensor, v: torch.Tensor, kv_max: int, d_head: int, dtype: to
     return page, n, strides[0] if n > 1 else max(strides[0], kv_max * page * d_head)
 
 
-def _scales(scales: torch.Tensor, n_pages: int, kv_max: int, page: int, dev: int) -> int:
-    """Address of the scales of an 8-bit cache, fp32 [n_pages][kv_max][page_size / 16][2] (K, V)."""
-    return _tensor("scales", scales, torch.float32, n_pages * kv_max * (page // 16) * 2, dev)
-
-
 def _cache_kind(k: torch.Tensor, scales: Optional[torch.Tensor]) -> int:
     """CACHE_BF16 or CACHE_E4M3, by the cache's type; an 8-bit cache has scales, a bf16 cache none."""
     kind = CACHE_E4M3 if k.dtype is torch.float8_e4m3fn else CACHE_BF16
@@ -560,9 +568,10 @@ _DECODE_PACK = struct.Struct("12i2q11Q")
 _Q8_PACK = struct.Struct("12i2q12Q")
 _WEIGHTS_PACK = struct.Struct("14i2q13Q")
 _EVICT_PACK = struct.Struct("12iq14Q")
+_CORE_WEIGHTS_PACK = struct.Struct("14i9Q")
 assert (_ROPE_PACK.size, _APPEND_PACK.size, _DECODE_PACK.size) == (C.sizeof(RopeArgs), C.sizeof(KvAppendArgs), C.sizeof(AttnDecodeArgs))
-assert (_Q8_PACK.size, _Q8_PACK.size, _WEIGHTS_PACK.size, _EVICT_PACK.size) == (
-    C.sizeof(KvAppendQ8Args), C.sizeof(AttnDecodeQ8Args), C.sizeof(AttnWeightsArgs), C.sizeof(KvEvictArgs))
+assert (_Q8_PACK.size, _Q8_PACK.size, _WEIGHTS_PACK.size, _EVICT_PACK.size, _CORE_WEIGHTS_PACK.size) == (
+    C.sizeof(KvAppendQ8Args), C.sizeof(AttnDecodeQ8Args), C.sizeof(AttnWeightsArgs), C.sizeof(KvEvictArgs), C.sizeof(AttnCoreWeightsArgs))
 
 
 def rope_args(dtype, n_subnets, tokens, head_keep, kv_max, d_head, rot_dims, seq_len=0, layout=ROPE_HALF, *, in_, out,
@@ -688,36 +697,23 @@ def kv_append_q8_args(dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_hea
     page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head, torch.float8_e4m3fn)
     if k_cache.get_device() != dev or v_cache.get_device() != dev or (q_out is not None and q_out.get_device() != dev):
         _elsewhere("k_cache / v_cache / q_out", k_cache, dev)
-    seqs, n = n_subnets * n_seqs, n_subnets * tokens * (head_keep + 2 * kv_max) * d_head
-    max_pages = page_table.shape[-1]
-    if not (qkv.dtype is bf and qkv.numel() == n and qkv.is_contiguous() and qkv.get_device() == dev
-            and page_table.dtype is i32 and page_table.numel() == seqs * max_pages and page_table.is_contiguous()
-            and page_table.get_device() == dev
-            and kv_len.dtype is i32 and kv_len.numel() == seqs and kv_len.is_contiguous() and kv_len.get_device() == dev):
-        _tensor("qkv", qkv, bf, n, dev)
-        _tensor("page_table", page_table, i32, seqs * max_pages, dev)
-        _tensor("kv_len", kv_len, i32, seqs, dev)
+    seqs, max_pages, f32 = n_subnets * n_seqs, page_table.shape[-1], torch.float32
+    at_qkv, at_scales, at_table, at_len, at_seen, at_begin, at_new, at_count, at_freq = _addresses(
+        dev, ("qkv", qkv, bf, n_subnets * tokens * (head_keep + 2 * kv_max) * d_head), ("scales", scales, f32, n_pages * kv_max * (page // 16) * 2),
+        ("page_table", page_table, i32, seqs * max_pages), ("kv_len", kv_len, i32, seqs), ("seen", seen, i32, seqs),
+        ("new_begin", new_begin, i32, n_subnets * (n_seqs + 1)), ("new_len", new_len, i32, seqs), ("kv_count", kv_count, i32, n_subnets),
+        ("inv_freq", inv_freq, torch.float64, rot_dims // 2))
     a = KvAppendQ8Args.from_buffer_copy(_Q8_PACK.pack(
         dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head, page, n_pages, max_pages, rot_dims, layout, stride,
-        0 if q_out is None else _rows("q_out", q_out, n_subnets, tokens, head_keep * d_head), qkv.data_ptr(),
-        0 if q_out is None else q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _scales(scales, n_pages, kv_max, page, dev),
-        page_table.data_ptr(), kv_len.data_ptr(), 0 if seen is None else _tensor("seen", seen, i32, seqs, dev),
-        0 if new_begin is None else _tensor("new_begin", new_begin, i32, n_subnets * (n_seqs + 1), dev),
-        0 if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
-        0 if kv_count is None else _tensor("kv_count", kv_count, i32, n_subnets, dev),
-        0 if inv_freq is None else _tensor("inv_freq", inv_freq, torch.float64, rot_dims // 2, dev)))
+        0 if q_out is None else _rows("q_out", q_out, n_subnets, tokens, head_keep * d_head), at_qkv,
+        0 if q_out is None else q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), at_scales, at_table, at_len, at_seen, at_begin,
+        at_new, at_count, at_freq))
     a._keepalive = (qkv, q_out, k_cache, v_cache, scales, page_table, kv_len, seen, new_begin, new_len, kv_count, inv_freq)
     return a
 
 
 def twist_kv_append_q8(a: KvAppendQ8Args):
     _check(lib().twist_kv_append_q8(C.byref(a), _stream()), "twist_kv_append_q8")
-
-
-def _shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev):
-    """Addresses of the two index arrays of grouped-query sharing (0 without)."""
-    return (0 if head_idx is None else _tensor("head_idx", head_idx, torch.int32, n_subnets * head_keep, dev),
-            0 if kv_pos is None else _tensor("kv_pos", kv_pos, torch.int32, n_subnets * n_kv_heads, dev))
 
 
 def attn_decode_q8_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads=0, n_kv_heads=0, max_len=0, *, q, k_cache,
@@ -729,22 +725,15 @@ def attn_decode_q8_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_h
     page, n_pages, stride = _cache(k_cache, v_cache, kv_max, d_head, torch.float8_e4m3fn)
     if k_cache.get_device() != dev or v_cache.get_device() != dev or q.get_device() != dev or ws.get_device() != dev:
         _elsewhere("k_cache / v_cache / q / ws", k_cache, dev)
-    seqs, width = n_subnets * n_seqs, head_keep * d_head
-    max_pages = page_table.shape[-1]
-    if not (page_table.dtype is i32 and page_table.numel() == seqs * max_pages and page_table.is_contiguous()
-            and page_table.get_device() == dev
-            and kv_len.dtype is i32 and kv_len.numel() == seqs and kv_len.is_contiguous() and kv_len.get_device() == dev
-            and out.dtype is bf and out.numel() == seqs * width and out.is_contiguous() and out.get_device() == dev):
-        _tensor("page_table", page_table, i32, seqs * max_pages, dev)
-        _tensor("kv_len", kv_len, i32, seqs, dev)
-        _tensor("out", out, bf, seqs * width, dev)
+    seqs, width, max_pages, f32 = n_subnets * n_seqs, head_keep * d_head, page_table.shape[-1], torch.float32
+    at_scales, at_table, at_len, at_heads, at_pos, at_out, at_lse = _addresses(
+        dev, ("scales", scales, f32, n_pages * kv_max * (page // 16) * 2), ("page_table", page_table, i32, seqs * max_pages),
+        ("kv_len", kv_len, i32, seqs), ("head_idx", head_idx, i32, n_subnets * head_keep), ("kv_pos", kv_pos, i32, n_subnets * n_kv_heads),
+        ("out", out, bf, seqs * width), ("lse", lse, f32, seqs * head_keep))
     a = AttnDecodeQ8Args.from_buffer_copy(_Q8_PACK.pack(
         dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, max_len, stride,
-        _rows("q", q, n_subnets, n_seqs, width), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-        _scales(scales, n_pages, kv_max, page, dev), page_table.data_ptr(), kv_len.data_ptr(),
-        *_shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev), out.data_ptr(),
-        0 if lse is None else _tensor("lse", lse, torch.float32, seqs * head_keep, dev), ws.data_ptr(),
-        ws.numel() * ws.element_size()))
+        _rows("q", q, n_subnets, n_seqs, width), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), at_scales, at_table, at_len, at_heads,
+        at_pos, at_out, at_lse, ws.data_ptr(), ws.numel() * ws.element_size()))
     a._keepalive = (q, k_cache, v_cache, scales, page_table, kv_len, out, ws, head_idx, kv_pos, lse)
     return a
 
@@ -766,16 +755,14 @@ def attn_weights_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_hea
     if k_cache.get_device() != dev or q.get_device() != dev:
         _elsewhere("k_cache / q", k_cache, dev)
     seqs, max_pages, slots = n_subnets * n_seqs, page_table.shape[-1], n_pages * kv_max * page
+    at = _addresses(
+        dev, ("lse", lse, f32, seqs * head_keep), ("scales", scales, f32, n_pages * kv_max * (page // 16) * 2),
+        ("page_table", page_table, i32, seqs * max_pages), ("kv_len", kv_len, i32, seqs), ("new_len", new_len, i32, seqs), ("seen", seen, i32, seqs),
+        ("head_idx", head_idx, i32, n_subnets * head_keep), ("kv_pos", kv_pos, i32, n_subnets * n_kv_heads), ("prior", prior, f32, slots),
+        ("weights", weights, f32, slots), ("slot_pos", slot_pos, i32, slots))
     a = AttnWeightsArgs.from_buffer_copy(_WEIGHTS_PACK.pack(
         dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, max_len, kind, 0, stride,
-        _rows("q", q, n_subnets, n_seqs, head_keep * d_head), q.data_ptr(), _tensor("lse", lse, f32, seqs * head_keep, dev),
-        k_cache.data_ptr(), 0 if scales is None else _scales(scales, n_pages, kv_max, page, dev),
-        _tensor("page_table", page_table, i32, seqs * max_pages, dev), _tensor("kv_len", kv_len, i32, seqs, dev),
-        0 if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
-        0 if seen is None else _tensor("seen", seen, i32, seqs, dev),
-        *_shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev),
-        0 if prior is None else _tensor("prior", prior, f32, slots, dev), _tensor("weights", weights, f32, slots, dev),
-        0 if slot_pos is None else _tensor("slot_pos", slot_pos, i32, slots, dev)))
+        _rows("q", q, n_subnets, n_seqs, head_keep * d_head), q.data_ptr(), at[0], k_cache.data_ptr(), *at[1:]))
     a._keepalive = (q, lse, k_cache, scales, page_table, kv_len, new_len, seen, head_idx, kv_pos, prior, weights, slot_pos)
     return a
 
@@ -795,14 +782,14 @@ def attn_core_weights_args(dtype, n_subnets, n_seqs, seq_len, head_keep, kv_max,
         raise ValueError("weights: expected fp32 [pages][%d][page_size], got %s" % (kv_max, tuple(weights.shape)))
     n_pages, _, page = weights.shape
     seqs, max_pages, tokens = n_subnets * n_seqs, page_table.shape[-1], n_subnets * n_seqs * seq_len
-    a = AttnCoreWeightsArgs(
-        dtype, n_subnets, n_seqs, seq_len, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, last_queries, 0,
-        _tensor("qkv", qkv, torch.bfloat16, tokens * (head_keep + 2 * kv_max) * d_head, dev),
-        _tensor("lse", lse, f32, tokens * head_keep, dev), _tensor("page_table", page_table, i32, seqs * max_pages, dev),
-        None if new_len is None else _tensor("new_len", new_len, i32, seqs, dev),
-        *(x or None for x in _shared_heads(head_idx, kv_pos, n_subnets, head_keep, n_kv_heads, dev)),
-        _tensor("weights", weights, f32, n_pages * kv_max * page, dev),
-        None if slot_pos is None else _tensor("slot_pos", slot_pos, i32, n_pages * kv_max * page, dev), _plan_ptr(plan))
+    at = _addresses(
+        dev, ("qkv", qkv, torch.bfloat16, tokens * (head_keep + 2 * kv_max) * d_head), ("lse", lse, f32, tokens * head_keep),
+        ("page_table", page_table, i32, seqs * max_pages), ("new_len", new_len, i32, seqs), ("head_idx", head_idx, i32, n_subnets * head_keep),
+        ("kv_pos", kv_pos, i32, n_subnets * n_kv_heads), ("weights", weights, f32, n_pages * kv_max * page),
+        ("slot_pos", slot_pos, i32, n_pages * kv_max * page))
+    a = AttnCoreWeightsArgs.from_buffer_copy(_CORE_WEIGHTS_PACK.pack(
+        dtype, n_subnets, n_seqs, seq_len, head_keep, kv_max, d_head, n_heads, n_kv_heads, page, n_pages, max_pages, last_queries, 0, *at,
+        _plan_ptr(plan) or 0))
     a._keepalive = (qkv, lse, page_table, new_len, head_idx, kv_pos, weights, slot_pos, plan)
     return a
 
@@ -826,14 +813,14 @@ def kv_evict_args(dtype, n_subnets, n_seqs, kv_max, d_head, recent, max_len=0, *
     seqs, max_pages, slots = n_subnets * n_seqs, page_table.shape[-1], n_pages * kv_max * page
     weights_out = weights if weights_out is None else weights_out
     slot_pos_out = slot_pos if slot_pos_out is None else slot_pos_out
+    at = _addresses(
+        dev, ("scales", scales, f32, n_pages * kv_max * (page // 16) * 2), ("page_table", page_table, i32, seqs * max_pages),
+        ("kv_len", kv_len, i32, seqs), ("keep", keep, i32, seqs), ("seen", seen, i32, seqs), ("kv_count", kv_count, i32, n_subnets),
+        ("weights", weights, f32, slots), ("slot_pos", slot_pos, i32, slots), ("weights_out", weights_out, f32, slots),
+        ("slot_pos_out", slot_pos_out, i32, slots))
     a = KvEvictArgs.from_buffer_copy(_EVICT_PACK.pack(
         dtype, n_subnets, n_seqs, kv_max, d_head, page, n_pages, max_pages, max_len, recent, kind, 0, stride, k_cache.data_ptr(),
-        v_cache.data_ptr(), 0 if scales is None else _scales(scales, n_pages, kv_max, page, dev),
-        _tensor("page_table", page_table, i32, seqs * max_pages, dev), _tensor("kv_len", kv_len, i32, seqs, dev),
-        _tensor("keep", keep, i32, seqs, dev), 0 if seen is None else _tensor("seen", seen, i32, seqs, dev),
-        0 if kv_count is None else _tensor("kv_count", kv_count, i32, n_subnets, dev), _tensor("weights", weights, f32, slots, dev),
-        _tensor("slot_pos", slot_pos, i32, slots, dev), _tensor("weights_out", weights_out, f32, slots, dev),
-        _tensor("slot_pos_out", slot_pos_out, i32, slots, dev), ws.data_ptr(), ws.numel() * ws.element_size()))
+        v_cache.data_ptr(), *at, ws.data_ptr(), ws.numel() * ws.element_size()))
     a._keepalive = (k_cache, v_cache, scales, page_table, kv_len, keep, seen, kv_count, weights, slot_pos, weights_out, slot_pos_out, ws)
     return a
 

@@ -152,10 +152,12 @@ def test_layout_checks_of_the_python_side(B):
         B._cache(pool[:, 0], pool[:, 1], 3, 32)                       # an 8-bit cache is no bf16 cache
     with pytest.raises(ValueError):
         B._cache(pool[:, 0].float(), pool[:, 1].float(), 3, 32, f8)
-    with pytest.raises(ValueError):
-        B._scales(torch.zeros(5, 3, 1), 5, 3, 16, -1)                 # K's and V's side by side are expected
-    with pytest.raises(ValueError):
-        B._scales(torch.zeros(5, 3, 1, 2, dtype=torch.float64), 5, 3, 16, -1)
+    f32 = torch.float32
+    assert B._addresses(-1, ("seen", None, f32, 30), ("scales", pool.float(), f32, pool.numel()))[0] == 0
+    with pytest.raises(ValueError, match="scales"):
+        B._addresses(-1, ("seen", None, f32, 30), ("scales", torch.zeros(5, 3, 1), f32, 30))    # K's and V's side by side are expected
+    with pytest.raises(ValueError, match="scales"):
+        B._addresses(-1, ("scales", torch.zeros(5, 3, 1, 2, dtype=torch.float64), f32, 30))
     assert B._cache_kind(pool, torch.zeros(1)) == B.CACHE_E4M3 and B._cache_kind(pool.float().bfloat16(), None) == B.CACHE_BF16
     with pytest.raises(ValueError):
         B._cache_kind(pool, None)
