@@ -543,14 +543,15 @@ int32_t twist_attn_decode(const twist_attn_decode_args* a /*host*/, void* stream
  * twist_kv_append_q8 -- twist_kv_append into such a cache.  The scale of a block is the smallest power of two 2^e, -110 <= e <=
  * 119, whose 448-fold is not below the largest finite magnitude of the block's new tokens; if the block holds tokens before the
  * new ones, it is not below the scale that they have either, and where it grows they are rounded again (a power of two only
- * costs bits of numbers that become subnormal: a token keeps four significant bits down to 2^-6 of the scale).  K is rotated in fp32
- * and rounded once.  Infinities and NaN are stored as NaN.
+ * costs bits of numbers that become subnormal: a token keeps four significant bits down to 2^-6 of the scale).  A scale that the call
+ * finds there and that is no such power of two counts as the next one above.  K is rotated in fp32 and rounded once.  Infinities
+ * and NaN are stored as NaN.
  *   seen (device int32 [S][n_seqs] or NULL): tokens of the sequence so far, the new ones included, where evictions have made
  *   the cache shorter than the sequence: new token i of n goes to slot kv_len[s][b] - n + i and is rotated by position
  *   seen[s][b] - n + i.  NULL: slots are positions.
- * Everything else is as in twist_kv_append.  Index data is checked on the device, by blocks: tokens of a sequence with seen <
- * kv_len, fewer cached tokens than new ones, or more of either than the table has slots are skipped, as are tokens whose page lies
- * outside the pool; TWIST_ERR_BAD_INDEX is recorded.
+ * Everything else is as in twist_kv_append; the new tokens of two sequences must not share a block either.  Index data is checked on
+ * the device, by blocks: tokens of a sequence with seen < kv_len, fewer cached tokens than new ones, or more of either than the
+ * table has slots are skipped, as are tokens whose page lies outside the pool; TWIST_ERR_BAD_INDEX is recorded.
  * dtype (of qkv and q_out) TWIST_BF16 only; d_head in {16, 32, 64, 128}. */
 typedef struct {
   int32_t dtype, n_subnets, n_seqs, tokens, head_keep, kv_max, d_head;
@@ -601,6 +602,7 @@ int32_t twist_attn_decode_q8(const twist_attn_decode_q8_args* a /*host*/, void* 
 
 /* The attention weight that a cached token has gathered, weights [n_pages][kv_max][page_size] fp32, and its position in the
  * sequence, slot_pos [n_pages][kv_max][page_size] int32: for each KV position on its own, in the places of the token's K and V.
+ * The calls that write them, and twist_kv_evict, want every page once: one that two sequences share may only be read.
  *
  * twist_attn_weights -- adds what one step's queries gave:
  *     weights[j] = (new token: 0, else prior[j]) + sum_h exp(q_h . k_j / sqrt(d_head) - lse_h)   over the heads that read the position,

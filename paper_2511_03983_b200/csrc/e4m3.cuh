@@ -15,6 +15,12 @@ __device__ inline float scale_for(float top) {
   const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);          // 448 = 1.75 * 2^8
   return __uint_as_float((uint32_t)(min(max(e, kScaleLow), kScaleHigh) + 127) << 23);
 }
+// The power of two in that range which counts for a block's old scale: the next one from it on; what is not positive counts for nothing.
+__device__ inline float scale_above(float old) {
+  const uint32_t u = __float_as_uint(old);
+  const int e = old > 0.f ? (int)(u >> 23) - 127 + ((u & 0x7fffffu) != 0) : kScaleLow;
+  return __uint_as_float((uint32_t)(min(max(e, kScaleLow), kScaleHigh) + 127) << 23);
+}
 // 1 / scale for a power of two in that range (exact).
 __device__ inline float inverse_scale(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
 

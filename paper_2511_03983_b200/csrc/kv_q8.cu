@@ -241,7 +241,7 @@ constexpr uint32_t kInfinity = 0x7f800000u;
 // take part, this one is number `lane` of them.
 template <int D>
 __device__ inline float rescale(uint8_t* cache, float* scale, float old, float top, int first, int lane, int lanes) {
-  const float now = fmaxf(scale_for(top), old);       // a NaN for an old scale counts for nothing
+  const float now = fmaxf(scale_for(top), scale_above(old));
   if (first > 0 && now != old) {
     const float f = old * inverse_scale(now);
     for (int k = lane; k < first * D / 8; k += lanes) {

@@ -248,6 +248,37 @@ def test_append_rotated(B, D, rot, layout, page, H, KV, form):
     assert torch.equal(same[~own], dx[~own])
 
 
+@pytest.mark.parametrize("form", ["one", "padded"])
+@pytest.mark.parametrize("D", [16, 64, 128])
+def test_append_to_blocks_of_any_scale(B, D, form):
+    """A block whose scale is no power of two (another program's): the next power of two counts, its tokens are rounded to the new scale."""
+    gen = torch.Generator().manual_seed(D)
+    olds = [1.5 * 2.0 ** -3, 3.7, 2.0 ** -2, 0.3, 1e-3, 1.0000001, 5e-36]
+    n, KV, page, held = len(olds), 2, 16, 5
+    fresh = 1 if form == "one" else 6
+    k, v, scales = pools(gen, n, KV, page, D)
+    scales[:] = torch.tensor(olds, dtype=torch.float32, device="cuda")[:, None, None, None] * torch.tensor([1.0, 1.25], device="cuda")
+    before = [f64(k), f64(v)]
+    old = host(scales)
+    x = (torch.randn(1, n * fresh, 3 * KV * D, generator=gen) * 20).to(BF)
+    call_append(B, 1, n, n * fresh, KV, KV, D, 0, 0, qkv=x.cuda(), q_out=None, k_cache=k, v_cache=v, scales=scales,
+                page_table=i32([[[b] for b in range(n)]]), kv_len=i32([[held + fresh] * n]))
+    assert B.twist_device_status() == 0
+    new = host(scales)
+    rows = host(x).reshape(n, fresh, 3 * KV, D)
+    for b in range(n):
+        for g in range(KV):
+            for which, cache in enumerate((k, v)):
+                part = rows[b, :, KV + which * KV + g]
+                was = old[b, g, 0, which]
+                s = max(need(np.abs(part).max()), 2.0 ** max(-110, math.ceil(math.log2(was))))
+                assert new[b, g, 0, which] == s
+                got = f64(cache)[b, g]
+                assert np.array_equal(got[held:held + fresh], code(part, s))
+                mine = (before[which][b, g, :held].astype(np.float32) * np.float32(was / s)).astype(np.float64)
+                assert np.array_equal(got[:held], code(mine, 1.0))
+
+
 def test_append_bad_index_data_is_skipped_and_reported(B):
     gen = torch.Generator().manual_seed(5)
     S, n, H, KV, D, page = 1, 4, 2, 1, 64, 16
