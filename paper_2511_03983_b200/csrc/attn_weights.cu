@@ -180,8 +180,8 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
     prefetch_q<D, B>(qbuf[warp], p, x.seq, col[g], lane);
     const int h0 = col[2 * t], h1 = col[2 * t + 1];
     const float* lse = w.lse + (long long)x.s * p.heads * p.n_seqs + (x.seq - x.s * p.n_seqs);
-    a.l0 = h0 >= 0 ? lse[(long long)h0 * p.n_seqs] : INFINITY;
-    a.l1 = h1 >= 0 ? lse[(long long)h1 * p.n_seqs] : INFINITY;
+    a.l0 = h0 >= 0 ? lse[(long long)h0 * p.n_seqs] : 0.f;
+    a.l1 = h1 >= 0 ? lse[(long long)h1 * p.n_seqs] : 0.f;
     a.fresh = w.new_len ? w.new_len[x.seq] : min(1, x.len);
     a.seen = w.seen ? w.seen[x.seq] : x.len;
     return a;
@@ -200,7 +200,8 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
     if (since >= 2) wait_copies_but<2>();
     else wait_copies();
     take_q<D, B>(q, qbuf[warp], lane);
-    const bool none = cols[warp][buf][0] < 0;
+    // columns without a head have zeros for a query, which give NaN where a key is infinite
+    const bool none = cols[warp][buf][0] < 0, has0 = cols[warp][buf][2 * t] >= 0, has1 = cols[warp][buf][2 * t + 1] >= 0;
     const Unit next = following(now);
     Ask then = mine;
     if (next.seq >= 0) then = ask(next, cols[warp][buf ^ 1]);
@@ -222,8 +223,8 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
           float sc[4];
           take_keys<D, B>(x, ring.tile[slot].k + 16 * D * B * s, g, t);
           step_scores<D, B>(sc, x, q, B == 1 ? ring.scale[slot][s].x : 1.f);
-          a[2 * s] = weight_of(sc[0], w.scale, mine.l0) + weight_of(sc[1], w.scale, mine.l1);
-          a[2 * s + 1] = weight_of(sc[2], w.scale, mine.l0) + weight_of(sc[3], w.scale, mine.l1);
+          a[2 * s] = (has0 ? weight_of(sc[0], w.scale, mine.l0) : 0.f) + (has1 ? weight_of(sc[1], w.scale, mine.l1) : 0.f);
+          a[2 * s + 1] = (has0 ? weight_of(sc[2], w.scale, mine.l0) : 0.f) + (has1 ? weight_of(sc[3], w.scale, mine.l1) : 0.f);
         }
         // over the four threads of a row, so that each ends with sums of its own: SUB = 4 both of step t, 2 one of step t / 2, 1 one
         // for two threads

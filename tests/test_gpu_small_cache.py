@@ -600,6 +600,34 @@ def test_weights_bad_index_data(B):
     assert call() == 0
 
 
+@pytest.mark.parametrize("D", [8, 16, 64, 128])
+def test_weights_of_keys_that_are_not_finite(B, D):
+    """A key with an infinity in a bf16 cache gives what its heads' scores say (here all of them -inf: nothing), also where fewer than
+    eight heads read it; a NaN gives NaN, and neither touches other keys."""
+    gen = torch.Generator().manual_seed(D)
+    H, page, m = 3, 16, 40
+    k = torch.randn(3, 1, page, D, generator=gen).to(BF)
+    k[0, 0, 5, 0] = float("inf")
+    k[1, 0, 7, 1] = float("nan")
+    q = torch.randn(1, 1, H, D, generator=gen).to(BF)
+    q[..., 0] = -1.0
+    weights, lse = torch.full((3, 1, page), -3.0, device="cuda"), torch.full((1, H, 1), 2.0, device="cuda")
+    B.twist_attn_weights(B.attn_weights_args(
+        B.BF16, 1, 1, H, 1, D, H, 1, q=q.view(1, 1, H * D).cuda(), lse=lse, k_cache=k.cuda(), page_table=i32([[[0, 1, 2]]]), kv_len=i32([[m]]),
+        head_idx=i32([[0, 1, 2]]), kv_pos=i32([[0]]), weights=weights))
+    got, x, y = host(weights).reshape(-1), host(q)[0, 0], host(k).reshape(-1, D)[:m]
+    with np.errstate(invalid="ignore"):
+        s = x @ y.T / math.sqrt(D)
+        want = np.exp(s - 2.0).sum(0)
+        e = (D + 4) * 2.0 ** -23 * (np.abs(x) @ np.abs(y).T) / math.sqrt(D) + 2.0 ** -22 * np.abs(s - 2.0) + 2.0 ** -21
+        bound = (np.exp(s - 2.0) * e).sum(0) + (H + 1) * 2.0 ** -24 * want
+    assert got[5] == 0.0 and np.isnan(got[16 + 7])
+    fine = [j for j in range(m) if j not in (5, 16 + 7)]
+    assert np.all(np.abs(got[fine] - want[fine]) <= bound[fine])
+    assert np.all(got[m:] == -3.0)
+    assert B.twist_device_status() == 0
+
+
 # ------------------------------------------------------------------------------------------------ prompts
 
 @pytest.mark.parametrize("last", [0, 1, 50])
