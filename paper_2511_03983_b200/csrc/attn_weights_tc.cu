@@ -67,8 +67,16 @@ __device__ inline f32x2 add2(f32x2 a, f32x2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// 2^t without the special-function unit, t <= 64 or so: t = n + f with n whole and |f| <= 1/2, 2^f by the polynomial of degree 5 of
-// least relative error there (7.5e-8, by Remez exchange), n into the exponent.  What is below 2^-126 comes out as 2^-126.
+// Barrier of the exponential warps; whether any of their threads says so.
+__device__ inline bool sync_any(bool mine) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(r) : "r"((uint32_t)mine), "n"(32 * kEw) : "memory");
+  return r != 0;
+}
+// 2^t without the special-function unit, t a number and t <= 64 or so: t = n + f with n whole and |f| <= 1/2, 2^f by the polynomial
+// of degree 5 of least relative error there (7.5e-8, by Remez exchange), n into the exponent.  What is below 2^-126 comes out as
+// 2^-126.
 __device__ inline f32x2 exp2_poly(f32x2 t) {
   float a, b;
   split(t, a, b);
@@ -215,9 +223,14 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
         ahead[j] = c0 * kBlock + q < len ? -lse[q] : 0.f;
       }
     };
+    bool odd;                                                            // a log-sum-exp that is not finite: the polynomial is not for those
     auto stage = [&](int to) {
+      odd = false;
 #pragma unroll
-      for (int j = 0; j < STAGED; ++j) lse_s[to][32 * kEw * j + threadIdx.x] = ahead[j];
+      for (int j = 0; j < STAGED; ++j) {
+        lse_s[to][32 * kEw * j + threadIdx.x] = ahead[j];
+        odd |= !(fabsf(ahead[j]) < INFINITY);
+      }
     };
     fetch(0, i0);
     stage(0);
@@ -227,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
     int n = 0, chunk = 0;
     for (int head = 0, c0 = i0; head < n_list_s; ++chunk) {           // a warp that gave up still meets the others
       // the chunk's statistics are there, and nobody reads those of the one before
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * kEw) : "memory");
+      const bool plain = !sync_any(odd);
       const int last = min(c0 + kChunk, end), next_c0 = last == end ? i0 : last, next_head = head + (last == end);
       fetch(next_head, next_c0);
       const float* lse = lse_s[chunk & 1] + kCols * part;
@@ -260,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
             if (c + 32 < kCols) tc_wait_ld();
           }
         };
-        if (i * kBlock < max(first, (kb + 1) * kBlock) || (i + 1) * kBlock > len) unit(std::true_type{});
+        if (!plain || i * kBlock < max(first, (kb + 1) * kBlock) || (i + 1) * kBlock > len) unit(std::true_type{});
         else unit(std::false_type{});
         float x, y;
         split(add2(add2(sum4[0], sum4[1]), add2(sum4[2], sum4[3])), x, y);

@@ -694,6 +694,38 @@ def test_core_weights(B, D, page, S, n, N, H, NH, NKV, last):
     assert np.all(got[~written] == -3.0) and np.all(where[~written] == -9)
 
 
+@pytest.mark.parametrize("row", [400, 401, 403, 640, 1100])
+@pytest.mark.parametrize("D", [16, 64, 128])
+def test_core_weights_of_a_query_that_is_not_a_number(B, D, row):
+    """Its head's keys up to it are NaN, the keys behind it and the other position's are not."""
+    gen = torch.Generator().manual_seed(D)
+    N, page = 1200, 64
+    x = torch.randn(1, N, 6 * D, generator=gen).to(BF)
+    x[0, row, 3] = float("nan")                                 # of head 0
+    z = host(x)[0]
+    lse = torch.empty(1, 2, N)
+    want = np.zeros((2, N))
+    for h in range(2):
+        with np.errstate(invalid="ignore"):
+            y = z[:, h * D:(h + 1) * D] @ z[:, (2 + h) * D:(3 + h) * D].T / math.sqrt(D)
+            y[np.triu_indices(N, 1)] = -np.inf
+            l = np.log(np.exp(y).sum(1))                        # the scores are small
+            want[h] = np.where(np.tril(np.ones((N, N))) > 0, np.exp(y - l[:, None]), 0).sum(0)
+        lse[0, h] = torch.from_numpy(l).float()
+    pages = -(-N // page)
+    weights = torch.full((pages, 2, page), -3.0, device="cuda")
+    B.twist_attn_core_weights(B.attn_core_weights_args(
+        B.BF16, 1, 1, N, 2, 2, D, qkv=x.cuda(), lse=lse.cuda(), page_table=i32([[list(range(pages))]]), weights=weights,
+        slot_pos=torch.zeros(weights.shape, dtype=torch.int32, device="cuda")))
+    got = host(weights).transpose(1, 0, 2).reshape(2, -1)[:, :N]
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.isnan(want).sum() == row + 1
+    fine = ~np.isnan(want)
+    # scores below 16 in magnitude: the tolerance of a weight's terms, with sum |q k| / sqrt(d) <= 6 sqrt(d) for these numbers
+    bound = (D + 4) * 2.0 ** -23 * 6 * math.sqrt(D) + 2.0 ** -22 * 32 + 2.0 ** -21 + N * 2.0 ** -24
+    assert np.all(np.abs(got - want)[fine] <= bound * want[fine])
+    assert B.twist_device_status() == 0
+
+
 # ------------------------------------------------------------------------------------------------ eviction
 
 def evict64(num, scales, w, pos, table, lens, keeps, seens, recent, held, page, q8):
