@@ -7,11 +7,16 @@
 //
 // One cluster of 1 to 8 CTAs per (sequence, KV position); its warps take contiguous runs of slots.
 //  1. A 32-bit key for each slot that orders as the tokens rank (protected tokens highest), kept in shared memory where it fits.
-//  2. The keep-th largest key by radix selection, 11 + 11 + 10 bits: histograms in shared memory, added over the cluster.
-//  3. Equal keys are admitted in the order of slots: a running count over the runs.  Then every warp knows who stays:
+//  2. The keep-th largest key by radix selection, 11 + 11 + 10 bits: histograms in shared memory, added over the cluster.  Once its
+//     bin holds few keys they are compared with each other, with their slots behind them (equal keys rank by slot).
+//  3. Many equal keys are admitted in the order of slots: a running count over the runs.  Then every warp knows who stays:
 //     bits to the workspace, with the number of free slots before each 32 and the list of the tokens that move.
-//  4. A warp takes 16 destination slots at a time (a block of the 8-bit cache, whose rows share a scale).  The block that
-//     `keep` cuts holds sources too; an 8-bit cache rescales it last, when they have been read.
+//  4. bf16: the rows that move, in turn.  8 bits: the blocks of 16 slots that take tokens in, whose rows share a scale, are coded anew,
+//     a warp a block.  The block that `keep` cuts holds sources too: it is last, when they have been read.
+//
+// Bound by the latency of these phases where a cache is a page over its budget (256 items of 1040 slots, d = 64 in 8 bits: 12.6 us of
+// 0.7 us of bytes; all three passes of the selection and a warp for every 64 slots in 4., moved or not: 19.3), by it and the
+// scattered rows for long prompts (64 items of up to 16000, d = 128 in bf16: 54 us, of which the moves are 28).
 #include <cooperative_groups.h>
 
 #include "e4m3.cuh"
@@ -26,11 +31,13 @@ constexpr int kKeyCache = 20480;          // keys that a CTA keeps in shared mem
 constexpr int kMaxEvictCluster = 8, kSlotsPerCta = 1024;
 constexpr int kLocalLen = 4096;           // longest sequence whose lists a CTA keeps there
 constexpr int kTableCache = 1024;         // page ids that a CTA keeps there
+// Candidates for the threshold that are compared with each other.  The long prompts above: 512 63 us, 256 58, 128 58.
+constexpr int kDirect = 256;
 
 struct EvictParams {
   uint8_t* k;                  // pages page_bytes apart
   uint8_t* v;
-  float* scales;               // [n_pages][kv][page / 16][2]
+  float2* scales;              // (K, V) [n_pages][kv][page / 16]
   const int32_t *table, *len, *keep, *seen, *kv_count;
   const float* weights;
   const int32_t* slot_pos;
@@ -70,15 +77,13 @@ struct Slots {
 __device__ inline long long row_of(const EvictParams& p, const Slots& sl, int slot) {
   return sl.page(slot) * p.page_bytes + ((sl.base << p.page_shift) + sl.offset(slot)) * p.row_bytes;
 }
-__device__ inline float* scale_at(const EvictParams& p, const Slots& sl, int slot, int which) {
-  return p.scales + 2 * ((((long long)sl.page(slot) * p.kv + sl.base) << (p.page_shift - 4)) + (sl.offset(slot) >> 4)) + which;
+__device__ inline float2* scale_at(const EvictParams& p, const Slots& sl, int slot) {
+  return p.scales + ((((long long)sl.page(slot) * p.kv + sl.base) << (p.page_shift - 4)) + (sl.offset(slot) >> 4));
 }
 
-// Sources of the 16 slots of a block, one per lane (of the first 16): itself, a token that moves, or -1 for a slot behind `end`.
-__device__ inline int source_of(const int32_t* bits, const int32_t* before, const int32_t* movers, int slot0, int keep, int end, int lane) {
-  const int slot = slot0 + (lane & 15), grp = slot >> 5, bit = slot & 31;
-  if (slot >= end) return -1;
-  if (slot >= keep) return slot;
+// The slot whose token goes to a slot below keep: itself, or one that moves.
+__device__ inline int source_of(const int32_t* bits, const int32_t* before, const int32_t* movers, int slot, int keep) {
+  const int grp = slot >> 5, bit = slot & 31;
   const uint32_t stay = (uint32_t)bits[grp];
   if (stay >> bit & 1) return slot;
   const uint32_t live = (2u << min(31, keep - 1 - 32 * grp)) - 1;      // slots of the 32 that are below keep
@@ -137,60 +142,82 @@ __device__ inline void move_rows(const EvictParams& p, const Slots& sl, const in
   }
 }
 
+// The largest magnitude of 16 e4m3 numbers, a NaN counting for nothing: magnitudes order as their bits do.
+__device__ inline float largest(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t most = 0;                                                   // two at a time
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = __vmaxu2(most, __vmaxu2(w[i] & 0x007f007fu, w[i] >> 8 & 0x007f007fu));
+  most = max(most & 0xffffu, most >> 16);
+  float a[4];
+  if (most < 0x7f) {
+    widen4(a, most);
+    return a[0];
+  }
+  float m = 0.f;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    widen4(a, i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+    m = fmaxf(fmaxf(m, fmaxf(fabsf(a[0]), fabsf(a[1]))), fmaxf(fabsf(a[2]), fabsf(a[3])));
+  }
+  return m;
+}
+
 // A block of an 8-bit cache that takes tokens in: all its rows coded anew with the scale that they need.
 template <int D>
 __device__ inline void move_block(const EvictParams& p, const Slots& sl, int slot0, int from, int lane) {
   constexpr int CH = D / 16, N = D >= 32 ? D / 32 : 1;               // pieces of 16 numbers of a row, of a lane
+  uint4 x[2][N];
+  float scale[2][N], top[2] = {0.f, 0.f};
+  int src[N];
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    uint8_t* cache = which ? p.v : p.k;
-    uint4 x[N];
-    float scale[N], top = 0.f;
-    int src[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int k = 32 * j + lane, r = k / CH, c = k % CH;
-      src[j] = __shfl_sync(0xffffffffu, from, r & 15);
-      if (r >= 16) src[j] = -1;
-      if (src[j] >= 0) {
-        x[j] = *reinterpret_cast<const uint4*>(cache + row_of(p, sl, src[j]) + 16 * c);
-        scale[j] = *scale_at(p, sl, src[j], which);
-      }
+  for (int j = 0; j < N; ++j) {
+    const int k = 32 * j + lane, r = k / CH, c = k % CH;
+    src[j] = __shfl_sync(0xffffffffu, from, r & 15);
+    if (r >= 16) src[j] = -1;
+    if (src[j] >= 0) {
+      const long long at = row_of(p, sl, src[j]) + 16 * c;
+      const float2 both = *scale_at(p, sl, src[j]);
+      x[0][j] = *reinterpret_cast<const uint4*>(p.k + at);
+      x[1][j] = *reinterpret_cast<const uint4*>(p.v + at);
+      scale[0][j] = both.x;
+      scale[1][j] = both.y;
     }
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if (src[j] < 0) continue;
-      const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-      float m = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float a[4];
-        widen4(a, w[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(a[e]));           // a NaN counts for nothing
-      }
-      top = fmaxf(top, m * scale[j]);
+      top[which] = fmaxf(top[which], largest(x[which][j]) * scale[which][j]);
     }
-    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-    const float now = scale_for(top), inv = inverse_scale(now);
-    __syncwarp();                                                      // everything has been read
+  float2 now;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    top[which] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top[which])));
+    (which ? now.y : now.x) = scale_for(top[which]);
+  }
+  __syncwarp();                                                        // everything has been read
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float to = which ? now.y : now.x, inv = inverse_scale(to);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int k = 32 * j + lane, r = k / CH, c = k % CH;
-      if (src[j] < 0 || (src[j] == slot0 + r && scale[j] == now)) continue;
-      const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-      const float f = scale[j] * inv;
+      if (src[j] < 0 || (src[j] == slot0 + r && scale[which][j] == to)) continue;
+      const uint32_t w[4] = {x[which][j].x, x[which][j].y, x[which][j].z, x[which][j].w};
+      const float f = scale[which][j] * inv;
       uint32_t y[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float a[4];
         widen4(a, w[i]);
-        y[i] = narrow4(a[0] * f, a[1] * f, a[2] * f, a[3] * f);
+        y[i] = narrow4_finite(a[0] * f, a[1] * f, a[2] * f, a[3] * f);     // (a NaN stays one)
       }
-      *reinterpret_cast<uint4*>(cache + row_of(p, sl, slot0 + r) + 16 * c) = make_uint4(y[0], y[1], y[2], y[3]);
+      *reinterpret_cast<uint4*>((which ? p.v : p.k) + row_of(p, sl, slot0 + r) + 16 * c) = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    if (lane == 0) *scale_at(p, sl, slot0, which) = now;
   }
+  if (lane == 0) *scale_at(p, sl, slot0) = now;
 }
 
 __device__ inline uint32_t inclusive(uint32_t v, int lane) {
@@ -212,32 +239,36 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
   __shared__ __align__(16) uint32_t hist[3][kBins];
   __shared__ int counts[3][WARPS];
   __shared__ uint32_t sums[WARPS];
-  __shared__ int guarded, bad;
+  __shared__ int ranks[kDirect];
+  __shared__ int guarded, bad, n_cand, thr_slot_s;
+  __shared__ uint32_t thr_key_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const long long item = blockIdx.x / ctas;
-  const long long seq = item / p.kv;
-  const int pos = (int)(item - seq * p.kv), s = (int)(seq / p.n_seqs);
+  const uint32_t item = blockIdx.x / (unsigned)ctas, seq_ = item / (unsigned)p.kv;
+  const long long seq = seq_;
+  const int pos = (int)(item - seq_ * p.kv), s = (int)(seq_ / (unsigned)p.n_seqs);
   auto sync = [&] {
     if (ctas == 1) __syncthreads();
     else cluster.sync();
   };
   griddep_launch_dependents();
+  for (int b = threadIdx.x; b < 3 * kBins; b += THREADS) hist[0][b] = 0;
+  if (threadIdx.x == 0) guarded = bad = n_cand = 0;
   griddep_wait();
-  if (p.kv_count && pos >= p.kv_count[s]) return;
+  // one round trip: the lengths, and the table whatever the length is
+  const int held = p.kv_count ? p.kv_count[s] : p.kv;
   int len = p.len[seq], keep = p.keep[seq];
   const int seen = p.seen ? p.seen[seq] : len;
+  for (int i = threadIdx.x; i < min(p.max_pages, kTableCache); i += THREADS) table[i] = p.table[seq * p.max_pages + i];
+  __syncthreads();
+  if (pos >= held) return;
   if (len < 0 || len > p.max_len || keep < 0 || keep > p.max_len) {
     if (threadIdx.x == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
     len = max(0, min(len, p.max_len));
     keep = max(0, min(keep, p.max_len));
   }
   const int pages = (len + (1 << p.page_shift) - 1) >> p.page_shift;
-  if (pages <= kTableCache) {
-    for (int i = threadIdx.x; i < pages; i += THREADS) table[i] = p.table[seq * p.max_pages + i];
-    __syncthreads();
-  }
   const Slots sl{pages <= kTableCache ? table : p.table + seq * p.max_pages, pos, p.kv, p.page_shift, p.n_pages};
   const bool in_place = p.weights == p.weights_out;
   if (len <= keep) {                                                   // all stay
@@ -252,8 +283,8 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
   if (keep == 0) return;
   const long long guard = (long long)seen - min(p.recent, keep);
   // the warp's run of slots
-  const int warps = ctas * WARPS, me = rank * WARPS + warp;
-  const int run = ((len + warps - 1) / warps + 31) / 32 * 32;
+  const int warps = ctas * WARPS, me = rank * WARPS + warp;           // a power of two
+  const int run = (((len + warps - 1) >> (__ffs(warps) - 1)) + 31) & ~31;
   const int lo = (int)min((long long)len, (long long)me * run), hi = min(len, lo + run);
   const int key0 = warp * run;                                         // of the run in shared memory
   auto compute_key = [&](int i) {
@@ -262,15 +293,20 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
   };
   auto key_at = [&](int i) { return key0 + (i - lo) < p.key_cache ? keys[key0 + (i - lo)] : compute_key(i); };
 
-  // Weights lie close together: lanes that hit the same bin add up first (one by one in shared memory they would wait in line).
+  // Lanes that agree add up first: the same weight everywhere would be counted one by one.  (Lanes that agree with any other, by a
+  // match over the warp: 15.7 and 58 us against 15.3 and 54 in the two cases above.)
   auto count = [&](uint32_t* bins, uint32_t bin, bool mine) {
-    const unsigned same = __match_any_sync(0xffffffffu, mine ? bin : 0xffffffffu);
-    if (mine && lane == __ffs(same) - 1) atomicAdd(&bins[bin], (uint32_t)__popc(same));
+    const unsigned live = __ballot_sync(0xffffffffu, mine);
+    if (live == 0) return;
+    const int leader = __ffs(live) - 1;
+    const bool alike = __shfl_sync(0xffffffffu, bin, leader) == bin;
+    if (__all_sync(0xffffffffu, alike || !mine)) {
+      if (lane == leader) atomicAdd(&bins[bin], (uint32_t)__popc(live));
+    } else if (mine) {
+      atomicAdd(&bins[bin], 1u);
+    }
   };
   // 1. keys
-  if (threadIdx.x == 0) { guarded = 0; bad = 0; }
-  for (int b = threadIdx.x; b < 3 * kBins; b += THREADS) hist[0][b] = 0;
-  __syncthreads();
   {
     int mine = 0;
     bool wrong = false;
@@ -323,14 +359,16 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
     sync();                                                            // the others have read the counters
     return;
   }
-  // 2. the threshold: keys above it stay, and `quota` of the `equal` ones that are it
+  // 2. the threshold: keys above it stay, and of those that are it the first `quota`, up to slot thr_slot
   uint32_t threshold = 0xffffffffu;
-  int quota = keep, equals = total_guarded;
+  int quota = keep, equals = total_guarded, thr_slot = 0x7fffffff;
   if (total_guarded < keep) {
     int need = keep - total_guarded;
     uint32_t prefix = 0;
+    int last = 0;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
+      if (pass > 0 && (equals <= kDirect || equals == need)) break;
       const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
       constexpr int kLast = 1024;
       const int bins = pass == 2 ? kLast : kBins;
@@ -378,9 +416,59 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
       equals = (int)__shfl_sync(0xffffffffu, n_bin, here);
       prefix |= (uint32_t)found_bin << shift;
       need -= found_above;
+      last = pass;
     }
     threshold = prefix;
     quota = need;
+    if (equals == need) {                                              // the whole bin stays: its lowest key will do
+      quota = 0x7fffffff;
+    } else if (equals <= kDirect) {
+      // The keys of the bin, with their slots, into every CTA; each is compared with the others.
+      const int at_shift = last == 0 ? 21 : (last == 1 ? 10 : 0);
+      // nobody reads these bins any more, or yet
+      unsigned long long* own = reinterpret_cast<unsigned long long*>(hist[last == 2 ? 0 : last + 1]), *all = own;
+      for (int g0 = lo; g0 < hi; g0 += 32) {
+        const int i = g0 + lane;
+        const uint32_t key = i < hi ? key_at(i) : 0xffffffffu;
+        const bool in_bin = key != 0xffffffffu && key >> at_shift == prefix >> at_shift;
+        const unsigned vote = __ballot_sync(0xffffffffu, in_bin);
+        if (vote == 0) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&n_cand, __popc(vote));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(vote & ((1u << lane) - 1));
+        if (in_bin) own[at] = (unsigned long long)key << 32 | (uint32_t)~i;
+      }
+      for (int i = threadIdx.x; i < equals; i += THREADS) ranks[i] = 0;
+      sync();
+      if (ctas > 1) {
+        all = own + kDirect;
+        for (int c = 0, at = 0; c < ctas; ++c) {
+          const int n = *cluster.map_shared_rank(&n_cand, c);
+          const unsigned long long* theirs = cluster.map_shared_rank(own, c);
+          for (int i = threadIdx.x; i < n; i += THREADS) all[at + i] = theirs[i];
+          at += n;
+        }
+        __syncthreads();
+      }
+      // 32 candidates to a warp, against a share of the others
+      const int log_groups = 32 - __clz((equals - 1) >> 5), parts = WARPS >> log_groups, part = warp >> log_groups;
+      const int mine = (warp & ((1 << log_groups) - 1)) * 32 + lane;
+      if (mine < equals) {
+        const unsigned long long me_ = all[mine];
+        int above = 0;
+        for (int i = part; i < equals; i += parts) above += all[i] > me_;
+        if (above) atomicAdd(&ranks[mine], above);
+      }
+      __syncthreads();
+      if (threadIdx.x < equals && ranks[threadIdx.x] == need - 1) {
+        thr_key_s = (uint32_t)(all[threadIdx.x] >> 32);
+        thr_slot_s = (int)~(uint32_t)all[threadIdx.x];
+      }
+      __syncthreads();
+      threshold = thr_key_s;
+      thr_slot = thr_slot_s;
+      quota = 0x7fffffff;
+    }
   }
   // numbers of the runs before this warp's
   auto before_me = [&](const int* of) {
@@ -407,7 +495,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
     const int i = g0 + lane;
     const uint32_t key = i < hi ? key_at(i) : 0u;
     const unsigned same = __ballot_sync(0xffffffffu, i < hi && key == threshold);
-    const bool stays = i < hi && (key > threshold || (key == threshold && equal + __popc(same & ((1u << lane) - 1)) < quota));
+    const bool stays = i < hi && (key > threshold || (key == threshold && i <= thr_slot && equal + __popc(same & ((1u << lane) - 1)) < quota));
     const unsigned stay = __ballot_sync(0xffffffffu, stays);
     const unsigned below = keep >= g0 + 32 ? 0xffffffffu : (keep <= g0 ? 0u : (1u << (keep - g0)) - 1);
     equal += __popc(same);
@@ -451,27 +539,40 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
         }
     return;
   }
-  const int cut = keep & 15 ? keep >> 4 : -1;                          // the block that keep cuts
-  auto fill = [&](int block) {
-    const int slot0 = block << 4, end = min(len, slot0 + 16);
-    const int from = source_of(bits, before, movers, slot0, keep, end, lane), slot = slot0 + (lane & 15);
-    const unsigned moved = __ballot_sync(0xffffffffu, lane < 16 && from >= 0 && from != slot);
-    if (lane < 16 && from >= 0 && slot < keep && (from != slot || !in_place)) {
-      const long long to = sl.at(slot), at = sl.at(from);
-      const float w = p.weights[at];
-      const int32_t x = p.slot_pos[at];
-      p.weights_out[to] = w;
-      p.slot_pos_out[to] = x;
+  // weights and positions
+  {
+    const int first = rank * THREADS + threadIdx.x, stride = ctas * THREADS;
+#pragma unroll 2
+    for (int slot = first; slot < keep; slot += stride) {
+      const int from = source_of(bits, before, movers, slot, keep);
+      if (from != slot || !in_place) {
+        const long long to = sl.at(slot), at = sl.at(from);
+        const float w = p.weights[at];
+        const int32_t x = p.slot_pos[at];
+        p.weights_out[to] = w;
+        p.slot_pos_out[to] = x;
+      }
     }
-    if (!moved) return;
+  }
+  // rows: the blocks that take tokens in, the one that `keep` cuts last (it holds sources too)
+  const int cut = keep & 15 ? keep >> 4 : -1;
+  auto fill = [&](int block) {
+    const int slot0 = block << 4, slot = slot0 + (lane & 15);
+    const int from = slot >= len ? -1 : slot >= keep ? slot : source_of(bits, before, movers, slot, keep);
     if constexpr (D > 0) move_block<D>(p, sl, slot0, from, lane);
   };
+  auto takes_in = [&](int block) { return (~(uint32_t)bits[block >> 1] >> (block & 1 ? 16 : 0) & 0xffffu & ((1u << min(16, keep - 16 * block)) - 1)) != 0; };
   const int blocks = (keep + 15) >> 4;
-  for (int b = me; b < blocks; b += warps)
-    if (b != cut) fill(b);
+  for (int b0 = 0, number = 0; b0 < blocks; b0 += 32) {                // the warps take them in turn
+    const bool mine = b0 + lane < blocks && b0 + lane != cut && takes_in(b0 + lane);
+    const unsigned vote = __ballot_sync(0xffffffffu, mine);
+    const int turn = number + __popc(vote & ((1u << lane) - 1));
+    for (unsigned todo = __ballot_sync(0xffffffffu, mine && ((turn ^ me) & (warps - 1)) == 0); todo; todo &= todo - 1) fill(b0 + __ffs(todo) - 1);
+    number += __popc(vote);
+  }
   if (cut >= 0) {
     sync();
-    if (me == 0) fill(cut);
+    if (me == 0 && takes_in(cut)) fill(cut);
   }
 }
 
@@ -546,7 +647,7 @@ extern "C" int32_t twist_kv_evict(const twist_kv_evict_args* a, void* stream) {
   memset(&p, 0, sizeof(p));
   p.k = static_cast<uint8_t*>(a->k_cache);
   p.v = static_cast<uint8_t*>(a->v_cache);
-  p.scales = a->scales;
+  p.scales = reinterpret_cast<float2*>(a->scales);
   p.table = a->page_table; p.len = a->kv_len; p.keep = a->keep; p.seen = a->seen; p.kv_count = a->kv_count;
   p.weights = a->weights; p.slot_pos = a->slot_pos; p.weights_out = a->weights_out; p.slot_pos_out = a->slot_pos_out;
   p.ws = static_cast<int32_t*>(a->ws);

@@ -866,6 +866,45 @@ def test_evict_more_slots_than_shared_memory_keeps(B):
     assert torch.equal(got[~low].long(), (keep + stays[keep:].nonzero().flatten()))        # movers in ascending order
 
 
+@pytest.mark.parametrize("m,keep,recent", [(1040, 1024, 0), (1040, 1024, 256), (300, 1, 0), (3000, 777, 100), (9000, 4001, 0), (9000, 8999, 50)])
+@pytest.mark.parametrize("kind", ["equal", "two", "low bits", "last bits", "some equal", "descending", "one bin"])
+def test_evict_weights_close_together(B, kind, m, keep, recent):
+    """The threshold among weights that differ late or not at all; a KV position whose other half has the weights in reverse."""
+    gen = torch.Generator().manual_seed(m + keep)
+    page, D = 64, 16
+    pages = -(-m // page)
+    one = {"equal": lambda: torch.full((m,), 0.75), "two": lambda: 1 + torch.randint(0, 2, (m,), generator=gen) * 2.0 ** -23,
+           "low bits": lambda: 1 + torch.randint(0, 8000, (m,), generator=gen) * 2.0 ** -23,
+           "last bits": lambda: 1 + torch.randint(0, 900, (m,), generator=gen) * 2.0 ** -23,
+           "some equal": lambda: torch.where(torch.rand(m, generator=gen) < 0.6, torch.tensor(0.5), torch.rand(m, generator=gen)),
+           "descending": lambda: 2.0 - torch.arange(m) / m, "one bin": lambda: 1 + 0.2 * torch.rand(m, generator=gen)}[kind]().float()
+    w = torch.zeros(2, pages * page)
+    w[0, :m], w[1, :m] = one, one.flip(0)
+    seq = torch.stack([torch.randperm(m, generator=gen) for _ in range(2)]).int()
+    pos = torch.full((2, pages * page), -1, dtype=torch.int32)
+    pos[:, :m] = seq
+    lay = lambda t: t.view(2, pages, page).transpose(0, 1).contiguous().cuda()
+    back = lambda t: t.cpu().transpose(0, 1).reshape(2, -1)
+    cache = torch.zeros(pages, 2, page, D, dtype=BF, device="cuda")
+    cache.view(torch.int32)[..., 3] = lay(pos)                       # the token's number in the row itself
+    w2, p2, v = lay(w), lay(pos), cache.clone()
+    ws = torch.empty(B.twist_kv_evict_workspace_bytes(1, 1, 2, m), dtype=torch.uint8, device="cuda")
+    B.twist_kv_evict(B.kv_evict_args(B.BF16, 1, 1, 2, D, recent, m, k_cache=cache, v_cache=v, weights=w2, slot_pos=p2,
+                                     page_table=torch.arange(pages, dtype=torch.int32, device="cuda").view(1, 1, -1), kv_len=i32([[m]]),
+                                     keep=i32([[keep]]), ws=ws))
+    assert B.twist_device_status() == 0
+    for g in range(2):
+        rank = torch.where(seq[g] >= m - min(recent, keep), float("inf"), w[g, :m])
+        stays = torch.zeros(m, dtype=torch.bool)
+        stays[torch.argsort(rank, descending=True, stable=True)[:keep]] = True
+        source = torch.arange(m)[:keep].clone()
+        source[~stays[:keep]] = keep + stays[keep:].nonzero().flatten()
+        assert torch.equal(back(p2)[g, :keep], pos[g, source])
+        assert torch.equal(back(w2)[g, :keep], w[g, source])
+        for t in (cache, v):
+            assert torch.equal(back(t.view(torch.int32)[..., 3])[g, :keep], pos[g, source])
+
+
 def test_evict_bad_index_data(B):
     gen = torch.Generator().manual_seed(4)
     page, D, KV = 16, 64, 2
