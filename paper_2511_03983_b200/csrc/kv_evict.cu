@@ -92,7 +92,7 @@ __device__ inline int source_of(const int32_t* bits, const int32_t* before, cons
 
 // Rows of a bf16 cache: the tokens movers[i] to slots[i].  A warp takes 32 at a time: a lane finds the places of one, then all
 // of them carry 16 bytes of K or V per turn, kTurns turns in flight.  CH: 16-byte pieces of a row, 1 to 16, a power of two.
-constexpr int kTurns = 4;                 // 64 items of up to 16000 tokens, d = 128: 61.6 us; eight turns (spilled) 80, two 63
+constexpr int kTurns = 4;                 // the long prompts above: 54 us; eight turns 73, two 59
 template <int CH>
 __device__ inline void carry_rows(const EvictParams& p, long long from, long long to, int n, int lane) {
   constexpr int PER = 32 / (2 * CH);                                  // tokens of a turn
@@ -578,7 +578,8 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
 
 template <int D>
 int run_evict(EvictParams& p, long long items, cudaStream_t st) {
-  // CTAs of an item: as many as still have kSlotsPerCta slots each, two for an SM (four: 129 us against 74 in the case above).
+  // CTAs of an item: as many as still have kSlotsPerCta slots each, two for an SM (four: 85 us against 54 for the long prompts above,
+  // one 74; a page over in two CTAs an item 30 against 12.6).
   int ctas = 1;
   while (ctas < kMaxEvictCluster && p.max_len > ctas * kSlotsPerCta && items * ctas <= sm_count()) ctas *= 2;
   const long long warps = (long long)ctas * kEvWarps, run = ((p.max_len + warps - 1) / warps + 31) / 32 * 32;
