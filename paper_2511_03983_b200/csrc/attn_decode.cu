@@ -1,4 +1,4 @@
-// twist_attn_decode: attention of one new token per sequence over a paged key-value cache,
+// twist_attn_decode and twist_attn_decode_q8: attention of one new token per sequence over a paged key-value cache,
 //     out_h = sum_j softmax_j(q_h . k_j / sqrt(d)) v_j,
 // split over the cache's length and joined.  Every cached K and V element is read once from memory and used by the few
 // heads that share it, so the kernel is bound by HBM: the design keeps as many bytes as possible in flight and spends as
@@ -29,6 +29,10 @@
 // run on across the borders of items (an item: the tiles of one KV position of one sequence).  A warp writes the items it
 // has whole; of an item that a border between warps cuts, every warp writes its unnormalised part (fp32 sums, maximum,
 // sum) to the workspace, and a second small launch joins the parts in the order of the warps.
+//
+// 8 bits (B = 1): the same, the numbers widened to fp16 between load and product (exact), K's scales multiplied into the scores and
+// V's into the probabilities.  A byte then costs twice the instructions, and a tile in registers is too little in flight: tiles
+// come through rings in shared memory, filled by bulk copies (see Ring).
 //
 // Calls whose length and number of items leave little to balance take a shorter way instead: one cluster of 1 to 8 CTAs
 // per item, whose warps take the item's tiles in turn and join through (distributed) shared memory: one launch, no
