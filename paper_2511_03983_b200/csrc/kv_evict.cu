@@ -16,7 +16,7 @@
 //
 // Bound by the latency of these phases where a cache is a page over its budget (256 items of 1040 slots, d = 64 in 8 bits: 12.6 us of
 // 0.7 us of bytes; all three passes of the selection and a warp for every 64 slots in 4., moved or not: 19.3), by it and the
-// scattered rows for long prompts (64 items of up to 16000, d = 128 in bf16: 54 us, of which the moves are 28).
+// scattered rows for long prompts (64 items of up to 16000, d = 128 in bf16: 52 us, of which the moves are 28).
 #include <cooperative_groups.h>
 
 #include "e4m3.cuh"
@@ -92,7 +92,7 @@ __device__ inline int source_of(const int32_t* bits, const int32_t* before, cons
 
 // Rows of a bf16 cache: the tokens movers[i] to slots[i].  A warp takes 32 at a time: a lane finds the places of one, then all
 // of them carry 16 bytes of K or V per turn, kTurns turns in flight.  CH: 16-byte pieces of a row, 1 to 16, a power of two.
-constexpr int kTurns = 4;                 // the long prompts above: 54 us; eight turns 73, two 59
+constexpr int kTurns = 4;                 // the long prompts above, eight turns 73 us, four 54, two 59
 template <int CH>
 __device__ inline void carry_rows(const EvictParams& p, long long from, long long to, int n, int lane) {
   constexpr int PER = 32 / (2 * CH);                                  // tokens of a turn
@@ -234,6 +234,7 @@ __device__ inline uint32_t inclusive(uint32_t v, int lane) {
 template <int D>
 __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams p) {
   constexpr int WARPS = kEvWarps, THREADS = kEvThreads;
+  static_assert(WARPS == 16 && kBins == 2048, "shifts below");
   extern __shared__ uint32_t keys[];
   __shared__ int32_t table[kTableCache];
   __shared__ __align__(16) uint32_t hist[3][kBins];
@@ -283,8 +284,8 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
   if (keep == 0) return;
   const long long guard = (long long)seen - min(p.recent, keep);
   // the warp's run of slots
-  const int warps = ctas * WARPS, me = rank * WARPS + warp;           // a power of two
-  const int run = (((len + warps - 1) >> (__ffs(warps) - 1)) + 31) & ~31;
+  const int log_ctas = __ffs(ctas) - 1, warps = ctas * WARPS, me = rank * WARPS + warp;           // a power of two
+  const int run = (((len + warps - 1) >> (4 + log_ctas)) + 31) & ~31;
   const int lo = (int)min((long long)len, (long long)me * run), hi = min(len, lo + run);
   const int key0 = warp * run;                                         // of the run in shared memory
   auto compute_key = [&](int i) {
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
   {
     int mine = 0;
     bool wrong = false;
-    constexpr int BATCH = 4;                                           // groups whose loads are in flight
+    constexpr int BATCH = 4;                                            // groups whose loads are in flight
     for (int g0 = lo; g0 < hi; g0 += 32 * BATCH) {
       float w[BATCH];
       int32_t x[BATCH];
@@ -348,11 +349,8 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
   sync();
   int total_guarded = guarded, any_bad = bad;
   if (ctas > 1) {
-    total_guarded = any_bad = 0;
-    for (int c = 0; c < ctas; ++c) {
-      total_guarded += *cluster.map_shared_rank(&guarded, c);
-      any_bad |= *cluster.map_shared_rank(&bad, c);
-    }
+    total_guarded = __reduce_add_sync(0xffffffffu, lane < ctas ? *cluster.map_shared_rank(&guarded, lane) : 0);
+    any_bad = __any_sync(0xffffffffu, lane < ctas && *cluster.map_shared_rank(&bad, lane));
   }
   if (any_bad) {
     if (threadIdx.x == 0 && rank == 0) atomicMin(p.status, (int)TWIST_ERR_BAD_INDEX);
@@ -382,25 +380,38 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
         sync();
       }
       // The bin from the top in which the need-th key is: every warp adds up a 16th of the bins, then every warp finds the 16th
-      // and the bin in it.
-      auto four = [&](int b) {                                         // bins b .. b + 3 of all CTAs
-        if (ctas == 1) return *reinterpret_cast<const uint4*>(hist[pass] + b);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        for (int c = 0; c < ctas; ++c) {
-          const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(hist[pass], c) + b);
-          v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-        }
-        return v;
-      };
+      // and the bin in it.  In a cluster every CTA adds up its share of all CTAs' bins first (each adding up everything moves a
+      // cluster's worth of histograms through every SM: 54 us against 52 for the long prompts above).
       const int group = bins / WARPS;                                  // 128, or 64: half of the lanes
       const bool reads = 4 * lane < group;
-      {
-        const uint4 v = reads ? four(warp * group + 4 * lane) : make_uint4(0, 0, 0, 0);
-        const uint32_t all = __reduce_add_sync(0xffffffffu, v.x + v.y + v.z + v.w);
-        if (lane == 0) sums[warp] = all;
+      const int share = bins >> log_ctas, groups = WARPS >> log_ctas;  // of a CTA
+      if (ctas > 1) {
+        for (int b = rank * share + threadIdx.x; b < (rank + 1) * share; b += THREADS) {
+          uint32_t n = 0;
+#pragma unroll
+          for (int c = 0; c < kMaxEvictCluster; ++c)                   // all on their way at once
+            if (c < ctas) n += cluster.map_shared_rank(hist[pass], c)[b];
+          hist[pass][b] = n;
+        }
+        __syncthreads();
       }
-      __syncthreads();
-      const uint32_t part = lane < WARPS ? sums[WARPS - 1 - lane] : 0u, upto = inclusive(part, lane);
+      auto four = [&](int b) {                                         // bins b .. b + 3
+        const uint32_t* from = ctas == 1 ? hist[pass] : cluster.map_shared_rank(hist[pass], b >> ((pass == 2 ? 10 : 11) - log_ctas));
+        return *reinterpret_cast<const uint4*>(from + b);
+      };
+      if (warp < groups) {
+        const int b = (rank * groups + warp) * group + 4 * lane;
+        const uint4 v = reads ? *reinterpret_cast<const uint4*>(hist[pass] + b) : make_uint4(0, 0, 0, 0);
+        const uint32_t all = __reduce_add_sync(0xffffffffu, v.x + v.y + v.z + v.w);
+        if (lane == 0) sums[rank * groups + warp] = all;
+      }
+      sync();
+      uint32_t part = 0;
+      if (lane < WARPS) {
+        const int of = WARPS - 1 - lane;
+        part = ctas == 1 ? sums[of] : cluster.map_shared_rank(sums, of >> (4 - log_ctas))[of];
+      }
+      const uint32_t upto = inclusive(part, lane);
       const int at = __ffs(__ballot_sync(0xffffffffu, upto >= (uint32_t)need)) - 1;
       const int top = bins - at * group - 4 - 4 * lane;                // the lane's four bins of it, from the highest down
       const uint4 v = reads ? four(top) : make_uint4(0, 0, 0, 0);
@@ -442,11 +453,11 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
       sync();
       if (ctas > 1) {
         all = own + kDirect;
-        for (int c = 0, at = 0; c < ctas; ++c) {
-          const int n = *cluster.map_shared_rank(&n_cand, c);
-          const unsigned long long* theirs = cluster.map_shared_rank(own, c);
-          for (int i = threadIdx.x; i < n; i += THREADS) all[at + i] = theirs[i];
-          at += n;
+        const int n = lane < ctas ? *cluster.map_shared_rank(&n_cand, lane) : 0;
+        const int before_them = (int)inclusive((uint32_t)n, lane) - n;
+        for (int c = 0; c < ctas; ++c) {
+          const int at = __shfl_sync(0xffffffffu, before_them, c), i = threadIdx.x;
+          if (i < __shfl_sync(0xffffffffu, n, c)) all[at + i] = cluster.map_shared_rank(own, c)[i];
         }
         __syncthreads();
       }
