@@ -304,11 +304,11 @@ int run_weights(WeightParams& w, long long max_len, cudaStream_t st) {
 
 constexpr int kCoreWarps = 4, kCoreThreads = 32 * kCoreWarps, kCoreKeys = 16 * kCoreWarps;
 
-// Small heads.  A CTA holds a tile of 64 keys of one KV position in registers (a warp 16 of them) and walks over the queries that
-// may look at them, head after head, tiles of QT through shared memory, the next one on its way.  The sums stay in the
-// registers of the threads that own the scores and are joined over the four threads of a row at the end.  Bound by the
-// chains of dependent instructions: more keys a warp mean longer ones and fewer CTAs (4 subnets of 4 prompts of 2048, 16 heads on 4
-// positions of d = 32: 16, 32 and 64 keys a warp 326, 454 and 544 us; the special-function units alone take 130).
+// Heads of 8, and of 16 and 32 where a key has few queries (see below).  A CTA holds a tile of 64 keys of one KV position in registers
+// (a warp 16 of them) and walks over the queries that may look at them, head after head, tiles of QT through shared memory, the
+// next one on its way.  The sums stay in the registers of the threads that own the scores and are joined over the four threads
+// of a row at the end.  Bound by the chains of dependent instructions: more keys a warp mean longer ones and fewer CTAs (4 subnets of
+// 4 prompts of 2048, 16 heads on 4 positions of d = 32: 16, 32 and 64 keys a warp 326, 454 and 544 us).
 template <int D, int QT>
 __global__ void __launch_bounds__(kCoreThreads) core_weights_kernel(const CoreParams p) {
   using Sh = Shape<D, 2>;
@@ -411,9 +411,12 @@ template <int D>
 int run_core(CoreParams& p, cudaStream_t st) {
   const long long grid = (long long)p.S * p.n_seqs * p.kv_max * ((p.seq_len + kCoreKeys - 1) / kCoreKeys);
   if (grid > 0x7fffffffll) return TWIST_ERR_UNSUPPORTED;
-  // Half as many queries a tile where a prompt has few tiles (6 prompts of 77, the last 32 queries, d = 32: 5.8 us against 8.4; the
-  // long ones above 363 against 326).
-  void (*kernel)(CoreParams) = p.seq_len <= 256 ? core_weights_kernel<D, 32> : core_weights_kernel<D, 64>;
+  // Tiles of few queries where there are few of them (6 prompts of 77, the last 32 queries, d = 32: 5.8 us against 8.4); long prompts
+  // with d = 8, which have no other kernel, take twice as many (those above at d = 16 in this kernel: 393 us against 320).
+  void (*kernel)(CoreParams) = core_weights_kernel<D, 32>;
+  if constexpr (D == 8) {
+    if (p.seq_len > 256) kernel = core_weights_kernel<D, 64>;
+  }
   TWIST_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)grid), dim3(kCoreThreads), 0, st, 1, p));
   return TWIST_OK;
 }
@@ -536,10 +539,16 @@ extern "C" int32_t twist_attn_core_weights(const twist_attn_core_weights_args* a
   p.status = device_status_ptr();
   if (!p.status) return TWIST_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  // Heads of 16 and 32 go to the tensor cores too, unless their keys have few queries over all heads: a CTA's set-up there costs 4 us.
+  // Average over the keys; d = 32, tensor cores against the other kernel: 64 prompts of up to 600, last 32 queries of 4 heads a
+  // position 28.2 us against 20.5; 128 of up to 500, one head a position 64 against 41; 64 of 700, one head 39.2 against 39.2; 64 of up
+  // to 200, 4 heads 19.5 against 28.3; one of 600, 4 heads 21.5 against 41.5; 16 of 2048, 4 heads 159 against 370.
+  const long long queries = a->last_queries > 0 && a->last_queries < a->seq_len ? a->last_queries : a->seq_len / 2;
+  const bool few = queries * a->head_keep < 320ll * a->kv_max;
   switch (dh) {
     case 8: return run_core<8>(p, st);
-    case 16: return run_core<16>(p, st);
-    case 32: return run_core<32>(p, st);
+    case 16: if (few) return run_core<16>(p, st); break;
+    case 32: if (few) return run_core<32>(p, st); break;
     default: break;
   }
   PlanScope scope(a->plan);

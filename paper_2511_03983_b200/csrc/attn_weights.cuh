@@ -1,5 +1,5 @@
-// Parameters and pieces that the kernels of twist_attn_core_weights share (small heads in attn_weights.cu, heads of 64 and 128 on
-// the tensor cores in attn_weights_tc.cu).
+// Parameters and pieces that the kernels of twist_attn_core_weights share (attn_weights.cu, and on the tensor cores
+// attn_weights_tc.cu).
 #pragma once
 #include "common.cuh"
 

@@ -1,4 +1,4 @@
-// Prompts of twist_attn_core_weights on the tensor cores, heads of 64 and 128:
+// Prompts of twist_attn_core_weights on the tensor cores, heads of 16 to 128:
 //     w_j = sum_h sum_{i >= j} exp(q_hi . k_j / sqrt(d) - lse_hi).
 //
 // One CTA per (block of 128 keys, KV position, sequence), blocks with the most queries first.  For every kept head that reads the
@@ -11,8 +11,10 @@
 // Bound by the exponentials: an SM's special-function units give 16 a cycle, 1024 cycles a block, against 128 (d = 64) of MMA,
 // and by the instructions beside them.  4 subnets of 4 prompts of 2048, 16 heads on 4 positions of d = 64 (130 us of special-function
 // unit): 531 us with warp-level MMA from shared memory, 192 us first on tcgen05, 172 with the log-sum-exps staged for eight blocks
-// at a time instead of for each, 160 with every fourth pair of exponentials by a polynomial (half of them: more instructions
-// than the unit has to spare).  Sixteen warps of 32 queries each: 182.
+// at a time instead of for each, 162 with every fourth pair of exponentials by a polynomial (half of them: more instructions
+// than the unit has to spare), 160 without the columns that count for no key of a warp (64 prompts of up to 1000, the last 32
+// queries of 32 heads: 100 us before, 67).  Sixteen warps of 32 queries each: 182.  Statistics staged for eight blocks across heads:
+// 172.  Smaller heads take as long: 159 at d = 32, 157 at 16.
 // Every wait is bounded; on expiry the CTA records TWIST_ERR_DEVICE_TIMEOUT and leaves.
 #include <type_traits>
 
@@ -38,9 +40,10 @@ __device__ inline float ex2(float x) {
 
 template <int D>
 struct Tc {
-  static constexpr int PANELS = D / 64;                       // boxes of 64 columns of a block
+  static constexpr int PANELS = D > 64 ? D / 64 : 1;          // boxes of 64 columns of a block (small heads: their neighbours come along)
+  static constexpr int STEPS = (D > 64 ? 64 : D) / 16;        // of the product, in a panel
   static constexpr int BOX = kBlock * 64 * 2, BLOCK = PANELS * BOX;
-  static constexpr int STAGES = D == 64 ? 3 : 2;              // of queries
+  static constexpr int STAGES = D <= 64 ? 3 : 2;              // of queries
   static constexpr int SMEM = BLOCK * (1 + STAGES) + 1024 + 256;
 };
 
@@ -153,6 +156,10 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
     fence_async_smem();
   }
   griddep_wait();
+  if (warp == 0) {                         // beside the round trip of the length
+    const int n = heads_of(p, s, pos, lane, list);
+    if (lane == 0) n_list_s = n;
+  }
   const int len = prompt_len(p, z);
   if (kb * kBlock >= len) return;
   auto load = [&](uint32_t to, uint32_t full, int col, int block) {
@@ -161,10 +168,6 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
     for (int j = 0; j < T::PANELS; ++j) tma_load_3d_local(to + j * T::BOX, &map, full, col + 64 * j, block * kBlock, z);
   };
   if (threadIdx.x == 32 * kEw) load(k_s, bar(K_FULL), (p.heads + pos) * D, kb);
-  if (warp == 0) {
-    const int n = heads_of(p, s, pos, lane, list);
-    if (lane == 0) n_list_s = n;
-  }
   if (warp == kEw) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"((uint32_t)kTmemCols) : "memory");
@@ -197,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
         for (int j = 0; j < T::PANELS; ++j) {
           const uint64_t ak = smem_desc(k_s + j * T::BOX, 16u, 1024u), bq = smem_desc(q_s + st * T::BLOCK + j * T::BOX, 16u, 1024u);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma1(tmem + 128u * buf, ak + 2u * k, bq + 2u * k, idesc, (j | k) != 0);
+          for (int k = 0; k < T::STEPS; ++k) mma1(tmem + 128u * buf, ak + 2u * k, bq + 2u * k, idesc, (j | k) != 0);
         }
         commit1(bar(S_FULL + buf));
         commit1(bar(Q_FREE + st));
@@ -253,14 +256,15 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
         f32x2 sum4[4] = {0, 0, 0, 0};
         auto unit = [&](auto masked) {
           constexpr bool MASKED = decltype(masked)::value;
-          const int q0 = i * kBlock + kCols * part, lo = max(first, key) - q0, hi = len - q0;
+          const int q0 = i * kBlock + kCols * part, lo = max(first, key) - q0, hi = len - q0, least = max(first, kb * kBlock + quarter * 32) - q0;
+          auto live = [&](int c) { return !MASKED || (c + 16 > least && c < hi); };      // some of them count for a key of the warp
           uint32_t va[16], vb[16];
           tc_ld16(from, va);
           tc_wait_ld();
 #pragma unroll
           for (int c = 0; c < kCols; c += 32) {
             tc_ld16(from + c + 16, vb);
-            add_row<MASKED>(sum4, va, lse + c, p.scale, lo - c, hi - c);
+            if (live(c)) add_row<MASKED>(sum4, va, lse + c, p.scale, lo - c, hi - c);
             tc_wait_ld();
             if (c + 32 < kCols) {
               tc_ld16(from + c + 32, va);
@@ -269,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 2) core_weights_tc_kernel(const __gr
               __syncwarp();
               if (lane == 0) mbar_arrive(bar(S_FREE + buf));
             }
-            add_row<MASKED>(sum4, vb, lse + c + 16, p.scale, lo - c - 16, hi - c - 16);
+            if (live(c + 16)) add_row<MASKED>(sum4, vb, lse + c + 16, p.scale, lo - c - 16, hi - c - 16);
             if (c + 32 < kCols) tc_wait_ld();
           }
         };
@@ -325,6 +329,13 @@ int run_tc(const CoreParams& p, cudaStream_t st) {
 
 }  // namespace
 
-int core_weights_tc(const CoreParams& p, int d_head, cudaStream_t st) { return d_head == 64 ? run_tc<64>(p, st) : run_tc<128>(p, st); }
+int core_weights_tc(const CoreParams& p, int d_head, cudaStream_t st) {
+  switch (d_head) {
+    case 16: return run_tc<16>(p, st);
+    case 32: return run_tc<32>(p, st);
+    case 64: return run_tc<64>(p, st);
+    default: return run_tc<128>(p, st);
+  }
+}
 
 }  // namespace twist

@@ -694,6 +694,15 @@ def test_core_weights(B, D, page, S, n, N, H, NH, NKV, last):
     assert np.all(got[~written] == -3.0) and np.all(where[~written] == -9)
 
 
+@pytest.mark.parametrize("last", [0, 1, 129, 400])
+@pytest.mark.parametrize("D,page,S,n,N,H,NH,NKV", [
+    (16, 16, 1, 2, 900, 1, 1, 1), (16, 64, 2, 2, 700, 3, 4, 2), (32, 32, 1, 2, 700, 5, 12, 4), (32, 16, 2, 1, 1025, 1, 2, 1),
+    (32, 16, 1, 3, 130, 12, 12, 1), (16, 128, 1, 1, 257, 8, 8, 1)])
+def test_core_weights_small_heads(B, D, page, S, n, N, H, NH, NKV, last):
+    """Rows narrower than the tile that is copied, neighbours in it, few and many queries a key."""
+    test_core_weights(B, D, page, S, n, N, H, NH, NKV, last)
+
+
 @pytest.mark.parametrize("row", [400, 401, 403, 640, 1100])
 @pytest.mark.parametrize("D", [16, 64, 128])
 def test_core_weights_of_a_query_that_is_not_a_number(B, D, row):
