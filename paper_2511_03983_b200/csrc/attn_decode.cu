@@ -66,8 +66,9 @@ template <int D, int B>
 struct State {
   float o[Shape<D, B>::MT][4];
   float m0, m1, l0, l1;
-  float unit, inverse;        // 8 bits: the sums o count in this (a scale of V); its inverse
+  float c0, c1, e0, e1;       // 8 bits: the sums o are c times what they stand for, c = 2^e
 };
+constexpr float kMostUp = 124.f;           // e at most: a probability of 1 beside the smallest scale of an append becomes 2^14
 
 template <int D, int B>
 __device__ inline void reset(State<D, B>& st) {
@@ -77,8 +78,8 @@ __device__ inline void reset(State<D, B>& st) {
     for (int e = 0; e < 4; ++e) st.o[i][e] = 0.f;
   st.m0 = st.m1 = -INFINITY;
   st.l0 = st.l1 = 0.f;
-  st.unit = 0.f;
-  st.inverse = INFINITY;
+  st.e0 = st.e1 = kMostUp;
+  st.c0 = st.c1 = 0x1p124f;
 }
 
 // Values of keys behind the end of `len` keys, cleared (see kClamp).
@@ -99,36 +100,85 @@ __device__ inline void clear_behind(Tile<D, B>& x, int key0, int len, int t) {
   }
 }
 
+// A step's probabilities from the scores against the reference r0, r1.
+__device__ inline void probabilities(float (&pr)[4], const float (&sc)[4], float scale_log2, float r0, float r1) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) pr[e] = ex2(fmaf(sc[e], scale_log2, (e & 1) ? -r1 : -r0));
+}
+
+// 8 bits: brings the sums to units in which the tile's products of probability and V's scale are below 2^15 for each head again.
+// Units only grow here, so nothing overflows.
+template <int D>
+__device__ inline void grow_units(State<D, 1>& st, const float (&sc)[Shape<D, 1>::SUB][4], const Scales<D, 1>& scale, float scale_log2, float r0, float r1, int steps) {
+  auto exponent = [](float x) { return (int)(__float_as_uint(x) >> 23 & 255u) - 127; };
+  int k0 = -1000, k1 = -1000, top = -1000;
+#pragma unroll
+  for (int s = 0; s < Shape<D, 1>::SUB; ++s) {
+    if (s > 0 && s >= steps) break;
+    float pr[4];
+    probabilities(pr, sc[s], scale_log2, r0, r1);
+    const int e = exponent(scale.of[s].y);
+    k0 = max(k0, e + exponent(fmaxf(pr[0], pr[2])));                   // (NaN beside a number counts for nothing)
+    k1 = max(k1, e + exponent(fmaxf(pr[1], pr[3])));
+    top = max(top, e);
+  }
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) {
+    k0 = max(k0, __shfl_xor_sync(0xffffffffu, k0, o));
+    k1 = max(k1, __shfl_xor_sync(0xffffffffu, k1, o));
+  }
+  const float n0 = fminf(st.e0, (float)min(13 - k0, 125 - top)), n1 = fminf(st.e1, (float)min(13 - k1, 125 - top));
+  const float f0 = ex2(n0 - st.e0), f1 = ex2(n1 - st.e1);
+#pragma unroll
+  for (int i = 0; i < Shape<D, 1>::MT; ++i) { st.o[i][0] *= f0; st.o[i][1] *= f1; st.o[i][2] *= f0; st.o[i][3] *= f1; }
+  st.e0 = n0; st.e1 = n1;
+  st.c0 = ex2(n0); st.c1 = ex2(n1);
+}
+// Whether one of the four is above 2^15 or NaN.
+__device__ inline bool beyond(uint32_t a, uint32_t b) {
+  const __half2 most = __hmax2_nan(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  return !__hble2(most, __half2half2(__ushort_as_half(0x7800)));
+}
+
 // The second half of tile_values for an 8-bit cache: probabilities from the scores against the reference r0, r1, and
-// O^T += V^T P^T.  The probabilities enter the product as fp16 (11 bits: half a step is an eighth of the result's own rounding, and V
-// has four bits; a second term would cost as many MMA instructions again), times the step's scale of V in units of st.unit: within
-// 2^4 of it no bits are lost and nothing overflows (a probability is at most 2^8); a scale further off becomes the unit, and the
-// sums so far are converted to it.
+// O^T += V^T P^T.  The probabilities enter the product as fp16 (11 bits: half a step is 2^-11, an eighth of the result's own rounding, and
+// V has four bits; a second term would cost as many MMA instructions again), times the step's scale of V, in units of each head's own:
+// the largest product of the two so far was 2^13 to 2^15 when it came, whichever of them made it large, and none is above 2^15.
+// What is 2^27 below it or less loses bits (to 2^-38 of it): a long tail behind a key that takes nearly all of the weight counts in
+// full, and blocks whose scales are any powers of two apart can neither overflow nor hide each other.  One check a tile, on the
+// packed products (a check a step keeps the steps apart: d = 16 36.6 us against 34.8, d = 32 40.2 against 39.2, for 64 sequences of up to
+// 16000 keys; in logarithms of the scores, before the tile's vote on the maximum, 34.8 and 38.7, but d = 64 57.6 against 55.6).
 template <int D>
 __device__ inline void add_values8(State<D, 1>& st, const float (&sc)[Shape<D, 1>::SUB][4], Tile<D, 1>& x, const Scales<D, 1>& scale, float scale_log2,
                                    float r0, float r1, int key0, int len, int t) {
   using Sh = Shape<D, 1>;
+  const int steps = (len - key0 + 15) >> 4;        // of the tile that have been copied
+  uint32_t h[Sh::SUB][2];
+  auto products = [&](bool sums) {                 // whether one of them is above 2^15 (or not a number: a factor beyond fp32 and a zero)
+    bool over = false;
+#pragma unroll
+    for (int s = 0; s < Sh::SUB; ++s) {
+      float pr[4];
+      probabilities(pr, sc[s], scale_log2, r0, r1);
+      if (sums) {
+        st.l0 += pr[0] + pr[2];
+        st.l1 += pr[1] + pr[3];
+      }
+      const float unit = s > 0 && s >= steps ? 0.f : scale.of[s].y, f0 = unit * st.c0, f1 = unit * st.c1;
+      h[s][0] = pack_f16(pr[0] * f0, pr[1] * f1);
+      h[s][1] = pack_f16(pr[2] * f0, pr[3] * f1);
+      over |= beyond(h[s][0], h[s][1]);
+    }
+    return over;
+  };
+  if (__any_sync(0xffffffffu, products(true))) {
+    grow_units<D>(st, sc, scale, scale_log2, r0, r1, steps);
+    products(false);
+  }
 #pragma unroll
   for (int s = 0; s < Sh::SUB; ++s) {
-    if (s > 0 && key0 + 16 * s >= len) break;                          // nothing has been copied
-    float pr[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) pr[e] = ex2(fmaf(sc[s][e], scale_log2, (e & 1) ? -r1 : -r0));
-    st.l0 += pr[0] + pr[2];
-    st.l1 += pr[1] + pr[3];
-    const float unit = scale.of[s].y;
-    float f = unit * st.inverse;
-    if (!(f <= 16.f && f >= 0.0625f)) {
-      const float inverse = 1.f / unit, down = st.unit * inverse;
-#pragma unroll
-      for (int i = 0; i < Sh::MT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st.o[i][e] *= down;
-      st.unit = unit;
-      st.inverse = inverse;
-      f = 1.f;
-    }
-    const uint32_t b0 = transpose8x8(pack_f16(pr[0] * f, pr[1] * f)), b1 = transpose8x8(pack_f16(pr[2] * f, pr[3] * f));
+    if (s > 0 && s >= steps) break;
+    const uint32_t b0 = transpose8x8(h[s][0]), b1 = transpose8x8(h[s][1]);
     if (s == 0) clear_behind(x, key0, len, t);
 #pragma unroll
     for (int c = 0; c < Sh::VCH; ++c)
@@ -146,6 +196,15 @@ __device__ inline void add_values8(State<D, 1>& st, const float (&sc)[Shape<D, 1
         }
       }
   }
+}
+
+// 8 bits: the reference rises by `up` (log2), and c may be 2^most.  c rises as far as it may with the reference, so that the sums keep
+// their size (nothing is lost when keys without values take the weight); returns the factor for the sums that is left, at most 1.
+__device__ inline float move_unit(float& e, float& c, float up, float most) {
+  const float n = fminf(e + up, fminf(most, kMostUp)), f = ex2(n - e - up);
+  e = n;
+  c = ex2(n);
+  return f;
 }
 
 // Softmax step and O^T += V^T P^T of the tile that begins at key0 of `len` keys.
@@ -172,10 +231,30 @@ __device__ inline void tile_values(State<D, B>& st, float (&sc)[Shape<D, B>::SUB
       mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
     }
     const float n0 = fmaxf(st.m0, mx0), n1 = fmaxf(st.m1, mx1);
-    const float f0 = st.m0 == -INFINITY ? 0.f : ex2((st.m0 - n0) * scale_log2);
-    const float f1 = st.m1 == -INFINITY ? 0.f : ex2((st.m1 - n1) * scale_log2);
-    st.m0 = n0; st.m1 = n1;
+    float f0 = st.m0 == -INFINITY ? 0.f : ex2((st.m0 - n0) * scale_log2);
+    float f1 = st.m1 == -INFINITY ? 0.f : ex2((st.m1 - n1) * scale_log2);
     st.l0 *= f0; st.l1 *= f1;
+    if constexpr (B == 1) {                          // units, by the largest product of probability and scale (log2), and the largest scale
+      float w0 = -INFINITY, w1 = -INFINITY, top = -INFINITY;
+#pragma unroll
+      for (int s = 0; s < Sh::SUB; ++s) {
+        const float unit = s > 0 && key0 + 16 * s >= len ? -INFINITY : __log2f(scale.of[s].y);
+        w0 = fmaxf(w0, fmaf(fmaxf(sc[s][0], sc[s][2]), scale_log2, unit));
+        w1 = fmaxf(w1, fmaf(fmaxf(sc[s][1], sc[s][3]), scale_log2, unit));
+        top = fmaxf(top, unit);
+      }
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        w0 = fmaxf(w0, __shfl_xor_sync(0xffffffffu, w0, o));
+        w1 = fmaxf(w1, __shfl_xor_sync(0xffffffffu, w1, o));
+      }
+      // (no reference yet: no sums)
+      const float g0 = move_unit(st.e0, st.c0, st.m0 == -INFINITY ? 0.f : (n0 - st.m0) * scale_log2, fminf(14.f - fmaf(-n0, scale_log2, w0), 125.f - top));
+      const float g1 = move_unit(st.e1, st.c1, st.m1 == -INFINITY ? 0.f : (n1 - st.m1) * scale_log2, fminf(14.f - fmaf(-n1, scale_log2, w1), 125.f - top));
+      f0 = st.m0 == -INFINITY ? 0.f : g0;
+      f1 = st.m1 == -INFINITY ? 0.f : g1;
+    }
+    st.m0 = n0; st.m1 = n1;
 #pragma unroll
     for (int i = 0; i < Sh::MT; ++i) { st.o[i][0] *= f0; st.o[i][1] *= f1; st.o[i][2] *= f0; st.o[i][3] *= f1; }
   }
@@ -230,10 +309,9 @@ __device__ inline void finish(State<D, B>& st, float scale_log2) {
   st.m0 *= scale_log2;
   st.m1 *= scale_log2;
   if constexpr (B == 1) {
+    const float u0 = ex2(-st.e0), u1 = ex2(-st.e1);
 #pragma unroll
-    for (int i = 0; i < Shape<D, B>::MT; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) st.o[i][e] *= st.unit;
+    for (int i = 0; i < Shape<D, B>::MT; ++i) { st.o[i][0] *= u0; st.o[i][1] *= u1; st.o[i][2] *= u0; st.o[i][3] *= u1; }
   }
 }
 
