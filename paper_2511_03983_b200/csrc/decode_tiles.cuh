@@ -458,7 +458,8 @@ __device__ inline void step_scores(float (&sc)[4], const uint32_t (&k)[2][Shape<
     }
   }
   if constexpr (B == 1) {
-    const float f0 = scale * q.f0, f1 = scale * q.f1;
+    // (finite: a product that is zero stays zero beside a scale and a query whose sizes are beyond fp32 together)
+    const float f0 = fminf(scale * q.f0, 0x1p127f), f1 = fminf(scale * q.f1, 0x1p127f);
     sc[0] *= f0; sc[1] *= f1; sc[2] *= f0; sc[3] *= f1;
   }
 }

@@ -1,5 +1,5 @@
 """The 8-bit decode over its whole range: sums that are large in units of a block whose values are all zero, scales at both ends of fp32,
-and probabilities far below the largest.
+probabilities far below the largest, and keys whose scale is large beside products that are zero.
 
 Tolerance of a result (the definition in 64 bits, p = exp(s - max), l = sum p, mass = sum p |v| / l):
  * its own rounding to bf16: half a step is 2^-8 of it, and 2^-134 where it is subnormal;
@@ -155,4 +155,18 @@ def test_probabilities_far_below_the_largest(B, D, below, way):
     blocks = np.arange(vs.shape[2]) % 16 == 0
     vs[:] = 0.7
     vs[:, 0, blocks] = 2.0 ** -40
+    check(*run(B, q, k, v, ks, vs, lens), lens, vs)
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("D", [16, 64, 128])
+def test_scores_that_are_zero_beside_a_large_scale(B, D, way):
+    """Keys of zeros in blocks whose scale times the queries' size is beyond fp32: their scores are zero."""
+    rng = np.random.default_rng(D)
+    n, m, lens, q, k, v, ks, vs = case(rng, way, D)
+    ks[:] = 2.0 ** -50
+    big = rng.random(ks.shape) < 0.3
+    ks[big] = 2.0 ** 119
+    k[np.repeat(big, BLOCK, 2)[:, :, :m]] = 0
+    q *= 2.0 ** 42
     check(*run(B, q, k, v, ks, vs, lens), lens, vs)
