@@ -615,8 +615,9 @@ int32_t twist_attn_decode_q8(const twist_attn_decode_q8_args* a /*host*/, void* 
  *   seen (device int32 [S][n_seqs] or NULL: kv_len).  slot_pos may be NULL.
  *   cache TWIST_CACHE_BF16 (scales NULL) or TWIST_CACHE_E4M3.  Only K is read.  Positions that no head reads, and slots from kv_len
  *   on, are left as they were.
- * Index data is checked on the device as by twist_attn_decode; a new_len outside [0, kv_len] is clamped and reported.  fp32
- * sums in a fixed order.  dtype TWIST_BF16; d_head in {8, 16, 32, 64, 128}, for e4m3 from 16 on; limits as twist_attn_decode. */
+ * Index data is checked on the device as by twist_attn_decode, but tokens whose page lies outside the pool are skipped: nothing is
+ * written for them; a new_len outside [0, kv_len] is clamped and reported.  fp32 sums in a fixed order.
+ * dtype TWIST_BF16; d_head in {8, 16, 32, 64, 128}, for e4m3 from 16 on; limits as twist_attn_decode. */
 enum { TWIST_CACHE_BF16 = 0, TWIST_CACHE_E4M3 = 1 };
 typedef struct {
   int32_t dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads, n_kv_heads;

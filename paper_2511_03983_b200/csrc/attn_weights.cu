@@ -48,7 +48,7 @@ struct KeyRing {
     float prior[TILE];
   } tile[kRing];
   float2 scale[kRing][SUB];
-  int page[kRing][SUB];
+  int page[kRing][SUB];                        // -1: outside the pool, nothing may be written
   alignas(16) uint64_t full[kRing];            // of every step: its bytes to expect and, 8 bits, its scale
 };
 
@@ -121,11 +121,12 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
   if (now.seq < 0) return;
   // The filling side walks the units by itself, kRing tiles ahead.
   Unit at = now, behind = now;
-  bool live = false;
+  bool live = false, inside = false;
   int tile = now.t0, n = 0, head_ids = 0, to = 0, id = 0, in_page = 0;
   int next_ids = fetch_pages<SUB>(p, now.seq, now.t0, 1, lane);
   auto window = [&](int ids) {                       // the page ids of the AHEAD tiles from `tile` on have come
     id = check_pages<SUB>(p, ids, at.len - 1, tile, 1, lane);
+    inside = id == ids;
     next_ids = fetch_pages<SUB>(p, at.seq, tile + AHEAD, 1, lane);
     const int key = (int)step_key<SUB>(tile, 1, lane);
     in_page = key & ((1 << p.page_shift) - 1);
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
     if (lane / SUB == n) {
       const int step = lane % SUB;
       const uint32_t bar = smem_u32(&ring.full[to]);
-      ring.page[to][step] = id;
+      ring.page[to][step] = inside ? id : -1;
       if (live) {
         const long long row = (((long long)id * p.kv_max + at.pos) << p.page_shift) + in_page;
         const bool prior = at.rt == 0 && w.prior;
@@ -243,10 +244,11 @@ __global__ void __launch_bounds__(kDecThreads, 4) weights_kernel(const WeightPar
           }
         }
         const int in_tile = g + (SUB == 4 ? 16 * t : SUB == 2 ? 8 * t : 8 * (t >> 1)), key = i * TILE + in_tile;
-        const long long to_ = (((long long)ring.page[slot][in_tile >> 4] * p.kv_max + now.pos) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+        const int page = ring.page[slot][in_tile >> 4];
+        const long long to_ = (((long long)page * p.kv_max + now.pos) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
 #pragma unroll
         for (int e = 0; e < (SUB == 4 ? 2 : 1); ++e) {
-          if (key + 8 * e < now.len && (SUB > 1 || (t & 1) == 0)) {
+          if (key + 8 * e < now.len && page >= 0 && (SUB > 1 || (t & 1) == 0)) {
             if (now.rt > 0) {
               w.weights[to_ + 8 * e] += a[e];        // the same thread wrote it
             } else {
