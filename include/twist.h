@@ -601,6 +601,11 @@ typedef struct {
 } twist_attn_decode_q8_args;
 
 int32_t twist_attn_decode_q8(const twist_attn_decode_q8_args* a /*host*/, void* stream);
+/* Self-test of what twist_attn_decode_q8 leaves when waits run out (for tests): the call through the line of work, in which every
+ * `every`-th warp gives up before tile `tile` of an item as if a copy had not come.  twist_device_status reports
+ * TWIST_ERR_DEVICE_TIMEOUT once; items that such a warp had a part in are undefined or keep their old output, all memory beside out
+ * and lse is left alone, and the scratch can be used by the next call.  d_head 64 only. */
+int32_t twist_selftest_decode_quit(const twist_attn_decode_q8_args* a /*host*/, int32_t every, int32_t tile, void* stream);
 
 /* The attention weight that a cached token has gathered, weights [n_pages][kv_max][page_size] fp32, and its position in the
  * sequence, slot_pos [n_pages][kv_max][page_size] int32: for each KV position on its own, in the places of the token's K and V.

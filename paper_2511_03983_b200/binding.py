@@ -39,7 +39,7 @@ EXPORTS = [
     "twist_plan_stats", "twist_workspace_bytes", "twist_aggregate_partial", "twist_aggregate_finish",
     "twist_rope_fwd", "twist_rope_bwd", "twist_kv_append", "twist_attn_decode", "twist_attn_decode_workspace_bytes",
     "twist_kv_append_q8", "twist_attn_decode_q8", "twist_attn_weights", "twist_attn_core_weights", "twist_kv_evict",
-    "twist_kv_evict_workspace_bytes",
+    "twist_kv_evict_workspace_bytes", "twist_selftest_decode_quit",
 ]
 
 
@@ -279,6 +279,7 @@ def lib() -> C.CDLL:
                      "twist_attn_decode", "twist_kv_append_q8", "twist_attn_decode_q8", "twist_attn_weights",
                      "twist_attn_core_weights", "twist_kv_evict"):
             getattr(h, name).argtypes = [C.c_void_p, C.c_void_p]
+        h.twist_selftest_decode_quit.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
         h.twist_attn_decode_workspace_bytes.restype = C.c_size_t
         h.twist_attn_decode_workspace_bytes.argtypes = [C.c_int32]
         h.twist_kv_evict_workspace_bytes.restype = C.c_size_t
@@ -740,6 +741,11 @@ def attn_decode_q8_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_h
 
 def twist_attn_decode_q8(a: AttnDecodeQ8Args):
     _check(lib().twist_attn_decode_q8(C.byref(a), _stream()), "twist_attn_decode_q8")
+
+
+def twist_selftest_decode_quit(a: AttnDecodeQ8Args, every: int, tile: int):
+    """The decode call in which every `every`-th warp gives up before tile `tile` of an item (for tests)."""
+    _check(lib().twist_selftest_decode_quit(C.byref(a), every, tile, _stream()), "twist_selftest_decode_quit")
 
 
 def attn_weights_args(dtype, n_subnets, n_seqs, head_keep, kv_max, d_head, n_heads=0, n_kv_heads=0, max_len=0, *, q, lse, k_cache,

@@ -565,7 +565,8 @@ constexpr int kRingBytes = B == 1 ? kDecWarps * (int)sizeof(Ring<D>) : (kStaged<
 
 constexpr int kCountCache = 256;      // KV positions of all subnets whose heads a CTA counts
 
-template <int D, int B>
+// QUITS: for the self-test of the way out that a warp takes when a wait of it has run out.
+template <int D, int B, bool QUITS = false>
 __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_kernel(const DecParams p) {
   using Sh = Shape<D, B>;
   __shared__ int cols[kDecWarps][2][kCols];
@@ -704,6 +705,21 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     }
     return x;
   };
+  // the entry of the item that begins with segment x
+  auto describe = [&](const Segment& x, int4 entry) {
+    if (lane != 0) return;
+    if (!p.by_item) {
+      p.desc[c] = entry;
+      return;
+    }
+    const int all = p.kv_max * p.row_tiles, item = x.pos * p.row_tiles + x.rt;
+    int4* desc = p.desc + (long long)x.seq * all;
+    desc[item] = entry;
+    // the neighbours in the table that are no items
+    auto is_item = [&](int k) { return k % p.row_tiles < row_tiles(x.s, k / p.row_tiles); };
+    for (int k = item + 1; k < all && !is_item(k); ++k) desc[k] = make_int4(0, 0, 0, 0);
+    for (int k = item - 1; k >= 0 && !is_item(k); --k) desc[k] = make_int4(0, 0, 0, 0);
+  };
   // a segment's result
   auto store = [&](const State<D, B>& st, const Segment& now, int hq) {
     const bool whole = now.t0 == 0 && now.t1 == now.nt;
@@ -718,17 +734,8 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     }
     if (now.t0 == 0 && (p.by_item || !whole)) {
       const int heads = __popc(__ballot_sync(0xffffffffu, hq >= 0 && t == 0));
-      if (lane == 0) {
-        const int parts = whole ? 0 : (int)(cut.piece_of(item0 + kItemCost<B> + now.nt - 1) - c);    // further parts of the item
-        const int all = p.kv_max * p.row_tiles, item = now.pos * p.row_tiles + now.rt;
-        int4* desc = p.desc + (p.by_item ? (long long)now.seq * all : (long long)c);
-        desc[p.by_item ? item : 0] = make_int4(now.seq, heads, parts, (int)c);
-        if (p.by_item) {                            // the neighbours in the table that are no items
-          auto is_item = [&](int k) { return k % p.row_tiles < row_tiles(now.s, k / p.row_tiles); };
-          for (int k = item + 1; k < all && !is_item(k); ++k) desc[k] = make_int4(0, 0, 0, 0);
-          for (int k = item - 1; k >= 0 && !is_item(k); --k) desc[k] = make_int4(0, 0, 0, 0);
-        }
-      }
+      const int parts = whole ? 0 : (int)(cut.piece_of(item0 + kItemCost<B> + now.nt - 1) - c);          // further parts of the item
+      describe(now, make_int4(now.seq, heads, parts, (int)c));
     }
   };
   if constexpr (B == 1) {
@@ -799,6 +806,14 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
     look();
 #pragma unroll 1
     for (int i = 0; i < kRing<D>; ++i) fill();
+    auto quits = [&](int tile) {
+      if (c % (uint32_t)p.quit_every != 0 || tile < p.quit_tile) return false;
+      if (lane == 0) {
+        abort_flag = 1;
+        note_status(p.status, (int)TWIST_ERR_DEVICE_TIMEOUT);
+      }
+      return true;
+    };
     int buf = 0, slot = 0, since = kRing<D>;
     uint32_t parity = 0;
     bool ok = true;
@@ -824,6 +839,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
       if (now.len > 0) {
         for (int i = now.t0; i < now.t1; ++i) {
           ok = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&ring8.full[slot]), parity, &abort_flag, p.status));
+          if constexpr (QUITS) ok = ok && !quits(i - now.t0);
           if (!ok) break;
           Tile<D, B> x;
           Scales<D, B> scale;
@@ -849,7 +865,17 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 4 : 3) decode_split_ker
       now = next;
       buf ^= 1;
     }
-    if (!ok) drain_after_abort(&abort_flag);
+    if (!ok) {
+      // the join will read an entry of every item: those that were to begin here get empty ones
+      while (p.by_item) {
+        if (now.t0 == 0) describe(now, make_int4(0, 0, 0, 0));
+        if (left <= (uint32_t)kItemCost<B>) break;
+        now = following(now);
+        now.t1 = (int)min((uint32_t)now.nt, left - kItemCost<B>);
+        left -= now.t1 + kItemCost<B>;
+      }
+      drain_after_abort(&abort_flag);
+    }
     return;
   } else {
   constexpr bool STAGED = kStaged<D, B>;
@@ -1015,7 +1041,7 @@ bool over_queries(const DecParams& p, int d) {
 size_t max_warps() { return (size_t)sm_count() * kMaxCtasPerSm * kDecWarps; }
 size_t desc_bytes() { return (max_warps() * sizeof(int4) + 255) / 256 * 256; }
 
-template <int D, int B>
+template <int D, int B, bool QUITS = false>
 int run(DecParams& p, long long max_len, cudaStream_t st) {
   const long long items = (long long)p.S * p.n_seqs * p.kv_max * p.row_tiles;
   // the line is counted in 32 bits
@@ -1030,8 +1056,8 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
     int n = 0;
     TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_join_kernel<D>, kJoinThreads, 0));
     join_resident[slot] = n < 1 ? 1 : n;
-    TWIST_CUDA_TRY(cudaFuncSetAttribute(decode_split_kernel<D, B>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<D, B>));
-    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_split_kernel<D, B>, kDecThreads, kRingBytes<D, B>));
+    TWIST_CUDA_TRY(cudaFuncSetAttribute(decode_split_kernel<D, B, QUITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<D, B>));
+    TWIST_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, decode_split_kernel<D, B, QUITS>, kDecThreads, kRingBytes<D, B>));
     resident[slot] = n < 1 ? 1 : (n > kMaxCtasPerSm ? kMaxCtasPerSm : n);
   }
   const long long grid = (long long)sm_count() * resident[slot];
@@ -1047,13 +1073,13 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   int cluster = 1;
   if (tiles > 2 * kDecWarps)
     while (cluster < kMaxCluster && 2 * cluster * items <= grid && tiles > kDecWarps * cluster) cluster *= 2;
-  if (items <= 2 * grid && tiles <= kShortTiles * kDecWarps * cluster &&
+  if (!QUITS && items <= 2 * grid && tiles <= kShortTiles * kDecWarps * cluster &&
       tiles * items <= (items <= grid ? kShortWork : kShortWaves) * grid * kDecWarps) {
     TWIST_CUDA_TRY(launch_overlapped(decode_whole_kernel<D, B>, dim3((unsigned)(items * cluster)), dim3(kDecThreads), 0, st, cluster, p));
     return TWIST_OK;
   }
   p.by_item = items <= grid * kDecWarps;
-  TWIST_CUDA_TRY(launch_overlapped(decode_split_kernel<D, B>, dim3((unsigned)grid), dim3(kDecThreads), kRingBytes<D, B>, st, 1, p));
+  TWIST_CUDA_TRY(launch_overlapped(decode_split_kernel<D, B, QUITS>, dim3((unsigned)grid), dim3(kDecThreads), kRingBytes<D, B>, st, 1, p));
   // An item of an even batch is cut into about warps / items parts: the fewer items, the more threads share the parts of
   // one, down to eight parts each, as long as all threads of the join run at once.  The whole call, with twice the threads
   // against without: where they fit, four heads on a position, 16 items, d = 16 and 32: 15.9 and 16.5 us against 17.5; one
@@ -1130,6 +1156,15 @@ long long bound_of(const A* a) {
   return a->max_len > 0 && a->max_len < table_len ? a->max_len : table_len;
 }
 
+int set_up_q8(const twist_attn_decode_q8_args* a, DecParams& p) {
+  const int rc = set_up(a, p, 16);
+  if (rc != TWIST_OK) return rc;
+  if (!a->scales) return TWIST_ERR_NULL;
+  if (!aligned16(a->scales)) return TWIST_ERR_SHAPE;
+  p.scales = reinterpret_cast<const float2*>(a->scales);
+  return TWIST_OK;
+}
+
 }  // namespace
 
 extern "C" int32_t twist_attn_decode(const twist_attn_decode_args* a, void* stream) {
@@ -1151,11 +1186,8 @@ extern "C" int32_t twist_attn_decode(const twist_attn_decode_args* a, void* stre
 extern "C" int32_t twist_attn_decode_q8(const twist_attn_decode_q8_args* a, void* stream) {
   if (!a) return TWIST_ERR_NULL;
   DecParams p;
-  const int rc = set_up(a, p, 16);
+  const int rc = set_up_q8(a, p);
   if (rc != TWIST_OK) return rc;
-  if (!a->scales) return TWIST_ERR_NULL;
-  if (!aligned16(a->scales)) return TWIST_ERR_SHAPE;
-  p.scales = reinterpret_cast<const float2*>(a->scales);
   const long long max_len = bound_of(a);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   switch (a->d_head) {
@@ -1164,4 +1196,16 @@ extern "C" int32_t twist_attn_decode_q8(const twist_attn_decode_q8_args* a, void
     case 64: return run<64, 1>(p, max_len, st);
     default: return run<128, 1>(p, max_len, st);
   }
+}
+
+extern "C" int32_t twist_selftest_decode_quit(const twist_attn_decode_q8_args* a, int32_t every, int32_t tile, void* stream) {
+  if (!a) return TWIST_ERR_NULL;
+  if (every <= 0 || tile < 0) return TWIST_ERR_SHAPE;
+  if (a->d_head != 64) return TWIST_ERR_UNSUPPORTED;
+  DecParams p;
+  const int rc = set_up_q8(a, p);
+  if (rc != TWIST_OK) return rc;
+  p.quit_every = every;
+  p.quit_tile = tile;
+  return run<64, 1, true>(p, bound_of(a), static_cast<cudaStream_t>(stream));
 }

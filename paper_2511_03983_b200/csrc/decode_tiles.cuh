@@ -37,6 +37,7 @@ struct DecParams {
   int by_item;                // desc has an entry for every item (few items), else one for every warp
   int page_shift, n_pages, max_pages;
   float scale_log2;
+  int quit_every, quit_tile;  // self-test: the warps that give up, and before which tile of an item
   int* status;
 };
 
