@@ -1178,10 +1178,12 @@ class DecodeSession:
     queries (its last `last_queries`, 0: all of them) and from every step's, and a sequence that has grown `slack` tokens (one
     page unless said otherwise) beyond K is cut to its K tokens of most weight, the `recent` newest always among them, before
     the next step.  The cut is each KV position's own.  max_len then bounds what a sequence holds, not how long it gets.  (What the
-    layers of a step that raises had added to the weights stays.)"""
+    layers of a step that raises had added to the weights stays.)  A cut that raises when some layers have been cut leaves the
+    layers with different tokens: the session then refuses everything but release until all its sequences have been released."""
 
     # what a session without these options has
     cache_bits, keep = 16, None
+    broken: Optional[str] = None                                    # why the cache cannot be used
 
     def __init__(self, eng: StackEngine, max_len: int, page_size: int = 16, n_pages: Optional[int] = None, graph: bool = False,
                  cache_bits: int = 16, keep: Optional[int] = None, recent: int = 0, slack: Optional[int] = None,
@@ -1294,7 +1296,13 @@ class DecodeSession:
         self.pages[s][b], self.lens[s][b] = [], 0
         if self.keep is not None:
             self.seen[s][b] = 0
+        if not any(map(any, self.lens)):
+            self.broken = None
         self._lengths()
+
+    def _usable(self):
+        if self.broken:
+            raise RuntimeError(self.broken)
 
     def _cache(self, l: int):
         scales = dict(scales=self.scales[l]) if self.cache_bits == 8 else {}
@@ -1305,25 +1313,36 @@ class DecodeSession:
         does this by itself, with beyond = slack."""
         if self.keep is None:
             raise ValueError("a session without keep holds every token")
+        self._usable()
         over = max(1, beyond)
         lens = [[self.keep if m >= self.keep + over else m for m in row] for row in self.lens]
         if lens == self.lens:
             return
         w, eng = self.eng.w, self.eng
         self.keep_len.copy_(torch.tensor(lens, dtype=torch.int32))
-        for l in range(w.n_layers):
+        calls = []
+        for l in range(w.n_layers):                                 # all of them before the first is launched: a refusal cuts nothing
             eng._bind(l)
-            with eng._timed("evict"):
-                B.twist_kv_evict(B.kv_evict_args(w.dtype, self.S, self.n, eng.kv_max, w.d_head, self.recent, weights=self.weights[l],
-                                                 slot_pos=self.slot_pos[l], keep=self.keep_len, seen=self.seen_len,
-                                                 kv_count=eng.kv_count[l], ws=self.evict_ws, **self._cache(l)))
-            eng.launches += 1
-        self.lens = lens
-        for s in range(self.S):
-            for b in range(self.n):
-                while (len(self.pages[s][b]) - 1) * self.page_size >= max(1, lens[s][b]):
-                    self.free.append(self.pages[s][b].pop())
-        self._lengths()
+            calls.append(B.kv_evict_args(w.dtype, self.S, self.n, eng.kv_max, w.d_head, self.recent, weights=self.weights[l],
+                                         slot_pos=self.slot_pos[l], keep=self.keep_len, seen=self.seen_len, kv_count=eng.kv_count[l],
+                                         ws=self.evict_ws, **self._cache(l)))
+        done = 0
+        try:
+            for args in calls:
+                with eng._timed("evict"):
+                    B.twist_kv_evict(args)
+                done += 1
+                eng.launches += 1
+            self.lens = lens
+            for s in range(self.S):
+                for b in range(self.n):
+                    while (len(self.pages[s][b]) - 1) * self.page_size >= max(1, lens[s][b]):
+                        self.free.append(self.pages[s][b].pop())
+            self._lengths()
+        except BaseException:
+            if done:
+                self.broken = "a cut of the cache failed when %d of %d layers had been cut: release all sequences" % (done, w.n_layers)
+            raise
 
     def _append(self, l: int, tokens: int, **t):
         """twist_kv_append into layer l's cache, whatever it is held in."""
