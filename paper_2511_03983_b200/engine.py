@@ -1320,10 +1320,10 @@ class DecodeSession:
             return
         w, eng = self.eng.w, self.eng
         self.keep_len.copy_(torch.tensor(lens, dtype=torch.int32))
-        calls = []
+        longest, calls = max(map(max, self.lens)), []               # the work is laid out for what there is, not for the room
         for l in range(w.n_layers):                                 # all of them before the first is launched: a refusal cuts nothing
             eng._bind(l)
-            calls.append(B.kv_evict_args(w.dtype, self.S, self.n, eng.kv_max, w.d_head, self.recent, weights=self.weights[l],
+            calls.append(B.kv_evict_args(w.dtype, self.S, self.n, eng.kv_max, w.d_head, self.recent, longest, weights=self.weights[l],
                                          slot_pos=self.slot_pos[l], keep=self.keep_len, seen=self.seen_len, kv_count=eng.kv_count[l],
                                          ws=self.evict_ws, **self._cache(l)))
         done = 0

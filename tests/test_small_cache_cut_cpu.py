@@ -71,3 +71,14 @@ def test_a_cut_that_is_refused_before_anything_was_cut_changes_nothing(monkeypat
     monkeypatch.setattr(E.B, "kv_evict_args", lambda *a, **k: k)
     s.evict()
     assert len(calls) == 2 and s.lens == [[8, 3], [0, 8]]
+
+
+def test_a_cut_is_laid_out_for_the_longest_sequence_not_for_the_room(monkeypatch):
+    s, _ = grown(monkeypatch)
+    bounds = []
+    monkeypatch.setattr(E.B, "kv_evict_args", lambda *a, **k: bounds.append(k.get("max_len", a[6] if len(a) > 6 else 0)) or k)
+    s.evict()
+    with s._growing([[1, 6], [0, 3]]):
+        pass
+    s.evict()
+    assert bounds == [14, 14, 11, 11]                             # of 24
