@@ -648,7 +648,8 @@ int32_t twist_attn_weights(const twist_attn_weights_args* a /*host*/, void* stre
 /* twist_attn_core_weights -- the same for prompts: what the queries of every sequence gave each of its tokens under the causal mask,
  *     weights[j] = sum_h sum_i exp(q_hi . k_j / sqrt(d_head) - lse_hi),   i >= j, i >= len - last_queries,
  *   written (not added) for the first len = new_len[s][b] tokens (NULL: seq_len) of the n_seqs sequences of seq_len rows, token j
- *   in slot j of the sequence's pages; slot_pos[j] = j (may be NULL).  last_queries 0: all queries.
+ *   in slot j of the sequence's pages; slot_pos[j] = j (may be NULL).  Positions that no head reads are left as they were (twist_kv_evict
+ *   ranks what stands there: kv_count keeps it from them).  last_queries 0: all queries.
  *   qkv, lse, head_idx, kv_pos as in twist_attn_core_args (qkv rotated, lse from twist_attn_core_fwd).  Rows behind len may hold anything.
  * Index data is checked on the device: a bad head entry is replaced by position 0, a len outside [0, seq_len] is clamped, tokens
  * whose page lies outside the table or the pool are skipped, and TWIST_ERR_BAD_INDEX recorded.  fp32 sums in a fixed order.

@@ -59,3 +59,33 @@ def test_weights_of_tokens_whose_page_is_bad_are_written_nowhere(B, D, page, len
                 rest = np.setdiff1d(np.arange(c["pool"]), lost)
                 assert np.array_equal(got[rest], want[rest]) and np.array_equal(at[rest], where[rest]), (entry, bad, in_place)
                 assert np.all(got[lost] == (host(prior)[lost] if in_place else -3.0)) and np.all(at[lost] == -9)
+
+
+@pytest.mark.parametrize("D,N", [(8, 70), (16, 40), (32, 300), (64, 129), (128, 200)])
+def test_positions_without_heads_are_left_as_they_were(B, D, N):
+    """Both heads read position 1 of three: the others' weights and positions stay, of prompts and of a step."""
+    gen = torch.Generator().manual_seed(D)
+    page, KV, H = 16, 3, 2
+    pages = -(-N // page)
+    table = i32([[list(range(1, pages + 1))]])
+    heads = dict(head_idx=i32([[2, 3]]), kv_pos=i32([[0, 1, 2]]))
+    x = torch.randn(1, N, (H + 2 * KV) * D, generator=gen).to(torch.bfloat16).cuda()
+    k = torch.randn(pages + 2, KV, page, D, generator=gen).to(torch.bfloat16).cuda()
+
+    def check(call):
+        w = torch.full((pages + 2, KV, page), -3.0, device="cuda")
+        pos = torch.full(w.shape, -9, dtype=torch.int32, device="cuda")
+        call(w, pos)
+        assert B.twist_device_status() == 0
+        mine = torch.zeros_like(w, dtype=torch.bool)
+        mine[1:pages + 1, 1] = True
+        mine[pages, 1, N - (pages - 1) * page:] = False
+        assert torch.all(w[~mine] == -3.0) and torch.all(pos[~mine] == -9) and torch.all(w[mine] >= 0)
+        return pos[mine]
+
+    lse = torch.full((1, H, N), 20.0, device="cuda")
+    assert torch.equal(check(lambda w, pos: B.twist_attn_core_weights(B.attn_core_weights_args(
+        B.BF16, 1, 1, N, H, KV, D, 6, 3, qkv=x, lse=lse, page_table=table, weights=w, slot_pos=pos, **heads))), torch.arange(N, dtype=torch.int32, device="cuda"))
+    check(lambda w, pos: B.twist_attn_weights(B.attn_weights_args(
+        B.BF16, 1, 1, H, KV, D, 6, 3, q=x[:, :1, :H * D], lse=lse[:, :, :1].contiguous(), k_cache=k, page_table=table, kv_len=i32([[N]]), new_len=i32([[N]]),
+        weights=w, slot_pos=pos, **heads)))
