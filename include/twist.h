@@ -686,7 +686,8 @@ int32_t twist_attn_core_weights(const twist_attn_core_weights_args* a /*host*/, 
  *   calls that may overlap on the GPU need scratch of their own.
  * Index data is checked on the device: kv_len and keep outside [0, max_len] are clamped, a KV position of a sequence that has a
  * page outside the pool is left as it is, and TWIST_ERR_BAD_INDEX is recorded.  Deterministic.
- * dtype TWIST_BF16; d_head a multiple of 8 (e4m3: 16), at most 256; n_subnets * n_seqs * kv_max <= 2^20, max_len <= 2^26. */
+ * dtype TWIST_BF16; d_head a multiple of 8, at most 256, for e4m3 in {16, 32, 64, 128}; n_subnets * n_seqs * kv_max <= 2^20, max_len
+ * <= 2^26. */
 typedef struct {
   int32_t dtype, n_subnets, n_seqs, kv_max, d_head, page_size, n_pages, max_pages;
   int32_t max_len, recent, cache, reserved;
