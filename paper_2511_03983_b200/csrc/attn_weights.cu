@@ -423,11 +423,6 @@ int run_core(CoreParams& p, cudaStream_t st) {
   return TWIST_OK;
 }
 
-bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
-}
-
 }  // namespace
 }  // namespace twist
 

@@ -38,5 +38,10 @@ inline int device_slot() {
 #define TWIST_LAUNCH_CHECK() TWIST_CUDA_TRY(cudaPeekAtLastError())
 
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Whether two ranges of bytes share one.
+static inline bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
 
 }  // namespace twist

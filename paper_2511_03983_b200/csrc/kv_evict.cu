@@ -67,7 +67,7 @@ __device__ inline uint32_t rank_key(float w, bool guarded) {
 struct Slots {
   const int32_t* table;        // of the sequence, in shared memory where it fits
   long long base;              // kv position
-  int kv, page_shift, n_pages;
+  int kv, page_shift;
   __device__ int page(int i) const { return table[i >> page_shift]; }
   __device__ int offset(int i) const { return i & ((1 << page_shift) - 1); }
   __device__ long long at(int i) const { return (((long long)page(i) * kv + base) << page_shift) + offset(i); }
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictParams 
     keep = max(0, min(keep, p.max_len));
   }
   const int pages = (len + (1 << p.page_shift) - 1) >> p.page_shift;
-  const Slots sl{pages <= kTableCache ? table : p.table + seq * p.max_pages, pos, p.kv, p.page_shift, p.n_pages};
+  const Slots sl{pages <= kTableCache ? table : p.table + seq * p.max_pages, pos, p.kv, p.page_shift};
   const bool in_place = p.weights == p.weights_out;
   if (len <= keep) {                                                   // all stay
     if (in_place) return;
@@ -605,11 +605,6 @@ int run_evict(EvictParams& p, long long items, cudaStream_t st) {
   const size_t smem = ((size_t)p.key_cache + (p.local ? item_words(p.max_len) : 0)) * 4;
   TWIST_CUDA_TRY(launch_overlapped(evict_kernel<D>, dim3((unsigned)(items * ctas)), dim3(kEvThreads), smem, st, ctas, p));
   return TWIST_OK;
-}
-
-bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
 
 constexpr long long kMaxItems = 1 << 20, kMaxSlots = 1 << 26;

@@ -493,11 +493,6 @@ __global__ void __launch_bounds__(kAppThreads) append_one_q8_kernel(const Append
   }
 }
 
-bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
-}
-
 template <int D>
 int launch(const AppendParams& p, int S, int layout, cudaStream_t st) {
   int mode;

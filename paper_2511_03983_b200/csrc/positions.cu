@@ -303,11 +303,6 @@ int launch(PosParams& p, int layout, cudaStream_t st) {
   return TWIST_OK;
 }
 
-bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
-}
-
 int check_heads(int dtype, int S, int T, int heads, int kv, int dh, int rot, int layout) {
   if (dtype != TWIST_BF16) return TWIST_ERR_UNSUPPORTED;
   if (S <= 0 || T <= 0 || heads <= 0 || kv <= 0 || dh <= 0 || dh % 8 != 0 || rot < 0 || rot > dh || rot % 2 != 0) return TWIST_ERR_SHAPE;
