@@ -577,9 +577,10 @@ int32_t twist_kv_append_q8(const twist_kv_append_q8_args* a /*host*/, void* stre
 /* twist_attn_decode_q8 -- twist_attn_decode over the 8-bit cache.  Scales may be any positive normal numbers, in any order and as far
  * apart as they are.  Queries enter the product as fp16 brought near 2^15 by a power of two (no bits of an element are lost
  * within 2^29 of its head's largest), cached values exactly, probabilities times scales of V as fp16: 11 bits, and what is
- * more than 2^27 below the largest such product of the head so far in steps of 2^-37 of that (or of 2^-148, if that is more).  Sums
- * are fp32 and divided at the end: values of V up to 2^88 cannot overflow them.  NaN in V makes its element of the heads that read it
- * NaN and touches no other.  The workspace is that of twist_attn_decode.
+ * more than 2^27 below the largest such product of the head so far in steps of 2^-37 of that (or of 2^-148, if that is more); a
+ * probability below 2^-126 of the largest may count for nothing.  Sums are fp32 and divided at the end: values of V up to 2^88 cannot
+ * overflow them.  NaN in V makes its element of the heads that read it NaN and touches no other.  The workspace is that of
+ * twist_attn_decode.
  * d_head in {16, 32, 64, 128}; limits as twist_attn_decode, t + 4 in place of t + 2, tiles of 64 keys, of 32 at d_head 64 and of 16
  * at 128. */
 typedef struct {

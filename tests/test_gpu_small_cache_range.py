@@ -6,6 +6,7 @@ Tolerance of a result (the definition in 64 bits, p = exp(s - max), l = sum p, m
  * a score's error e_s = (d + 4) 2^-23 sum|q k| / sqrt(d) and 2^-20 for the exponential are relative errors of p, once in the sum and once in l;
  * a probability as fp16: half a step is 2^-11 of it, or, below fp16's normal numbers, 2^-25 of numbers scaled so that the largest p * scale so
    far is 2^13 at least: 2^-38 of max(p * scale) for every key, times its number, at most 448;
+ * probabilities, and factors of parts that are joined, below 2^-126 are zero: 2^-126 |v| of every key, twice;
  * sums over n keys in fp32, 2 n 2^-23, and 2^-16 for sums brought to other units (an exponent of up to 2^7, 2^-24 of it, a few times)."""
 import math
 
@@ -35,10 +36,10 @@ def cache_of(k, v, ks, vs, page):
     per = -(-m // page)
     fill = lambda x, to, value: np.concatenate([x, np.full((*x.shape[:2], to - x.shape[2], *x.shape[3:]), value)], 2)
     pages = lambda x: torch.from_numpy(fill(x, per * page, 0.0).reshape(n, KV, per, page, D).transpose(0, 2, 1, 3, 4).reshape(n * per, KV, page, D)
-                                       .astype(np.float32)).to(F8).cuda()
+                                       .astype(np.float32, order="C")).to(F8).cuda()
     sc = np.stack([fill(s, per * page // BLOCK, 1.0).reshape(n, KV, per, page // BLOCK).transpose(0, 2, 1, 3).reshape(n * per, KV, -1)
                    for s in (ks, vs)], -1)
-    return pages(k), pages(v), torch.from_numpy(sc.astype(np.float32)).cuda(), np.arange(n * per).reshape(n, per)
+    return pages(k), pages(v), torch.from_numpy(sc.astype(np.float32, order="C")).cuda(), np.arange(n * per).reshape(n, per)
 
 
 def run(B, q, k, v, ks, vs, lens, page=64):
@@ -74,7 +75,7 @@ def check(got, lse, q, k, v, weights, lens, vs):
             l = p.sum()
             want, mass = p @ vv / l, p @ np.abs(vv) / l
             scale = np.repeat(vs[b, h // 2], BLOCK)[:m]
-            tiny = m * 2.0 ** -38 * (p * scale).max() * 448 / l
+            tiny = m * 2.0 ** -38 * (p * scale).max() * 448 / l + 2.0 ** -125 * np.abs(vv).sum(0) / l
             tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -134 + (2 * e + 2.0 ** -20 + 2.0 ** -11 + 2.0 ** -16 + 2 * m * 2.0 ** -23) * mass + tiny
             assert np.all(np.isfinite(got[b, h])), (b, h)
             worst = max(worst, np.max(np.abs(got[b, h] - want) / tol))
@@ -88,7 +89,7 @@ def check(got, lse, q, k, v, weights, lens, vs):
                 d = x - lse[h, b]
                 terms.append((np.exp(d), np.exp(d) * (e + 2.0 ** -22 * np.abs(d) + 2.0 ** -21)))
             w = terms[0][0] + terms[1][0]
-            assert np.all(np.abs(weights[b, g, :m] - w) <= terms[0][1] + terms[1][1] + 3 * 2.0 ** -24 * w)
+            assert np.all(np.abs(weights[b, g, :m] - w) <= terms[0][1] + terms[1][1] + 3 * 2.0 ** -24 * w + 2 * 2.0 ** -126)   # (a term below 2^-126 is 0)
 
 
 def case(rng, way, D, KV=2):
