@@ -46,7 +46,7 @@ namespace {
 
 constexpr int kMaxCtasPerSm = 4;
 // What changing to the next item costs a warp, in tiles.  8 bits, 1 / 2 / 3 / 5: 952 ragged sequences of up to 274 keys on 4
-// positions of d = 128 57.3 / 50.4 / 48.5 / 48.1 us, eight subnets of long ones 194.8 / 195.8 / 187.5 / 186.9.
+// positions of d = 128 58.0 / 51.9 / 49.7 / 50.0 us, eight subnets of long ones 200 / 200 / 191 / 189.
 template <int B>
 constexpr int kItemCost = B == 1 ? 3 : 1;
 constexpr int kMinCost = 2;                // least work of a warp, in tiles
@@ -526,9 +526,9 @@ constexpr int kLenCache = 512;        // sequences whose lengths a CTA keeps in 
 // An 8-bit cache's tiles in the split kernel: a ring of them per warp, filled by bulk copies (the 16 rows of a step lie next to
 // each other in their page: one copy for K, one for V).  Half the bytes for the same arithmetic: with the next tile in
 // registers, as in 16 bits, the loads in flight do not cover a tile's time (eight subnets of d = 128 246 us, 64 ragged sequences
-// with 32 heads on 4 positions of d = 64 75; through rings 205 and 60).  Three tiles of 16 keys and 12 warps an SM at d = 128
-// (two: 199 us against 195, two of 32 keys and 8 warps: 204), two of 32 keys and 16 warps at d = 64 (of 64 keys and 12 warps:
-// 63 against 58, three of 32 and 12: 63, three of 16 keys: 63 to 70).
+// with 32 heads on 4 positions of d = 64 75; through rings, at first, 205 and 60).  Three tiles of 16 keys and 12 warps an SM at d = 128
+// (two: 193 us against 191; two of 32 keys and 8 warps, at 195: 204), two of 32 keys and 16 warps at d = 64 (three and 12 warps:
+// 57.6 against 55.1; two of 64 keys and 12 warps and three of 16, at 58: 63 and 63 to 70).
 template <int D>
 constexpr int kRing = D == 128 ? 3 : 2;
 template <int D>
@@ -1067,7 +1067,7 @@ int run(DecParams& p, long long max_len, cudaStream_t st) {
   // than kShortTiles tiles, where the items fill the GPU kShortWork tiles a warp deep (256 ragged items of up to 2048
   // keys: 21 us against 27 to 34), and earlier where they do not run at once (512 items of 256 keys, d = 128: 18.2
   // against 19.6).  An 8-bit cache is counted in the same 16 keys from d = 64 on (256 ragged items of up to 2048 keys, d = 64:
-  // 18.4 us through the line, 22.1 the short way; 512 items of 512 keys 12.9 the short way, 16.7 through the line).
+  // 17.0 us through the line, 22.7 the short way; 512 items of 512 keys 13.2 the short way, 15.5 through the line).
   constexpr int UNIT = D >= 64 ? 16 : Shape<D, B>::TILE;
   const long long tiles = (max_len + UNIT - 1) / UNIT;
   int cluster = 1;

@@ -36,9 +36,10 @@ __device__ inline float weight_of(float score, float scale, float lse) { return 
 
 // A warp's ring of two tiles of SUB * 16 keys, filled by bulk copies: the 16 rows of a step lie next to each other in their page,
 // and so do their prior weights.  Tiles of up to 4 KB and 16 warps an SM.  Measured (eight subnets of 16 ragged sequences of up to
-// 8192 keys, e4m3, d = 128, 630 MB: 132 us; 64 ragged sequences of up to 16000, 32 heads on 4 positions of d = 64, 152 MB: 53):
-// three tiles 157 and 64, d = 128 by 4 steps 155; keys straight into registers 180 and 84 to 105, 16 keys (32 at d = 64) at a
-// time through rings 181 and 75: what a tile costs beside its keys has to be spread over many of them.
+// 8192 keys, e4m3, d = 128, 630 MB: 133 us; 64 ragged sequences of up to 16000, 32 heads on 4 positions of d = 64, 152 MB: 55.5).
+// When these took 132 and 53 (before pages outside the pool and scores beyond fp32 were looked at): three tiles 157 and 64, d = 128 by
+// 4 steps 155; keys straight into registers 180 and 84 to 105, 16 keys (32 at d = 64) at a time through rings 181 and 75: what a tile
+// costs beside its keys has to be spread over many of them.
 constexpr int kRing = 2;
 template <int D, int B>
 struct KeyRing {
